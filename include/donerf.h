@@ -297,6 +297,140 @@ int donerf_debug_mfma_peak(donerf_t* h, int32_t workgroups, int32_t iters, float
 int donerf_targets(donerf_t* h, const float* depth, int32_t P, int32_t H, int32_t W, int32_t K, int32_t Z,
                    float* out);
 
+/* ------------------------------------------------------------------------
+ * Layers of the networks as operators of their own: products with 4-bit weights
+ * for serving, and a layer's forward and backward pass for training, with its
+ * activations kept in 8 bits in between.
+ *
+ * They take matrices in device memory, row by row, and work on any sizes: in and
+ * out of a layer need not be those of the handle's networks, whose weights they
+ * do not touch.  The handle gives them its device and its stream.  They allocate
+ * nothing, launch kernels only and keep nothing between calls, so they can be
+ * captured into a HIP graph; calls that overlap on different streams are safe as
+ * far as their buffers (the workspace among them) are different ones.
+ * ------------------------------------------------------------------------ */
+
+typedef enum donerf_type {
+    DONERF_TYPE_FP32 = 0,
+    DONERF_TYPE_BF16 = 1,
+    DONERF_TYPE_MXFP4 = 2, /* microscaled E2M1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and
+                              their negatives)                                */
+    DONERF_TYPE_MXFP8 = 3  /* microscaled E4M3 (largest value 448)            */
+} donerf_type;
+
+/*
+ * A matrix in device memory.  fp32 and bf16: rows of values, at least `cols`
+ * apart.  Microscaled: a row's columns form blocks of 32, the last one filled
+ * up with zeros, and the values of a block are its elements times its scale
+ * 2^(c - 127), c one byte, 255 for NaN (OCP Microscaling Formats v1.0).
+ *   data    fp32, bf16: aligned to the type's size.  Microscaled: the elements'
+ *           codes, aligned to 16 bytes; 16 bytes a block in MXFP4 (the even
+ *           column in a byte's low half), 32 bytes a block in MXFP8
+ *   ld      from row to row: values (fp32, bf16) or bytes, a multiple of 16
+ *           (microscaled); at least a row's length
+ *   scales  microscaled: one byte per block, aligned to 8 bytes; else NULL
+ *   ld_scales  bytes from one row's scales to the next's, a multiple of 8 and at
+ *           least a row's blocks.  Bytes behind the last block's are neither
+ *           used nor written
+ * Both directions of every conversion treat a block the same way: its scale is
+ * the smallest power of two, 2^-127 or more, that holds its largest value as an
+ * element (6 or 448 times the scale), and elements are rounded to the nearest,
+ * ties to even.  In MXFP8 a value other than zero never becomes zero but at
+ * least the smallest element, and NaN and infinities become NaN.  In MXFP4 a block
+ * that holds a NaN or an infinity gets the scale NaN, and all of it reads as NaN.
+ */
+typedef struct donerf_mat {
+    void* data;
+    int64_t ld;
+    uint8_t* scales;
+    int64_t ld_scales;
+    int32_t type; /* donerf_type */
+} donerf_mat;
+
+/* Largest number of columns, and of a layer's inputs and outputs. */
+#define DONERF_MAX_COLS 65536
+
+/*
+ * Convert x (FP32 or BF16) to q (MXFP4 or MXFP8), and back (MXFP4 or MXFP8 to
+ * FP32 or BF16; the values are exact but for the rounding of the smallest and the
+ * overflow of the largest scales, and of MXFP8 below BF16's smallest numbers).
+ *   rows  0..2^31 - 1; with 0 the call does nothing
+ *   cols  1..DONERF_MAX_COLS
+ * x, q and y must not overlap.
+ * Errors: E_INVALID_ARG (NULL handle or matrix, a size, type, alignment or ld
+ * that the above rules out), E_DEVICE (the current device is not the handle's),
+ * E_HIP.
+ */
+int donerf_mx_quantize(donerf_t* h, const donerf_mat* x, const donerf_mat* q, int64_t rows, int32_t cols);
+int donerf_mx_dequantize(donerf_t* h, const donerf_mat* q, const donerf_mat* y, int64_t rows, int32_t cols);
+
+/*
+ * y = act(x w^T + bias) with both factors in MXFP4.
+ *   x     rows x in: MXFP4, or FP32 or BF16, converted on the way as
+ *         donerf_mx_quantize does
+ *   w     out x in, MXFP4
+ *   bias  device, out fp32, or NULL
+ *   relu  0: act is the identity; 1: max(z, 0), NaN kept
+ *   y     rows x out: FP32, BF16 or MXFP4 (converted from the fp32 results)
+ *   workspace  device, 16-byte aligned, at least donerf_mx_linear_workspace(...)
+ *         bytes, the call's own until it is done; may be NULL if that is 0
+ * Products are exact, sums fp32.  y must not overlap the inputs.
+ * rows 0..2^31 - 1 (0: nothing is done), in and out 1..DONERF_MAX_COLS.
+ * Errors: as above, and E_SIZE (workspace too small), E_UNSUPPORTED (rows x out
+ * of 2^38 or more).
+ */
+int donerf_mx_linear(donerf_t* h, const donerf_mat* x, const donerf_mat* w, const float* bias, int32_t relu,
+                     const donerf_mat* y, int64_t rows, int32_t in, int32_t out, void* workspace,
+                     size_t workspace_bytes);
+
+/* Bytes of workspace for x of this donerf_type; 0 for sizes that are refused. */
+size_t donerf_mx_linear_workspace(int32_t x_type, int64_t rows, int32_t in);
+
+/*
+ * A layer's forward pass for training: y = act(x w^T + bias) in BF16, and kept,
+ * the same values (before their rounding to BF16) in MXFP8 for the backward pass
+ * of the layer that reads them.
+ *   x     rows x in, BF16
+ *   w     out x in, BF16
+ *   bias, relu  as above
+ *   y     rows x out, BF16, or NULL
+ *   kept  rows x out, MXFP8, or NULL; one of the two at least
+ * fp32 accumulation.  The outputs overlap neither each other nor the inputs.
+ * Sizes and errors: as for donerf_mx_linear.
+ */
+int donerf_train_linear(donerf_t* h, const donerf_mat* x, const donerf_mat* w, const float* bias, int32_t relu,
+                        const donerf_mat* y, const donerf_mat* kept, int64_t rows, int32_t in, int32_t out);
+
+/*
+ * The layer's backward pass, from the gradient dz of its z = x w^T + bias:
+ *   dx = dz w (rounded to BF16), dw = dz^T x, db = the sum of dz's rows.
+ *   dz    rows x out, BF16
+ *   x     rows x in: what the forward pass of the layer before kept (MXFP8), or
+ *         BF16 (a network's input)
+ *   relu  1: x is a ReLU's output, and dx is the gradient of that ReLU's input:
+ *         0 where x is zero.  0: dx is the gradient of x
+ *   w     out x in, BF16; may be NULL without dx
+ *   dx    rows x in, BF16, or NULL
+ *   dw    out x in, FP32, or NULL
+ *   db    device, out fp32, or NULL
+ *   accumulate  0: dw and db are written; 1: they are added to
+ *   workspace  device, 16-byte aligned, donerf_train_linear_backward_workspace(...)
+ *         bytes at least, the call's own until it is done
+ * fp32 accumulation; the same call gives the same bits.  With rows = 0, dw and
+ * db are zero (or stay, with accumulate).  Outputs overlap nothing.
+ * Sizes and errors: as for donerf_mx_linear.
+ */
+int donerf_train_linear_backward(donerf_t* h, const donerf_mat* dz, const donerf_mat* x, int32_t relu,
+                                 const donerf_mat* w, const donerf_mat* dx, const donerf_mat* dw, float* db,
+                                 int32_t accumulate, int64_t rows, int32_t in, int32_t out, void* workspace,
+                                 size_t workspace_bytes);
+
+/* Bytes of workspace on the handle's device; 0 for sizes that are refused. */
+size_t donerf_train_linear_backward_workspace(const donerf_t* h, int64_t rows, int32_t in, int32_t out);
+
+/* The device and the stream that a handle's work goes to; each may be NULL. */
+int donerf_get_stream(const donerf_t* h, int32_t* device, void** stream);
+
 /*
  * Copy the handle's depth-class table to host memory: bounds (B + 1 values,
  * may be NULL), centres (B), widths (B).  Bounds b_k = d_min + (d_max - d_min

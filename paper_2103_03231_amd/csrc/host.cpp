@@ -544,6 +544,84 @@ int render_impl(donerf_t* h, const float* poses, int32_t P, int32_t H, int32_t W
     return DONERF_OK;
 }
 
+// ---- matrices of the layer operators
+
+bool microscaled(int type) { return type == DONERF_TYPE_MXFP4 || type == DONERF_TYPE_MXFP8; }
+
+// Bytes of a row's codes.
+int64_t code_bytes(int type, int32_t cols) {
+    const int64_t blocks = (cols + 31) / 32;
+    return type == DONERF_TYPE_MXFP4 ? 16 * blocks : 32 * blocks;
+}
+
+constexpr int kF32Bit = 1 << DONERF_TYPE_FP32, kBf16Bit = 1 << DONERF_TYPE_BF16, kMx4Bit = 1 << DONERF_TYPE_MXFP4,
+              kMx8Bit = 1 << DONERF_TYPE_MXFP8;
+
+// Checks one matrix argument against the types (bits) that its place takes.
+int validate_mat(const char* name, const donerf_mat* m, int types, int64_t rows, int32_t cols) {
+    auto bad = [&](const char* what) { return fail(DONERF_E_INVALID_ARG, std::string(name) + ": " + what); };
+    if (!m) return bad("NULL");
+    if (m->type < DONERF_TYPE_FP32 || m->type > DONERF_TYPE_MXFP8 || !(types & (1 << m->type)))
+        return bad("this type is not taken here");
+    const bool mx = microscaled(m->type);
+    const int64_t least = mx ? code_bytes(m->type, cols) : cols;
+    if (m->ld < least || m->ld > ((int64_t)1 << 40)) return bad("ld out of range");
+    if (mx) {
+        if (m->ld % 16) return bad("ld must be a multiple of 16 bytes");
+        if (m->ld_scales < (cols + 31) / 32 || m->ld_scales > ((int64_t)1 << 40) || m->ld_scales % 8)
+            return bad("ld_scales must be a multiple of 8 and hold a row's blocks");
+    } else if (m->scales) {
+        return bad("scales given for a type without them");
+    }
+    if (rows == 0) return DONERF_OK;   // no row, no memory
+    if (!m->data || (mx && !m->scales)) return bad("NULL buffer");
+    const uintptr_t align = mx ? 16 : m->type == DONERF_TYPE_FP32 ? 4 : 2;
+    if ((uintptr_t)m->data % align || (mx && (uintptr_t)m->scales % 8))
+        return bad("buffer not aligned");
+    return DONERF_OK;
+}
+
+// Sizes of a layer operator.
+int validate_layer(int64_t rows, int32_t in, int32_t out) {
+    if (rows < 0 || rows > INT32_MAX) return fail(DONERF_E_INVALID_ARG, "rows must lie in [0, 2^31)");
+    if (in < 1 || in > DONERF_MAX_COLS || out < 1 || out > DONERF_MAX_COLS)
+        return fail(DONERF_E_INVALID_ARG, "columns must lie in [1, 65536]");
+    return DONERF_OK;
+}
+// The handle, and that the device the call would launch on is its own.
+int validate_handle(const donerf_t* h) {
+    if (!h) return fail(DONERF_E_INVALID_ARG, "handle is NULL");
+    int dev = -1;
+    const hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
+    if (dev != h->device) return fail(DONERF_E_DEVICE, "the current device is not the handle's");
+    return DONERF_OK;
+}
+// A product's tiles, 128 x 128 or more wherever there are many, in the 32-bit grid.
+int validate_tiles(int64_t rows, int32_t cols) {
+    if (rows * (int64_t)cols >= (int64_t)1 << 38 || ((rows + 127) / 128) * ((cols + 127) / 128) >= 1 << 24)
+        return fail(DONERF_E_UNSUPPORTED, "more results than a launch takes");
+    return DONERF_OK;
+}
+
+int validate_workspace(const void* p, size_t have, size_t need) {
+    if (need == 0) return DONERF_OK;
+    if (have < need)
+        return fail(DONERF_E_SIZE, "workspace of " + std::to_string(have) + " bytes, " + std::to_string(need) + " are needed");
+    if (!p) return fail(DONERF_E_INVALID_ARG, "workspace is NULL");
+    if ((uintptr_t)p % 16) return fail(DONERF_E_INVALID_ARG, "workspace not aligned to 16 bytes");
+    return DONERF_OK;
+}
+
+MxIn mx_in(const donerf_mat* m) { return MxIn{(const uint8_t*)m->data, m->ld, m->scales, m->ld_scales}; }
+MxOut mx_out(const donerf_mat* m) { return MxOut{(uint8_t*)m->data, m->ld, m->scales, m->ld_scales}; }
+// bf16 rows, ld in bytes.
+MxIn bf16_in(const donerf_mat* m) { return MxIn{(const uint8_t*)m->data, m->ld * 2, nullptr, 0}; }
+
+// Workspace of mx_linear: x's codes, then its scales.
+size_t quantized_codes(int64_t rows, int32_t in) { return (size_t)rows * (size_t)code_bytes(DONERF_TYPE_MXFP4, in); }
+int64_t scale_row(int32_t cols) { return ((int64_t)(cols + 31) / 32 + 7) / 8 * 8; }
+
 }  // namespace
 
 extern "C" {
@@ -769,6 +847,167 @@ int donerf_targets(donerf_t* h, const float* depth, int32_t P, int32_t H, int32_
         (float)(1.0 / std::log2((double)h->cfg.far_dist - (double)h->cfg.near_dist + 1.0));
     hipError_t e = launch_targets(depth, P, H, W, h->bins + 2 * B, B, K, Z, inv_l2span, out, h->stream);
     if (e != hipSuccess) return hip_fail(e, "targets launch");
+    return DONERF_OK;
+}
+
+int donerf_mx_quantize(donerf_t* h, const donerf_mat* x, const donerf_mat* q, int64_t rows, int32_t cols) {
+    g_err.clear();
+    int rc = validate_layer(rows, cols, 1);
+    if (rc || (rc = validate_mat("x", x, kF32Bit | kBf16Bit, rows, cols)) ||
+        (rc = validate_mat("q", q, kMx4Bit | kMx8Bit, rows, cols)) || (rc = validate_handle(h)))
+        return rc;
+    const hipError_t e = launch_mx_quantize(x->data, x->ld, x->type == DONERF_TYPE_BF16, mx_out(q),
+                                            q->type == DONERF_TYPE_MXFP8, rows, cols, h->n_cu, h->stream);
+    return e == hipSuccess ? DONERF_OK : hip_fail(e, "mx_quantize launch");
+}
+
+int donerf_mx_dequantize(donerf_t* h, const donerf_mat* q, const donerf_mat* y, int64_t rows, int32_t cols) {
+    g_err.clear();
+    int rc = validate_layer(rows, cols, 1);
+    if (rc || (rc = validate_mat("q", q, kMx4Bit | kMx8Bit, rows, cols)) ||
+        (rc = validate_mat("y", y, kF32Bit | kBf16Bit, rows, cols)) || (rc = validate_handle(h)))
+        return rc;
+    const hipError_t e = launch_mx_dequantize(mx_in(q), q->type == DONERF_TYPE_MXFP8, y->data, y->ld,
+                                              y->type == DONERF_TYPE_BF16, rows, cols, h->n_cu, h->stream);
+    return e == hipSuccess ? DONERF_OK : hip_fail(e, "mx_dequantize launch");
+}
+
+size_t donerf_mx_linear_workspace(int32_t x_type, int64_t rows, int32_t in) {
+    if (rows < 1 || rows > INT32_MAX || in < 1 || in > DONERF_MAX_COLS) return 0;
+    if (x_type != DONERF_TYPE_FP32 && x_type != DONERF_TYPE_BF16) return 0;
+    return quantized_codes(rows, in) + (size_t)rows * (size_t)scale_row(in);
+}
+
+int donerf_mx_linear(donerf_t* h, const donerf_mat* x, const donerf_mat* w, const float* bias, int32_t relu,
+                     const donerf_mat* y, int64_t rows, int32_t in, int32_t out, void* workspace,
+                     size_t workspace_bytes) {
+    g_err.clear();
+    int rc = validate_layer(rows, in, out);
+    if (rc || (rc = validate_mat("x", x, kF32Bit | kBf16Bit | kMx4Bit, rows, in)) ||
+        (rc = validate_mat("w", w, kMx4Bit, out, in)) ||
+        (rc = validate_mat("y", y, kF32Bit | kBf16Bit | kMx4Bit, rows, out)))
+        return rc;
+    if ((uintptr_t)bias % 4) return fail(DONERF_E_INVALID_ARG, "bias not aligned");
+    if (relu != 0 && relu != 1) return fail(DONERF_E_INVALID_ARG, "relu must be 0 or 1");
+    if ((rc = validate_tiles(rows, out)) ||
+        (rc = validate_workspace(workspace, workspace_bytes, donerf_mx_linear_workspace(x->type, rows, in))) ||
+        (rc = validate_handle(h)))
+        return rc;
+    if (rows == 0) return DONERF_OK;
+    GemmArgs g{};
+    g.a = mx_in(w);
+    hipError_t e;
+    if (x->type == DONERF_TYPE_MXFP4) {
+        g.b = mx_in(x);
+    } else {
+        uint8_t* ws = (uint8_t*)workspace;
+        const MxOut q{ws, code_bytes(DONERF_TYPE_MXFP4, in), ws + quantized_codes(rows, in), scale_row(in)};
+        e = launch_mx_quantize(x->data, x->ld, x->type == DONERF_TYPE_BF16, q, false, rows, in, h->n_cu, h->stream);
+        if (e != hipSuccess) return hip_fail(e, "mx_quantize launch");
+        g.b = MxIn{q.codes, q.ld, q.scales, q.ld_scales};
+    }
+    g.bias = bias;
+    g.relu = relu;
+    int kind = kOutMx4;
+    if (y->type == DONERF_TYPE_MXFP4) {
+        g.q = mx_out(y);
+    } else {
+        kind = y->type == DONERF_TYPE_BF16 ? kOutBf16 : kOutF32;
+        g.y = (uint8_t*)y->data;
+        g.ldy = y->ld;
+    }
+    g.M = (int32_t)rows;
+    g.N = out;
+    g.K = in;
+    e = launch_mx_linear(g, kind, h->n_cu, h->stream);
+    return e == hipSuccess ? DONERF_OK : hip_fail(e, "mx_linear launch");
+}
+
+int donerf_train_linear(donerf_t* h, const donerf_mat* x, const donerf_mat* w, const float* bias, int32_t relu,
+                        const donerf_mat* y, const donerf_mat* kept, int64_t rows, int32_t in, int32_t out) {
+    g_err.clear();
+    int rc = validate_layer(rows, in, out);
+    if (rc || (rc = validate_mat("x", x, kBf16Bit, rows, in)) || (rc = validate_mat("w", w, kBf16Bit, out, in)) ||
+        (y && (rc = validate_mat("y", y, kBf16Bit, rows, out))) ||
+        (kept && (rc = validate_mat("kept", kept, kMx8Bit, rows, out))))
+        return rc;
+    if (!y && !kept) return fail(DONERF_E_INVALID_ARG, "neither y nor kept is given");
+    if ((uintptr_t)bias % 4) return fail(DONERF_E_INVALID_ARG, "bias not aligned");
+    if (relu != 0 && relu != 1) return fail(DONERF_E_INVALID_ARG, "relu must be 0 or 1");
+    if ((rc = validate_tiles(rows, out)) || (rc = validate_handle(h))) return rc;
+    if (rows == 0) return DONERF_OK;
+    GemmArgs g{};
+    g.a = bf16_in(w);
+    g.b = bf16_in(x);
+    g.bias = bias;
+    g.relu = relu;
+    if (y) {
+        g.y = (uint8_t*)y->data;
+        g.ldy = y->ld;
+    }
+    if (kept) g.q = mx_out(kept);
+    g.M = (int32_t)rows;
+    g.N = out;
+    g.K = in;
+    const hipError_t e = launch_train_linear(g, h->n_cu, h->stream);
+    return e == hipSuccess ? DONERF_OK : hip_fail(e, "train_linear launch");
+}
+
+size_t donerf_train_linear_backward_workspace(const donerf_t* h, int64_t rows, int32_t in, int32_t out) {
+    if (!h || rows < 0 || rows > INT32_MAX || in < 1 || in > DONERF_MAX_COLS || out < 1 || out > DONERF_MAX_COLS) return 0;
+    return backward_workspace(rows, out, in, h->n_cu);
+}
+
+int donerf_train_linear_backward(donerf_t* h, const donerf_mat* dz, const donerf_mat* x, int32_t relu,
+                                 const donerf_mat* w, const donerf_mat* dx, const donerf_mat* dw, float* db,
+                                 int32_t accumulate, int64_t rows, int32_t in, int32_t out, void* workspace,
+                                 size_t workspace_bytes) {
+    g_err.clear();
+    int rc = validate_layer(rows, in, out);
+    if (rc || (rc = validate_mat("dz", dz, kBf16Bit, rows, out)) ||
+        (rc = validate_mat("x", x, kBf16Bit | kMx8Bit, rows, in)) ||
+        ((w || dx) && (rc = validate_mat("w", w, kBf16Bit, out, in))) ||
+        (dx && (rc = validate_mat("dx", dx, kBf16Bit, rows, in))) ||
+        (dw && (rc = validate_mat("dw", dw, kF32Bit, out, in))))
+        return rc;
+    if (!dx && !dw && !db) return fail(DONERF_E_INVALID_ARG, "no gradient is asked for");
+    if ((uintptr_t)db % 4) return fail(DONERF_E_INVALID_ARG, "db not aligned");
+    if ((relu != 0 && relu != 1) || (accumulate != 0 && accumulate != 1))
+        return fail(DONERF_E_INVALID_ARG, "relu and accumulate must be 0 or 1");
+    if ((rc = validate_tiles(rows, in)) || (rc = validate_handle(h)) ||
+        (rc = validate_workspace(workspace, workspace_bytes, backward_workspace(rows, out, in, h->n_cu))))
+        return rc;
+    BackwardArgs a{};
+    a.dz = (const uint16_t*)dz->data;
+    a.lddz = dz->ld;
+    a.x_bf16 = x->type == DONERF_TYPE_BF16;
+    a.x = a.x_bf16 ? bf16_in(x) : mx_in(x);
+    a.relu = relu;
+    if (dx) {
+        a.w = (const uint16_t*)w->data;
+        a.ldw = w->ld;
+        a.dx = (uint16_t*)dx->data;
+        a.lddx = dx->ld;
+    }
+    if (dw) {
+        a.dw = (float*)dw->data;
+        a.lddw = dw->ld;
+    }
+    a.db = db;
+    a.accumulate = accumulate;
+    a.M = (int32_t)rows;
+    a.N = out;
+    a.K = in;
+    a.workspace = (uint8_t*)workspace;
+    const hipError_t e = launch_train_linear_backward(a, h->n_cu, h->stream);
+    return e == hipSuccess ? DONERF_OK : hip_fail(e, "train_linear_backward launch");
+}
+
+int donerf_get_stream(const donerf_t* h, int32_t* device, void** stream) {
+    g_err.clear();
+    if (!h) return fail(DONERF_E_INVALID_ARG, "handle is NULL");
+    if (device) *device = h->device;
+    if (stream) *stream = h->stream;
     return DONERF_OK;
 }
 

@@ -134,4 +134,74 @@ constexpr int kTgtMaxK = 15;
 hipError_t launch_targets(const float* depth, int P, int H, int W, const float* bounds, int B, int K, int Z,
                           float inv_l2span, float* out, hipStream_t stream);
 
+// ---- layer operators (include/donerf.h): microscaled formats (mx_convert.hip),
+// products with 4-bit weights (mx_linear.hip), layers whose activations are kept
+// in 8 bits (train_linear.hip).
+
+// A matrix's rows as bytes: codes of a microscaled one, or the values of a bf16
+// one.  ld: bytes from row to row.
+struct MxIn {
+    const uint8_t* codes;
+    int64_t ld;
+    const uint8_t* scales;   // microscaled only
+    int64_t ld_scales;
+};
+struct MxOut {
+    uint8_t* codes;
+    int64_t ld;
+    uint8_t* scales;
+    int64_t ld_scales;
+};
+
+// A product y[m][n] = sum_k a[n][k] b[m][k] and what follows it (layer_gemm.h).
+constexpr int kMaskNone = 0, kMaskMx8 = 1, kMaskBf16 = 2;
+struct GemmArgs {
+    MxIn a, b;               // N and M rows of K columns
+    const float* bias;       // N, or null
+    uint8_t* y;              // bf16 or fp32 rows, or null
+    int64_t ldy;             // values from row to row
+    MxOut q;                 // microscaled outputs
+    const uint8_t* mask;     // E4M3 codes or bf16 rows
+    int64_t ld_mask;         // bytes (E4M3) or values (bf16)
+    int32_t mask_type;
+    int32_t M, N, K;
+    int32_t relu;
+    uint32_t tiles_n, tiles_m;
+};
+
+// Outputs of mx_linear.
+constexpr int kOutBf16 = 0, kOutF32 = 1, kOutMx4 = 2;
+
+hipError_t launch_mx_quantize(const void* x, int64_t ldx, bool x_bf16, const MxOut& q, bool fp8, int64_t rows, int cols,
+                              int n_cu, hipStream_t stream);
+hipError_t launch_mx_dequantize(const MxIn& q, bool fp8, void* y, int64_t ldy, bool y_bf16, int64_t rows, int cols,
+                                int n_cu, hipStream_t stream);
+// g.a, g.b E2M1.
+hipError_t launch_mx_linear(const GemmArgs& g, int out, int n_cu, hipStream_t stream);
+// g.a, g.b bf16; y and q may each be null.
+hipError_t launch_train_linear(const GemmArgs& g, int n_cu, hipStream_t stream);
+
+// The backward pass of a layer: dz (M x N bf16), x (M x K, E4M3 or bf16), w
+// (N x K bf16).  dx, dw and db may each be null.
+struct BackwardArgs {
+    const uint16_t* dz;
+    int64_t lddz;
+    MxIn x;                  // E4M3, or bf16 rows (x_bf16), ld in bytes
+    int32_t x_bf16;
+    int32_t relu;            // x is a ReLU's output
+    const uint16_t* w;
+    int64_t ldw;
+    uint16_t* dx;
+    int64_t lddx;
+    float* dw;
+    int64_t lddw;
+    float* db;
+    int32_t accumulate;      // dw and db are added to
+    int32_t M, N, K;
+    uint8_t* workspace;
+};
+// Bytes of workspace for these sizes.
+size_t backward_workspace(int64_t M, int N, int K, int n_cu);
+hipError_t launch_train_linear_backward(const BackwardArgs& a, int n_cu, hipStream_t stream);
+
 }  // namespace donerf

@@ -1,0 +1,170 @@
+// mx.h - microscaled formats on gfx950 (include/donerf.h donerf_type): blocks of
+// 32 consecutive columns of a row share one power of two, 2^(c - 127) with c one
+// byte (E8M0, 255 = NaN).
+//
+// The scale of a block is the smallest 2^s that holds its largest value,
+// max|v| <= M 2^s with M the elements' largest (6 for E2M1, 448 for E4M3), as
+// the fp8 networks choose theirs: nothing is clamped, so every element is off by
+// at most half a step of its own binade or of the smallest one.  Both
+// conversions, to elements (rounded to nearest even) and back, are single
+// instructions that take the scale as the exponent field of an fp32.
+#pragma once
+
+#include "device.h"
+
+namespace donerf {
+namespace {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kMxBlock = 32;      // columns that share a scale
+constexpr int kMxNaN = 255;       // scale code
+
+__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// Largest |v| as its bits: integers order as the values do, infinities and then
+// NaN above every number.
+template <int N>
+__device__ __forceinline__ uint32_t top_bits(const float* v) {
+    uint32_t t = abs_bits(v[0]);
+#pragma unroll
+    for (int i = 1; i < N; ++i) t = max(t, abs_bits(v[i]));
+    return t;
+}
+// The same among finite values only.
+template <int N>
+__device__ __forceinline__ uint32_t finite_top_bits(const float* v) {
+    uint32_t t = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) t = max(t, abs_bits(v[i]) < 0x7f800000u ? abs_bits(v[i]) : 0u);
+    return t;
+}
+
+// Scale code of a block whose largest |v| has the bits top: the exponent of
+// 1.5 * 2^2 (E2M1) or 1.75 * 2^8 (E4M3) below it, one more where its mantissa is
+// larger; at least 0, where every fp32 below the smallest normal number fits.
+__device__ __forceinline__ int mx4_code(uint32_t top) {
+    if (top >= 0x7f800000u) return kMxNaN;   // a block that holds an infinity or NaN reads as NaN
+    return max(0, (int)(top >> 23) - 2 + ((top & 0x7fffffu) > 0x400000u));
+}
+__device__ __forceinline__ int mx8_code(uint32_t top) {
+    return max(0, (int)(top >> 23) - 8 + ((top & 0x7fffffu) > 0x600000u));
+}
+__device__ __forceinline__ float scale_arg(int code) { return __uint_as_float((uint32_t)code << 23); }
+
+// 8 values as E2M1, the first in the lowest nibble.
+__device__ __forceinline__ uint32_t to_e2m1x8(const float* v, int code) {
+    const float s = scale_arg(code);
+    uint32_t p = 0;
+    p = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(p, v[0], v[1], s, 0);
+    p = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(p, v[2], v[3], s, 1);
+    p = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(p, v[4], v[5], s, 2);
+    p = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(p, v[6], v[7], s, 3);
+    return code == kMxNaN ? 0u : p;
+}
+
+// 4 values as E4M3, the first in the lowest byte.  A value other than zero keeps
+// at least the smallest code (2^-9 of the scale, 2^-17.8 of the block's largest
+// value), so a checkpoint still tells which units a ReLU let through.  NaN and
+// infinities become NaN: E4M3 has no infinity.
+__device__ __forceinline__ uint32_t to_e4m3x4(const float* v, int code) {
+    const float s = scale_arg(code);
+    // 2^-9 of the scale; below the normal numbers as far as fp32 goes
+    const float least = ldexpf(1.0f, code - 127 - 9);
+    float w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float m = v[i] == 0.0f ? 0.0f : fmaxf(fabsf(v[i]), least);
+        w[i] = copysignf(m, v[i]);
+    }
+    s16x2 p = {0, 0};
+    p = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(p, w[0], w[1], s, false);
+    p = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(p, w[2], w[3], s, true);
+    uint32_t q = __builtin_bit_cast(uint32_t, p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (abs_bits(v[i]) >= 0x7f800000u) q |= 0x7fu << (8 * i);
+    return q;
+}
+
+// 8 E2M1 or 4 E4M3 elements as fp32.
+__device__ __forceinline__ void from_e2m1x8(uint32_t p, int code, float* v) {
+    const float s = scale_arg(code);
+    sfor<4>([&](auto I) {
+        const f32x2 t = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(p, s, CV(I));
+        v[2 * CV(I)] = code == kMxNaN ? __uint_as_float(0x7fc00000u) : t[0];
+        v[2 * CV(I) + 1] = code == kMxNaN ? __uint_as_float(0x7fc00000u) : t[1];
+    });
+}
+__device__ __forceinline__ void from_e4m3x4(uint32_t p, int code, float* v) {
+    const float s = scale_arg(code);
+    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8((int)p, s, false);
+    const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8((int)p, s, true);
+    const float t[4] = {a[0], a[1], b[0], b[1]};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = code == kMxNaN ? __uint_as_float(0x7fc00000u) : t[i];
+}
+
+// 8 consecutive values of a row from column k on as fp32, zeros behind the last
+// of `cols`.  Rows may start at any multiple of their type's size: gfx950 takes
+// wide loads at such addresses.
+template <class T>
+struct Row8;
+template <>
+struct Row8<float> {
+    __device__ static __forceinline__ void load(const float* row, int k, int cols, float* v) {
+        if (k + 8 <= cols) {
+            __builtin_memcpy(v, row + k, 32);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = k + i < cols ? row[k + i] : 0.0f;
+        }
+    }
+    __device__ static __forceinline__ void store(float* row, int k, int cols, const float* v) {
+        if (k + 8 <= cols) {
+            __builtin_memcpy(row + k, v, 32);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (k + i < cols) row[k + i] = v[i];
+        }
+    }
+};
+template <>
+struct Row8<uint16_t> {   // bf16
+    __device__ static __forceinline__ u32x4 load_raw(const uint16_t* row, int k, int cols) {
+        u32x4 p = {0, 0, 0, 0};
+        if (k + 8 <= cols) {
+            __builtin_memcpy(&p, row + k, 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (k + i < cols) p[i / 2] |= (uint32_t)row[k + i] << (16 * (i & 1));
+        }
+        return p;
+    }
+    __device__ static __forceinline__ void load(const uint16_t* row, int k, int cols, float* v) {
+        const u32x4 p = load_raw(row, k, cols);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = __uint_as_float(p[i] << 16);
+            v[2 * i + 1] = __uint_as_float(p[i] & 0xffff0000u);
+        }
+    }
+    __device__ static __forceinline__ void store(uint16_t* row, int k, int cols, const float* v) {
+        uint32_t p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+        if (k + 8 <= cols) {
+            __builtin_memcpy(row + k, p, 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (k + i < cols) row[k + i] = (uint16_t)(p[i / 2] >> (16 * (i & 1)));
+        }
+    }
+};
+
+}  // namespace
+}  // namespace donerf

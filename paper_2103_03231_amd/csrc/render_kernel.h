@@ -25,39 +25,13 @@
 
 #include <hip/hip_runtime.h>
 
-#include <utility>
-
+#include "device.h"
 #include "internal.h"
 
 namespace donerf {
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-
-// ------------------------------------------------------------------ compile-time loops
-
-template <class F, int... I>
-__device__ __forceinline__ void sfor_impl(F& f, std::integer_sequence<int, I...>) {
-    (f(std::integral_constant<int, I>{}), ...);
-}
-template <int N, class F>
-__device__ __forceinline__ void sfor(F&& f) {
-    sfor_impl(f, std::make_integer_sequence<int, N>{});
-}
-#define CV(x) decltype(x)::value
-
 // ------------------------------------------------------------------ precision traits
-
-__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
-    f32x2 v = {lo, hi};
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
-}
 
 template <int PR>
 struct Prec;
@@ -111,13 +85,6 @@ struct Prec<kFP8> {
 
 // ------------------------------------------------------------------ LDS weight stream
 
-__device__ __forceinline__ void lds_barrier() {
-    // Orders LDS traffic only; outstanding global prefetches stay in flight.
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-}
-
 // Orders one wave's LDS accesses across its lanes: LDS executes a wave's
 // instructions in order, so only the compiler has to keep them in place.
 __device__ __forceinline__ void wave_lds_fence() {
@@ -134,13 +101,6 @@ constexpr int kChunkVec = kChunkBytes / 16;  // u32x4 per chunk
 #define DONERF_FRAG_AHEAD 10
 #endif
 constexpr int kFragAhead = DONERF_FRAG_AHEAD;
-
-// s_waitcnt with only the vector-memory counter constrained (gfx9 encoding).
-template <int VM>
-__device__ __forceinline__ void wait_vmcnt() {
-    static_assert(VM >= 0 && VM < 64, "vmcnt range");
-    __builtin_amdgcn_s_waitcnt((VM & 15) | ((VM >> 4) << 14) | (7 << 4) | (15 << 8));
-}
 
 // The workgroup consumes one logical sequence of chunks: every depth-network
 // chunk, then the shading-network chunks once per sample.  Chunks travel

@@ -1,0 +1,360 @@
+"""A layer's forward and backward pass with its activations kept in 8 bits, against
+the oracle and against differences, through the public entry points.
+
+bf16 products are exact in fp32 and E4M3 elements exact in bf16, so an fp32 result
+is off by its sums' roundings alone: at most (terms + 2) steps of 2^-23 of the
+terms' summed magnitudes.  bf16 results are off by half a bf16 step, 2^-8, more, and
+what is kept by half an E4M3 step at its block's scale."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import layers_oracle as L
+from paper_2103_03231_amd import binding as b
+from paper_2103_03231_amd import inputs
+from test_gpu_mx import device, host, numbers
+
+pytestmark = pytest.mark.gpu
+STEP = 2.0 ** -23
+BF16_HALF = torch.finfo(torch.bfloat16).eps / 2
+
+
+@pytest.fixture(scope="module")
+def r():
+    r = b.Renderer(b.Config(), inputs.make_weights(128, 0))
+    yield r
+    r.close()
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+def normal(seed, *shape, scale=1.0):
+    return (torch.randn(*shape, generator=torch.Generator().manual_seed(seed)) * scale).bfloat16().cuda()
+
+
+def close(got, ref, tol, extra=BF16_HALF):
+    """|got - ref| within the sums' bound and `extra` of a rounding of the result."""
+    got = f64(got) if isinstance(got, torch.Tensor) else got
+    d = np.abs(got - ref) - (tol + extra * (np.abs(ref) + tol))
+    assert (d <= 0).all(), (d.max(), np.argwhere(d > 0)[:4])
+
+
+def check_forward(r, x, w, bias, relu):
+    vb = None if bias is None else f64(bias)
+    ref = L.linear(f64(x), f64(w), vb, relu)
+    tol = (x.shape[1] + 2) * STEP * L.linear_magnitude(f64(x), f64(w), vb)
+    y, kept = r.train_linear(x, w, bias, relu)
+    close(y, ref, tol)
+    _, scales = host(kept)
+    v = numbers(kept)
+    assert (np.abs(v - ref) <= L.half_step(np.abs(ref) + tol, scales, "mxfp8") + tol).all()
+    # no larger a scale than the block's largest value asks for
+    blocks = -(-ref.shape[1] // 32)
+    top = np.abs(np.pad(ref, ((0, 0), (0, blocks * 32 - ref.shape[1])))).reshape(len(ref), blocks, 32).max(2)
+    slack = np.pad(tol, ((0, 0), (0, blocks * 32 - ref.shape[1]))).reshape(len(ref), blocks, 32).max(2)
+    assert (top + slack <= 448 * np.exp2(scales.astype(float) - 127) + 2 * slack).all()
+    assert ((top + slack >= 224 * np.exp2(scales.astype(float) - 127) * (1 - 1e-6)) | (scales == 0)).all()
+    if relu:   # the checkpoint tells which units passed, as y's fp32 value did
+        assert ((v == 0) | (f64(y) > 0) | (ref <= tol)).all() and ((v > 0) | (ref <= tol)).all()
+    y2, none = r.train_linear(x, w, bias, relu, keep=False)
+    assert none is None and torch.equal(y2, y)
+    return y, kept
+
+
+SIZES = [(1, 1, 1), (1, 256, 256), (2, 64, 33), (5, 8, 8), (13, 256, 128), (31, 31, 31), (33, 72, 40), (64, 64, 64), (65, 257, 129),
+         (100, 200, 300), (257, 255, 65), (1000, 256, 128), (1021, 283, 100), (3000, 90, 256), (40, 1000, 1100)]
+
+
+@pytest.mark.parametrize("relu", [False, True])
+@pytest.mark.parametrize("rows,n_in,n_out", SIZES)
+def test_forward(r, rows, n_in, n_out, relu):
+    x, w = normal(rows, rows, n_in), normal(n_in, n_out, n_in, scale=n_in ** -0.5)
+    check_forward(r, x, w, normal(1, n_out).float(), relu)
+    check_forward(r, x, w, None, relu)
+
+
+def check_backward(r, dz, x, w, relu, **kw):
+    vx = numbers(x) if isinstance(x, b.MxTensor) else f64(x)
+    dx, dw, db = r.train_linear_backward(dz, x, w, relu, **kw)
+    rx, rw, rb = L.backward(f64(dz), vx, f64(w), relu)
+    rows, n_out = dz.shape
+    mag = [np.abs(v) for v in (f64(dz), vx, f64(w))]
+    if dx is not None:
+        close(dx, rx, (n_out + 2) * STEP * (mag[0] @ mag[2]))
+        if relu:
+            assert (f64(dx)[vx == 0] == 0).all()
+    close(dw, rw, (rows + 2) * STEP * (mag[0].T @ mag[1]), 0.0)
+    close(db, rb, (rows + 2) * STEP * mag[0].sum(0), 0.0)
+    return dx, dw, db
+
+
+def activations(seed, rows, cols, relu):
+    x = torch.randn(rows, cols, generator=torch.Generator().manual_seed(seed))
+    return (torch.relu(x) if relu else x).bfloat16().cuda()
+
+
+@pytest.mark.parametrize("relu", [False, True])
+@pytest.mark.parametrize("kept", [False, True])
+@pytest.mark.parametrize("rows,n_in,n_out", SIZES)
+def test_backward(r, rows, n_in, n_out, kept, relu):
+    x = activations(rows, rows, n_in, relu)
+    dz, w = normal(2, rows, n_out, scale=1 / rows), normal(n_in, n_out, n_in, scale=n_in ** -0.5)
+    x = r.mx_quantize(x, b.MXFP8) if kept else x
+    first = check_backward(r, dz, x, w, relu)
+    again = r.train_linear_backward(dz, x, w, relu)
+    assert all(torch.equal(u, v) for u, v in zip(first, again))     # the same bits
+    none, dw, db = r.train_linear_backward(dz, x, w, relu, need_dx=False)
+    assert none is None and torch.equal(dw, first[1]) and torch.equal(db, first[2])
+
+
+@pytest.mark.parametrize("rows,n_in,n_out", [(20000, 64, 48), (70001, 33, 130), (9000, 300, 520)])
+def test_many_rows(r, rows, n_in, n_out):
+    x = r.mx_quantize(activations(3, rows, n_in, True), b.MXFP8)
+    vx = r.mx_dequantize(x, torch.float32).double()
+    dz, w = normal(4, rows, n_out, scale=1 / rows), normal(5, n_out, n_in, scale=0.1)
+    dx, dw, db = r.train_linear_backward(dz, x, w, True)
+    z = dz.double()
+    close(dx, f64((z @ w.double()) * (vx != 0)), f64((n_out + 2) * STEP * (z.abs() @ w.double().abs())))
+    # sums over the batch: splits of at most 64 rows a step, so far fewer roundings in a row than rows; the bound by rows holds
+    close(dw, f64(z.t() @ vx), f64((rows + 2) * STEP * (z.abs().t() @ vx.abs())), 0.0)
+    close(db, f64(z.sum(0)), f64((rows + 2) * STEP * z.abs().sum(0)), 0.0)
+    # and in the norm, where roundings of either sign average out: 2e-6 is 16 roundings in a row of half a step, 2^-24, each at full size
+    assert torch.linalg.norm(dw.double() - z.t() @ vx) <= 2e-6 * torch.linalg.norm(z.t() @ vx) + 2.0 ** -24 * torch.linalg.norm(z.abs().t() @ vx.abs())
+
+
+def test_accumulates(r):
+    for rows in (50, 5000):     # one part, and several that are summed afterwards
+        x, w = r.mx_quantize(activations(3, rows, 70, True), b.MXFP8), normal(5, 45, 70)
+        dz = normal(4, rows, 45)
+        _, dw, db = r.train_linear_backward(dz, x, w, True)
+        dw0, db0 = torch.randn(45, 70, device="cuda"), torch.randn(45, device="cuda")
+        gw, gb = dw0.clone(), db0.clone()
+        _, gw2, gb2 = r.train_linear_backward(dz, x, w, True, dw=gw, db=gb)
+        assert gw2 is gw and gb2 is gb and torch.equal(gw, dw0 + dw) and torch.equal(gb, db0 + db)
+
+
+def test_each_gradient_alone(r):
+    """Through the C names: any of the three outputs may be absent."""
+    for rows in (60, 4000):
+        x, w, dz = activations(1, rows, 40, True), normal(2, 30, 40), normal(3, rows, 30)
+        ref = r.train_linear_backward(dz, x, w, True)
+        need = b.donerf_train_linear_backward_workspace(r.h, rows, 40, 30)
+        ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+        bf, f32 = b.TYPE_BF16, b.TYPE_FP32
+        for which in range(1, 8):
+            dx = torch.full((rows, 40), 3.0, dtype=torch.bfloat16, device="cuda")
+            dw, db = torch.full((30, 40), 3.0, device="cuda"), torch.full((30,), 3.0, device="cuda")
+            b.donerf_train_linear_backward(r.h, (dz.data_ptr(), 30, bf), (x.data_ptr(), 40, bf), 1,
+                                           (w.data_ptr(), 40, bf) if which & 1 else None, (dx.data_ptr(), 40, bf) if which & 1 else None,
+                                           (dw.data_ptr(), 40, f32) if which & 2 else None, db.data_ptr() if which & 4 else None, 0,
+                                           rows, 40, 30, ws.data_ptr(), need)
+            for bit, (u, v) in enumerate(zip((dx, dw, db), ref)):
+                assert torch.equal(u, v) if which >> bit & 1 else (u == 3).all(), (which, bit)
+
+
+def test_no_rows(r):
+    w = normal(2, 30, 40)
+    x, dz = torch.empty(0, 40, dtype=torch.bfloat16, device="cuda"), torch.empty(0, 30, dtype=torch.bfloat16, device="cuda")
+    y, kept = r.train_linear(x, w)
+    assert y.shape == (0, 30) and kept.rows == 0
+    dx, dw, db = r.train_linear_backward(dz, r.mx_quantize(x, b.MXFP8), w)
+    assert dx.shape == (0, 40) and (dw == 0).all() and (db == 0).all() and dw.shape == (30, 40)
+    gw, gb = torch.ones(30, 40, device="cuda"), torch.ones(30, device="cuda")
+    r.train_linear_backward(dz, x, w, dw=gw, db=gb)
+    assert (gw == 1).all() and (gb == 1).all()
+
+
+def test_strides_and_surroundings(r):
+    """Cut-outs of wider matrices at odd addresses as inputs and outputs."""
+    def cut(rows, cols, dtype=torch.bfloat16, fill=5.0):
+        big = torch.full(((rows + 3) * (cols + 37) + 1,), fill, dtype=dtype, device="cuda")[1:].view(rows + 3, cols + 37)
+        return big, big[1:1 + rows, 3:3 + cols]
+
+    rows, n_in, n_out = 150, 72, 56
+    x, w, dz = activations(1, rows, n_in, True), normal(2, n_out, n_in), normal(3, rows, n_out)
+    parts = []
+    for t in (x, w, dz):
+        big, c = cut(*t.shape, fill=float("nan"))    # what lies between the rows must not be read into results
+        c.copy_(t)
+        parts.append(c)
+    y, kept = r.train_linear(x, w, None, True)
+    y2, kept2 = r.train_linear(parts[0], parts[1], None, True)
+    assert torch.equal(y, y2) and torch.equal(kept.codes, kept2.codes)
+    ref = r.train_linear_backward(dz, x, w, True)
+    got = r.train_linear_backward(parts[2], parts[0], parts[1], True)
+    assert all(torch.equal(u, v) for u, v in zip(ref, got))
+    by, cy = cut(rows, n_out)
+    codes, scales = torch.full((rows + 2, 96), 5, dtype=torch.uint8, device="cuda"), torch.full((rows + 2, 16), 5, dtype=torch.uint8, device="cuda")
+    q = b.MxTensor(codes[1:rows + 1, 16:80], scales[1:rows + 1, 8:16], n_out, b.MXFP8)
+    bf = torch.bfloat16
+    b.donerf_train_linear(r.h, r._rows("x", x, (bf,), device=0), r._rows("w", w, (bf,), device=0), None, 1, r._rows("y", cy, (bf,), device=0),
+                          r._mx("kept", q, (b.MXFP8,), device=0), rows, n_in, n_out)
+    assert torch.equal(cy, y) and all(np.array_equal(u, v) for u, v in zip(host(q), host(kept)))
+    cy.fill_(5.0)
+    codes[1:rows + 1, 16:80] = 5
+    scales[1:rows + 1, 8:10] = 5
+    assert (by == 5).all() and (codes == 5).all() and (scales == 5).all()
+    bx, cx = cut(rows, n_in)
+    bw, cw = cut(n_out, n_in, torch.float32)
+    db = torch.full((n_out + 2,), 5.0, device="cuda")
+    need = b.donerf_train_linear_backward_workspace(r.h, rows, n_in, n_out)
+    ws = torch.full((need + 64,), 5, dtype=torch.uint8, device="cuda")
+    b.donerf_train_linear_backward(r.h, r._rows("dz", dz, (bf,), device=0), r._rows("x", x, (bf,), device=0), 1, r._rows("w", w, (bf,), device=0),
+                                   r._rows("dx", cx, (bf,), device=0), r._rows("dw", cw, (torch.float32,), device=0), db[1:].data_ptr(), 0,
+                                   rows, n_in, n_out, ws.data_ptr(), need)
+    assert torch.equal(cx, ref[0]) and torch.equal(cw, ref[1]) and torch.equal(db[1:-1], ref[2])
+    cx.fill_(5.0)
+    cw.fill_(5.0)
+    assert (bx == 5).all() and (bw == 5).all() and db[0] == 5 and db[-1] == 5 and (ws[need:] == 5).all()
+
+
+def test_rows_far_apart(r):
+    """Offsets past 2^32 bytes."""
+    pitch, rows = 1 << 21, 2100
+    store = torch.empty(pitch * (rows - 1) + 64, dtype=torch.bfloat16, device="cuda")
+    far = lambda t: store.as_strided((rows, t.shape[1]), (pitch, 1)).copy_(t)
+    x, w, dz = activations(1, rows, 64, True), normal(2, 40, 64), normal(3, rows, 40)
+    y, kept = r.train_linear(x, w)
+    y2, kept2 = r.train_linear(far(x), w)
+    assert torch.equal(y, y2) and torch.equal(kept.codes, kept2.codes)
+    q = r.mx_quantize(x, b.MXFP8)
+    ref = r.train_linear_backward(dz, q, w, True)
+    assert all(torch.equal(u, v) for u, v in zip(ref, r.train_linear_backward(far(dz), q, w, True)))
+    codes = store.view(torch.uint8).as_strided((rows, 64), (2 * pitch, 1))
+    codes.copy_(q.codes)
+    assert all(torch.equal(u, v) for u, v in zip(ref, r.train_linear_backward(dz, b.MxTensor(codes, q.scales, 64, b.MXFP8), w, True)))
+
+
+def test_not_finite(r):
+    """NaN and infinities reach the results that they belong to and no others."""
+    x, w, dz = activations(1, 200, 70, True), normal(2, 40, 70), normal(3, 200, 40)
+    x[7, 3] = float("nan")
+    w[5, 60] = float("inf")
+    y, kept = r.train_linear(x, w, None, True)
+    v, z = numbers(kept), f64(y)
+    assert np.isnan(z[7]).all() and np.isnan(v[7]).all()      # ReLU keeps NaN
+    bad = ~np.isfinite(z)
+    assert not bad[np.arange(200) != 7][:, np.arange(40) != 5].any() and np.array_equal(np.isnan(v), bad)
+    q = r.mx_quantize(x, b.MXFP8)
+    dx, dw, db = r.train_linear_backward(dz, q, normal(2, 40, 70), True)
+    assert np.isfinite(f64(dx)).all() and np.isfinite(f64(db)).all()
+    assert np.isnan(f64(dw)[:, 3]).all() and np.isfinite(np.delete(f64(dw), 3, 1)).all()
+    assert (f64(dx)[7, 3] != 0)       # the gradient passes where the activation was NaN
+    dz[9, 2] = float("inf")
+    dx, dw, db = r.train_linear_backward(dz, q, normal(2, 40, 70), True)
+    assert np.isinf(f64(db)[2]) and np.isfinite(np.delete(f64(db), 2)).all() and not np.isfinite(f64(dw)[2]).any()
+    assert np.isfinite(np.delete(f64(dx), 9, 0)).all()
+    # the smallest activations pass the gradient on: 2^-60 of the block's largest value
+    x = torch.zeros(4, 64, dtype=torch.bfloat16, device="cuda")
+    x[:, 0], x[:, 1] = 1.0, 2.0 ** -60
+    dx, _, _ = r.train_linear_backward(dz[:4], r.mx_quantize(x, b.MXFP8), normal(2, 40, 64), True)
+    assert (f64(dx)[:, :2] != 0).all() and (f64(dx)[:, 2:] == 0).all()
+
+
+def test_gradients_against_differences(r):
+    """Of the 64-bit forward pass, at activations that E4M3 holds exactly.  The
+    loss is linear in each argument within its half step of 1/64."""
+    rng = np.random.default_rng(8)
+    u = rng.choice([-1.0, -0.5, 0.25, 0.5, 0.75, 1.0, 1.5], (6, 40))
+    dz, w, bias = (torch.from_numpy(rng.standard_normal(s)).bfloat16().double().numpy() for s in ((6, 33), (33, 40), (33,)))
+    loss = lambda u, w, bias: float((dz * L.linear(np.maximum(u, 0), w, bias)).sum())
+    t = lambda v: torch.from_numpy(v).bfloat16().cuda()
+    got = r.train_linear_backward(t(dz), r.mx_quantize(t(np.maximum(u, 0)), b.MXFP8), t(w), True)
+    terms = (np.abs(dz) @ np.abs(w), np.abs(dz).T @ np.abs(np.maximum(u, 0)), np.abs(dz).sum(0))
+    for i, (v, g, mag) in enumerate(zip((u, w, bias), got, terms)):
+        for at in list(np.ndindex(v.shape))[::7]:
+            d = np.zeros(v.shape)
+            d[at] = 1 / 64
+            hi, lo = [u, w, bias], [u, w, bias]
+            hi[i], lo[i] = v + d, v - d
+            diff = (loss(*hi) - loss(*lo)) * 32
+            tol = 42 * STEP * mag[at]
+            assert abs(diff - float(f64(g)[at])) <= tol + (BF16_HALF * (abs(diff) + tol) if i == 0 else 0) + 1e-10, (i, at)
+
+
+def test_training_step_of_the_depth_network(r):
+    """The depth network's layers run as a training step: targets from depth maps,
+    the forward pass with kept activations, the gradient of the cross entropy, and
+    the backward pass down to the first layer, each call against the oracle on its
+    own inputs; then the hidden weights in 4 bits and the same rows through them."""
+    B, rows = 128, 32 * 24
+    torch.manual_seed(9)
+    depth = torch.rand(1, 24, 32, device="cuda") * 9 + 0.5
+    target = r.targets(depth, 5, 5).view(rows, B)
+    sizes = [90] + [256] * 7 + [B]
+    x = normal(1, rows, 90)
+    ws = [((torch.rand(o, i, device="cuda") * 2 - 1) * (6 / i) ** 0.5).bfloat16() for i, o in zip(sizes, sizes[1:])]
+    bs = [torch.randn(o, device="cuda") * 0.1 for o in sizes[1:]]
+    h, kept = x, [x]
+    for i, (w, bias) in enumerate(zip(ws, bs)):
+        h, q = check_forward(r, h, w, bias, i < 7)
+        kept.append(q)
+    dz = ((torch.sigmoid(h.float()) - target) / rows).bfloat16()
+    for i in reversed(range(8)):
+        dz, dw, db = check_backward(r, dz, kept[i], ws[i], i > 0, need_dx=i > 0)
+        assert dw.shape == ws[i].shape
+    assert dz is None
+    h = r.train_linear(x, ws[0], bs[0], True, keep=False)[0]
+    for w, bias in zip(ws[1:7], bs[1:7]):
+        q = r.mx_quantize(w, b.MXFP4)
+        vx = L.values(*L.quantize(f64(h), "mxfp4"), 256, "mxfp4")
+        ref, mag = L.linear(vx, numbers(q), f64(bias), True), L.linear_magnitude(vx, numbers(q), f64(bias))
+        h = r.mx_linear(h, q, bias, True)
+        close(h, ref, 258 * STEP * mag)
+
+
+def test_refusals(r):
+    x, w, dz = activations(1, 20, 40, True), normal(2, 30, 40), normal(3, 20, 30)
+    q = r.mx_quantize(x, b.MXFP8)
+    for bad in (lambda: r.train_linear(x.float(), w), lambda: r.train_linear(x, w.float()), lambda: r.train_linear(x, w.t()),
+                lambda: r.train_linear(x[:, :32], w), lambda: r.train_linear(q, w), lambda: r.train_linear(x, w, torch.randn(31, device="cuda")),
+                lambda: r.train_linear(x, w, w[0]), lambda: r.train_linear(x, w[:0]),
+                lambda: r.train_linear_backward(dz.float(), q, w), lambda: r.train_linear_backward(dz[:10], q, w),
+                lambda: r.train_linear_backward(dz, q, w[:20]), lambda: r.train_linear_backward(dz, r.mx_quantize(x, b.MXFP4), w),
+                lambda: r.train_linear_backward(dz, q, w, dw=torch.zeros(30, 40, device="cuda")),
+                lambda: r.train_linear_backward(dz, q, w, dw=torch.zeros(40, 30, device="cuda"), db=torch.zeros(30, device="cuda"))):
+        with pytest.raises(ValueError):
+            bad()
+    need = b.donerf_train_linear_backward_workspace(r.h, 20, 40, 30)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    bf = torch.bfloat16
+    with pytest.raises(b.DonerfError) as e:
+        b.donerf_train_linear_backward(r.h, r._rows("dz", dz, (bf,), device=0), r._rows("x", x, (bf,), device=0), 0, None, None, None,
+                                       dz.data_ptr(), 0, 20, 40, 30, ws.data_ptr(), need - 1)
+    assert e.value.status == b.E_SIZE
+
+
+def test_replays_from_a_graph(r):
+    """Forward and backward captured together, with an eager handle's work of the
+    same tensors between the replays; two graphs, each with workspaces of its own."""
+    x, w, dz = activations(1, 3000, 72, True), normal(2, 48, 72), normal(3, 3000, 48)
+    other = b.Renderer(b.Config(), inputs.make_weights(128, 0))
+
+    def work(r):
+        q = r.mx_quantize(x, b.MXFP8)
+        y, kept = r.train_linear(x, w, None, True)
+        return (y, kept.codes, *r.train_linear_backward(dz, q, w, True))
+
+    ref = [t.clone() for t in work(r)]
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            b.donerf_set_stream(r.h, torch.cuda.current_stream().cuda_stream)
+            out = work(r)
+        graphs.append((g, out))
+    b.donerf_set_stream(r.h, torch.cuda.current_stream().cuda_stream)
+    for _ in range(3):
+        for g, out in graphs:
+            for t in out:
+                t.zero_()
+            g.replay()
+        torch.cuda.synchronize()
+        for g, out in graphs:
+            assert all(torch.equal(u, v) for u, v in zip(out, ref))
+        assert all(torch.equal(u, v) for u, v in zip(work(other), ref))
+    del graphs
+    other.close()

@@ -246,8 +246,7 @@ def _mat(m):
     (data, ld, type, scales, ld_scales) of microscaled ones, addresses as integers."""
     if m is None:
         return None
-    data, ld, kind = m[:3]
-    scales, ld_scales = m[3:] or (None, 0)
+    data, ld, kind, scales, ld_scales = m if len(m) == 5 else (*m, None, 0)
     return ctypes.byref(donerf_mat(data, ld, scales, ld_scales, kind))
 
 
@@ -315,6 +314,9 @@ class Renderer:
         self.cfg = cfg
         self.h = donerf_create(cfg, weights)
         donerf_set_stream(self.h, torch.cuda.current_stream().cuda_stream)
+        # where donerf_get_stream answers
+        self._device, self._stream = ctypes.c_int32(), ctypes.c_void_p()
+        self._device_ref, self._stream_ref = ctypes.byref(self._device), ctypes.byref(self._stream)
 
     def close(self):
         if self.h:
@@ -340,80 +342,111 @@ class Renderer:
     # ---- layer operators.  Matrices are 2-D tensors with unit column stride (any row
     # stride); they and the current stream must be those of the handle.
 
+    # Checks are written for few attribute reads: on small calls they are most
+    # of the time.
+
     def _bind(self):
         """The handle's device, once it is certain that outputs allocated now
         belong to the stream that the kernels will run on."""
-        device, stream = donerf_get_stream(self.h)
-        if self.torch.cuda.current_device() != device:
+        _check(lib().donerf_get_stream(self.h, self._device_ref, self._stream_ref))
+        device, c = self._device.value, self.torch._C
+        if c._cuda_getDevice() != device:
             raise ValueError(f"the handle is on cuda:{device}, which is not the current device")
-        if self.torch.cuda.current_stream().cuda_stream != stream:
+        # the address of torch.cuda.current_stream(), without building the object
+        if c._cuda_getCurrentRawStream(device) != (self._stream.value or 0):
             raise ValueError("torch's current stream is not the handle's (donerf_set_stream)")
         return device
 
     def _rows(self, name, x, dtypes, shape=None, device=None):
         t = self.torch
-        if not isinstance(x, t.Tensor) or x.dim() != 2 or x.dtype not in dtypes:
+        if not isinstance(x, t.Tensor) or x.dtype not in dtypes or x.dim() != 2:
             raise ValueError(f"{name} must be a 2-D tensor of {' or '.join(str(d) for d in dtypes)}")
-        if not x.is_cuda or x.device.index != device:
+        if x.get_device() != device:
             raise ValueError(f"{name} must be on the handle's device")
-        if shape is not None and tuple(x.shape) != tuple(shape):
-            raise ValueError(f"{name} is {tuple(x.shape)}, not {tuple(shape)}")
         rows, cols = x.shape
-        if cols < 1 or cols > MAX_COLS:
+        if shape is not None and (rows, cols) != shape:
+            raise ValueError(f"{name} is {(rows, cols)}, not {shape}")
+        if not 1 <= cols <= MAX_COLS:
             raise ValueError(f"{name} has {cols} columns: 1 to {MAX_COLS} are taken")
-        if cols > 1 and x.stride(1) != 1 or rows > 1 and x.stride(0) < cols:
+        ld, step = x.stride()
+        if rows <= 1:
+            ld = cols
+        if step != 1 and cols > 1 or ld < cols:
             raise ValueError(f"{name}: columns must be adjacent and rows must not overlap")
-        return x.data_ptr(), (x.stride(0) if rows > 1 else cols), TYPE_FP32 if x.dtype == t.float32 else TYPE_BF16
+        return x.data_ptr(), ld, TYPE_FP32 if x.dtype is t.float32 else TYPE_BF16, None, 0
 
     def _mx(self, name, q, formats, shape=None, device=None):
         t = self.torch
         if not isinstance(q, MxTensor) or q.format not in formats:
             raise ValueError(f"{name} must be a microscaled tensor of format {' or '.join(str(f) for f in formats)}")
-        if shape is not None and (q.rows, q.cols) != tuple(shape):
-            raise ValueError(f"{name} is {(q.rows, q.cols)}, not {tuple(shape)}")
-        blocks = -(-q.cols // 32)
-        width = blocks * (16 if q.format == MXFP4 else 32)
-        for part, x, least, unit in (("codes", q.codes, width, 16), ("scales", q.scales, -(-blocks // 8) * 8, 8)):
-            if not (isinstance(x, t.Tensor) and x.dtype == t.uint8 and x.dim() == 2 and x.is_cuda and x.device.index == device):
-                raise ValueError(f"{name}: {part} must be a 2-D uint8 tensor on the handle's device")
-            if x.shape[0] != q.rows or x.shape[1] < least or x.stride(1) != 1 or q.rows > 1 and x.stride(0) < least:
-                raise ValueError(f"{name}: {part} must hold {q.rows} rows of {least} bytes")
-        pitch = lambda x, least: x.stride(0) if q.rows > 1 else least
-        return (q.codes.data_ptr(), pitch(q.codes, width), q.format, q.scales.data_ptr(),
-                pitch(q.scales, -(-blocks // 8) * 8))
+        codes, scales, cols = q.codes, q.scales, q.cols
+        if not (isinstance(codes, t.Tensor) and isinstance(scales, t.Tensor) and codes.dtype is t.uint8 and scales.dtype is t.uint8
+                and codes.dim() == 2 and scales.dim() == 2 and codes.get_device() == device and scales.get_device() == device):
+            raise ValueError(f"{name}: codes and scales must be 2-D uint8 tensors on the handle's device")
+        (rows, wide), (rows_s, wide_s) = codes.shape, scales.shape
+        if shape is not None and (rows, cols) != shape:
+            raise ValueError(f"{name} is {(rows, cols)}, not {shape}")
+        if not 1 <= cols <= MAX_COLS:
+            raise ValueError(f"{name} has {cols} columns: 1 to {MAX_COLS} are taken")
+        blocks = (cols + 31) // 32
+        least, least_s = blocks * (16 if q.format == MXFP4 else 32), (blocks + 7) // 8 * 8
+        (ld, step), (ld_s, step_s) = codes.stride(), scales.stride()
+        if rows <= 1:
+            ld, ld_s = least, least_s
+        if rows_s != rows or wide < least or wide_s < least_s or ld < least or ld_s < least_s or step != 1 or step_s != 1:
+            raise ValueError(f"{name}: codes must hold {rows} rows of {least} bytes and scales {rows} of {least_s}")
+        return codes.data_ptr(), ld, q.format, scales.data_ptr(), ld_s
 
     def _vector(self, name, v, n, device):
         if v is None:
             return None
         t = self.torch
-        if not (isinstance(v, t.Tensor) and v.dtype == t.float32 and v.is_cuda and v.device.index == device
-                and v.is_contiguous() and tuple(v.shape) == (n,)):
+        if not (isinstance(v, t.Tensor) and v.dtype is t.float32 and v.get_device() == device and v.dim() == 1
+                and v.shape[0] == n and v.is_contiguous()):
             raise ValueError(f"{name} must be a contiguous float32 tensor of {n} on the handle's device")
         return v.data_ptr()
 
+    def _new(self, rows, cols, dtype, device):
+        """A new matrix and itself as an argument."""
+        y = self.torch.empty((rows, cols), dtype=dtype, device=device)
+        return y, (y.data_ptr(), cols, TYPE_FP32 if dtype is self.torch.float32 else TYPE_BF16, None, 0)
+
+    def _mx_new(self, rows, cols, format, device):
+        empty, u8 = self.torch.empty, self.torch.uint8
+        blocks = (cols + 31) // 32
+        ld, ld_s = blocks * (16 if format == MXFP4 else 32), (blocks + 7) // 8 * 8
+        q = MxTensor(empty((rows, ld), dtype=u8, device=device), empty((rows, ld_s), dtype=u8, device=device), cols, format)
+        return q, (q.codes.data_ptr(), ld, format, q.scales.data_ptr(), ld_s)
+
+    def _workspace(self, n, device):
+        return self.torch.empty(n, dtype=self.torch.uint8, device=device) if n else None
+
     def mx_empty(self, rows, cols, format):
-        """An uninitialised microscaled matrix on the current device."""
-        t = self.torch
+        """An uninitialised microscaled matrix on the handle's device."""
         if format not in (MXFP4, MXFP8) or rows < 0 or not 1 <= cols <= MAX_COLS:
             raise ValueError("no such microscaled matrix")
-        blocks = -(-cols // 32)
-        return MxTensor(t.empty((rows, blocks * (16 if format == MXFP4 else 32)), dtype=t.uint8, device="cuda"),
-                        t.empty((rows, -(-blocks // 8) * 8), dtype=t.uint8, device="cuda"), cols, format)
+        return self._mx_new(rows, cols, format, self._bind())[0]
 
     def mx_quantize(self, x, format):
         """(rows, cols) fp32 or bf16 -> MxTensor (donerf_mx_quantize)."""
         t, dev = self.torch, self._bind()
-        mx = self._rows("x", x, (t.float32, t.bfloat16), device=dev)
-        q = self.mx_empty(x.shape[0], x.shape[1], format)
-        donerf_mx_quantize(self.h, mx, self._mx("q", q, (MXFP4, MXFP8), device=dev), *x.shape)
+        mx = self._rows("x", x, (t.float32, t.bfloat16), None, dev)
+        if format not in (MXFP4, MXFP8):
+            raise ValueError("format must be MXFP4 or MXFP8")
+        rows, cols = x.shape
+        q, mq = self._mx_new(rows, cols, format, dev)
+        donerf_mx_quantize(self.h, mx, mq, rows, cols)
         return q
 
     def mx_dequantize(self, q, dtype=None):
         """MxTensor -> (rows, cols) bf16 (default) or fp32 (donerf_mx_dequantize)."""
         t, dev = self.torch, self._bind()
-        mq = self._mx("q", q, (MXFP4, MXFP8), device=dev)
-        y = t.empty((q.rows, q.cols), dtype=dtype or t.bfloat16, device="cuda")
-        donerf_mx_dequantize(self.h, mq, self._rows("y", y, (t.float32, t.bfloat16), device=dev), q.rows, q.cols)
+        mq = self._mx("q", q, (MXFP4, MXFP8), None, dev)
+        dtype = dtype or t.bfloat16
+        if dtype not in (t.float32, t.bfloat16):
+            raise ValueError("dtype must be torch.float32 or torch.bfloat16")
+        y, my = self._new(q.rows, q.cols, dtype, dev)
+        donerf_mx_dequantize(self.h, mq, my, q.rows, q.cols)
         return y
 
     def mx_linear(self, x, w, bias=None, relu=False, out=None):
@@ -422,40 +455,46 @@ class Renderer:
         torch.float32 or MXFP4, the result's type, or a tensor that takes it."""
         t, dev = self.torch, self._bind()
         if isinstance(x, MxTensor):
+            mx = self._mx("x", x, (MXFP4,), None, dev)
             rows, n_in = x.rows, x.cols
-            mx = self._mx("x", x, (MXFP4,), device=dev)
         else:
-            mx = self._rows("x", x, (t.float32, t.bfloat16), device=dev)
+            mx = self._rows("x", x, (t.float32, t.bfloat16), None, dev)
             rows, n_in = x.shape
-        mw = self._mx("w", w, (MXFP4,), device=dev)
+        mw = self._mx("w", w, (MXFP4,), None, dev)
         if w.cols != n_in:
             raise ValueError(f"x has {n_in} columns and w {w.cols}")
         n_out = w.rows
+        if not 1 <= n_out <= MAX_COLS:
+            raise ValueError(f"w has {n_out} rows: 1 to {MAX_COLS} are taken")
         pb = self._vector("bias", bias, n_out, dev)
-        if isinstance(out, int):
-            y = self.mx_empty(rows, n_out, out)
+        if isinstance(out, MxTensor):
+            y, my = out, self._mx("out", out, (MXFP4,), (rows, n_out), dev)
+        elif isinstance(out, t.Tensor):
+            y, my = out, self._rows("out", out, (t.float32, t.bfloat16), (rows, n_out), dev)
+        elif out is None or out in (t.float32, t.bfloat16):
+            y, my = self._new(rows, n_out, out or t.bfloat16, dev)
+        elif out == MXFP4:
+            y, my = self._mx_new(rows, n_out, MXFP4, dev)
         else:
-            y = out if isinstance(out, (t.Tensor, MxTensor)) else t.empty((rows, n_out), dtype=out or t.bfloat16, device="cuda")
-        my = (self._mx("out", y, (MXFP4,), (rows, n_out), dev) if isinstance(y, MxTensor)
-              else self._rows("out", y, (t.float32, t.bfloat16), (rows, n_out), dev))
+            raise ValueError("out must be torch.bfloat16, torch.float32, MXFP4 or a tensor")
         need = donerf_mx_linear_workspace(mx[2], rows, n_in)
-        ws = t.empty(need, dtype=t.uint8, device="cuda") if need else None
-        donerf_mx_linear(self.h, mx, mw, pb, int(bool(relu)), my, rows, n_in, n_out, ws.data_ptr() if need else None, need)
+        ws = self._workspace(need, dev)
+        donerf_mx_linear(self.h, mx, mw, pb, 1 if relu else 0, my, rows, n_in, n_out, ws.data_ptr() if need else None, need)
         return y
 
     def train_linear(self, x, w, bias=None, relu=False, keep=True):
         """A layer's forward pass (donerf_train_linear): x (rows, in) and w (out,
         in) bf16 -> (y (rows, out) bf16, the same in MXFP8 or None without keep)."""
         t, dev = self.torch, self._bind()
-        mx, mw = self._rows("x", x, (t.bfloat16,), device=dev), self._rows("w", w, (t.bfloat16,), device=dev)
-        (rows, n_in), n_out = x.shape, w.shape[0]
-        if w.shape[1] != n_in or n_out < 1:
+        bf16 = (t.bfloat16,)
+        mx, mw = self._rows("x", x, bf16, None, dev), self._rows("w", w, bf16, None, dev)
+        (rows, n_in), (n_out, w_in) = x.shape, w.shape
+        if w_in != n_in or not 1 <= n_out <= MAX_COLS:
             raise ValueError(f"x is {tuple(x.shape)} and w {tuple(w.shape)}")
         pb = self._vector("bias", bias, n_out, dev)
-        y = t.empty((rows, n_out), dtype=t.bfloat16, device="cuda")
-        kept = self.mx_empty(rows, n_out, MXFP8) if keep else None
-        donerf_train_linear(self.h, mx, mw, pb, int(bool(relu)), self._rows("y", y, (t.bfloat16,), device=dev),
-                            self._mx("kept", kept, (MXFP8,), device=dev) if keep else None, rows, n_in, n_out)
+        y, my = self._new(rows, n_out, t.bfloat16, dev)
+        kept, mk = self._mx_new(rows, n_out, MXFP8, dev) if keep else (None, None)
+        donerf_train_linear(self.h, mx, mw, pb, 1 if relu else 0, my, mk, rows, n_in, n_out)
         return y, kept
 
     def train_linear_backward(self, dz, x, w, relu=False, need_dx=True, dw=None, db=None):
@@ -464,25 +503,27 @@ class Renderer:
         out of a ReLU; w (out, in) bf16 -> (dx bf16 or None, dw fp32, db fp32).
         Where dw and db are given, they are added to."""
         t, dev = self.torch, self._bind()
-        mz, mw = self._rows("dz", dz, (t.bfloat16,), device=dev), self._rows("w", w, (t.bfloat16,), device=dev)
-        (rows, n_out), n_in = dz.shape, w.shape[1]
-        if w.shape[0] != n_out:
+        bf16 = (t.bfloat16,)
+        mz, mw = self._rows("dz", dz, bf16, None, dev), self._rows("w", w, bf16, None, dev)
+        (rows, n_out), (w_out, n_in) = dz.shape, w.shape
+        if w_out != n_out:
             raise ValueError(f"dz is {tuple(dz.shape)} and w {tuple(w.shape)}")
         mx = (self._mx("x", x, (MXFP8,), (rows, n_in), dev) if isinstance(x, MxTensor)
-              else self._rows("x", x, (t.bfloat16,), (rows, n_in), dev))
-        if (dw is None) != (db is None):
-            raise ValueError("dw and db are given together or not at all")
+              else self._rows("x", x, bf16, (rows, n_in), dev))
         add = dw is not None
-        if not add:
-            dw = t.empty((n_out, n_in), dtype=t.float32, device="cuda")
-            db = t.empty(n_out, dtype=t.float32, device="cuda")
-        mdw, pdb = self._rows("dw", dw, (t.float32,), (n_out, n_in), dev), self._vector("db", db, n_out, dev)
-        dx = t.empty((rows, n_in), dtype=t.bfloat16, device="cuda") if need_dx else None
+        if add != (db is not None):
+            raise ValueError("dw and db are given together or not at all")
+        if add:
+            mdw = self._rows("dw", dw, (t.float32,), (n_out, n_in), dev)
+        else:
+            dw, mdw = self._new(n_out, n_in, t.float32, dev)
+            db = t.empty(n_out, dtype=t.float32, device=dev)
+        pdb = self._vector("db", db, n_out, dev)
+        dx, mdx = self._new(rows, n_in, t.bfloat16, dev) if need_dx else (None, None)
         need = donerf_train_linear_backward_workspace(self.h, rows, n_in, n_out)
-        ws = t.empty(need, dtype=t.uint8, device="cuda")
-        donerf_train_linear_backward(self.h, mz, mx, int(bool(relu)), mw,
-                                     self._rows("dx", dx, (t.bfloat16,), device=dev) if need_dx else None, mdw, pdb,
-                                     int(add), rows, n_in, n_out, ws.data_ptr(), need)
+        ws = self._workspace(need, dev)
+        donerf_train_linear_backward(self.h, mz, mx, 1 if relu else 0, mw, mdx, mdw, pdb, 1 if add else 0,
+                                     rows, n_in, n_out, ws.data_ptr() if need else None, need)
         return dx, dw, db
 
     def mfma_peak(self, workgroups, iters):

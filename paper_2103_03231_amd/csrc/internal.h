@@ -154,16 +154,14 @@ struct MxOut {
 };
 
 // A product y[m][n] = sum_k a[n][k] b[m][k] and what follows it (layer_gemm.h).
-constexpr int kMaskNone = 0, kMaskMx8 = 1, kMaskBf16 = 2;
 struct GemmArgs {
     MxIn a, b;               // N and M rows of K columns
     const float* bias;       // N, or null
     uint8_t* y;              // bf16 or fp32 rows, or null
     int64_t ldy;             // values from row to row
     MxOut q;                 // microscaled outputs
-    const uint8_t* mask;     // E4M3 codes or bf16 rows
+    const uint8_t* mask;     // E4M3 codes or bf16 rows of masked epilogues
     int64_t ld_mask;         // bytes (E4M3) or values (bf16)
-    int32_t mask_type;
     int32_t M, N, K;
     int32_t relu;
     uint32_t tiles_n, tiles_m;

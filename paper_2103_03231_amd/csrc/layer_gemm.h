@@ -26,72 +26,154 @@ constexpr int kStageBytes = 128;   // of each row
 constexpr int kStageChunks = kStageBytes / 16;
 
 // What follows the product.
-constexpr int kEpiBf16 = 0;    // y bf16
-constexpr int kEpiF32 = 1;     // y fp32
-constexpr int kEpiMx4 = 2;     // y E2M1
-constexpr int kEpiKept = 3;    // y bf16 and its E4M3 checkpoint, either may be absent
-constexpr int kEpiMasked = 4;  // y bf16, zero where the ReLU's output (E4M3 or bf16) is
+constexpr int kEpiBf16 = 0;      // y bf16
+constexpr int kEpiF32 = 1;       // y fp32
+constexpr int kEpiMx4 = 2;       // y E2M1
+constexpr int kEpiKept = 3;      // y bf16 and its E4M3 checkpoint, either may be absent
+constexpr int kEpiMaskMx8 = 4;   // y bf16, zero where the ReLU's output (E4M3) is
+constexpr int kEpiMaskBf16 = 5;  // the same, the ReLU's output in bf16
+constexpr bool masked(int epi) { return epi == kEpiMaskMx8 || epi == kEpiMaskBf16; }
 
 // 16 zero bytes: what a lane copies in place of chunks behind the last column.
 __device__ const uint32_t kZeroChunk[4] = {0, 0, 0, 0};
 
-// 16 bytes of a row: 8 bf16 or a block of 32 E2M1.  Zeros behind the last column.
-template <int OP>
-__device__ __forceinline__ u32x4 load_chunk(const uint8_t* row, int chunk, int K) {
-    if (OP == kOpBf16) {
-        if (chunk * 8 >= K) return u32x4{0, 0, 0, 0};
-        return Row8<uint16_t>::load_raw((const uint16_t*)row, chunk * 8, K);
-    }
-    return chunk * kMxBlock < K ? *(const u32x4*)(row + (size_t)chunk * 16) : u32x4{0, 0, 0, 0};
-}
-
-// Copies of one operand's rows [row0, row0 + ROWS) into a stage in LDS.
+// Copies of one operand's rows [row0, row0 + ROWS) into a stage in LDS: straight
+// into it (DIRECT: rows of whole, 16-byte aligned chunks), or, for bf16 rows of
+// any other kind, by way of registers that are stored after the products which
+// run meanwhile.
 template <int OP, int ROWS, int NW, bool DIRECT>
 struct StageCopy {
     static constexpr int PER = ROWS / 8 / NW;   // copies per wave, 8 rows each
     static_assert(ROWS % (8 * NW) == 0, "rows split evenly over the waves");
-    const uint8_t* row[PER];   // of this lane, in each copy
+    static_assert(DIRECT || OP == kOpBf16, "microscaled rows are aligned");
+    const uint8_t* row[DIRECT ? PER : 1];   // of this lane, in each copy
     u32x4 held[DIRECT ? 1 : PER];
+    Bf16Rows any;
+    int64_t first;             // row of this lane in the wave's first copy
     int chunk;                 // of this lane, in every row
-    __device__ __forceinline__ void init(const MxIn& src, int64_t row0, int64_t rows, int wave, int lane) {
+    __device__ __forceinline__ void init(const MxIn& src, int64_t row0, int64_t rows, int K, int wave, int lane) {
         chunk = (lane & 7) ^ (lane >> 3);
+        first = row0 + wave * 8 + (lane >> 3);
+        if constexpr (DIRECT) {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            // rows behind the last one repeat it: their results are not stored
-            int64_t r = row0 + (i * NW + wave) * 8 + (lane >> 3);
-            r = r < rows ? r : rows - 1;
-            row[i] = src.codes + r * src.ld;
+            for (int i = 0; i < PER; ++i) row[i] = src.codes + row_of(i, rows) * src.ld;
+        } else {
+            any = Bf16Rows((const uint16_t*)src.codes, src.ld / 2, rows, K);
         }
     }
-    // Straight into LDS (rows of 16-byte alignment), or into registers, to be
-    // stored after the products that run meanwhile.
+    // rows behind the last one repeat it: their results are not stored
+    __device__ __forceinline__ int64_t row_of(int i, int64_t rows) const {
+        const int64_t r = first + i * NW * 8;
+        return r < rows ? r : rows - 1;
+    }
     __device__ __forceinline__ void issue(u32x4* lds, int stage, int K, int wave) {
         const int c = stage * kStageChunks + chunk;
         constexpr int per_chunk = OP == kOpBf16 ? 8 : kMxBlock;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             if constexpr (DIRECT) {
-                const uint8_t* p = c * per_chunk < K ? row[i] + (size_t)c * 16 : (const uint8_t*)kZeroChunk;
+                const uint8_t* p = row[i] + (size_t)c * 16;
+                p = c * per_chunk < K ? p : (const uint8_t*)kZeroChunk;
                 __builtin_amdgcn_global_load_lds((const u32x4*)p, lds + (i * NW + wave) * 64, 16, 0, 0);
             } else {
-                held[i] = load_chunk<OP>(row[i], c, K);
+                held[i] = any.load(row_of(i, any.rows), c * 8);
             }
         }
     }
-    __device__ __forceinline__ void store(u32x4* lds, int wave, int lane) {
-        if constexpr (!DIRECT)
+    __device__ __forceinline__ void store(u32x4* lds, int stage, int wave, int lane) {
+        if constexpr (!DIRECT) {
+            const int c = stage * kStageChunks + chunk;
+            if ((stage + 1) * kStageChunks * 8 > any.cols)   // the stage that holds the rows' ends
+#pragma unroll
+                for (int i = 0; i < PER; ++i) held[i] = any.fix(held[i], row_of(i, any.rows), c * 8);
 #pragma unroll
             for (int i = 0; i < PER; ++i) lds[(i * NW + wave) * 64 + lane] = held[i];
+        }
     }
 };
 
-// One row's scales of a stage as the four steps' MFMAs take them: byte s the
-// scale of block 2 s + half.  Blocks behind the last column get 2^-127.
-__device__ __forceinline__ uint32_t stage_scales(const uint8_t* scales, int stage, int K, int half) {
+// Where chunk c (8 columns) of row m of a stage with CHUNKS chunks a row lies, if
+// the stage is read by columns: a transposing read takes 64 bytes of eight rows at
+// once, and rows that follow each other start 64 bytes apart in the banks.
+template <int CHUNKS>
+__device__ __forceinline__ int column_slot(int m, int c) { return m * CHUNKS + (c ^ ((m & (CHUNKS >= 16 ? 3 : 1)) << 2)); }
+
+// The MFMA operand of 32 columns from column n on and 16 rows from row m on of
+// such a stage: lane l has column n + (l & 31), rows m + 8 (l >> 5) + (0..7).
+// Sixteen lanes read four rows of 16 columns, 8 bytes each, and get a column each.
+template <int CHUNKS>
+__device__ __forceinline__ bf16x8 read_columns(const u32x4* lds, int m, int n, int lane) {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    const int col = n + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+    const int row = m + 8 * (lane >> 5) + ((lane >> 2) & 3);
+    struct { s16x4 lo, hi; } v;
+    const char* base = (const char*)lds;
+    v.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(base + column_slot<CHUNKS>(row, col >> 3) * 16 + (col & 7) * 2));
+    v.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(base + column_slot<CHUNKS>(row + 4, col >> 3) * 16 + (col & 7) * 2));
+    return __builtin_bit_cast(bf16x8, v);
+}
+
+// Copies of a bf16 operand that is transposed in memory: a stage is ROWS of its
+// rows (the products' terms) by COLS of its columns.  Rows behind `rows` are zeros.
+template <int ROWS, int COLS, int NW, bool DIRECT>
+struct ColumnCopy {
+    static constexpr int CHUNKS = COLS / 8, EACH = 64 / CHUNKS;   // rows per copy of 64 chunks
+    static constexpr int PER = ROWS / EACH / NW;
+    static_assert(ROWS % (EACH * NW) == 0 && CHUNKS <= 64, "rows split evenly over the waves");
+    Bf16Rows any;
+    u32x4 held[DIRECT ? 1 : PER];
+    int64_t begin, end;   // rows
+    int row, col, col0;   // of this lane in the wave's first copy; first column of the stage
+    __device__ __forceinline__ void init(const uint16_t* p, int64_t ld, int64_t rows, int cols, int64_t begin_, int64_t end_,
+                                         int col0_, int wave, int lane) {
+        any = Bf16Rows(p, ld, rows, cols);
+        begin = begin_;
+        end = end_;
+        row = wave * EACH + lane / CHUNKS;
+        // the chunk whose slot is the lane's; the swizzle goes by the row's low
+        // bits, which further copies of a wave, multiples of four rows away, keep
+        static_assert((EACH * NW) % 4 == 0, "swizzle");
+        col0 = col0_;
+        col = col0_ + ((lane % CHUNKS) ^ (column_slot<CHUNKS>(row, 0) - row * CHUNKS)) * 8;
+    }
+    __device__ __forceinline__ void issue(u32x4* lds, int stage, int wave) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int64_t m = begin + (int64_t)stage * ROWS + row + i * EACH * NW;
+            if constexpr (DIRECT) {
+                const uint8_t* p = (const uint8_t*)(any.base + m * any.ld + col);
+                p = m < end && col < any.cols ? p : (const uint8_t*)kZeroChunk;
+                __builtin_amdgcn_global_load_lds((const u32x4*)p, lds + (i * NW + wave) * 64, 16, 0, 0);
+            } else {
+                held[i] = any.load(m < end ? m : end - 1, col);
+            }
+        }
+    }
+    __device__ __forceinline__ void store(u32x4* lds, int stage, int wave, int lane) {
+        if constexpr (!DIRECT) {
+            if (col0 + COLS > any.cols || begin + (int64_t)(stage + 1) * ROWS > end)
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    const int64_t m = begin + (int64_t)stage * ROWS + row + i * EACH * NW;
+                    held[i] = m < end ? any.fix(held[i], m, col) : u32x4{0, 0, 0, 0};
+                }
+#pragma unroll
+            for (int i = 0; i < PER; ++i) lds[(i * NW + wave) * 64 + lane] = held[i];
+        }
+    }
+};
+
+// The eight scales of one row's stage as the four steps' MFMAs take them: byte s
+// the scale of block 2 s + half.  Blocks behind the last column get 2^-127.
+__device__ __forceinline__ uint32_t pack_scales(uint64_t w, int stage, int K, int half) {
     const int left = (K + kMxBlock - 1) / kMxBlock - stage * 8;
-    uint64_t w = *(const uint64_t*)(scales + (size_t)stage * 8);
-    if (left < 8) w &= ((uint64_t)1 << (8 * left)) - 1;
+    if (left < 8) w = left <= 0 ? 0 : w & (((uint64_t)1 << (8 * left)) - 1);
     return __builtin_amdgcn_perm((uint32_t)(w >> 32), (uint32_t)w, half ? 0x07050301u : 0x06040200u);
+}
+__device__ __forceinline__ uint32_t stage_scales(const uint8_t* scales, int stage, int K, int half) {
+    const int at = stage * 8 * kMxBlock < K ? stage * 8 : 0;
+    return pack_scales(*(const uint64_t*)(scales + at), stage, K, half);
 }
 
 template <int OP, int S>
@@ -126,20 +208,73 @@ __device__ __forceinline__ uint32_t pair_max(uint32_t v) {
     return max(p[0], p[1]);
 }
 
+// The bias of 16 outputs from column n on; zeros without one.
+__device__ __forceinline__ void load_bias16(const GemmArgs& g, int n, float* bias) {
+    if (!g.bias) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) bias[i] = 0.0f;
+    } else if (n + 16 <= g.N) {
+        __builtin_memcpy(bias, g.bias + n, 16 * sizeof(float));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) bias[i] = g.bias[n + i < g.N ? n + i : g.N - 1];
+    }
+}
+
+// What a masked epilogue reads for 16 outputs from column n on of batch row m:
+// loaded early, used late.
+struct Mask16 {
+    u32x4 lo, hi;
+};
+template <int EPI>
+__device__ __forceinline__ Mask16 load_mask16(const GemmArgs& g, int64_t m, int n) {
+    Mask16 k;
+    const int64_t r = m < g.M ? m : g.M - 1;
+    if constexpr (EPI == kEpiMaskMx8) {
+        // a half block is whole in memory; behind the last block any will do
+        const int last = (g.N - 1) / kMxBlock * kMxBlock + 16;
+        k.lo = *(const u32x4*)(g.mask + r * g.ld_mask + (n < last ? n : last));
+    } else if constexpr (EPI == kEpiMaskBf16) {
+        const Bf16Rows x((const uint16_t*)g.mask, g.ld_mask, g.M, g.N);
+        k.lo = x.load(r, n);
+        k.hi = x.load(r, n + 8);
+    }
+    return k;
+}
+template <int EPI>
+__device__ __forceinline__ void apply_mask16(const GemmArgs& g, Mask16& k, int64_t m, int n, float* v) {
+    if constexpr (EPI == kEpiMaskMx8) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = (k.lo[i / 4] >> (8 * (i % 4))) & 0x7fu ? v[i] : 0.0f;
+    } else if constexpr (EPI == kEpiMaskBf16) {
+        if (n + 16 > g.N) {
+            const Bf16Rows x((const uint16_t*)g.mask, g.ld_mask, g.M, g.N);
+            const int64_t r = m < g.M ? m : g.M - 1;
+            k.lo = x.fix(k.lo, r, n);
+            k.hi = x.fix(k.hi, r, n + 8);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const uint32_t w = i < 8 ? k.lo[(i / 2) & 3] : k.hi[(i / 2) & 3];
+            v[i] = (w >> (16 * (i & 1))) & 0x7fffu ? v[i] : 0.0f;
+        }
+    }
+}
+
 // 16 consecutive outputs from column n on of batch row m, in a block of 32 that
 // this lane shares with the one 32 further; every lane of the wave calls it.
 template <int EPI>
-__device__ __forceinline__ void epilogue16(const GemmArgs& g, float* v, int64_t m, int n) {
+__device__ __forceinline__ void epilogue16(const GemmArgs& g, float* v, const float* bias, Mask16& mask, int64_t m, int n) {
     const bool live = m < g.M;
-    if (EPI != kEpiMasked) {
-        if (g.bias) {
+    if constexpr (!masked(EPI)) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] += n + i < g.N ? g.bias[n + i] : 0.0f;
-        }
+        for (int i = 0; i < 16; ++i) v[i] += bias[i];
         if (g.relu) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) v[i] = v[i] <= 0.0f ? 0.0f : v[i];   // NaN stays
         }
+    } else {
+        apply_mask16<EPI>(g, mask, m, n, v);
     }
     if constexpr (EPI == kEpiMx4 || EPI == kEpiKept) {
         // values behind the last column are zero in the block
@@ -176,21 +311,6 @@ __device__ __forceinline__ void epilogue16(const GemmArgs& g, float* v, int64_t 
         if (!g.y) return;
     }
     if (!live || n >= g.N) return;
-    if constexpr (EPI == kEpiMasked) {
-        if (g.mask_type == kMaskMx8) {   // a whole half block is there to be read
-            const u32x4 c = *(const u32x4*)(g.mask + m * g.ld_mask + n);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = (c[i / 4] >> (8 * (i % 4))) & 0x7fu ? v[i] : 0.0f;
-        } else if (g.mask_type == kMaskBf16) {
-            const uint16_t* row = (const uint16_t*)g.mask + m * g.ld_mask;
-            const u32x4 c0 = Row8<uint16_t>::load_raw(row, n, g.N), c1 = Row8<uint16_t>::load_raw(row, n + 8, g.N);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const uint32_t w = i < 8 ? c0[(i / 2) & 3] : c1[(i / 2) & 3];
-                v[i] = (w >> (16 * (i & 1))) & 0x7fffu ? v[i] : 0.0f;
-            }
-        }
-    }
     if constexpr (EPI == kEpiF32) {
         float* row = (float*)g.y + m * g.ldy;
         Row8<float>::store(row, n, g.N, v);
@@ -202,9 +322,11 @@ __device__ __forceinline__ void epilogue16(const GemmArgs& g, float* v, int64_t 
     }
 }
 
-template <int OP, int BN, int BM, int WN, int WM, bool DA, bool DB, int EPI>
-__global__ void __launch_bounds__(64 * WN * WM) layer_gemm_kernel(GemmArgs g) {
+// TA: the weights are transposed in memory, a[k][n] (bf16 only).
+template <int OP, int BN, int BM, int WN, int WM, bool TA, bool DA, bool DB, int EPI>
+__global__ void __launch_bounds__(64 * WN * WM, 2) layer_gemm_kernel(GemmArgs g) {
     constexpr int NW = WN * WM, TN = BN / (32 * WN), TM = BM / (32 * WM);
+    static_assert(!TA || OP == kOpBf16, "transposed weights are bf16");
     __shared__ u32x4 ring0[(BN + BM) * kStageChunks];
     __shared__ u32x4 ring1[(BN + BM) * kStageChunks];
     const int lane = threadIdx.x & 63;
@@ -220,10 +342,14 @@ __global__ void __launch_bounds__(64 * WN * WM) layer_gemm_kernel(GemmArgs g) {
     const int n0 = (int)(t % g.tiles_n) * BN;
     const int64_t m0 = (int64_t)(t / g.tiles_n) * BM;
 
-    StageCopy<OP, BN, NW, DA> ca;
+    constexpr int stage_cols = OP == kOpBf16 ? 64 : 256;
+    const int stages = (g.K + stage_cols - 1) / stage_cols;
+    StageCopy<OP, BN, NW, DA || OP != kOpBf16> ca;
+    ColumnCopy<64, BN, NW, DA> ct;
     StageCopy<OP, BM, NW, DB> cb;
-    ca.init(g.a, n0, g.N, wave, lane);
-    cb.init(g.b, m0, g.M, wave, lane);
+    if constexpr (TA) ct.init((const uint16_t*)g.a.codes, g.a.ld / 2, g.K, g.N, 0, g.K, n0, wave, lane);
+    else ca.init(g.a, n0, g.N, g.K, wave, lane);
+    cb.init(g.b, m0, g.M, g.K, wave, lane);
     const uint8_t *sa[TN], *sb[TM];
     if constexpr (OP == kOpMx4) {
 #pragma unroll
@@ -245,8 +371,18 @@ __global__ void __launch_bounds__(64 * WN * WM) layer_gemm_kernel(GemmArgs g) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
 
-    constexpr int stage_cols = OP == kOpBf16 ? 64 : 256;
-    const int stages = (g.K + stage_cols - 1) / stage_cols;
+    auto issue = [&](u32x4* lds, int stage) {
+        if constexpr (TA) ct.issue(lds, stage, wave);
+        else ca.issue(lds, stage, g.K, wave);
+        cb.issue(lds + BN * kStageChunks, stage, g.K, wave);
+    };
+    auto arrive = [&](u32x4* lds, int stage) {
+        if constexpr (TA) ct.store(lds, stage, wave, lane);
+        else ca.store(lds, stage, wave, lane);
+        cb.store(lds + BN * kStageChunks, stage, wave, lane);
+        wait_vmcnt<0>();
+        lds_barrier();
+    };
     auto compute = [&](const u32x4* lds, int stage) {
         uint32_t va[TN], vb[TM];
         if constexpr (OP == kOpMx4) {
@@ -259,7 +395,10 @@ __global__ void __launch_bounds__(64 * WN * WM) layer_gemm_kernel(GemmArgs g) {
             const int c = (2 * CV(S) + half) ^ (col & 7);
             u32x4 fa[TN], fb[TM];
 #pragma unroll
-            for (int i = 0; i < TN; ++i) fa[i] = lds[((wn * TN + i) * 32 + col) * kStageChunks + c];
+            for (int i = 0; i < TN; ++i) {
+                if constexpr (TA) fa[i] = __builtin_bit_cast(u32x4, read_columns<BN / 8>(lds, CV(S) * 16, (wn * TN + i) * 32, lane));
+                else fa[i] = lds[((wn * TN + i) * 32 + col) * kStageChunks + c];
+            }
 #pragma unroll
             for (int j = 0; j < TM; ++j) fb[j] = lds[(BN + (wm * TM + j) * 32 + col) * kStageChunks + c];
 #pragma unroll
@@ -271,47 +410,233 @@ __global__ void __launch_bounds__(64 * WN * WM) layer_gemm_kernel(GemmArgs g) {
     };
     auto step = [&](u32x4* now, u32x4* next, int stage) {
         const bool more = stage + 1 < stages;
-        if (more) {
-            ca.issue(next, stage + 1, g.K, wave);
-            cb.issue(next + BN * kStageChunks, stage + 1, g.K, wave);
-        }
+        if (more) issue(next, stage + 1);
         compute(now, stage);
-        if (more) {
-            ca.store(next, wave, lane);
-            cb.store(next + BN * kStageChunks, wave, lane);
-            wait_vmcnt<0>();
-            lds_barrier();
-        }
+        if (more) arrive(next, stage + 1);
     };
-    ca.issue(ring0, 0, g.K, wave);
-    cb.issue(ring0 + BN * kStageChunks, 0, g.K, wave);
-    ca.store(ring0, wave, lane);
-    cb.store(ring0 + BN * kStageChunks, wave, lane);
-    wait_vmcnt<0>();
-    lds_barrier();
+    issue(ring0, 0);
+    arrive(ring0, 0);
     for (int s = 0; s < stages; s += 2) {
         step(ring0, ring1, s);
         if (s + 1 < stages) step(ring1, ring0, s + 1);
     }
 #pragma unroll
-    for (int i = 0; i < TN; ++i)
+    for (int i = 0; i < TN; ++i) {
+        const int n = n0 + (wn * TN + i) * 32 + 16 * half;
+        float bias[16];
+        Mask16 mask[TM];
+        if constexpr (!masked(EPI)) load_bias16(g, n, bias);
+#pragma unroll
+        for (int j = 0; j < TM; ++j) mask[j] = load_mask16<EPI>(g, m0 + (wm * TM + j) * 32 + col, n);
 #pragma unroll
         for (int j = 0; j < TM; ++j) {
             float v[16];
             consecutive_rows(acc[i][j], v);
-            epilogue16<EPI>(g, v, m0 + (wm * TM + j) * 32 + col, n0 + (wn * TN + i) * 32 + 16 * half);
+            epilogue16<EPI>(g, v, bias, mask[j], m0 + (wm * TM + j) * 32 + col, n);
         }
+    }
 }
 
-template <int OP, bool DA, bool DB, int EPI>
+// A layer whose weights fit into one workgroup's registers: up to 256 outputs
+// (32 per wave) of KS stages of 128 bytes.  They are read once per workgroup, and
+// tiles of batch rows (32 KiB) stream past them through a ring of four, three
+// ahead, so that the batch is read once and nothing else moves but the results.
+// WN waves along the outputs, 8 / WN along the rows.
+template <int OP, int KS, int WN, bool TA, bool DB, int EPI>
+__global__ void __launch_bounds__(512, 2) layer_rows_kernel(GemmArgs g) {
+    constexpr int NW = 8, WM = NW / WN, RT = 256 / KS, RB = RT / 32 / WM, CP = 4;
+    __shared__ u32x4 ring0[RT * KS * kStageChunks], ring1[RT * KS * kStageChunks];
+    __shared__ u32x4 ring2[RT * KS * kStageChunks], ring3[RT * KS * kStageChunks];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 31, half = lane >> 5;
+    const int wn = wave % WN, wm = wave / WN;
+    const int n = wn * 32 + 16 * half;   // this lane's first output
+    const uint32_t tiles = g.tiles_m;
+
+    // ---- the weights
+    u32x4 fa[KS][4];
+    uint32_t va[KS];
+    if constexpr (TA) {
+        // stages of 64 rows by all outputs, through the ring
+        u32x4* const rings[4] = {ring0, ring1, ring2, ring3};
+        ColumnCopy<64, 256, NW, false> ct[KS];
+        sfor<KS>([&](auto S) {
+            ct[CV(S)].init((const uint16_t*)g.a.codes, g.a.ld / 2, g.K, g.N, 0, g.K, 0, wave, lane);
+            ct[CV(S)].issue(rings[CV(S)], CV(S), wave);
+        });
+        sfor<KS>([&](auto S) { ct[CV(S)].store(rings[CV(S)], CV(S), wave, lane); });
+        lds_barrier();
+        sfor<KS>([&](auto S) {
+            sfor<4>([&](auto I) {
+                fa[CV(S)][CV(I)] = __builtin_bit_cast(u32x4, read_columns<32>(rings[CV(S)], CV(I) * 16, wn * 32, lane));
+            });
+        });
+        lds_barrier();
+    } else {
+        const int64_t r = wn * 32 + col < g.N ? wn * 32 + col : g.N - 1;
+        const Bf16Rows rows((const uint16_t*)g.a.codes, g.a.ld / 2, g.N, g.K);
+        sfor<KS>([&](auto S) {
+            sfor<4>([&](auto I) {
+                const int c = CV(S) * kStageChunks + 2 * CV(I) + half;
+                if constexpr (OP == kOpBf16) {
+                    fa[CV(S)][CV(I)] = rows.fix(rows.load(r, c * 8), r, c * 8);
+                } else {
+                    const uint8_t* p = c * kMxBlock < g.K ? g.a.codes + r * g.a.ld + c * 16 : (const uint8_t*)kZeroChunk;
+                    fa[CV(S)][CV(I)] = *(const u32x4*)p;
+                }
+            });
+            if constexpr (OP == kOpMx4) va[CV(S)] = stage_scales(g.a.scales + r * g.a.ld_scales, CV(S), g.K, half);
+        });
+    }
+    float bias[16];
+    if constexpr (!masked(EPI)) load_bias16(g, n, bias);
+
+    // ---- the batch
+    const int chunk = (lane & 7) ^ (lane >> 3);
+    const Bf16Rows rows((const uint16_t*)g.b.codes, g.b.ld / 2, g.M, g.K);
+    u32x4 held[DB ? 1 : CP];
+    // copy i of a wave: eight rows of one stage
+    auto place = [&](uint32_t tile, int i, int64_t& r, int& c) {
+        const int q = i * NW + wave;
+        r = (int64_t)tile * RT + (q % (RT / 8)) * 8 + (lane >> 3);
+        r = r < g.M ? r : g.M - 1;
+        c = q / (RT / 8) * kStageChunks + chunk;
+    };
+    auto issue = [&](u32x4* lds, uint32_t tile) {
+#pragma unroll
+        for (int i = 0; i < CP; ++i) {
+            int64_t r;
+            int c;
+            place(tile, i, r, c);
+            if constexpr (DB) {
+                const uint8_t* p = g.b.codes + r * g.b.ld + c * 16;
+                p = c * (OP == kOpBf16 ? 8 : kMxBlock) < g.K ? p : (const uint8_t*)kZeroChunk;
+                __builtin_amdgcn_global_load_lds((const u32x4*)p, lds + (i * NW + wave) * 64, 16, 0, 0);
+            } else {
+                held[i] = rows.load(r, c * 8);
+            }
+        }
+    };
+    auto store = [&](u32x4* lds, uint32_t tile) {
+        if constexpr (!DB)
+#pragma unroll
+            for (int i = 0; i < CP; ++i) {
+                int64_t r;
+                int c;
+                place(tile, i, r, c);
+                lds[(i * NW + wave) * 64 + lane] = rows.fix(held[i], r, c * 8);
+            }
+    };
+    // scales and masks of a tile, loaded a tile ahead
+    uint64_t scales[RB][KS];
+    auto load_scales = [&](uint32_t tile) {
+        if constexpr (OP == kOpMx4)
+#pragma unroll
+            for (int j = 0; j < RB; ++j) {
+                int64_t r = (int64_t)tile * RT + (wm * RB + j) * 32 + col;
+                r = r < g.M ? r : g.M - 1;
+                sfor<KS>([&](auto S) {
+                    // a row holds whole words of eight scales, up to its last block
+                    const int w = CV(S) * 8 * kMxBlock < g.K ? CV(S) : 0;
+                    scales[j][CV(S)] = *(const uint64_t*)(g.b.scales + r * g.b.ld_scales + w * 8);
+                });
+            }
+    };
+    auto compute = [&](const u32x4* lds, uint32_t tile, uint32_t next) {
+        Mask16 mask[RB];
+        uint64_t sc[RB][KS];
+#pragma unroll
+        for (int j = 0; j < RB; ++j)
+#pragma unroll
+            for (int s = 0; s < KS; ++s) sc[j][s] = scales[j][s];
+        if (next < tiles) load_scales(next);
+#pragma unroll
+        for (int j = 0; j < RB; ++j) mask[j] = load_mask16<EPI>(g, (int64_t)tile * RT + (wm * RB + j) * 32 + col, n);
+        return [=, &g, &fa, &va, &bias](void) mutable {
+#pragma unroll
+            for (int j = 0; j < RB; ++j) {
+                f32x16 acc;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
+                sfor<KS>([&](auto S) {
+                    uint32_t vb = 0;
+                    if constexpr (OP == kOpMx4) vb = pack_scales(sc[j][CV(S)], CV(S), g.K, half);
+                    sfor<4>([&](auto I) {
+                        const int row = (wm * RB + j) * 32 + col;
+                        const u32x4 fb = lds[(CV(S) * RT + row) * kStageChunks + ((2 * CV(I) + half) ^ (col & 7))];
+                        acc = mma_step<OP, CV(I)>(fa[CV(S)][CV(I)], fb, acc, OP == kOpMx4 ? va[CV(S)] : 0u, vb);
+                    });
+                });
+                float v[16];
+                consecutive_rows(acc, v);
+                epilogue16<EPI>(g, v, bias, mask[j], (int64_t)tile * RT + (wm * RB + j) * 32 + col, n);
+            }
+        };
+    };
+    const uint32_t G = gridDim.x;
+    auto step = [&](u32x4* now, u32x4* into, uint32_t tile) {
+        if constexpr (DB) {
+            // the wave's copies of this tile are done once no more than those
+            // of the two tiles after it are outstanding
+            if (tile + 2 * G < tiles) wait_vmcnt<2 * CP>();
+            else wait_vmcnt<0>();
+        }
+        lds_barrier();
+        auto work = compute(now, tile, tile + G);
+        const uint32_t ahead = tile + (DB ? 3 : 1) * G;
+        if (ahead < tiles) issue(into, ahead);
+        work();
+        if (!DB && ahead < tiles) store(into, ahead);
+    };
+    uint32_t tile = blockIdx.x;
+    load_scales(tile);
+    issue(ring0, tile);
+    store(ring0, tile);
+    if constexpr (DB) {
+        if (tile + G < tiles) issue(ring1, tile + G);
+        if (tile + 2 * G < tiles) issue(ring2, tile + 2 * G);
+    }
+    while (true) {
+        step(ring0, DB ? ring3 : ring1, tile);
+        if ((tile += G) >= tiles) break;
+        step(ring1, DB ? ring0 : ring2, tile);
+        if ((tile += G) >= tiles) break;
+        step(ring2, DB ? ring1 : ring3, tile);
+        if ((tile += G) >= tiles) break;
+        step(ring3, DB ? ring2 : ring0, tile);
+        if ((tile += G) >= tiles) break;
+    }
+}
+
+#ifndef LG_ROWS
+#define LG_ROWS 1
+#endif
+template <int OP, int KS, bool TA, bool DB, int EPI>
+hipError_t launch_layer_rows(GemmArgs g, int n_cu, hipStream_t stream) {
+    g.tiles_m = (uint32_t)(((int64_t)g.M * KS + 255) / 256);
+    const dim3 grid(g.tiles_m < (uint32_t)n_cu ? g.tiles_m : (uint32_t)n_cu);
+    if (g.N > 128) hipLaunchKernelGGL((layer_rows_kernel<OP, KS, 8, TA, DB, EPI>), grid, dim3(512), 0, stream, g);
+    else hipLaunchKernelGGL((layer_rows_kernel<OP, KS, 4, TA, DB, EPI>), grid, dim3(512), 0, stream, g);
+    return hipGetLastError();
+}
+
+template <int OP, bool TA, bool DA, bool DB, int EPI>
 hipError_t launch_layer_gemm(GemmArgs g, int n_cu, hipStream_t stream) {
+    constexpr int stage_cols = OP == kOpBf16 ? 64 : 256;
+    const int stages = (g.K + stage_cols - 1) / stage_cols;
+    if (LG_ROWS && g.N <= 256 && stages <= 4 && (int64_t)g.M * stages >= 256 * (int64_t)n_cu) {
+        if (stages == 1) return launch_layer_rows<OP, 1, TA, DB, EPI>(g, n_cu, stream);
+        if (stages == 2) return launch_layer_rows<OP, 2, TA, DB, EPI>(g, n_cu, stream);
+        return launch_layer_rows<OP, 4, TA, DB, EPI>(g, n_cu, stream);
+    }
     auto tiles = [&](int b) { return (uint64_t)((g.N + b - 1) / b) * (uint64_t)((g.M + b - 1) / b); };
     const int b = tiles(128) >= (uint64_t)n_cu ? 128 : 64;
     g.tiles_n = (uint32_t)((g.N + b - 1) / b);
     g.tiles_m = (uint32_t)((g.M + b - 1) / b);
     const dim3 grid((g.tiles_n * g.tiles_m + 7) / 8 * 8);
-    if (b == 128) hipLaunchKernelGGL((layer_gemm_kernel<OP, 128, 128, 2, 2, DA, DB, EPI>), grid, dim3(256), 0, stream, g);
-    else hipLaunchKernelGGL((layer_gemm_kernel<OP, 64, 64, 2, 2, DA, DB, EPI>), grid, dim3(256), 0, stream, g);
+    if (b == 128) hipLaunchKernelGGL((layer_gemm_kernel<OP, 128, 128, 2, 2, TA, DA, DB, EPI>), grid, dim3(256), 0, stream, g);
+    else hipLaunchKernelGGL((layer_gemm_kernel<OP, 64, 64, 2, 2, TA, DA, DB, EPI>), grid, dim3(256), 0, stream, g);
     return hipGetLastError();
 }
 

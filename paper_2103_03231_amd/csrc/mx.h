@@ -88,22 +88,37 @@ __device__ __forceinline__ uint32_t to_e4m3x4(const float* v, int code) {
     return q;
 }
 
-// 8 E2M1 or 4 E4M3 elements as fp32.
+// 8 E2M1 or 4 E4M3 elements as fp32; a NaN scale gives NaN.
 __device__ __forceinline__ void from_e2m1x8(uint32_t p, int code, float* v) {
-    const float s = scale_arg(code);
     sfor<4>([&](auto I) {
-        const f32x2 t = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(p, s, CV(I));
-        v[2 * CV(I)] = code == kMxNaN ? __uint_as_float(0x7fc00000u) : t[0];
-        v[2 * CV(I) + 1] = code == kMxNaN ? __uint_as_float(0x7fc00000u) : t[1];
+        const f32x2 t = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(p, scale_arg(code), CV(I));
+        v[2 * CV(I)] = t[0];
+        v[2 * CV(I) + 1] = t[1];
     });
 }
 __device__ __forceinline__ void from_e4m3x4(uint32_t p, int code, float* v) {
+    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8((int)p, scale_arg(code), false);
+    const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8((int)p, scale_arg(code), true);
+    v[0] = a[0];
+    v[1] = a[1];
+    v[2] = b[0];
+    v[3] = b[1];
+}
+// The same as bf16, 8 elements: exact, but for results below bf16's smallest
+// numbers and overflow.
+__device__ __forceinline__ u32x4 e2m1x8_as_bf16(uint32_t p, int code) {
     const float s = scale_arg(code);
-    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8((int)p, s, false);
-    const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8((int)p, s, true);
-    const float t[4] = {a[0], a[1], b[0], b[1]};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = code == kMxNaN ? __uint_as_float(0x7fc00000u) : t[i];
+    return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(p, s, 0)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(p, s, 1)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(p, s, 2)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(p, s, 3))};
+}
+__device__ __forceinline__ u32x4 e4m3x8_as_bf16(u32x2 p, int code) {
+    const float s = scale_arg(code);
+    return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)p[0], s, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)p[0], s, true)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)p[1], s, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)p[1], s, true))};
 }
 
 // 8 consecutive values of a row from column k on as fp32, zeros behind the last
@@ -153,16 +168,57 @@ struct Row8<uint16_t> {   // bf16
         }
     }
     __device__ static __forceinline__ void store(uint16_t* row, int k, int cols, const float* v) {
-        uint32_t p[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+        store_raw(row, k, cols, u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
+                                      pack_bf16x2(v[6], v[7])});
+    }
+    __device__ static __forceinline__ void store_raw(uint16_t* row, int k, int cols, u32x4 p) {
         if (k + 8 <= cols) {
-            __builtin_memcpy(row + k, p, 16);
+            __builtin_memcpy(row + k, &p, 16);
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if (k + i < cols) row[k + i] = (uint16_t)(p[i / 2] >> (16 * (i & 1)));
         }
+    }
+};
+
+// bf16 rows of any stride and address (2-byte aligned), read in chunks of 8
+// columns by unconditional 16-byte loads: guarded ones would each be waited for
+// before the next.  A chunk that reaches behind its row's end reads on into what
+// follows, except at the very end of the matrix, where the load stays within it;
+// fix() brings the chunk's columns into place and clears what is not the row's.
+struct Bf16Rows {
+    const uint16_t* base;
+    int64_t ld;
+    int64_t rows;
+    int cols;
+    int64_t last;    // offset of the last 16 bytes of the matrix; negative if it has fewer
+    __device__ __forceinline__ Bf16Rows() {}
+    __device__ __forceinline__ Bf16Rows(const uint16_t* p, int64_t ld_, int64_t rows_, int cols_)
+        : base(p), ld(ld_), rows(rows_), cols(cols_), last((rows_ - 1) * ld_ + cols_ - 8) {}
+    // The chunk at column k of a row < rows; k may lie behind the last column.
+    __device__ __forceinline__ u32x4 load(int64_t row, int k) const {
+        if (last < 0) return Row8<uint16_t>::load_raw(base + row * ld, k, cols);   // fewer than 16 bytes
+        const int64_t at = row * ld + k;
+        u32x4 v;
+        __builtin_memcpy(&v, base + (at < last ? at : last), 16);
+        return v;
+    }
+    __device__ __forceinline__ u32x4 fix(u32x4 v, int64_t row, int k) const {
+        if (last >= 0) {
+            const int64_t past = row * ld + k - last;
+            const int s = past < 0 ? 0 : past > 8 ? 8 : (int)past;
+            if (s & 8) v = u32x4{0, 0, 0, 0};
+            if (s & 4) v = u32x4{v[2], v[3], 0, 0};
+            if (s & 2) v = u32x4{v[1], v[2], v[3], 0};
+            if (s & 1) v = u32x4{(v[0] >> 16) | (v[1] << 16), (v[1] >> 16) | (v[2] << 16), (v[2] >> 16) | (v[3] << 16), v[3] >> 16};
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int left = cols - k - 2 * i;
+            v[i] &= left >= 2 ? 0xffffffffu : left == 1 ? 0xffffu : 0u;
+        }
+        return v;
     }
 };
 

@@ -51,15 +51,21 @@ __global__ void __launch_bounds__(kConvThreads) mx_dequantize_kernel(MxIn q, T* 
         if ((int)c * 8 >= cols) continue;
         const uint8_t* src = q.codes + row * q.ld;
         const int code = q.scales[row * q.ld_scales + (c >> 2)];
-        float v[8];
-        if (FP8) {
-            const u32x2 p = *(const u32x2*)(src + (size_t)c * 8);
-            from_e4m3x4(p[0], code, v);
-            from_e4m3x4(p[1], code, v + 4);
+        u32x2 p = {0, 0};
+        if (FP8) p = *(const u32x2*)(src + (size_t)c * 8);
+        else p[0] = *(const uint32_t*)(src + (size_t)c * 4);
+        if constexpr (sizeof(T) == 2) {
+            Row8<T>::store_raw(y + row * ldy, (int)c * 8, cols, FP8 ? e4m3x8_as_bf16(p, code) : e2m1x8_as_bf16(p[0], code));
         } else {
-            from_e2m1x8(*(const uint32_t*)(src + (size_t)c * 4), code, v);
+            float v[8];
+            if (FP8) {
+                from_e4m3x4(p[0], code, v);
+                from_e4m3x4(p[1], code, v + 4);
+            } else {
+                from_e2m1x8(p[0], code, v);
+            }
+            Row8<T>::store(y + row * ldy, (int)c * 8, cols, v);
         }
-        Row8<T>::store(y + row * ldy, (int)c * 8, cols, v);
     }
 }
 

@@ -3,7 +3,7 @@
 //
 //   forward   z = x W^T + b, y = act(z): layer_gemm.h with W as its weights.
 //   backward  dx = (dz W) where x is not zero (x a ReLU's output), the same
-//             product with W transposed once into the workspace;
+//             product with weights that are transposed in memory;
 //             dW = dz^T x and db = sum of dz over the rows, weight_grad_kernel.
 #include "layer_gemm.h"
 
@@ -15,28 +15,9 @@ bool whole_chunks(const MxIn& x, int cols) {
     return ((uintptr_t)x.codes & 15) == 0 && (x.ld & 15) == 0 && cols % 8 == 0;
 }
 
-// ---------------------------------------------------------------- W transposed
-
-constexpr int kTrTile = 64;
-
-// out[k][n] = w[n][k], columns from N to ldo zero.
-__global__ void __launch_bounds__(256) transpose_kernel(const uint16_t* w, int64_t ldw, int N, int K, uint16_t* out,
-                                                        int64_t ldo) {
-    __shared__ uint16_t tile[kTrTile][kTrTile + 2];
-    const int n0 = blockIdx.x * kTrTile, k0 = blockIdx.y * kTrTile;
-    const int c = threadIdx.x & 63, r0 = threadIdx.x >> 6;
-    for (int r = r0; r < kTrTile; r += 4)
-        tile[r][c] = n0 + r < N && k0 + c < K ? w[(int64_t)(n0 + r) * ldw + k0 + c] : (uint16_t)0;
-    __syncthreads();
-    for (int r = r0; r < kTrTile; r += 4)
-        if (k0 + r < K && n0 + c < ldo) out[(int64_t)(k0 + r) * ldo + n0 + c] = tile[c][r];
-}
-
 // ---------------------------------------------------------------- dW, db
 
-constexpr int kGradTile = 128;    // weight rows and columns of a workgroup
-constexpr int kGradRows = 64;     // batch rows of a stage
-constexpr int kGradChunks = kGradTile / 8;
+constexpr int kGradTileN = 128;   // weight rows of a workgroup
 
 struct GradArgs {
     const uint16_t* dz;
@@ -44,8 +25,8 @@ struct GradArgs {
     MxIn x;
     int32_t x_bf16;
     int32_t M, N, K;
-    int32_t rows_per_split;  // a multiple of kGradRows
-    uint32_t tiles_n, tiles_k;
+    int32_t rows_per_split;  // a multiple of the kernel's stage
+    uint32_t tiles_n, tiles_k, splits;
     float* dw;               // splits x N x K, or the result, or null
     int64_t split_stride;    // values from one split's dw to the next's
     int64_t lddw;
@@ -53,153 +34,158 @@ struct GradArgs {
     int32_t accumulate;      // only where dw is the result
 };
 
-// Where chunk c (8 columns) of row m of a stage lies.  A transposing read takes
-// 64 bytes of eight rows at once; rows that follow each other start 64 bytes
-// apart in the banks.
-__device__ __forceinline__ int grad_slot(int m, int c) { return m * kGradChunks + (c ^ ((m & 3) << 2)); }
-
-// The MFMA operand of 32 columns from column n on and 16 rows from row m on of a
-// stage: lane l has column n + (l & 31), rows m + 8 (l >> 5) + (0..7).  Sixteen
-// lanes read four rows of 16 columns, 8 bytes each, and get a column each.
-__device__ __forceinline__ bf16x8 read_columns(const u32x4* lds, int m, int n, int lane) {
-    typedef short s16x4 __attribute__((ext_vector_type(4)));
-    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    const int col = n + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-    const int row = m + 8 * (lane >> 5) + ((lane >> 2) & 3);
-    struct { s16x4 lo, hi; } v;
-    const char* base = (const char*)lds;
-    v.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(base + grad_slot(row, col >> 3) * 16 + (col & 7) * 2));
-    v.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(base + grad_slot(row + 4, col >> 3) * 16 + (col & 7) * 2));
-    return __builtin_bit_cast(bf16x8, v);
-}
-
-// 8 E4M3 elements as bf16: exact, but for results below bf16's smallest numbers.
-__device__ __forceinline__ u32x4 e4m3x8_as_bf16(u32x2 p, int code) {
-    float v[8];
-    from_e4m3x4(p[0], code, v);
-    from_e4m3x4(p[1], code, v + 4);
-    return u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
-}
-
-__global__ void __launch_bounds__(256) weight_grad_kernel(GradArgs g) {
-    constexpr int kPer = kGradRows * kGradChunks / 256;   // chunks per thread, of dz and of x
-    __shared__ u32x4 ring0[2 * kGradRows * kGradChunks];
-    __shared__ u32x4 ring1[2 * kGradRows * kGradChunks];
+// One split's part of dW[n][k] = sum_m dz[m][n] x[m][k] for 128 weight rows and
+// 64 TK columns, in stages of R batch rows.  dz goes straight into LDS (DIRECT:
+// rows of 16-byte alignment, N a multiple of 8), x through registers, where E4M3
+// becomes bf16, loaded two stages ahead.
+template <bool DIRECT, bool X_BF16, int TK, int R>
+__global__ void __launch_bounds__(256, 2) weight_grad_kernel(GradArgs g) {
+    constexpr int kTileK = 64 * TK, kChunksK = kTileK / 8;
+    constexpr int kPerX = R * kChunksK / 256;               // chunks of x per thread
+    constexpr int kRowsX = 256 / kChunksK;                  // rows between them
+    __shared__ u32x4 z0[R * kGradTileN / 8], z1[R * kGradTileN / 8];
+    __shared__ u32x4 x0[R * kChunksK], x1[R * kChunksK];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wn = wave & 1, wk = wave >> 1;
-    const uint32_t tile = blockIdx.x % (g.tiles_n * g.tiles_k);
-    const int split = (int)(blockIdx.x / (g.tiles_n * g.tiles_k));
-    const int n0 = (int)(tile % g.tiles_n) * kGradTile, k0 = (int)(tile / g.tiles_n) * kGradTile;
+    // A split's tiles go to one XCD, or few: its L2 reads the split's rows once.
+    const uint32_t tiles = g.tiles_n * g.tiles_k, all = tiles * g.splits, per_xcd = (all + 7) / 8;
+    const uint32_t t = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+    if (t >= all) return;
+    const uint32_t tile = t % tiles;
+    const int split = (int)(t / tiles);
+    const int n0 = (int)(tile % g.tiles_n) * kGradTileN, k0 = (int)(tile / g.tiles_n) * kTileK;
     const int64_t m_begin = (int64_t)split * g.rows_per_split;
     const int64_t m_end = m_begin + g.rows_per_split < g.M ? m_begin + g.rows_per_split : (int64_t)g.M;
-    const int chunk = threadIdx.x % kGradChunks, row0 = threadIdx.x / kGradChunks;
-    const int nc = n0 + chunk * 8, kc = k0 + chunk * 8;
-    const bool sums = g.db && k0 == 0;
-    const int k_whole = (g.K + kMxBlock - 1) / kMxBlock * kMxBlock;   // codes of a row
+    const int stages = (int)((m_end - m_begin + R - 1) / R);
+    const bool sums = g.db && k0 == 0 && wk == 0;
 
-    float db[8];
+    ColumnCopy<R, kGradTileN, 4, DIRECT> z;
+    z.init(g.dz, g.lddz, g.M, g.N, m_begin, m_end, n0, wave, lane);
+    // x: chunks of 8 columns
+    struct Held {
+        u32x4 v[kPerX];
+        int code[kPerX];
+    } ha, hb;
+    const int xrow = threadIdx.x / kChunksK, xcol = k0 + (threadIdx.x % kChunksK) * 8;
+    const Bf16Rows xrows((const uint16_t*)g.x.codes, g.x.ld / 2, g.M, g.K);
+    // codes behind the last block: the last block's, whose products are not stored
+    const int k_codes = (g.K + kMxBlock - 1) / kMxBlock * kMxBlock, xcode = xcol < k_codes ? xcol : k_codes - 8;
+    auto row_x = [&](int stage, int i) {
+        const int64_t m = m_begin + (int64_t)stage * R + xrow + i * kRowsX;
+        return m < m_end ? m : m_end - 1;
+    };
+    auto load_x = [&](Held& h, int stage) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) db[i] = 0.0f;
-    u32x4 hz[kPer], hx[kPer];
-    uint32_t hs[kPer];
-    auto load = [&](int64_t m0) {
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int64_t m = m0 + row0 + i * (256 / kGradChunks);
-            hz[i] = hx[i] = u32x4{0, 0, 0, 0};
-            hs[i] = 0;
-            if (m < m_end) {
-                if (nc < g.N) hz[i] = Row8<uint16_t>::load_raw(g.dz + m * g.lddz, nc, g.N);
-                if (g.x_bf16) {
-                    if (kc < g.K) hx[i] = Row8<uint16_t>::load_raw((const uint16_t*)(g.x.codes + m * g.x.ld), kc, g.K);
-                } else if (kc < k_whole) {
-                    const u32x2 p = *(const u32x2*)(g.x.codes + m * g.x.ld + kc);
-                    hx[i][0] = p[0];
-                    hx[i][1] = p[1];
-                    hs[i] = g.x.scales[m * g.x.ld_scales + kc / kMxBlock];
-                }
+        for (int i = 0; i < kPerX; ++i) {
+            const int64_t m = row_x(stage, i);
+            if constexpr (X_BF16) {
+                h.v[i] = xrows.load(m, xcol);
+            } else {
+                const u32x2 p = *(const u32x2*)(g.x.codes + m * g.x.ld + xcode);
+                h.v[i][0] = p[0];
+                h.v[i][1] = p[1];
+                h.code[i] = g.x.scales[m * g.x.ld_scales + xcode / kMxBlock];
             }
         }
     };
-    auto store = [&](u32x4* lds) {
+    auto store_x = [&](u32x4* lds, Held& h, int stage) {
+        const bool last = m_begin + (int64_t)(stage + 1) * R > m_end;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int slot = grad_slot(row0 + i * (256 / kGradChunks), chunk);
-            lds[slot] = hz[i];
-            lds[kGradRows * kGradChunks + slot] = g.x_bf16 ? hx[i] : e4m3x8_as_bf16(u32x2{hx[i][0], hx[i][1]}, (int)hs[i]);
-            if (sums)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    db[e] += __uint_as_float(e & 1 ? hz[i][e / 2] & 0xffff0000u : hz[i][e / 2] << 16);
+        for (int i = 0; i < kPerX; ++i) {
+            u32x4 v;
+            if constexpr (X_BF16) {
+                v = h.v[i];
+                if (k0 + kTileK > g.K) v = xrows.fix(v, row_x(stage, i), xcol);
+            } else {
+                v = e4m3x8_as_bf16(u32x2{h.v[i][0], h.v[i][1]}, h.code[i]);
+            }
+            // a repeated row may hold NaN, which zeros of dz would not cancel
+            if (last && m_begin + (int64_t)stage * R + xrow + i * kRowsX >= m_end) v = u32x4{0, 0, 0, 0};
+            lds[column_slot<kChunksK>(xrow + i * kRowsX, threadIdx.x % kChunksK)] = v;
         }
     };
-    f32x16 acc[2][2];
+    f32x16 acc[2][TK];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < TK; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-    auto compute = [&](const u32x4* lds) {
-        sfor<kGradRows / 16>([&](auto S) {
-            bf16x8 a[2], b[2];
+    float db[2] = {0.0f, 0.0f};   // of this lane's column and half of the rows
+    auto compute = [&](const u32x4* zs, const u32x4* xs) {
+        sfor<R / 16>([&](auto S) {
+            bf16x8 a[2], b[TK];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) a[i] = read_columns(lds, CV(S) * 16, (wn * 2 + i) * 32, lane);
+            for (int i = 0; i < 2; ++i) a[i] = read_columns<kGradTileN / 8>(zs, CV(S) * 16, (wn * 2 + i) * 32, lane);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) b[j] = read_columns(lds + kGradRows * kGradChunks, CV(S) * 16, (wk * 2 + j) * 32, lane);
+            for (int j = 0; j < TK; ++j) b[j] = read_columns<kChunksK>(xs, CV(S) * 16, (wk * TK + j) * 32, lane);
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+                for (int j = 0; j < TK; ++j)
                     acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], b[j], acc[i][j], 0, 0, 0);
+            if (sums)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) db[i] += (float)a[i][e];
         });
     };
-    auto step = [&](u32x4* now, u32x4* next, int64_t m0) {
-        const bool more = m0 + kGradRows < m_end;
-        if (more) load(m0 + kGradRows);
-        compute(now);
+    // Stage s is multiplied while dz of s + 1 is copied, x of s + 1 stands in
+    // `now` and x of s + 2 is loaded into `later`.
+    auto step = [&](u32x4* zs, u32x4* zn, u32x4* xs, u32x4* xn, Held& now, Held& later, int s) {
+        const bool more = s + 1 < stages;
+        if (more) z.issue(zn, s + 1, wave);
+        if (s + 2 < stages) load_x(later, s + 2);
+        compute(zs, xs);
         if (more) {
-            store(next);
+            z.store(zn, s + 1, wave, lane);
+            store_x(xn, now, s + 1);
+            if constexpr (DIRECT) wait_vmcnt<0>();
             lds_barrier();
         }
     };
-    load(m_begin);
-    store(ring0);
+    z.issue(z0, 0, wave);
+    load_x(hb, 0);
+    if (stages > 1) load_x(ha, 1);
+    z.store(z0, 0, wave, lane);
+    store_x(x0, hb, 0);
+    if constexpr (DIRECT) wait_vmcnt<0>();
     lds_barrier();
-    for (int64_t m0 = m_begin; m0 < m_end; m0 += 2 * kGradRows) {
-        step(ring0, ring1, m0);
-        if (m0 + kGradRows < m_end) step(ring1, ring0, m0 + kGradRows);
+    for (int s = 0; s < stages; s += 2) {
+        step(z0, z1, x0, x1, ha, hb, s);
+        if (s + 1 < stages) step(z1, z0, x1, x0, hb, ha, s + 1);
     }
 
-    float* out = g.dw + (int64_t)split * g.split_stride;
-    if (g.dw)
+    if (g.dw) {
+        float* out = g.dw + (int64_t)split * g.split_stride;
+        const bool whole = n0 + kGradTileN <= g.N && k0 + kTileK <= g.K;
+        auto each = [&](auto f) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int k = k0 + (wk * 2 + j) * 32 + (lane & 31);
+                for (int j = 0; j < TK; ++j) {
+                    const int k = k0 + (wk * TK + j) * 32 + (lane & 31);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int n = n0 + (wn * 2 + i) * 32 + (e & 3) + 8 * (e >> 2) + 4 * (lane >> 5);
-                if (n < g.N && k < g.K) {
-                    float* p = out + (int64_t)n * g.lddw + k;
-                    *p = g.accumulate ? *p + acc[i][j][e] : acc[i][j][e];
+                    for (int e = 0; e < 16; ++e) {
+                        const int n = n0 + (wn * 2 + i) * 32 + (e & 3) + 8 * (e >> 2) + 4 * (lane >> 5);
+                        if (whole || (n < g.N && k < g.K)) f(out + (int64_t)n * g.lddw + k, acc[i][j][e]);
+                    }
                 }
-            }
-        }
-    if (sums) {   // the threads of a chunk's sixteen rows, summed in their order
-        lds_barrier();
-        float* part = (float*)ring0;
+        };
+        if (g.accumulate) each([](float* p, float v) { *p += v; });
+        else each([](float* p, float v) { *p = v; });
+    }
+    if (sums) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) part[row0 * kGradTile + chunk * 8 + e] = db[e];
-        lds_barrier();
-        const int c = threadIdx.x;
-        if (c < kGradTile && n0 + c < g.N) {
-            float s = 0.0f;
-            for (int r = 0; r < 256 / kGradChunks; ++r) s += part[r * kGradTile + c];
-            float* p = g.db + (int64_t)split * g.N + n0 + c;
-            *p = g.accumulate ? *p + s : s;
+        for (int i = 0; i < 2; ++i) {
+            const int n = n0 + (wn * 2 + i) * 32 + (lane & 31);
+            const float s = db[i] + __shfl_xor(db[i], 32);
+            if (lane < 32 && n < g.N) {
+                float* p = g.db + (int64_t)split * g.N + n;
+                *p = g.accumulate ? *p + s : s;
+            }
         }
     }
 }
@@ -223,65 +209,76 @@ __global__ void __launch_bounds__(256) grad_sum_kernel(const float* dw_parts, co
 
 struct GradPlan {
     int tiles_n, tiles_k, splits, rows_per_split;
-    size_t transposed, parts;   // bytes
+    size_t parts;   // bytes
 };
 
+#ifndef GW_TK
+#define GW_TK 2
+#endif
+#ifndef GW_R
+#define GW_R 64
+#endif
+#ifndef GW_WG
+#define GW_WG 2
+#endif
+constexpr int kGradRows = GW_R;
 // The batch is split until two workgroups per compute unit have work.
 GradPlan grad_plan(int64_t M, int N, int K, int n_cu) {
     GradPlan p;
-    p.tiles_n = (N + kGradTile - 1) / kGradTile;
-    p.tiles_k = (K + kGradTile - 1) / kGradTile;
+    p.tiles_n = (N + kGradTileN - 1) / kGradTileN;
+    p.tiles_k = (K + 64 * GW_TK - 1) / (64 * GW_TK);
     const int64_t stages = (M + kGradRows - 1) / kGradRows;
     const int64_t tiles = (int64_t)p.tiles_n * p.tiles_k;
-    int64_t want = 2 * (int64_t)n_cu / tiles;
+    int64_t want = GW_WG * (int64_t)n_cu / tiles;
     want = want < 1 ? 1 : want > stages ? (stages < 1 ? 1 : stages) : want;
     const int64_t per = (stages + want - 1) / want;
     p.rows_per_split = (int)(per < 1 ? kGradRows : per * kGradRows);
     p.splits = M == 0 ? 0 : (int)((M + p.rows_per_split - 1) / p.rows_per_split);
-    p.transposed = ((size_t)K * ((size_t)(N + 7) / 8 * 8) * 2 + 255) / 256 * 256;
     p.parts = p.splits > 1 ? (size_t)p.splits * ((size_t)N * K + N) * sizeof(float) : 0;
     return p;
+}
+
+// dx: the weights as they lie in memory, a row of them per term.
+template <int EPI>
+hipError_t launch_input_grad(const GemmArgs& g, int n_cu, hipStream_t stream) {
+    const bool da = whole_chunks(g.a, g.N), db = whole_chunks(g.b, g.K);
+    if (da && db) return launch_layer_gemm<kOpBf16, true, true, true, EPI>(g, n_cu, stream);
+    return launch_layer_gemm<kOpBf16, true, false, false, EPI>(g, n_cu, stream);
 }
 
 }  // namespace
 
 hipError_t launch_train_linear(const GemmArgs& g, int n_cu, hipStream_t stream) {
     const bool da = whole_chunks(g.a, g.K), db = whole_chunks(g.b, g.K);
-    if (da && db) return launch_layer_gemm<kOpBf16, true, true, kEpiKept>(g, n_cu, stream);
-    return launch_layer_gemm<kOpBf16, false, false, kEpiKept>(g, n_cu, stream);
+    if (da && db) return launch_layer_gemm<kOpBf16, false, true, true, kEpiKept>(g, n_cu, stream);
+    return launch_layer_gemm<kOpBf16, false, false, false, kEpiKept>(g, n_cu, stream);
 }
 
 size_t backward_workspace(int64_t M, int N, int K, int n_cu) {
     const GradPlan p = grad_plan(M, N, K, n_cu);
-    return p.transposed + p.parts;
+    return p.parts;
 }
 
 hipError_t launch_train_linear_backward(const BackwardArgs& a, int n_cu, hipStream_t stream) {
     const GradPlan p = grad_plan(a.M, a.N, a.K, n_cu);
     hipError_t e = hipSuccess;
     if (a.dx && a.M > 0) {
-        uint16_t* wt = (uint16_t*)a.workspace;
-        const int64_t ldt = (a.N + 7) / 8 * 8;
-        const dim3 grid((uint32_t)((ldt + kTrTile - 1) / kTrTile), (uint32_t)((a.K + kTrTile - 1) / kTrTile));
-        hipLaunchKernelGGL(transpose_kernel, grid, dim3(256), 0, stream, a.w, a.ldw, a.N, a.K, wt, ldt);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
         GemmArgs g{};
-        g.a = MxIn{(const uint8_t*)wt, ldt * 2, nullptr, 0};
+        g.a = MxIn{(const uint8_t*)a.w, a.ldw * 2, nullptr, 0};
         g.b = MxIn{(const uint8_t*)a.dz, a.lddz * 2, nullptr, 0};
         g.y = (uint8_t*)a.dx;
         g.ldy = a.lddx;
         g.mask = a.x.codes;
         g.ld_mask = a.x_bf16 ? a.x.ld / 2 : a.x.ld;
-        g.mask_type = !a.relu ? kMaskNone : a.x_bf16 ? kMaskBf16 : kMaskMx8;
         g.M = a.M;
         g.N = a.K;
         g.K = a.N;
-        e = whole_chunks(g.b, g.K) ? launch_layer_gemm<kOpBf16, true, true, kEpiMasked>(g, n_cu, stream)
-                                   : launch_layer_gemm<kOpBf16, true, false, kEpiMasked>(g, n_cu, stream);
+        e = !a.relu ? launch_input_grad<kEpiBf16>(g, n_cu, stream)
+            : a.x_bf16 ? launch_input_grad<kEpiMaskBf16>(g, n_cu, stream) : launch_input_grad<kEpiMaskMx8>(g, n_cu, stream);
         if (e != hipSuccess) return e;
     }
     if (!a.dw && !a.db) return e;
-    float* dw_parts = (float*)(a.workspace + p.transposed);
+    float* dw_parts = (float*)a.workspace;
     float* db_parts = dw_parts + (size_t)p.splits * a.N * a.K;
     if (p.splits >= 1) {
         const bool direct = p.splits == 1;
@@ -296,13 +293,18 @@ hipError_t launch_train_linear_backward(const BackwardArgs& a, int n_cu, hipStre
         g.rows_per_split = p.rows_per_split;
         g.tiles_n = (uint32_t)p.tiles_n;
         g.tiles_k = (uint32_t)p.tiles_k;
+        g.splits = (uint32_t)p.splits;
         g.dw = !a.dw ? nullptr : direct ? a.dw : dw_parts;
         g.split_stride = direct ? 0 : (int64_t)a.N * a.K;
         g.lddw = direct ? a.lddw : a.K;
         g.db = !a.db ? nullptr : direct ? a.db : db_parts;
         g.accumulate = direct ? a.accumulate : 0;
-        const dim3 grid((uint32_t)((size_t)p.tiles_n * p.tiles_k * p.splits));
-        hipLaunchKernelGGL(weight_grad_kernel, grid, dim3(256), 0, stream, g);
+        const dim3 grid(((uint32_t)p.tiles_n * p.tiles_k * p.splits + 7) / 8 * 8);
+        const bool copies = whole_chunks(MxIn{(const uint8_t*)a.dz, a.lddz * 2, nullptr, 0}, a.N);
+        if (copies && !a.x_bf16) hipLaunchKernelGGL((weight_grad_kernel<true, false, GW_TK, GW_R>), grid, dim3(256), 0, stream, g);
+        else if (copies) hipLaunchKernelGGL((weight_grad_kernel<true, true, GW_TK, GW_R>), grid, dim3(256), 0, stream, g);
+        else if (!a.x_bf16) hipLaunchKernelGGL((weight_grad_kernel<false, false, GW_TK, GW_R>), grid, dim3(256), 0, stream, g);
+        else hipLaunchKernelGGL((weight_grad_kernel<false, true, GW_TK, GW_R>), grid, dim3(256), 0, stream, g);
         if ((e = hipGetLastError()) != hipSuccess || direct) return e;
     }
     const int64_t total = (int64_t)a.N * a.K + a.N;

@@ -317,13 +317,15 @@ def test_refusals(r):
                 lambda: r.train_linear_backward(dz, q, w, dw=torch.zeros(40, 30, device="cuda"), db=torch.zeros(30, device="cuda"))):
         with pytest.raises(ValueError):
             bad()
-    need = b.donerf_train_linear_backward_workspace(r.h, 20, 40, 30)
-    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    x, dz = activations(1, 5000, 40, True), normal(3, 5000, 30)       # rows enough for parts in a workspace
+    need = b.donerf_train_linear_backward_workspace(r.h, 5000, 40, 30)
+    ws, db = torch.empty(need, dtype=torch.uint8, device="cuda"), torch.empty(30, device="cuda")
     bf = torch.bfloat16
-    with pytest.raises(b.DonerfError) as e:
-        b.donerf_train_linear_backward(r.h, r._rows("dz", dz, (bf,), device=0), r._rows("x", x, (bf,), device=0), 0, None, None, None,
-                                       dz.data_ptr(), 0, 20, 40, 30, ws.data_ptr(), need - 1)
-    assert e.value.status == b.E_SIZE
+    for size, status in ((need - 1, b.E_SIZE), (0, b.E_SIZE)):
+        with pytest.raises(b.DonerfError) as e:
+            b.donerf_train_linear_backward(r.h, r._rows("dz", dz, (bf,), device=0), r._rows("x", x, (bf,), device=0), 0, None, None, None,
+                                           db.data_ptr(), 0, 5000, 40, 30, ws.data_ptr(), size)
+        assert e.value.status == status
 
 
 def test_replays_from_a_graph(r):

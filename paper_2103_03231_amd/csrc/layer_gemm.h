@@ -208,17 +208,24 @@ __device__ __forceinline__ uint32_t pair_max(uint32_t v) {
     return max(p[0], p[1]);
 }
 
-// The bias of 16 outputs from column n on; zeros without one.
-__device__ __forceinline__ void load_bias16(const GemmArgs& g, int n, float* bias) {
-    if (!g.bias) {
+// The bias of the 32 outputs from column n on where a lane's accumulators start
+// from it; zeros without one.
+__device__ __forceinline__ f32x16 bias_rows(const GemmArgs& g, int n, int half) {
+    f32x16 v;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) bias[i] = 0.0f;
-    } else if (n + 16 <= g.N) {
-        __builtin_memcpy(bias, g.bias + n, 16 * sizeof(float));
-    } else {
+    for (int q = 0; q < 4; ++q) {
+        const int at = n + 8 * q + 4 * half;
+        float b[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (g.bias && at + 4 <= g.N) {
+            __builtin_memcpy(b, g.bias + at, sizeof b);
+        } else if (g.bias) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) bias[i] = g.bias[n + i < g.N ? n + i : g.N - 1];
+            for (int i = 0; i < 4; ++i) b[i] = g.bias[at + i < g.N ? at + i : g.N - 1];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[4 * q + i] = b[i];
     }
+    return v;
 }
 
 // What a masked epilogue reads for 16 outputs from column n on of batch row m:
@@ -264,14 +271,12 @@ __device__ __forceinline__ void apply_mask16(const GemmArgs& g, Mask16& k, int64
 // 16 consecutive outputs from column n on of batch row m, in a block of 32 that
 // this lane shares with the one 32 further; every lane of the wave calls it.
 template <int EPI>
-__device__ __forceinline__ void epilogue16(const GemmArgs& g, float* v, const float* bias, Mask16& mask, int64_t m, int n) {
+__device__ __forceinline__ void epilogue16(const GemmArgs& g, float* v, Mask16& mask, int64_t m, int n) {
     const bool live = m < g.M;
     if constexpr (!masked(EPI)) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] += bias[i];
         if (g.relu) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = v[i] <= 0.0f ? 0.0f : v[i];   // NaN stays
+            for (int i = 0; i < 16; ++i) v[i] = __builtin_elementwise_maximum(v[i], 0.0f);   // NaN stays
         }
     } else {
         apply_mask16<EPI>(g, mask, m, n, v);
@@ -297,12 +302,23 @@ __device__ __forceinline__ void epilogue16(const GemmArgs& g, float* v, const fl
     if constexpr (EPI == kEpiKept) {
         if (g.q.codes) {
             uint32_t top = pair_max(top_bits<16>(v));
-            if (__any(top >= 0x7f800000u)) {
+            const bool bad = __any(top >= kInfBits);
+            if (bad) {
                 const uint32_t fin = pair_max(finite_top_bits<16>(v));
-                top = top >= 0x7f800000u ? fin : top;
+                top = top >= kInfBits ? fin : top;
             }
             const int code = mx8_code(top);
-            const u32x4 p = {to_e4m3x4(v, code), to_e4m3x4(v + 4, code), to_e4m3x4(v + 8, code), to_e4m3x4(v + 12, code)};
+            u32x4 p;
+            if (g.relu) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) p[i] = to_e4m3x4<true>(v + 4 * i, code);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) p[i] = to_e4m3x4<false>(v + 4 * i, code);
+            }
+            if (bad)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) p[i] = e4m3_not_finite(p[i], v + 4 * i);
             if (in_block) {
                 *(u32x4*)(g.q.codes + m * g.q.ld + n) = p;
                 if (!(n & 16)) g.q.scales[m * g.q.ld_scales + block] = (uint8_t)code;
@@ -365,11 +381,11 @@ __global__ void __launch_bounds__(64 * WN * WM, 2) layer_gemm_kernel(GemmArgs g)
     }
     f32x16 acc[TN][TM];
 #pragma unroll
-    for (int i = 0; i < TN; ++i)
+    for (int i = 0; i < TN; ++i) {
+        const f32x16 bias = bias_rows(g, n0 + (wn * TN + i) * 32, half);
 #pragma unroll
-        for (int j = 0; j < TM; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+        for (int j = 0; j < TM; ++j) acc[i][j] = bias;
+    }
 
     auto issue = [&](u32x4* lds, int stage) {
         if constexpr (TA) ct.issue(lds, stage, wave);
@@ -423,16 +439,14 @@ __global__ void __launch_bounds__(64 * WN * WM, 2) layer_gemm_kernel(GemmArgs g)
 #pragma unroll
     for (int i = 0; i < TN; ++i) {
         const int n = n0 + (wn * TN + i) * 32 + 16 * half;
-        float bias[16];
         Mask16 mask[TM];
-        if constexpr (!masked(EPI)) load_bias16(g, n, bias);
 #pragma unroll
         for (int j = 0; j < TM; ++j) mask[j] = load_mask16<EPI>(g, m0 + (wm * TM + j) * 32 + col, n);
 #pragma unroll
         for (int j = 0; j < TM; ++j) {
             float v[16];
             consecutive_rows(acc[i][j], v);
-            epilogue16<EPI>(g, v, bias, mask[j], m0 + (wm * TM + j) * 32 + col, n);
+            epilogue16<EPI>(g, v, mask[j], m0 + (wm * TM + j) * 32 + col, n);
         }
     }
 }
@@ -489,8 +503,7 @@ __global__ void __launch_bounds__(512, 2) layer_rows_kernel(GemmArgs g) {
             if constexpr (OP == kOpMx4) va[CV(S)] = stage_scales(g.a.scales + r * g.a.ld_scales, CV(S), g.K, half);
         });
     }
-    float bias[16];
-    if constexpr (!masked(EPI)) load_bias16(g, n, bias);
+    const f32x16 bias = bias_rows(g, wn * 32, half);
 
     // ---- the batch
     const int chunk = (lane & 7) ^ (lane >> 3);
@@ -556,9 +569,7 @@ __global__ void __launch_bounds__(512, 2) layer_rows_kernel(GemmArgs g) {
         return [=, &g, &fa, &va, &bias](void) mutable {
 #pragma unroll
             for (int j = 0; j < RB; ++j) {
-                f32x16 acc;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
+                f32x16 acc = bias;
                 sfor<KS>([&](auto S) {
                     uint32_t vb = 0;
                     if constexpr (OP == kOpMx4) vb = pack_scales(sc[j][CV(S)], CV(S), g.K, half);
@@ -570,7 +581,7 @@ __global__ void __launch_bounds__(512, 2) layer_rows_kernel(GemmArgs g) {
                 });
                 float v[16];
                 consecutive_rows(acc, v);
-                epilogue16<EPI>(g, v, bias, mask[j], (int64_t)tile * RT + (wm * RB + j) * 32 + col, n);
+                epilogue16<EPI>(g, v, mask[j], (int64_t)tile * RT + (wm * RB + j) * 32 + col, n);
             }
         };
     };

@@ -22,22 +22,22 @@ constexpr int kMxBlock = 32;      // columns that share a scale
 constexpr int kMxNaN = 255;       // scale code
 
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+constexpr uint32_t kInfBits = 0x7f800000u;   // and above: NaN
 
-// Largest |v| as its bits: integers order as the values do, infinities and then
-// NaN above every number.
+// Largest |v| as its bits, NaN if there is one (v_maximum3_f32 keeps it).
 template <int N>
 __device__ __forceinline__ uint32_t top_bits(const float* v) {
-    uint32_t t = abs_bits(v[0]);
+    float t = __builtin_fabsf(v[0]);
 #pragma unroll
-    for (int i = 1; i < N; ++i) t = max(t, abs_bits(v[i]));
-    return t;
+    for (int i = 1; i < N; ++i) t = __builtin_elementwise_maximum(t, __builtin_fabsf(v[i]));
+    return abs_bits(t);
 }
 // The same among finite values only.
 template <int N>
 __device__ __forceinline__ uint32_t finite_top_bits(const float* v) {
     uint32_t t = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) t = max(t, abs_bits(v[i]) < 0x7f800000u ? abs_bits(v[i]) : 0u);
+    for (int i = 0; i < N; ++i) t = max(t, abs_bits(v[i]) < kInfBits ? abs_bits(v[i]) : 0u);
     return t;
 }
 
@@ -45,7 +45,7 @@ __device__ __forceinline__ uint32_t finite_top_bits(const float* v) {
 // 1.5 * 2^2 (E2M1) or 1.75 * 2^8 (E4M3) below it, one more where its mantissa is
 // larger; at least 0, where every fp32 below the smallest normal number fits.
 __device__ __forceinline__ int mx4_code(uint32_t top) {
-    if (top >= 0x7f800000u) return kMxNaN;   // a block that holds an infinity or NaN reads as NaN
+    if (top >= kInfBits) return kMxNaN;   // a block that holds an infinity or NaN reads as NaN
     return max(0, (int)(top >> 23) - 2 + ((top & 0x7fffffu) > 0x400000u));
 }
 __device__ __forceinline__ int mx8_code(uint32_t top) {
@@ -64,10 +64,12 @@ __device__ __forceinline__ uint32_t to_e2m1x8(const float* v, int code) {
     return code == kMxNaN ? 0u : p;
 }
 
-// 4 values as E4M3, the first in the lowest byte.  A value other than zero keeps
-// at least the smallest code (2^-9 of the scale, 2^-17.8 of the block's largest
-// value), so a checkpoint still tells which units a ReLU let through.  NaN and
-// infinities become NaN: E4M3 has no infinity.
+// 4 finite values as E4M3, the first in the lowest byte.  A value other than zero
+// keeps at least the smallest code (2^-9 of the scale, 2^-17.8 of the block's
+// largest value), so a checkpoint still tells which units a ReLU let through.
+// NONNEG: none is negative or -0; then max(u - 1, least - 1) + 1 on the bits
+// leaves 0 (whose predecessor is the largest number) and lifts what is below.
+template <bool NONNEG>
 __device__ __forceinline__ uint32_t to_e4m3x4(const float* v, int code) {
     const float s = scale_arg(code);
     // 2^-9 of the scale; below the normal numbers as far as fp32 goes
@@ -75,17 +77,25 @@ __device__ __forceinline__ uint32_t to_e4m3x4(const float* v, int code) {
     float w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float m = v[i] == 0.0f ? 0.0f : fmaxf(fabsf(v[i]), least);
-        w[i] = copysignf(m, v[i]);
+        if (NONNEG) {
+            w[i] = __uint_as_float(max(__float_as_uint(v[i]) - 1u, __float_as_uint(least) - 1u) + 1u);
+        } else {
+            const float m = v[i] == 0.0f ? 0.0f : fmaxf(fabsf(v[i]), least);
+            w[i] = copysignf(m, v[i]);
+        }
     }
     s16x2 p = {0, 0};
     p = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(p, w[0], w[1], s, false);
     p = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(p, w[2], w[3], s, true);
-    uint32_t q = __builtin_bit_cast(uint32_t, p);
+    return __builtin_bit_cast(uint32_t, p);
+}
+// The codes p of 4 values with NaN in the place of those that are not finite
+// (E4M3 has no infinity).
+__device__ __forceinline__ uint32_t e4m3_not_finite(uint32_t p, const float* v) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        if (abs_bits(v[i]) >= 0x7f800000u) q |= 0x7fu << (8 * i);
-    return q;
+        if (abs_bits(v[i]) >= kInfBits) p |= 0x7fu << (8 * i);
+    return p;
 }
 
 // 8 E2M1 or 4 E4M3 elements as fp32; a NaN scale gives NaN.

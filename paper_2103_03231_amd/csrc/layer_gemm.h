@@ -228,113 +228,144 @@ __device__ __forceinline__ f32x16 bias_rows(const GemmArgs& g, int n, int half) 
     return v;
 }
 
+// A lane's places in 32 rows of results from the 32 outputs from column n0 on:
+// bytes from those rows' first ones, where 32 bits count them.
+struct LanePlace {
+    uint32_t y, q, scale, mask;
+};
+template <int EPI>
+__device__ __forceinline__ LanePlace lane_place(const GemmArgs& g, int n0, int lane) {
+    const int col = lane & 31, n = n0 + 16 * (lane >> 5);
+    LanePlace p;
+    p.y = (uint32_t)(col * g.ldy + n) * (EPI == kEpiF32 ? 4 : 2);
+    p.q = (uint32_t)(col * g.q.ld + (EPI == kEpiMx4 ? n / 2 : n));
+    p.scale = (uint32_t)(col * g.q.ld_scales + n / kMxBlock);
+    p.mask = (uint32_t)(col * g.ld_mask + n) * (EPI == kEpiMaskBf16 ? 2 : 1);
+    return p;
+}
+// Whether 32 rows of results and masks lie within such offsets.
+__device__ __forceinline__ bool near_rows(const GemmArgs& g) {
+    constexpr int64_t most = (int64_t)1 << 24;
+    return g.ldy < most && g.q.ld < most && g.q.ld_scales < most && g.ld_mask < most;
+}
+
 // What a masked epilogue reads for 16 outputs from column n on of batch row m:
-// loaded early, used late.
+// loaded early, used late.  WHOLE: of 32 rows from m0 on that all exist, as all
+// the outputs do; the others' loads are kept within the matrix.
 struct Mask16 {
     u32x4 lo, hi;
 };
-template <int EPI>
-__device__ __forceinline__ Mask16 load_mask16(const GemmArgs& g, int64_t m, int n) {
+template <int EPI, bool WHOLE>
+__device__ __forceinline__ Mask16 load_mask16(const GemmArgs& g, int64_t m0, int n0, int lane, const LanePlace& at) {
     Mask16 k;
-    const int64_t r = m < g.M ? m : g.M - 1;
+    const int n = n0 + 16 * (lane >> 5);
+    int64_t r = m0 + (lane & 31);
+    r = r < g.M ? r : g.M - 1;
     if constexpr (EPI == kEpiMaskMx8) {
-        // a half block is whole in memory; behind the last block any will do
-        const int last = (g.N - 1) / kMxBlock * kMxBlock + 16;
-        k.lo = *(const u32x4*)(g.mask + r * g.ld_mask + (n < last ? n : last));
+        if constexpr (WHOLE) {
+            k.lo = *(const u32x4*)(g.mask + m0 * g.ld_mask + at.mask);
+        } else {
+            // a half block is whole in memory; behind the last block any will do
+            const int last = (g.N - 1) / kMxBlock * kMxBlock + 16;
+            k.lo = *(const u32x4*)(g.mask + r * g.ld_mask + (n < last ? n : last));
+        }
     } else if constexpr (EPI == kEpiMaskBf16) {
-        const Bf16Rows x((const uint16_t*)g.mask, g.ld_mask, g.M, g.N);
-        k.lo = x.load(r, n);
-        k.hi = x.load(r, n + 8);
+        if constexpr (WHOLE) {
+            const uint8_t* p = g.mask + m0 * g.ld_mask * 2 + at.mask;
+            __builtin_memcpy(&k.lo, p, 16);
+            __builtin_memcpy(&k.hi, p + 16, 16);
+        } else {
+            const Bf16Rows x((const uint16_t*)g.mask, g.ld_mask, g.M, g.N);
+            k.lo = x.fix(x.load(r, n), r, n);
+            k.hi = x.fix(x.load(r, n + 8), r, n + 8);
+        }
     }
     return k;
 }
-template <int EPI>
-__device__ __forceinline__ void apply_mask16(const GemmArgs& g, Mask16& k, int64_t m, int n, float* v) {
-    if constexpr (EPI == kEpiMaskMx8) {
+
+// What follows the product for 32 batch rows from m0 on and the 32 outputs from
+// n0 on, a wave's accumulator.  WHOLE: all of them exist; every lane calls it.
+template <int EPI, bool WHOLE>
+__device__ __forceinline__ void epilogue(const GemmArgs& g, const f32x16& acc, const Mask16& mask, int64_t m0, int n0, int lane,
+                                         const LanePlace& at) {
+    const int n = n0 + 16 * (lane >> 5);
+    const int64_t m = m0 + (lane & 31);
+    const bool live = WHOLE || m < g.M;
+    float v[16];
+    consecutive_rows(acc, v);
+    if constexpr (!masked(EPI)) {
+        const float floor = g.relu ? 0.0f : -__builtin_inff();
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = (k.lo[i / 4] >> (8 * (i % 4))) & 0x7fu ? v[i] : 0.0f;
-    } else if constexpr (EPI == kEpiMaskBf16) {
-        if (n + 16 > g.N) {
-            const Bf16Rows x((const uint16_t*)g.mask, g.ld_mask, g.M, g.N);
-            const int64_t r = m < g.M ? m : g.M - 1;
-            k.lo = x.fix(k.lo, r, n);
-            k.hi = x.fix(k.hi, r, n + 8);
-        }
+        for (int i = 0; i < 16; ++i) v[i] = __builtin_elementwise_maximum(v[i], floor);   // NaN stays
+    } else {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const uint32_t w = i < 8 ? k.lo[(i / 2) & 3] : k.hi[(i / 2) & 3];
-            v[i] = (w >> (16 * (i & 1))) & 0x7fffu ? v[i] : 0.0f;
+            bool pass;
+            if constexpr (EPI == kEpiMaskMx8) pass = (mask.lo[i / 4] >> (8 * (i % 4))) & 0x7fu;
+            else pass = ((i < 8 ? mask.lo[(i / 2) & 3] : mask.hi[(i / 2) & 3]) >> (16 * (i & 1))) & 0x7fffu;
+            v[i] = pass ? v[i] : 0.0f;
         }
     }
-}
-
-// 16 consecutive outputs from column n on of batch row m, in a block of 32 that
-// this lane shares with the one 32 further; every lane of the wave calls it.
-template <int EPI>
-__device__ __forceinline__ void epilogue16(const GemmArgs& g, float* v, Mask16& mask, int64_t m, int n) {
-    const bool live = m < g.M;
-    if constexpr (!masked(EPI)) {
-        if (g.relu) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = __builtin_elementwise_maximum(v[i], 0.0f);   // NaN stays
-        }
-    } else {
-        apply_mask16<EPI>(g, mask, m, n, v);
-    }
-    if constexpr (EPI == kEpiMx4 || EPI == kEpiKept) {
+    if constexpr (!WHOLE && (EPI == kEpiMx4 || EPI == kEpiKept)) {
         // values behind the last column are zero in the block
-        if (n + 16 > g.N) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = n + i < g.N ? v[i] : 0.0f;
-        }
+        for (int i = 0; i < 16; ++i) v[i] = n + i < g.N ? v[i] : 0.0f;
     }
-    const int block = n / kMxBlock;
-    const bool in_block = live && block * kMxBlock < g.N;
-    if constexpr (EPI == kEpiMx4) {
-        const int code = mx4_code(pair_max(top_bits<16>(v)));
-        const u32x2 p = {to_e2m1x8(v, code), to_e2m1x8(v + 8, code)};
-        if (in_block) {
-            *(u32x2*)(g.q.codes + m * g.q.ld + n / 2) = p;
-            if (!(n & 16)) g.q.scales[m * g.q.ld_scales + block] = (uint8_t)code;
-        }
-        return;
-    }
-    if constexpr (EPI == kEpiKept) {
-        if (g.q.codes) {
+    const bool in_block = WHOLE || (live && n / kMxBlock * kMxBlock < g.N);
+    if constexpr (EPI == kEpiMx4 || EPI == kEpiKept) {
+        if (EPI == kEpiMx4 || g.q.codes) {
+            uint8_t* codes = WHOLE ? g.q.codes + m0 * g.q.ld + at.q : g.q.codes + m * g.q.ld + (EPI == kEpiMx4 ? n / 2 : n);
+            uint8_t* scale = WHOLE ? g.q.scales + m0 * g.q.ld_scales + at.scale : g.q.scales + m * g.q.ld_scales + n / kMxBlock;
             uint32_t top = pair_max(top_bits<16>(v));
-            const bool bad = __any(top >= kInfBits);
-            if (bad) {
-                const uint32_t fin = pair_max(finite_top_bits<16>(v));
-                top = top >= kInfBits ? fin : top;
-            }
-            const int code = mx8_code(top);
-            u32x4 p;
-            if (g.relu) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) p[i] = to_e4m3x4<true>(v + 4 * i, code);
+            int code;
+            if constexpr (EPI == kEpiMx4) {
+                code = mx4_code(top);
+                const u32x2 p = {to_e2m1x8(v, code), to_e2m1x8(v + 8, code)};
+                if (in_block) *(u32x2*)codes = p;
             } else {
+                const bool bad = __any(top >= kInfBits);
+                if (bad) {
+                    const uint32_t fin = pair_max(finite_top_bits<16>(v));
+                    top = top >= kInfBits ? fin : top;
+                }
+                code = mx8_code(top);
+                u32x4 p;
+                if (g.relu) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) p[i] = to_e4m3x4<false>(v + 4 * i, code);
-            }
-            if (bad)
+                    for (int i = 0; i < 4; ++i) p[i] = to_e4m3x4<true>(v + 4 * i, code);
+                } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) p[i] = e4m3_not_finite(p[i], v + 4 * i);
-            if (in_block) {
-                *(u32x4*)(g.q.codes + m * g.q.ld + n) = p;
-                if (!(n & 16)) g.q.scales[m * g.q.ld_scales + block] = (uint8_t)code;
+                    for (int i = 0; i < 4; ++i) p[i] = to_e4m3x4<false>(v + 4 * i, code);
+                }
+                if (bad)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) p[i] = e4m3_not_finite(p[i], v + 4 * i);
+                if (in_block) *(u32x4*)codes = p;
             }
+            if (in_block && lane < 32) *scale = (uint8_t)code;
         }
-        if (!g.y) return;
+        if (EPI == kEpiMx4 || !g.y) return;
     }
-    if (!live || n >= g.N) return;
-    if constexpr (EPI == kEpiF32) {
-        float* row = (float*)g.y + m * g.ldy;
-        Row8<float>::store(row, n, g.N, v);
-        Row8<float>::store(row, n + 8, g.N, v + 8);
-    } else {
-        uint16_t* row = (uint16_t*)g.y + m * g.ldy;
-        Row8<uint16_t>::store(row, n, g.N, v);
-        Row8<uint16_t>::store(row, n + 8, g.N, v + 8);
+    if constexpr (WHOLE) {
+        uint8_t* y = g.y + m0 * g.ldy * (EPI == kEpiF32 ? 4 : 2) + at.y;
+        if constexpr (EPI == kEpiF32) {
+            __builtin_memcpy(y, v, 64);
+        } else {
+            uint32_t p[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+            __builtin_memcpy(y, p, 32);
+        }
+    } else if (live && n < g.N) {
+        if constexpr (EPI == kEpiF32) {
+            float* row = (float*)g.y + m * g.ldy;
+            Row8<float>::store(row, n, g.N, v);
+            Row8<float>::store(row, n + 8, g.N, v + 8);
+        } else {
+            uint16_t* row = (uint16_t*)g.y + m * g.ldy;
+            Row8<uint16_t>::store(row, n, g.N, v);
+            Row8<uint16_t>::store(row, n + 8, g.N, v + 8);
+        }
     }
 }
 
@@ -436,36 +467,41 @@ __global__ void __launch_bounds__(64 * WN * WM, 2) layer_gemm_kernel(GemmArgs g)
         step(ring0, ring1, s);
         if (s + 1 < stages) step(ring1, ring0, s + 1);
     }
+    auto finish = [&](auto whole) {
+        constexpr bool W = decltype(whole)::value;
 #pragma unroll
-    for (int i = 0; i < TN; ++i) {
-        const int n = n0 + (wn * TN + i) * 32 + 16 * half;
-        Mask16 mask[TM];
+        for (int i = 0; i < TN; ++i) {
+            const int n = n0 + (wn * TN + i) * 32;
+            const LanePlace at = lane_place<EPI>(g, n, lane);
+            Mask16 mask[TM];
 #pragma unroll
-        for (int j = 0; j < TM; ++j) mask[j] = load_mask16<EPI>(g, m0 + (wm * TM + j) * 32 + col, n);
+            for (int j = 0; j < TM; ++j) mask[j] = load_mask16<EPI, W>(g, m0 + (wm * TM + j) * 32, n, lane, at);
 #pragma unroll
-        for (int j = 0; j < TM; ++j) {
-            float v[16];
-            consecutive_rows(acc[i][j], v);
-            epilogue16<EPI>(g, v, mask[j], m0 + (wm * TM + j) * 32 + col, n);
+            for (int j = 0; j < TM; ++j) epilogue<EPI, W>(g, acc[i][j], mask[j], m0 + (wm * TM + j) * 32, n, lane, at);
         }
-    }
+    };
+    if (n0 + BN <= g.N && m0 + BM <= g.M && near_rows(g)) finish(std::true_type{});
+    else finish(std::false_type{});
 }
 
 // A layer whose weights fit into one workgroup's registers: up to 256 outputs
 // (32 per wave) of KS stages of 128 bytes.  They are read once per workgroup, and
-// tiles of batch rows (32 KiB) stream past them through a ring of four, three
-// ahead, so that the batch is read once and nothing else moves but the results.
-// WN waves along the outputs, 8 / WN along the rows.
+// tiles of RT batch rows stream past them through a ring of four, three ahead, so
+// that the batch is read once and nothing else moves but the results.  WN waves
+// along the outputs, 8 / WN along the rows.
+constexpr int rows_tile(int ks) { return ks == 1 ? 128 : 64; }
 template <int OP, int KS, int WN, bool TA, bool DB, int EPI>
 __global__ void __launch_bounds__(512, 2) layer_rows_kernel(GemmArgs g) {
-    constexpr int NW = 8, WM = NW / WN, RT = 256 / KS, RB = RT / 32 / WM, CP = 4;
-    __shared__ u32x4 ring0[RT * KS * kStageChunks], ring1[RT * KS * kStageChunks];
-    __shared__ u32x4 ring2[RT * KS * kStageChunks], ring3[RT * KS * kStageChunks];
+    constexpr int NW = 8, WM = NW / WN, RT = rows_tile(KS), RB = RT / 32 / WM, CP = RT * KS / 8 / NW;
+    // a tile: its stages, then the rows' scales, KS words of eight each
+    constexpr int kChunks = RT * KS * kStageChunks, kScaleWords = OP == kOpMx4 ? RT * KS * 2 : 0;
+    constexpr int kRing = TA ? 64 * 32 : 0;   // a stage of transposed weights passes through, too
+    constexpr int kSlot = kChunks + kScaleWords / 4 > kRing ? kChunks + kScaleWords / 4 : kRing;
+    __shared__ u32x4 ring0[kSlot], ring1[kSlot], ring2[kSlot], ring3[kSlot];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, half = lane >> 5;
     const int wn = wave % WN, wm = wave / WN;
-    const int n = wn * 32 + 16 * half;   // this lane's first output
     const uint32_t tiles = g.tiles_m;
 
     // ---- the weights
@@ -517,6 +553,16 @@ __global__ void __launch_bounds__(512, 2) layer_rows_kernel(GemmArgs g) {
         c = q / (RT / 8) * kStageChunks + chunk;
     };
     auto issue = [&](u32x4* lds, uint32_t tile) {
+        if constexpr (OP == kOpMx4) {
+            const int word = wave * 64 + lane, w = word % (2 * KS);   // of the tile, of its row
+            if (wave * 64 < kScaleWords) {
+                int64_t r = (int64_t)tile * RT + word / (2 * KS);
+                r = r < g.M ? r : g.M - 1;
+                const uint8_t* p = g.b.scales + r * g.b.ld_scales + w * 4;
+                p = w / 2 * 8 * kMxBlock < g.K ? p : (const uint8_t*)kZeroChunk;
+                __builtin_amdgcn_global_load_lds((const uint32_t*)p, (uint32_t*)(lds + kChunks) + wave * 64, 4, 0, 0);
+            }
+        }
 #pragma unroll
         for (int i = 0; i < CP; ++i) {
             int64_t r;
@@ -541,49 +587,41 @@ __global__ void __launch_bounds__(512, 2) layer_rows_kernel(GemmArgs g) {
                 lds[(i * NW + wave) * 64 + lane] = rows.fix(held[i], r, c * 8);
             }
     };
-    // scales and masks of a tile, loaded a tile ahead
-    uint64_t scales[RB][KS];
-    auto load_scales = [&](uint32_t tile) {
-        if constexpr (OP == kOpMx4)
-#pragma unroll
-            for (int j = 0; j < RB; ++j) {
-                int64_t r = (int64_t)tile * RT + (wm * RB + j) * 32 + col;
-                r = r < g.M ? r : g.M - 1;
-                sfor<KS>([&](auto S) {
-                    // a row holds whole words of eight scales, up to its last block
-                    const int w = CV(S) * 8 * kMxBlock < g.K ? CV(S) : 0;
-                    scales[j][CV(S)] = *(const uint64_t*)(g.b.scales + r * g.b.ld_scales + w * 8);
-                });
-            }
+    const LanePlace at = lane_place<EPI>(g, wn * 32, lane);
+    const bool near_whole = wn * 32 + 32 <= g.N && near_rows(g);
+    auto product = [&](const u32x4* lds, int j) {
+        f32x16 acc = bias;
+        const int row = (wm * RB + j) * 32 + col;
+        sfor<KS>([&](auto S) {
+            uint32_t vb = 0;
+            if constexpr (OP == kOpMx4) vb = pack_scales(((const uint64_t*)(lds + kChunks))[row * KS + CV(S)], CV(S), g.K, half);
+            sfor<4>([&](auto I) {
+                const u32x4 fb = lds[(CV(S) * RT + row) * kStageChunks + ((2 * CV(I) + half) ^ (col & 7))];
+                acc = mma_step<OP, CV(I)>(fa[CV(S)][CV(I)], fb, acc, OP == kOpMx4 ? va[CV(S)] : 0u, vb);
+            });
+        });
+        return acc;
     };
-    auto compute = [&](const u32x4* lds, uint32_t tile, uint32_t next) {
+    // A tile: the next block's products run while a block's results are finished,
+    // where registers for both are left.
+    constexpr bool kTwo = DB || KS < 4;
+    auto work = [&](const u32x4* lds, uint32_t tile, auto whole, auto ahead) {
+        constexpr bool W = decltype(whole)::value;
+        const int64_t m0 = (int64_t)tile * RT + wm * RB * 32;
         Mask16 mask[RB];
-        uint64_t sc[RB][KS];
 #pragma unroll
-        for (int j = 0; j < RB; ++j)
+        for (int j = 0; j < RB; ++j) mask[j] = load_mask16<EPI, W>(g, m0 + j * 32, wn * 32, lane, at);
+        ahead();
+        f32x16 acc;
+        if (kTwo) acc = product(lds, 0);
 #pragma unroll
-            for (int s = 0; s < KS; ++s) sc[j][s] = scales[j][s];
-        if (next < tiles) load_scales(next);
-#pragma unroll
-        for (int j = 0; j < RB; ++j) mask[j] = load_mask16<EPI>(g, (int64_t)tile * RT + (wm * RB + j) * 32 + col, n);
-        return [=, &g, &fa, &va, &bias](void) mutable {
-#pragma unroll
-            for (int j = 0; j < RB; ++j) {
-                f32x16 acc = bias;
-                sfor<KS>([&](auto S) {
-                    uint32_t vb = 0;
-                    if constexpr (OP == kOpMx4) vb = pack_scales(sc[j][CV(S)], CV(S), g.K, half);
-                    sfor<4>([&](auto I) {
-                        const int row = (wm * RB + j) * 32 + col;
-                        const u32x4 fb = lds[(CV(S) * RT + row) * kStageChunks + ((2 * CV(I) + half) ^ (col & 7))];
-                        acc = mma_step<OP, CV(I)>(fa[CV(S)][CV(I)], fb, acc, OP == kOpMx4 ? va[CV(S)] : 0u, vb);
-                    });
-                });
-                float v[16];
-                consecutive_rows(acc, v);
-                epilogue16<EPI>(g, v, mask[j], (int64_t)tile * RT + (wm * RB + j) * 32 + col, n);
-            }
-        };
+        for (int j = 0; j < RB; ++j) {
+            f32x16 after;
+            if (!kTwo) acc = product(lds, j);
+            if (kTwo && j + 1 < RB) after = product(lds, j + 1);
+            epilogue<EPI, W>(g, acc, mask[j], m0 + j * 32, wn * 32, lane, at);
+            if (kTwo) acc = after;
+        }
     };
     const uint32_t G = gridDim.x;
     auto step = [&](u32x4* now, u32x4* into, uint32_t tile) {
@@ -594,14 +632,13 @@ __global__ void __launch_bounds__(512, 2) layer_rows_kernel(GemmArgs g) {
             else wait_vmcnt<0>();
         }
         lds_barrier();
-        auto work = compute(now, tile, tile + G);
         const uint32_t ahead = tile + (DB ? 3 : 1) * G;
-        if (ahead < tiles) issue(into, ahead);
-        work();
+        auto copy = [&] { if (ahead < tiles) issue(into, ahead); };
+        if (near_whole && (int64_t)(tile + 1) * RT <= g.M) work(now, tile, std::true_type{}, copy);
+        else work(now, tile, std::false_type{}, copy);
         if (!DB && ahead < tiles) store(into, ahead);
     };
     uint32_t tile = blockIdx.x;
-    load_scales(tile);
     issue(ring0, tile);
     store(ring0, tile);
     if constexpr (DB) {
@@ -625,7 +662,7 @@ __global__ void __launch_bounds__(512, 2) layer_rows_kernel(GemmArgs g) {
 #endif
 template <int OP, int KS, bool TA, bool DB, int EPI>
 hipError_t launch_layer_rows(GemmArgs g, int n_cu, hipStream_t stream) {
-    g.tiles_m = (uint32_t)(((int64_t)g.M * KS + 255) / 256);
+    g.tiles_m = (uint32_t)(((int64_t)g.M + rows_tile(KS) - 1) / rows_tile(KS));
     const dim3 grid(g.tiles_m < (uint32_t)n_cu ? g.tiles_m : (uint32_t)n_cu);
     if (g.N > 128) hipLaunchKernelGGL((layer_rows_kernel<OP, KS, 8, TA, DB, EPI>), grid, dim3(512), 0, stream, g);
     else hipLaunchKernelGGL((layer_rows_kernel<OP, KS, 4, TA, DB, EPI>), grid, dim3(512), 0, stream, g);

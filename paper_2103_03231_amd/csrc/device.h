@@ -44,6 +44,12 @@ __device__ __forceinline__ void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// A barrier that waits for nothing but the other waves.  lds_barrier's release also
+// waits for every copy into LDS that is under way; where those of later stages are
+// to stay in flight, the caller waits for the ones that it needs, and its LDS reads
+// are done (their values have been used).
+__device__ __forceinline__ void bare_barrier() { asm volatile("s_barrier" ::: "memory"); }
+
 // s_waitcnt with only the vector-memory counter constrained (gfx9 encoding).
 template <int VM>
 __device__ __forceinline__ void wait_vmcnt() {

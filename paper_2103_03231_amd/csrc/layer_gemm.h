@@ -10,9 +10,9 @@
 // one runs while the other is multiplied.
 //
 // The weights are the MFMA's A operand and the batch its B operand, so a lane's
-// accumulators are 16 of a block's 32 outputs of one batch row, and a swap of
-// registers with the lane 32 further makes them 16 consecutive ones: bias, ReLU,
-// the block scales of microscaled outputs and wide stores need nothing else.
+// accumulators are 16 of a block's 32 outputs of one batch row, which it shares
+// with the lane 32 further: bias, ReLU, the scales of microscaled outputs and wide
+// stores need no more than exchanges of registers between the two.
 #pragma once
 
 #include "internal.h"
@@ -188,18 +188,16 @@ __device__ __forceinline__ f32x16 mma_step(u32x4 a, u32x4 b, f32x16 c, uint32_t 
     }
 }
 
-// A 32 x 32 accumulator (lane: column lane & 31, row (i & 3) + 8 (i >> 2) +
-// 4 (lane >> 5)) as the 16 consecutive rows from 16 (lane >> 5) on.
-__device__ __forceinline__ void consecutive_rows(const f32x16& acc, float* v) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i]), __float_as_uint(acc[8 + i]), false, false);
-        auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[4 + i]), __float_as_uint(acc[12 + i]), false, false);
-        v[i] = __uint_as_float(p[0]);
-        v[4 + i] = __uint_as_float(p[1]);
-        v[8 + i] = __uint_as_float(q[0]);
-        v[12 + i] = __uint_as_float(q[1]);
-    }
+// A 32 x 32 accumulator holds, in a lane, 16 rows of column lane & 31: four
+// consecutive ones, from 4 (lane >> 5) on, of every eight.  Where they are stored, a
+// lane shall hold the 16 consecutive ones from 16 (lane >> 5) on instead: with four
+// registers a (b) for the first (third) or the second (fourth) eight rows, whatever
+// their type, this exchange makes a the first half of eight consecutive rows and b
+// the second.  It is its own inverse.
+__device__ __forceinline__ void exchange(uint32_t& a, uint32_t& b) {
+    const auto p = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+    a = p[0];
+    b = p[1];
 }
 
 // The larger of this lane's and the lane's 32 further.
@@ -237,9 +235,9 @@ template <int EPI>
 __device__ __forceinline__ LanePlace lane_place(const GemmArgs& g, int n0, int lane) {
     const int col = lane & 31, n = n0 + 16 * (lane >> 5);
     LanePlace p;
-    p.y = (uint32_t)(col * g.ldy + n) * (EPI == kEpiF32 ? 4 : 2);
+    p.y = EPI == kEpiF32 ? (uint32_t)(col * g.ldy + n0 + 4 * (lane >> 5)) * 4 : (uint32_t)(col * g.ldy + n) * 2;
     p.q = (uint32_t)(col * g.q.ld + (EPI == kEpiMx4 ? n / 2 : n));
-    p.scale = (uint32_t)(col * g.q.ld_scales + n / kMxBlock);
+    p.scale = (uint32_t)(col * g.q.ld_scales + n0 / kMxBlock);
     p.mask = (uint32_t)(col * g.ld_mask + n) * (EPI == kEpiMaskBf16 ? 2 : 1);
     return p;
 }
@@ -288,83 +286,118 @@ __device__ __forceinline__ Mask16 load_mask16(const GemmArgs& g, int64_t m0, int
 template <int EPI, bool WHOLE>
 __device__ __forceinline__ void epilogue(const GemmArgs& g, const f32x16& acc, const Mask16& mask, int64_t m0, int n0, int lane,
                                          const LanePlace& at) {
-    const int n = n0 + 16 * (lane >> 5);
+    const int half = lane >> 5, n = n0 + 16 * half;
     const int64_t m = m0 + (lane & 31);
     const bool live = WHOLE || m < g.M;
-    float v[16];
-    consecutive_rows(acc, v);
-    if constexpr (!masked(EPI)) {
-        const float floor = g.relu ? 0.0f : -__builtin_inff();
+    const float floor = g.relu ? 0.0f : -__builtin_inff();
+    float v[16];   // outputs n0 + 8 (i / 4) + 4 half + i % 4
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = __builtin_elementwise_maximum(v[i], floor);   // NaN stays
-    } else {
+    for (int i = 0; i < 16; ++i) {
+        v[i] = acc[i];
+        // NaN stays.  E2M1 codes have their ReLU afterwards
+        if constexpr (!masked(EPI) && EPI != kEpiMx4) v[i] = __builtin_elementwise_maximum(v[i], floor);
+    }
+    if constexpr (EPI == kEpiMaskMx8) {
+        uint32_t d[4] = {mask.lo.x, mask.lo.z, mask.lo.y, mask.lo.w};
+        exchange(d[0], d[2]);
+        exchange(d[1], d[3]);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            bool pass;
-            if constexpr (EPI == kEpiMaskMx8) pass = (mask.lo[i / 4] >> (8 * (i % 4))) & 0x7fu;
-            else pass = ((i < 8 ? mask.lo[(i / 2) & 3] : mask.hi[(i / 2) & 3]) >> (16 * (i & 1))) & 0x7fffu;
-            v[i] = pass ? v[i] : 0.0f;
-        }
+        for (int i = 0; i < 16; ++i) v[i] = d[i / 4] & (0x7fu << (8 * (i % 4))) ? v[i] : 0.0f;
+    } else if constexpr (EPI == kEpiMaskBf16) {
+        uint32_t d[8] = {mask.lo.x, mask.lo.y, mask.hi.x, mask.hi.y, mask.lo.z, mask.lo.w, mask.hi.z, mask.hi.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) exchange(d[i], d[4 + i]);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = d[i / 2] & (0x7fffu << (16 * (i % 2))) ? v[i] : 0.0f;
     }
     if constexpr (!WHOLE && (EPI == kEpiMx4 || EPI == kEpiKept)) {
         // values behind the last column are zero in the block
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = n + i < g.N ? v[i] : 0.0f;
+        for (int i = 0; i < 16; ++i) v[i] = n0 + 8 * (i / 4) + 4 * half + i % 4 < g.N ? v[i] : 0.0f;
     }
-    const bool in_block = WHOLE || (live && n / kMxBlock * kMxBlock < g.N);
     if constexpr (EPI == kEpiMx4 || EPI == kEpiKept) {
+        const bool in_block = WHOLE || (live && n0 < g.N);
         if (EPI == kEpiMx4 || g.q.codes) {
             uint8_t* codes = WHOLE ? g.q.codes + m0 * g.q.ld + at.q : g.q.codes + m * g.q.ld + (EPI == kEpiMx4 ? n / 2 : n);
-            uint8_t* scale = WHOLE ? g.q.scales + m0 * g.q.ld_scales + at.scale : g.q.scales + m * g.q.ld_scales + n / kMxBlock;
-            uint32_t top = pair_max(top_bits<16>(v));
+            uint8_t* scale = WHOLE ? g.q.scales + m0 * g.q.ld_scales + at.scale : g.q.scales + m * g.q.ld_scales + n0 / kMxBlock;
             int code;
             if constexpr (EPI == kEpiMx4) {
-                code = mx4_code(top);
-                const u32x2 p = {to_e2m1x8(v, code), to_e2m1x8(v + 8, code)};
+                float t = g.relu ? 0.0f : __builtin_fabsf(v[0]);
+                if (g.relu) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) t = __builtin_elementwise_maximum(t, v[i]);
+                } else {
+#pragma unroll
+                    for (int i = 1; i < 16; ++i) t = __builtin_elementwise_maximum(t, __builtin_fabsf(v[i]));
+                }
+                code = mx4_code(pair_max(abs_bits(t)));
+                // four outputs are two bytes; this lane's of the first and second eight
+                // rows, of the third and fourth
+                uint32_t a = to_e2m1x8(v, code), b = to_e2m1x8(v + 8, code);
+                exchange(a, b);
+                u32x2 p = {__builtin_amdgcn_perm(b, a, 0x05040100u), __builtin_amdgcn_perm(b, a, 0x07060302u)};
+                if (g.relu) p = u32x2{relu_e2m1x8(p.x), relu_e2m1x8(p.y)};
                 if (in_block) *(u32x2*)codes = p;
             } else {
+                uint32_t top = pair_max(top_bits<16>(v));
                 const bool bad = __any(top >= kInfBits);
                 if (bad) {
                     const uint32_t fin = pair_max(finite_top_bits<16>(v));
                     top = top >= kInfBits ? fin : top;
                 }
                 code = mx8_code(top);
-                u32x4 p;
-                if (g.relu) {
+                // values other than zero that would round to it: few tiles have any
+                uint32_t low = 0xffffffffu;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) p[i] = to_e4m3x4<true>(v + 4 * i, code);
+                for (int i = 0; i < 16; ++i) low = min(low, (g.relu ? __float_as_uint(v[i]) : abs_bits(v[i])) - 1u);
+                const bool tiny = __any(low < __float_as_uint(least_e4m3(code)));
+                uint32_t p[4];
+                if (tiny) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) p[i] = to_e4m3x4(v + 4 * i, code);
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) p[i] = to_e4m3x4<false>(v + 4 * i, code);
+                    for (int i = 0; i < 4; ++i) p[i] = round_e4m3x4(v + 4 * i, code);
                 }
                 if (bad)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) p[i] = e4m3_not_finite(p[i], v + 4 * i);
-                if (in_block) *(u32x4*)codes = p;
+                exchange(p[0], p[2]);
+                exchange(p[1], p[3]);
+                if (in_block) *(u32x4*)codes = u32x4{p[0], p[2], p[1], p[3]};
             }
             if (in_block && lane < 32) *scale = (uint8_t)code;
         }
         if (EPI == kEpiMx4 || !g.y) return;
     }
-    if constexpr (WHOLE) {
-        uint8_t* y = g.y + m0 * g.ldy * (EPI == kEpiF32 ? 4 : 2) + at.y;
-        if constexpr (EPI == kEpiF32) {
-            __builtin_memcpy(y, v, 64);
-        } else {
-            uint32_t p[8];
+    if constexpr (EPI == kEpiF32) {
+        // four outputs are 16 bytes: stored as they are
 #pragma unroll
-            for (int i = 0; i < 8; ++i) p[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
-            __builtin_memcpy(y, p, 32);
+        for (int q = 0; q < 4; ++q) {
+            if constexpr (WHOLE) {
+                __builtin_memcpy(g.y + m0 * g.ldy * 4 + at.y + q * 32, v + 4 * q, 16);
+            } else {
+                const int c = n0 + 8 * q + 4 * half;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (live && c + i < g.N) ((float*)g.y)[m * g.ldy + c + i] = v[4 * q + i];
+            }
         }
-    } else if (live && n < g.N) {
-        if constexpr (EPI == kEpiF32) {
-            float* row = (float*)g.y + m * g.ldy;
-            Row8<float>::store(row, n, g.N, v);
-            Row8<float>::store(row, n + 8, g.N, v + 8);
-        } else {
+    } else {
+        uint32_t p[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) exchange(p[i], p[4 + i]);
+        const u32x4 lo = {p[0], p[1], p[4], p[5]}, hi = {p[2], p[3], p[6], p[7]};
+        if constexpr (WHOLE) {
+            uint8_t* y = g.y + m0 * g.ldy * 2 + at.y;
+            __builtin_memcpy(y, &lo, 16);
+            __builtin_memcpy(y + 16, &hi, 16);
+        } else if (live && n < g.N) {
             uint16_t* row = (uint16_t*)g.y + m * g.ldy;
-            Row8<uint16_t>::store(row, n, g.N, v);
-            Row8<uint16_t>::store(row, n + 8, g.N, v + 8);
+            Row8<uint16_t>::store_raw(row, n, g.N, lo);
+            Row8<uint16_t>::store_raw(row, n + 8, g.N, hi);
         }
     }
 }
@@ -624,14 +657,26 @@ __global__ void __launch_bounds__(512, 2) layer_rows_kernel(GemmArgs g) {
         }
     };
     const uint32_t G = gridDim.x;
+    // Store instructions of a wave's whole tile, at the least: 16 bytes a lane each.
+    constexpr int kStores = RB * (EPI == kEpiF32 ? 4 : 2);
+    const bool stores_all = EPI == kEpiKept && g.y && g.q.codes;
+    // Waits until this wave's copies of `tile` are done.  Copies and stores leave
+    // the counter in the order of their issue, and those of the tiles after it,
+    // and the stores of the three tiles that were finished since, came later.
+    auto wait_copies = [&](uint32_t tile, auto stores) {
+        constexpr int S = 3 * CV(stores);
+        if (tile + 2 * G < tiles) wait_vmcnt<2 * CP + S>();
+        else if (tile + G < tiles) wait_vmcnt<CP + S>();
+        else wait_vmcnt<S>();
+    };
     auto step = [&](u32x4* now, u32x4* into, uint32_t tile) {
         if constexpr (DB) {
-            // the wave's copies of this tile are done once no more than those
-            // of the two tiles after it are outstanding
-            if (tile + 2 * G < tiles) wait_vmcnt<2 * CP>();
-            else wait_vmcnt<0>();
+            if (!near_whole || tile < 3 * G) wait_copies(tile, std::integral_constant<int, 0>{});
+            else if (stores_all) wait_copies(tile, std::integral_constant<int, EPI == kEpiKept ? 2 * kStores : kStores>{});
+            else wait_copies(tile, std::integral_constant<int, kStores>{});
         }
-        lds_barrier();
+        if constexpr (DB) bare_barrier();
+        else lds_barrier();
         const uint32_t ahead = tile + (DB ? 3 : 1) * G;
         auto copy = [&] { if (ahead < tiles) issue(into, ahead); };
         if (near_whole && (int64_t)(tile + 1) * RT <= g.M) work(now, tile, std::true_type{}, copy);

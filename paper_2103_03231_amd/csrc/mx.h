@@ -63,31 +63,35 @@ __device__ __forceinline__ uint32_t to_e2m1x8(const float* v, int code) {
     p = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(p, v[6], v[7], s, 3);
     return code == kMxNaN ? 0u : p;
 }
+// 8 E2M1 codes with those of negative values, and -0, zero.
+__device__ __forceinline__ uint32_t relu_e2m1x8(uint32_t p) {
+    const uint32_t s = p & 0x88888888u;
+    return p & ~(s | (s - (s >> 3)));
+}
 
-// 4 finite values as E4M3, the first in the lowest byte.  A value other than zero
-// keeps at least the smallest code (2^-9 of the scale, 2^-17.8 of the block's
-// largest value), so a checkpoint still tells which units a ReLU let through.
-// NONNEG: none is negative or -0; then max(u - 1, least - 1) + 1 on the bits
-// leaves 0 (whose predecessor is the largest number) and lifts what is below.
-template <bool NONNEG>
-__device__ __forceinline__ uint32_t to_e4m3x4(const float* v, int code) {
+// 4 finite values as E4M3, the first in the lowest byte.
+__device__ __forceinline__ uint32_t round_e4m3x4(const float* v, int code) {
     const float s = scale_arg(code);
-    // 2^-9 of the scale; below the normal numbers as far as fp32 goes
-    const float least = ldexpf(1.0f, code - 127 - 9);
+    s16x2 p = {0, 0};
+    p = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(p, v[0], v[1], s, false);
+    p = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(p, v[2], v[3], s, true);
+    return __builtin_bit_cast(uint32_t, p);
+}
+// The smallest element, 2^-9 of the scale; below the normal numbers as far as fp32
+// goes.
+__device__ __forceinline__ float least_e4m3(int code) { return ldexpf(1.0f, code - 127 - 9); }
+// The same, where a value other than zero keeps at least the smallest code (2^-17.8
+// of the block's largest value), so a checkpoint still tells which units a ReLU let
+// through.
+__device__ __forceinline__ uint32_t to_e4m3x4(const float* v, int code) {
+    const float least = least_e4m3(code);
     float w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if (NONNEG) {
-            w[i] = __uint_as_float(max(__float_as_uint(v[i]) - 1u, __float_as_uint(least) - 1u) + 1u);
-        } else {
-            const float m = v[i] == 0.0f ? 0.0f : fmaxf(fabsf(v[i]), least);
-            w[i] = copysignf(m, v[i]);
-        }
+        const float m = v[i] == 0.0f ? 0.0f : fmaxf(fabsf(v[i]), least);
+        w[i] = copysignf(m, v[i]);
     }
-    s16x2 p = {0, 0};
-    p = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(p, w[0], w[1], s, false);
-    p = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(p, w[2], w[3], s, true);
-    return __builtin_bit_cast(uint32_t, p);
+    return round_e4m3x4(w, code);
 }
 // The codes p of 4 values with NaN in the place of those that are not finite
 // (E4M3 has no infinity).

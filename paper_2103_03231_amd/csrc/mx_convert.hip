@@ -33,7 +33,7 @@ __global__ void __launch_bounds__(kConvThreads) mx_quantize_kernel(const T* x, i
             const bool bad = __any(top >= kInfBits);
             if (bad && top >= kInfBits) top = quad_max(finite_top_bits<8>(v));   // whole quads
             code = mx8_code(top);
-            u32x2 p = {to_e4m3x4<false>(v, code), to_e4m3x4<false>(v + 4, code)};
+            u32x2 p = {to_e4m3x4(v, code), to_e4m3x4(v + 4, code)};
             if (bad) p = u32x2{e4m3_not_finite(p[0], v), e4m3_not_finite(p[1], v + 4)};
             *(u32x2*)(dst + (size_t)c * 8) = p;
         } else {

@@ -226,126 +226,109 @@ __device__ __forceinline__ f32x16 bias_rows(const GemmArgs& g, int n, int half) 
     return v;
 }
 
-// A lane's places in 32 rows of results from the 32 outputs from column n0 on:
-// bytes from those rows' first ones, where 32 bits count them.
-struct LanePlace {
-    uint32_t y, q, scale, mask;
-};
-template <int EPI>
-__device__ __forceinline__ LanePlace lane_place(const GemmArgs& g, int n0, int lane) {
-    const int col = lane & 31, n = n0 + 16 * (lane >> 5);
-    LanePlace p;
-    p.y = EPI == kEpiF32 ? (uint32_t)(col * g.ldy + n0 + 4 * (lane >> 5)) * 4 : (uint32_t)(col * g.ldy + n) * 2;
-    p.q = (uint32_t)(col * g.q.ld + (EPI == kEpiMx4 ? n / 2 : n));
-    p.scale = (uint32_t)(col * g.q.ld_scales + n0 / kMxBlock);
-    p.mask = (uint32_t)(col * g.ld_mask + n) * (EPI == kEpiMaskBf16 ? 2 : 1);
-    return p;
-}
-// Whether 32 rows of results and masks lie within such offsets.
-__device__ __forceinline__ bool near_rows(const GemmArgs& g) {
-    constexpr int64_t most = (int64_t)1 << 24;
-    return g.ldy < most && g.q.ld < most && g.q.ld_scales < most && g.ld_mask < most;
-}
-
-// What a masked epilogue reads for 16 outputs from column n on of batch row m:
-// loaded early, used late.  WHOLE: of 32 rows from m0 on that all exist, as all
-// the outputs do; the others' loads are kept within the matrix.
+// What a masked epilogue reads for the 32 outputs from n0 on of 32 batch rows from
+// m0 on: loaded early, used late.
 struct Mask16 {
     u32x4 lo, hi;
 };
-template <int EPI, bool WHOLE>
-__device__ __forceinline__ Mask16 load_mask16(const GemmArgs& g, int64_t m0, int n0, int lane, const LanePlace& at) {
+template <int EPI>
+__device__ __forceinline__ Mask16 load_mask(const GemmArgs& g, int64_t m0, int n0, int lane) {
     Mask16 k;
     const int n = n0 + 16 * (lane >> 5);
     int64_t r = m0 + (lane & 31);
     r = r < g.M ? r : g.M - 1;
     if constexpr (EPI == kEpiMaskMx8) {
-        if constexpr (WHOLE) {
-            k.lo = *(const u32x4*)(g.mask + m0 * g.ld_mask + at.mask);
-        } else {
-            // a half block is whole in memory; behind the last block any will do
-            const int last = (g.N - 1) / kMxBlock * kMxBlock + 16;
-            k.lo = *(const u32x4*)(g.mask + r * g.ld_mask + (n < last ? n : last));
-        }
+        // a half block is whole in memory; behind the last block any will do
+        const int last = (g.N - 1) / kMxBlock * kMxBlock + 16;
+        k.lo = *(const u32x4*)(g.mask + r * g.ld_mask + (n < last ? n : last));
     } else if constexpr (EPI == kEpiMaskBf16) {
-        if constexpr (WHOLE) {
-            const uint8_t* p = g.mask + m0 * g.ld_mask * 2 + at.mask;
-            __builtin_memcpy(&k.lo, p, 16);
-            __builtin_memcpy(&k.hi, p + 16, 16);
-        } else {
-            const Bf16Rows x((const uint16_t*)g.mask, g.ld_mask, g.M, g.N);
-            k.lo = x.fix(x.load(r, n), r, n);
-            k.hi = x.fix(x.load(r, n + 8), r, n + 8);
+        const Bf16Rows x((const uint16_t*)g.mask, g.ld_mask, g.M, g.N);
+        k.lo = x.load(r, n);
+        k.hi = x.load(r, n + 8);
+        if (n0 + 32 > g.N) {
+            k.lo = x.fix(k.lo, r, n);
+            k.hi = x.fix(k.hi, r, n + 8);
         }
     }
     return k;
 }
 
-// What follows the product for 32 batch rows from m0 on and the 32 outputs from
-// n0 on, a wave's accumulator.  WHOLE: all of them exist; every lane calls it.
-template <int EPI, bool WHOLE>
-__device__ __forceinline__ void epilogue(const GemmArgs& g, const f32x16& acc, const Mask16& mask, int64_t m0, int n0, int lane,
-                                         const LanePlace& at) {
-    const int half = lane >> 5, n = n0 + 16 * half;
-    const int64_t m = m0 + (lane & 31);
-    const bool live = WHOLE || m < g.M;
-    const float floor = g.relu ? 0.0f : -__builtin_inff();
-    float v[16];   // outputs n0 + 8 (i / 4) + 4 half + i % 4
+// A tile's results on their way out, ROWS batch rows by COLS outputs: waves put
+// theirs into LDS, then all threads store whole rows.  A wave's own 32 outputs of 32
+// rows would be that many pieces of 16 to 64 bytes (stored like that, six 4-bit hidden
+// layers of 640000 rows took 412 us, and 186 us without their stores).  In LDS, a row's
+// 16-byte chunks are permuted, chunk c at c ^ (row & 7).
+template <int EPI, int ROWS, int COLS>
+struct Outgoing {
+    static constexpr bool kY = EPI != kEpiMx4, kQ = EPI == kEpiMx4 || EPI == kEpiKept;
+    static constexpr int kYChunks = kY ? COLS * (EPI == kEpiF32 ? 4 : 2) / 16 : 0;    // per row
+    static constexpr int kQChunks = !kQ ? 0 : EPI == kEpiMx4 ? COLS / 32 : COLS / 16;
+    static constexpr int kBlocks = COLS / kMxBlock;                                     // scales per row
+    static constexpr int kAt = ROWS * kYChunks, kScaleAt = kAt + ROWS * kQChunks;
+    static constexpr int kSize = kScaleAt + (kQ ? ROWS * kBlocks / 16 : 0);             // chunks
+    static_assert(ROWS * kBlocks % 16 == 0, "whole chunks");
+
+    template <int CHUNKS>
+    __device__ static __forceinline__ int slot(int row, int c) { return row * CHUNKS + (c ^ (row & 7 & (CHUNKS - 1))); }
+
+    // What follows the product for the accumulator of rows [r0, r0 + 32) and
+    // outputs [c0, c0 + 32) of the tile, which starts at output n_tile.
+    __device__ static __forceinline__ void put(u32x4* lds, const GemmArgs& g, const f32x16& acc, const Mask16& mask, int r0,
+                                               int c0, int n_tile, int lane) {
+        const int half = lane >> 5, row = r0 + (lane & 31), n0 = n_tile + c0;
+        const float floor = g.relu ? 0.0f : -__builtin_inff();
+        float v[16];   // outputs n0 + 8 (i / 4) + 4 half + i % 4
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        v[i] = acc[i];
-        // NaN stays.  E2M1 codes have their ReLU afterwards
-        if constexpr (!masked(EPI) && EPI != kEpiMx4) v[i] = __builtin_elementwise_maximum(v[i], floor);
-    }
-    if constexpr (EPI == kEpiMaskMx8) {
-        uint32_t d[4] = {mask.lo.x, mask.lo.z, mask.lo.y, mask.lo.w};
-        exchange(d[0], d[2]);
-        exchange(d[1], d[3]);
+        for (int i = 0; i < 16; ++i) {
+            v[i] = acc[i];
+            // NaN stays.  E2M1 codes have their ReLU afterwards
+            if constexpr (!masked(EPI) && EPI != kEpiMx4) v[i] = __builtin_elementwise_maximum(v[i], floor);
+        }
+        if constexpr (EPI == kEpiMaskMx8) {
+            uint32_t d[4] = {mask.lo.x, mask.lo.z, mask.lo.y, mask.lo.w};
+            exchange(d[0], d[2]);
+            exchange(d[1], d[3]);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = d[i / 4] & (0x7fu << (8 * (i % 4))) ? v[i] : 0.0f;
-    } else if constexpr (EPI == kEpiMaskBf16) {
-        uint32_t d[8] = {mask.lo.x, mask.lo.y, mask.hi.x, mask.hi.y, mask.lo.z, mask.lo.w, mask.hi.z, mask.hi.w};
+            for (int i = 0; i < 16; ++i) v[i] = d[i / 4] & (0x7fu << (8 * (i % 4))) ? v[i] : 0.0f;
+        } else if constexpr (EPI == kEpiMaskBf16) {
+            uint32_t d[8] = {mask.lo.x, mask.lo.y, mask.hi.x, mask.hi.y, mask.lo.z, mask.lo.w, mask.hi.z, mask.hi.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) exchange(d[i], d[4 + i]);
+            for (int i = 0; i < 4; ++i) exchange(d[i], d[4 + i]);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = d[i / 2] & (0x7fffu << (16 * (i % 2))) ? v[i] : 0.0f;
-    }
-    if constexpr (!WHOLE && (EPI == kEpiMx4 || EPI == kEpiKept)) {
-        // values behind the last column are zero in the block
+            for (int i = 0; i < 16; ++i) v[i] = d[i / 2] & (0x7fffu << (16 * (i % 2))) ? v[i] : 0.0f;
+        }
+        if constexpr (kQ)
+            if (n0 + 32 > g.N)   // values behind the last column are zero in the block
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = n0 + 8 * (i / 4) + 4 * half + i % 4 < g.N ? v[i] : 0.0f;
-    }
-    if constexpr (EPI == kEpiMx4 || EPI == kEpiKept) {
-        const bool in_block = WHOLE || (live && n0 < g.N);
-        if (EPI == kEpiMx4 || g.q.codes) {
-            uint8_t* codes = WHOLE ? g.q.codes + m0 * g.q.ld + at.q : g.q.codes + m * g.q.ld + (EPI == kEpiMx4 ? n / 2 : n);
-            uint8_t* scale = WHOLE ? g.q.scales + m0 * g.q.ld_scales + at.scale : g.q.scales + m * g.q.ld_scales + n0 / kMxBlock;
-            int code;
-            if constexpr (EPI == kEpiMx4) {
-                float t = g.relu ? 0.0f : __builtin_fabsf(v[0]);
-                if (g.relu) {
+                for (int i = 0; i < 16; ++i) v[i] = n0 + 8 * (i / 4) + 4 * half + i % 4 < g.N ? v[i] : 0.0f;
+        if constexpr (EPI == kEpiMx4) {
+            float t = g.relu ? 0.0f : __builtin_fabsf(v[0]);
+            if (g.relu) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) t = __builtin_elementwise_maximum(t, v[i]);
-                } else {
-#pragma unroll
-                    for (int i = 1; i < 16; ++i) t = __builtin_elementwise_maximum(t, __builtin_fabsf(v[i]));
-                }
-                code = mx4_code(pair_max(abs_bits(t)));
-                // four outputs are two bytes; this lane's of the first and second eight
-                // rows, of the third and fourth
-                uint32_t a = to_e2m1x8(v, code), b = to_e2m1x8(v + 8, code);
-                exchange(a, b);
-                u32x2 p = {__builtin_amdgcn_perm(b, a, 0x05040100u), __builtin_amdgcn_perm(b, a, 0x07060302u)};
-                if (g.relu) p = u32x2{relu_e2m1x8(p.x), relu_e2m1x8(p.y)};
-                if (in_block) *(u32x2*)codes = p;
+                for (int i = 0; i < 16; ++i) t = __builtin_elementwise_maximum(t, v[i]);
             } else {
+#pragma unroll
+                for (int i = 1; i < 16; ++i) t = __builtin_elementwise_maximum(t, __builtin_fabsf(v[i]));
+            }
+            const int code = mx4_code(pair_max(abs_bits(t)));
+            // four outputs are two bytes; this lane's of the first and second eight
+            // rows, of the third and fourth
+            uint32_t a = to_e2m1x8(v, code), b = to_e2m1x8(v + 8, code);
+            exchange(a, b);
+            u32x2 p = {__builtin_amdgcn_perm(b, a, 0x05040100u), __builtin_amdgcn_perm(b, a, 0x07060302u)};
+            if (g.relu) p = u32x2{relu_e2m1x8(p.x), relu_e2m1x8(p.y)};
+            ((u32x2*)(lds + kAt))[slot<kQChunks>(row, c0 / 32) * 2 + half] = p;
+            if (lane < 32) ((uint8_t*)(lds + kScaleAt))[row * kBlocks + c0 / kMxBlock] = (uint8_t)code;
+        }
+        if constexpr (EPI == kEpiKept) {
+            if (g.q.codes) {
                 uint32_t top = pair_max(top_bits<16>(v));
                 const bool bad = __any(top >= kInfBits);
                 if (bad) {
                     const uint32_t fin = pair_max(finite_top_bits<16>(v));
                     top = top >= kInfBits ? fin : top;
                 }
-                code = mx8_code(top);
+                const int code = mx8_code(top);
                 // values other than zero that would round to it: few tiles have any
                 uint32_t low = 0xffffffffu;
 #pragma unroll
@@ -364,51 +347,98 @@ __device__ __forceinline__ void epilogue(const GemmArgs& g, const f32x16& acc, c
                     for (int i = 0; i < 4; ++i) p[i] = e4m3_not_finite(p[i], v + 4 * i);
                 exchange(p[0], p[2]);
                 exchange(p[1], p[3]);
-                if (in_block) *(u32x4*)codes = u32x4{p[0], p[2], p[1], p[3]};
-            }
-            if (in_block && lane < 32) *scale = (uint8_t)code;
-        }
-        if (EPI == kEpiMx4 || !g.y) return;
-    }
-    if constexpr (EPI == kEpiF32) {
-        // four outputs are 16 bytes: stored as they are
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            if constexpr (WHOLE) {
-                __builtin_memcpy(g.y + m0 * g.ldy * 4 + at.y + q * 32, v + 4 * q, 16);
-            } else {
-                const int c = n0 + 8 * q + 4 * half;
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (live && c + i < g.N) ((float*)g.y)[m * g.ldy + c + i] = v[4 * q + i];
+                lds[kAt + slot<kQChunks>(row, c0 / 16 + half)] = u32x4{p[0], p[2], p[1], p[3]};
+                if (lane < 32) ((uint8_t*)(lds + kScaleAt))[row * kBlocks + c0 / kMxBlock] = (uint8_t)code;
             }
         }
-    } else {
-        uint32_t p[8];
+        if constexpr (EPI == kEpiF32) {
+            // four outputs are a chunk
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+            for (int q = 0; q < 4; ++q) {
+                u32x4 p;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) exchange(p[i], p[4 + i]);
-        const u32x4 lo = {p[0], p[1], p[4], p[5]}, hi = {p[2], p[3], p[6], p[7]};
-        if constexpr (WHOLE) {
-            uint8_t* y = g.y + m0 * g.ldy * 2 + at.y;
-            __builtin_memcpy(y, &lo, 16);
-            __builtin_memcpy(y + 16, &hi, 16);
-        } else if (live && n < g.N) {
-            uint16_t* row = (uint16_t*)g.y + m * g.ldy;
-            Row8<uint16_t>::store_raw(row, n, g.N, lo);
-            Row8<uint16_t>::store_raw(row, n + 8, g.N, hi);
+                for (int i = 0; i < 4; ++i) p[i] = __float_as_uint(v[4 * q + i]);
+                lds[slot<kYChunks>(row, c0 / 4 + 2 * q + half)] = p;
+            }
+        } else if constexpr (kY) {
+            uint32_t p[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) exchange(p[i], p[4 + i]);
+            lds[slot<kYChunks>(row, c0 / 8 + 2 * half)] = u32x4{p[0], p[1], p[4], p[5]};
+            lds[slot<kYChunks>(row, c0 / 8 + 2 * half + 1)] = u32x4{p[2], p[3], p[6], p[7]};
         }
     }
-}
+
+    // Store instructions of a wave of THREADS / 64 for a tile whose rows all exist,
+    // at the least: every instruction has some row's first chunk.
+    static constexpr int stores_y(int threads) { return ROWS * kYChunks / threads; }
+    static constexpr int stores_q(int threads) { return ROWS * kQChunks / threads; }
+
+    // The tile at batch row m0 and output n_tile goes to memory.
+    template <int THREADS>
+    __device__ static __forceinline__ void store(const u32x4* lds, const GemmArgs& g, int64_t m0, int n_tile, int tid) {
+        const int rows = g.M - m0 < ROWS ? (int)(g.M - m0) : ROWS;
+        const bool whole = n_tile + COLS <= g.N;
+        if constexpr (kY) {
+            if (EPI != kEpiKept || g.y) {
+                constexpr int E = EPI == kEpiF32 ? 4 : 8;   // outputs of a chunk
+#pragma unroll
+                for (int q = 0; q < (ROWS * kYChunks + THREADS - 1) / THREADS; ++q) {
+                    if (ROWS * kYChunks % THREADS && q * THREADS + tid >= ROWS * kYChunks) break;
+                    const int at = q * THREADS + tid, row = at / kYChunks, c = at % kYChunks, n = n_tile + c * E;
+                    const u32x4 v = lds[slot<kYChunks>(row, c)];
+                    uint8_t* y = g.y + ((m0 + row) * g.ldy + n) * (16 / E);
+                    if (row < rows && (whole || n + E <= g.N)) {
+                        __builtin_memcpy(y, &v, 16);
+                    } else if (row < rows) {
+#pragma unroll
+                        for (int i = 0; i < E; ++i) {
+                            if (n + i >= g.N) continue;
+                            if constexpr (E == 4) ((float*)y)[i] = __uint_as_float(v[i]);
+                            else ((uint16_t*)y)[i] = (uint16_t)(v[i / 2] >> (16 * (i & 1)));
+                        }
+                    }
+                }
+            }
+        }
+        if constexpr (kQ) {
+            if (EPI == kEpiKept && !g.q.codes) return;
+            constexpr int E = COLS / kQChunks;              // outputs of a chunk: a block, or half of one
+#pragma unroll
+            for (int q = 0; q < (ROWS * kQChunks + THREADS - 1) / THREADS; ++q) {
+                if (ROWS * kQChunks % THREADS && q * THREADS + tid >= ROWS * kQChunks) break;
+                const int at = q * THREADS + tid, row = at / kQChunks, c = at % kQChunks, n = n_tile + c * E;
+                const u32x4 v = lds[kAt + slot<kQChunks>(row, c)];
+                if (row < rows && n / kMxBlock * kMxBlock < g.N)
+                    *(u32x4*)(g.q.codes + (m0 + row) * g.q.ld + (EPI == kEpiMx4 ? n / 2 : n)) = v;
+            }
+            if (tid < rows) {
+                const uint8_t* from = (const uint8_t*)(lds + kScaleAt) + tid * kBlocks;
+                uint8_t* to = g.q.scales + (m0 + tid) * g.q.ld_scales + n_tile / kMxBlock;
+                const int left = (g.N - n_tile + kMxBlock - 1) / kMxBlock;
+                if (left >= kBlocks) {
+                    __builtin_memcpy(to, from, kBlocks);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < kBlocks; ++i)
+                        if (i < left) to[i] = from[i];
+                }
+            }
+        }
+    }
+};
 
 // TA: the weights are transposed in memory, a[k][n] (bf16 only).
 template <int OP, int BN, int BM, int WN, int WM, bool TA, bool DA, bool DB, int EPI>
 __global__ void __launch_bounds__(64 * WN * WM, 2) layer_gemm_kernel(GemmArgs g) {
     constexpr int NW = WN * WM, TN = BN / (32 * WN), TM = BM / (32 * WM);
     static_assert(!TA || OP == kOpBf16, "transposed weights are bf16");
+    using Out = Outgoing<EPI, 32 * WM, BN>;   // of the results, a block of each wave at a time
     __shared__ u32x4 ring0[(BN + BM) * kStageChunks];
     __shared__ u32x4 ring1[(BN + BM) * kStageChunks];
+    static_assert(Out::kSize <= (BN + BM) * kStageChunks, "results pass through the stages' memory");
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, half = lane >> 5;
@@ -439,7 +469,7 @@ __global__ void __launch_bounds__(64 * WN * WM, 2) layer_gemm_kernel(GemmArgs g)
         }
 #pragma unroll
         for (int j = 0; j < TM; ++j) {
-            const int64_t r = m0 + (wm * TM + j) * 32 + col;
+            const int64_t r = m0 + (j * WM + wm) * 32 + col;
             sb[j] = g.b.scales + (r < g.M ? r : g.M - 1) * g.b.ld_scales;
         }
     }
@@ -480,7 +510,7 @@ __global__ void __launch_bounds__(64 * WN * WM, 2) layer_gemm_kernel(GemmArgs g)
                 else fa[i] = lds[((wn * TN + i) * 32 + col) * kStageChunks + c];
             }
 #pragma unroll
-            for (int j = 0; j < TM; ++j) fb[j] = lds[(BN + (wm * TM + j) * 32 + col) * kStageChunks + c];
+            for (int j = 0; j < TM; ++j) fb[j] = lds[(BN + (j * WM + wm) * 32 + col) * kStageChunks + c];
 #pragma unroll
             for (int i = 0; i < TN; ++i)
 #pragma unroll
@@ -500,37 +530,39 @@ __global__ void __launch_bounds__(64 * WN * WM, 2) layer_gemm_kernel(GemmArgs g)
         step(ring0, ring1, s);
         if (s + 1 < stages) step(ring1, ring0, s + 1);
     }
-    auto finish = [&](auto whole) {
-        constexpr bool W = decltype(whole)::value;
+    lds_barrier();
 #pragma unroll
-        for (int i = 0; i < TN; ++i) {
-            const int n = n0 + (wn * TN + i) * 32;
-            const LanePlace at = lane_place<EPI>(g, n, lane);
-            Mask16 mask[TM];
+    for (int j = 0; j < TM; ++j) {
+        u32x4* const out = j & 1 ? ring1 : ring0;
+        Mask16 mask[TN];
 #pragma unroll
-            for (int j = 0; j < TM; ++j) mask[j] = load_mask16<EPI, W>(g, m0 + (wm * TM + j) * 32, n, lane, at);
+        for (int i = 0; i < TN; ++i) mask[i] = load_mask<EPI>(g, m0 + (j * WM + wm) * 32, n0 + (wn * TN + i) * 32, lane);
+        if (j > 1) lds_barrier();
 #pragma unroll
-            for (int j = 0; j < TM; ++j) epilogue<EPI, W>(g, acc[i][j], mask[j], m0 + (wm * TM + j) * 32, n, lane, at);
-        }
-    };
-    if (n0 + BN <= g.N && m0 + BM <= g.M && near_rows(g)) finish(std::true_type{});
-    else finish(std::false_type{});
+        for (int i = 0; i < TN; ++i) Out::put(out, g, acc[i][j], mask[i], wm * 32, (wn * TN + i) * 32, n0, lane);
+        lds_barrier();
+        if (m0 + j * 32 * WM < g.M) Out::template store<64 * NW>(out, g, m0 + j * 32 * WM, n0, threadIdx.x);
+    }
 }
 
 // A layer whose weights fit into one workgroup's registers: up to 256 outputs
 // (32 per wave) of KS stages of 128 bytes.  They are read once per workgroup, and
-// tiles of RT batch rows stream past them through a ring of four, three ahead, so
+// tiles of 64 batch rows stream past them through a ring of three, two ahead, so
 // that the batch is read once and nothing else moves but the results.  WN waves
 // along the outputs, 8 / WN along the rows.
-constexpr int rows_tile(int ks) { return ks == 1 ? 128 : 64; }
+constexpr int kRowsTile = 64;
+// Workgroups that share a compute unit.
+constexpr int rows_workgroups(int op, int ks) { return op == kOpMx4 && ks == 1 ? 2 : 1; }
 template <int OP, int KS, int WN, bool TA, bool DB, int EPI>
-__global__ void __launch_bounds__(512, 2) layer_rows_kernel(GemmArgs g) {
-    constexpr int NW = 8, WM = NW / WN, RT = rows_tile(KS), RB = RT / 32 / WM, CP = RT * KS / 8 / NW;
+__global__ void __launch_bounds__(512, rows_workgroups(OP, KS) * 2) layer_rows_kernel(GemmArgs g) {
+    constexpr int NW = 8, WM = NW / WN, RT = kRowsTile, RB = RT / 32 / WM, CP = RT * KS / 8 / NW;
+    using Out = Outgoing<EPI, RT, 32 * WN>;
     // a tile: its stages, then the rows' scales, KS words of eight each
     constexpr int kChunks = RT * KS * kStageChunks, kScaleWords = OP == kOpMx4 ? RT * KS * 2 : 0;
     constexpr int kRing = TA ? 64 * 32 : 0;   // a stage of transposed weights passes through, too
     constexpr int kSlot = kChunks + kScaleWords / 4 > kRing ? kChunks + kScaleWords / 4 : kRing;
-    __shared__ u32x4 ring0[kSlot], ring1[kSlot], ring2[kSlot], ring3[kSlot];
+    __shared__ u32x4 ring0[kSlot], ring1[kSlot], ring2[kSlot];
+    __shared__ u32x4 out[Out::kSize];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, half = lane >> 5;
@@ -541,21 +573,24 @@ __global__ void __launch_bounds__(512, 2) layer_rows_kernel(GemmArgs g) {
     u32x4 fa[KS][4];
     uint32_t va[KS];
     if constexpr (TA) {
-        // stages of 64 rows by all outputs, through the ring
-        u32x4* const rings[4] = {ring0, ring1, ring2, ring3};
-        ColumnCopy<64, 256, NW, false> ct[KS];
-        sfor<KS>([&](auto S) {
-            ct[CV(S)].init((const uint16_t*)g.a.codes, g.a.ld / 2, g.K, g.N, 0, g.K, 0, wave, lane);
-            ct[CV(S)].issue(rings[CV(S)], CV(S), wave);
-        });
-        sfor<KS>([&](auto S) { ct[CV(S)].store(rings[CV(S)], CV(S), wave, lane); });
-        lds_barrier();
-        sfor<KS>([&](auto S) {
-            sfor<4>([&](auto I) {
-                fa[CV(S)][CV(I)] = __builtin_bit_cast(u32x4, read_columns<32>(rings[CV(S)], CV(I) * 16, wn * 32, lane));
+        // stages of 64 rows by all outputs, through the ring, two at a time
+        u32x4* const rings[2] = {ring0, ring1};
+        sfor<(KS + 1) / 2>([&](auto P) {
+            constexpr int S0 = 2 * CV(P), PAIR = KS - S0 < 2 ? 1 : 2;
+            ColumnCopy<64, 256, NW, false> ct[PAIR];
+            sfor<PAIR>([&](auto S) {
+                ct[CV(S)].init((const uint16_t*)g.a.codes, g.a.ld / 2, g.K, g.N, 0, g.K, 0, wave, lane);
+                ct[CV(S)].issue(rings[CV(S)], S0 + CV(S), wave);
             });
+            sfor<PAIR>([&](auto S) { ct[CV(S)].store(rings[CV(S)], S0 + CV(S), wave, lane); });
+            lds_barrier();
+            sfor<PAIR>([&](auto S) {
+                sfor<4>([&](auto I) {
+                    fa[S0 + CV(S)][CV(I)] = __builtin_bit_cast(u32x4, read_columns<32>(rings[CV(S)], CV(I) * 16, wn * 32, lane));
+                });
+            });
+            lds_barrier();
         });
-        lds_barrier();
     } else {
         const int64_t r = wn * 32 + col < g.N ? wn * 32 + col : g.N - 1;
         const Bf16Rows rows((const uint16_t*)g.a.codes, g.a.ld / 2, g.N, g.K);
@@ -620,8 +655,6 @@ __global__ void __launch_bounds__(512, 2) layer_rows_kernel(GemmArgs g) {
                 lds[(i * NW + wave) * 64 + lane] = rows.fix(held[i], r, c * 8);
             }
     };
-    const LanePlace at = lane_place<EPI>(g, wn * 32, lane);
-    const bool near_whole = wn * 32 + 32 <= g.N && near_rows(g);
     auto product = [&](const u32x4* lds, int j) {
         f32x16 acc = bias;
         const int row = (wm * RB + j) * 32 + col;
@@ -638,66 +671,61 @@ __global__ void __launch_bounds__(512, 2) layer_rows_kernel(GemmArgs g) {
     // A tile: the next block's products run while a block's results are finished,
     // where registers for both are left.
     constexpr bool kTwo = DB || KS < 4;
-    auto work = [&](const u32x4* lds, uint32_t tile, auto whole, auto ahead) {
-        constexpr bool W = decltype(whole)::value;
-        const int64_t m0 = (int64_t)tile * RT + wm * RB * 32;
+    const uint32_t G = gridDim.x;
+    // Store instructions of a wave in a tile whose rows all exist, at the least.
+    constexpr int kStoresY = Out::stores_y(512), kStoresQ = Out::stores_q(512);
+    const bool has_y = EPI != kEpiKept || g.y, has_q = EPI != kEpiKept || g.q.codes;
+    // Waits until this wave's copies of `tile` are done.  Copies and stores leave
+    // the counter in the order of their issue; those of the tile after it, and the
+    // stores of the two tiles that were finished since, came later.
+    auto wait_copies = [&](uint32_t tile, auto stores) {
+        constexpr int S = 2 * CV(stores);
+        if (tile + G < tiles) wait_vmcnt<CP + S>();
+        else wait_vmcnt<S>();
+    };
+    auto step = [&](u32x4* now, u32x4* next, u32x4* into, uint32_t tile) {
+        if constexpr (DB) {
+            if (tile < 2 * G) wait_copies(tile, std::integral_constant<int, 0>{});
+            else if (EPI != kEpiKept || (has_y && has_q)) wait_copies(tile, std::integral_constant<int, kStoresY + kStoresQ>{});
+            else if (has_y) wait_copies(tile, std::integral_constant<int, kStoresY>{});
+            else wait_copies(tile, std::integral_constant<int, kStoresQ>{});
+            bare_barrier();
+        } else {
+            lds_barrier();
+        }
+        const int64_t m0 = (int64_t)tile * RT;
         Mask16 mask[RB];
 #pragma unroll
-        for (int j = 0; j < RB; ++j) mask[j] = load_mask16<EPI, W>(g, m0 + j * 32, wn * 32, lane, at);
-        ahead();
+        for (int j = 0; j < RB; ++j) mask[j] = load_mask<EPI>(g, m0 + (wm * RB + j) * 32, wn * 32, lane);
+        const uint32_t ahead = tile + (DB ? 2 : 1) * G;
+        u32x4* const to = DB ? into : next;
+        if (ahead < tiles) issue(to, ahead);
         f32x16 acc;
-        if (kTwo) acc = product(lds, 0);
+        if (kTwo) acc = product(now, 0);
 #pragma unroll
         for (int j = 0; j < RB; ++j) {
             f32x16 after;
-            if (!kTwo) acc = product(lds, j);
-            if (kTwo && j + 1 < RB) after = product(lds, j + 1);
-            epilogue<EPI, W>(g, acc, mask[j], m0 + j * 32, wn * 32, lane, at);
+            if (!kTwo) acc = product(now, j);
+            if (kTwo && j + 1 < RB) after = product(now, j + 1);
+            Out::put(out, g, acc, mask[j], (wm * RB + j) * 32, wn * 32, 0, lane);
             if (kTwo) acc = after;
         }
-    };
-    const uint32_t G = gridDim.x;
-    // Store instructions of a wave's whole tile, at the least: 16 bytes a lane each.
-    constexpr int kStores = RB * (EPI == kEpiF32 ? 4 : 2);
-    const bool stores_all = EPI == kEpiKept && g.y && g.q.codes;
-    // Waits until this wave's copies of `tile` are done.  Copies and stores leave
-    // the counter in the order of their issue, and those of the tiles after it,
-    // and the stores of the three tiles that were finished since, came later.
-    auto wait_copies = [&](uint32_t tile, auto stores) {
-        constexpr int S = 3 * CV(stores);
-        if (tile + 2 * G < tiles) wait_vmcnt<2 * CP + S>();
-        else if (tile + G < tiles) wait_vmcnt<CP + S>();
-        else wait_vmcnt<S>();
-    };
-    auto step = [&](u32x4* now, u32x4* into, uint32_t tile) {
-        if constexpr (DB) {
-            if (!near_whole || tile < 3 * G) wait_copies(tile, std::integral_constant<int, 0>{});
-            else if (stores_all) wait_copies(tile, std::integral_constant<int, EPI == kEpiKept ? 2 * kStores : kStores>{});
-            else wait_copies(tile, std::integral_constant<int, kStores>{});
-        }
-        if constexpr (DB) bare_barrier();
-        else lds_barrier();
-        const uint32_t ahead = tile + (DB ? 3 : 1) * G;
-        auto copy = [&] { if (ahead < tiles) issue(into, ahead); };
-        if (near_whole && (int64_t)(tile + 1) * RT <= g.M) work(now, tile, std::true_type{}, copy);
-        else work(now, tile, std::false_type{}, copy);
-        if (!DB && ahead < tiles) store(into, ahead);
+        if (!DB && ahead < tiles) store(to, ahead);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        bare_barrier();
+        Out::template store<512>(out, g, m0, 0, threadIdx.x);
     };
     uint32_t tile = blockIdx.x;
     issue(ring0, tile);
     store(ring0, tile);
-    if constexpr (DB) {
+    if constexpr (DB)
         if (tile + G < tiles) issue(ring1, tile + G);
-        if (tile + 2 * G < tiles) issue(ring2, tile + 2 * G);
-    }
     while (true) {
-        step(ring0, DB ? ring3 : ring1, tile);
+        step(ring0, ring1, ring2, tile);
         if ((tile += G) >= tiles) break;
-        step(ring1, DB ? ring0 : ring2, tile);
+        step(ring1, ring2, ring0, tile);
         if ((tile += G) >= tiles) break;
-        step(ring2, DB ? ring1 : ring3, tile);
-        if ((tile += G) >= tiles) break;
-        step(ring3, DB ? ring2 : ring0, tile);
+        step(ring2, ring0, ring1, tile);
         if ((tile += G) >= tiles) break;
     }
 }
@@ -707,8 +735,9 @@ __global__ void __launch_bounds__(512, 2) layer_rows_kernel(GemmArgs g) {
 #endif
 template <int OP, int KS, bool TA, bool DB, int EPI>
 hipError_t launch_layer_rows(GemmArgs g, int n_cu, hipStream_t stream) {
-    g.tiles_m = (uint32_t)(((int64_t)g.M + rows_tile(KS) - 1) / rows_tile(KS));
-    const dim3 grid(g.tiles_m < (uint32_t)n_cu ? g.tiles_m : (uint32_t)n_cu);
+    g.tiles_m = (uint32_t)(((int64_t)g.M + kRowsTile - 1) / kRowsTile);
+    const uint32_t most = rows_workgroups(OP, KS) * (uint32_t)n_cu;
+    const dim3 grid(g.tiles_m < most ? g.tiles_m : most);
     if (g.N > 128) hipLaunchKernelGGL((layer_rows_kernel<OP, KS, 8, TA, DB, EPI>), grid, dim3(512), 0, stream, g);
     else hipLaunchKernelGGL((layer_rows_kernel<OP, KS, 4, TA, DB, EPI>), grid, dim3(512), 0, stream, g);
     return hipGetLastError();
@@ -718,10 +747,10 @@ template <int OP, bool TA, bool DA, bool DB, int EPI>
 hipError_t launch_layer_gemm(GemmArgs g, int n_cu, hipStream_t stream) {
     constexpr int stage_cols = OP == kOpBf16 ? 64 : 256;
     const int stages = (g.K + stage_cols - 1) / stage_cols;
-    if (LG_ROWS && g.N <= 256 && stages <= 4 && (int64_t)g.M * stages >= 256 * (int64_t)n_cu) {
+    if (LG_ROWS && g.N <= 256 && stages <= (OP == kOpMx4 ? 2 : 4) && (int64_t)g.M >= 64 * (int64_t)n_cu) {
         if (stages == 1) return launch_layer_rows<OP, 1, TA, DB, EPI>(g, n_cu, stream);
         if (stages == 2) return launch_layer_rows<OP, 2, TA, DB, EPI>(g, n_cu, stream);
-        return launch_layer_rows<OP, 4, TA, DB, EPI>(g, n_cu, stream);
+        if constexpr (OP == kOpBf16) return launch_layer_rows<OP, 4, TA, DB, EPI>(g, n_cu, stream);
     }
     auto tiles = [&](int b) { return (uint64_t)((g.N + b - 1) / b) * (uint64_t)((g.M + b - 1) / b); };
     const int b = tiles(128) >= (uint64_t)n_cu ? 128 : 64;

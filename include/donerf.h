@@ -383,7 +383,8 @@ int donerf_mx_linear(donerf_t* h, const donerf_mat* x, const donerf_mat* w, cons
                      const donerf_mat* y, int64_t rows, int32_t in, int32_t out, void* workspace,
                      size_t workspace_bytes);
 
-/* Bytes of workspace for x of this donerf_type; 0 for sizes that are refused. */
+/* Bytes of workspace for x of this donerf_type: 0 where none is needed (MXFP4, a
+   few rows), and for sizes that are refused. */
 size_t donerf_mx_linear_workspace(int32_t x_type, int64_t rows, int32_t in);
 
 /*
@@ -425,7 +426,8 @@ int donerf_train_linear_backward(donerf_t* h, const donerf_mat* dz, const donerf
                                  int32_t accumulate, int64_t rows, int32_t in, int32_t out, void* workspace,
                                  size_t workspace_bytes);
 
-/* Bytes of workspace on the handle's device; 0 for sizes that are refused. */
+/* Bytes of workspace on the handle's device: 0 where none is needed (a few rows),
+   and for sizes that are refused. */
 size_t donerf_train_linear_backward_workspace(const donerf_t* h, int64_t rows, int32_t in, int32_t out);
 
 /* The device and the stream that a handle's work goes to; each may be NULL. */

@@ -875,6 +875,7 @@ int donerf_mx_dequantize(donerf_t* h, const donerf_mat* q, const donerf_mat* y, 
 size_t donerf_mx_linear_workspace(int32_t x_type, int64_t rows, int32_t in) {
     if (rows < 1 || rows > INT32_MAX || in < 1 || in > DONERF_MAX_COLS) return 0;
     if (x_type != DONERF_TYPE_FP32 && x_type != DONERF_TYPE_BF16) return 0;
+    if (rows <= kFewRows) return 0;   // converted where it is multiplied
     return quantized_codes(rows, in) + (size_t)rows * (size_t)scale_row(in);
 }
 
@@ -894,6 +895,29 @@ int donerf_mx_linear(donerf_t* h, const donerf_mat* x, const donerf_mat* w, cons
         (rc = validate_handle(h)))
         return rc;
     if (rows == 0) return DONERF_OK;
+    const int kind = y->type == DONERF_TYPE_MXFP4 ? kOutMx4 : y->type == DONERF_TYPE_BF16 ? kOutBf16 : kOutF32;
+    if (rows <= kFewRows) {
+        FewRowsArgs f{};
+        f.x = (const uint8_t*)x->data;
+        f.ldx = x->ld;
+        f.x_scales = x->scales;
+        f.ldx_scales = x->ld_scales;
+        f.w = (const uint8_t*)w->data;
+        f.ldw = w->ld;
+        f.w_scales = w->scales;
+        f.ldw_scales = w->ld_scales;
+        f.bias = bias;
+        if (kind == kOutMx4) f.q = mx_out(y);
+        f.y = (uint8_t*)y->data;
+        f.ldy = y->ld;
+        f.M = (int32_t)rows;
+        f.N = out;
+        f.K = in;
+        f.relu = relu;
+        f.out = kind;
+        const hipError_t e = launch_mx_few_rows(f, x->type == DONERF_TYPE_MXFP4 ? 2 : x->type, h->stream);
+        return e == hipSuccess ? DONERF_OK : hip_fail(e, "mx_linear launch");
+    }
     GemmArgs g{};
     g.a = mx_in(w);
     hipError_t e;
@@ -908,11 +932,9 @@ int donerf_mx_linear(donerf_t* h, const donerf_mat* x, const donerf_mat* w, cons
     }
     g.bias = bias;
     g.relu = relu;
-    int kind = kOutMx4;
-    if (y->type == DONERF_TYPE_MXFP4) {
+    if (kind == kOutMx4) {
         g.q = mx_out(y);
     } else {
-        kind = y->type == DONERF_TYPE_BF16 ? kOutBf16 : kOutF32;
         g.y = (uint8_t*)y->data;
         g.ldy = y->ld;
     }

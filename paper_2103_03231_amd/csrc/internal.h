@@ -176,6 +176,24 @@ hipError_t launch_mx_dequantize(const MxIn& q, bool fp8, void* y, int64_t ldy, b
                                 int n_cu, hipStream_t stream);
 // g.a, g.b E2M1.
 hipError_t launch_mx_linear(const GemmArgs& g, int out, int n_cu, hipStream_t stream);
+// The same for up to kFewRows rows, x fp32 (0), bf16 (1) or E2M1 (2).
+constexpr int kFewRows = 32;
+struct FewRowsArgs {
+    const uint8_t* x;
+    int64_t ldx;             // values, or bytes of E2M1 rows
+    const uint8_t* x_scales;
+    int64_t ldx_scales;
+    const uint8_t* w;
+    int64_t ldw;             // bytes
+    const uint8_t* w_scales;
+    int64_t ldw_scales;
+    const float* bias;
+    uint8_t* y;              // fp32 or bf16 rows
+    int64_t ldy;
+    MxOut q;                 // or E2M1 ones
+    int32_t M, N, K, relu, out;
+};
+hipError_t launch_mx_few_rows(const FewRowsArgs& g, int x_kind, hipStream_t stream);
 // g.a, g.b bf16; y and q may each be null.
 hipError_t launch_train_linear(const GemmArgs& g, int n_cu, hipStream_t stream);
 

@@ -137,11 +137,14 @@ def test_flags_bias_and_workspace():
     refused(backward(relu=-1), "must be 0 or 1")
     refused(backward(accumulate=2), "must be 0 or 1")
     refused(backward(db=A + 1), "db not aligned")
-    need = b.donerf_mx_linear_workspace(BF16, 4, 100)
-    assert need == 4 * 64 + 4 * 8
-    refused(linear(ws_bytes=need - 1), "workspace of", b.E_SIZE)
-    refused(linear(ws=None), "workspace is NULL")
-    refused(linear(ws=A + 8), "workspace not aligned")
+    need = b.donerf_mx_linear_workspace(BF16, 100, 100)
+    assert need == 100 * 64 + 100 * 8
+    refused(linear(rows=100, ws_bytes=need - 1), "workspace of", b.E_SIZE)
+    refused(linear(rows=100, ws=None), "workspace is NULL")
+    refused(linear(rows=100, ws=A + 8), "workspace not aligned")
+    # a few rows need none
+    assert b.donerf_mx_linear_workspace(BF16, 32, 100) == 0 < b.donerf_mx_linear_workspace(BF16, 33, 100)
+    refused(linear(rows=32, ws=None), "handle is NULL")
     assert b.donerf_mx_linear_workspace(b.MXFP4, 4, 100) == 0 == b.donerf_mx_linear_workspace(F32, -1, 100)
     assert b.donerf_mx_linear_workspace(F32, 4, 0) == 0 == b.donerf_mx_linear_workspace(F32, 4, b.MAX_COLS + 1)
     assert b.donerf_train_linear_backward_workspace(None, 4, 4, 4) == 0

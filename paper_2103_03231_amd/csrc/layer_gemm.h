@@ -4,10 +4,9 @@
 //
 // A workgroup computes a tile of BN weight rows by BM batch rows in stages of
 // 128 bytes of every row (64 bf16 or 256 E2M1 columns).  In LDS a row's eight
-// 16-byte chunks are permuted, chunk c at position c ^ (row & 7), so that the
-// eight lanes which an LDS cycle serves, eight rows of one chunk, meet eight
-// different bank groups.  Two such stages alternate in two arrays: the copy of
-// one runs while the other is multiplied.
+// 16-byte chunks are permuted (row_key), so that reads of one chunk of sixteen rows
+// meet all 64 banks.  Two such stages alternate in two arrays: the copy of one runs
+// while the other is multiplied.
 //
 // The weights are the MFMA's A operand and the batch its B operand, so a lane's
 // accumulators are 16 of a block's 32 outputs of one batch row, which it shares
@@ -34,6 +33,15 @@ constexpr int kEpiMaskMx8 = 4;   // y bf16, zero where the ReLU's output (E4M3) 
 constexpr int kEpiMaskBf16 = 5;  // the same, the ReLU's output in bf16
 constexpr bool masked(int epi) { return epi == kEpiMaskMx8 || epi == kEpiMaskBf16; }
 
+// In LDS, chunk c of a row of CHUNKS 16-byte chunks lies at c ^ row_key(row): sixteen
+// consecutive rows' chunks c then cover the banks' 256 bytes, to which the row's own
+// place adds what CHUNKS leaves of it.
+template <int CHUNKS>
+__device__ __forceinline__ int row_key(int row) {
+    if constexpr (CHUNKS >= 16) return row & 15;
+    else return (row / (16 / CHUNKS)) & (CHUNKS - 1);
+}
+
 // 16 zero bytes: what a lane copies in place of chunks behind the last column.
 __device__ const uint32_t kZeroChunk[4] = {0, 0, 0, 0};
 
@@ -52,7 +60,9 @@ struct StageCopy {
     int64_t first;             // row of this lane in the wave's first copy
     int chunk;                 // of this lane, in every row
     __device__ __forceinline__ void init(const MxIn& src, int64_t row0, int64_t rows, int K, int wave, int lane) {
-        chunk = (lane & 7) ^ (lane >> 3);
+        // copies of a wave are 8 NW rows apart, which the key does not see
+        static_assert(NW % 2 == 0, "row_key");
+        chunk = (lane & 7) ^ row_key<kStageChunks>(wave * 8 + (lane >> 3));
         first = row0 + wave * 8 + (lane >> 3);
         if constexpr (DIRECT) {
 #pragma unroll
@@ -257,7 +267,7 @@ __device__ __forceinline__ Mask16 load_mask(const GemmArgs& g, int64_t m0, int n
 // theirs into LDS, then all threads store whole rows.  A wave's own 32 outputs of 32
 // rows would be that many pieces of 16 to 64 bytes (stored like that, six 4-bit hidden
 // layers of 640000 rows took 412 us, and 186 us without their stores).  In LDS, a row's
-// 16-byte chunks are permuted, chunk c at c ^ (row & 7).
+// 16-byte chunks are permuted (row_key).
 template <int EPI, int ROWS, int COLS>
 struct Outgoing {
     static constexpr bool kY = EPI != kEpiMx4, kQ = EPI == kEpiMx4 || EPI == kEpiKept;
@@ -269,7 +279,7 @@ struct Outgoing {
     static_assert(ROWS * kBlocks % 16 == 0, "whole chunks");
 
     template <int CHUNKS>
-    __device__ static __forceinline__ int slot(int row, int c) { return row * CHUNKS + (c ^ (row & 7 & (CHUNKS - 1))); }
+    __device__ static __forceinline__ int slot(int row, int c) { return row * CHUNKS + (c ^ row_key<CHUNKS>(row)); }
 
     // What follows the product for the accumulator of rows [r0, r0 + 32) and
     // outputs [c0, c0 + 32) of the tile, which starts at output n_tile.
@@ -502,7 +512,7 @@ __global__ void __launch_bounds__(64 * WN * WM, 2) layer_gemm_kernel(GemmArgs g)
             for (int j = 0; j < TM; ++j) vb[j] = stage_scales(sb[j], stage, g.K, half);
         }
         sfor<4>([&](auto S) {
-            const int c = (2 * CV(S) + half) ^ (col & 7);
+            const int c = (2 * CV(S) + half) ^ row_key<kStageChunks>(col);
             u32x4 fa[TN], fb[TM];
 #pragma unroll
             for (int i = 0; i < TN; ++i) {
@@ -610,7 +620,8 @@ __global__ void __launch_bounds__(512, rows_workgroups(OP, KS) * 2) layer_rows_k
     const f32x16 bias = bias_rows(g, wn * 32, half);
 
     // ---- the batch
-    const int chunk = (lane & 7) ^ (lane >> 3);
+    static_assert(RT == 8 * NW, "a wave's copies are the same rows of each stage");
+    const int chunk = (lane & 7) ^ row_key<kStageChunks>(wave * 8 + (lane >> 3));
     const Bf16Rows rows((const uint16_t*)g.b.codes, g.b.ld / 2, g.M, g.K);
     u32x4 held[DB ? 1 : CP];
     // copy i of a wave: eight rows of one stage
@@ -662,7 +673,7 @@ __global__ void __launch_bounds__(512, rows_workgroups(OP, KS) * 2) layer_rows_k
             uint32_t vb = 0;
             if constexpr (OP == kOpMx4) vb = pack_scales(((const uint64_t*)(lds + kChunks))[row * KS + CV(S)], CV(S), g.K, half);
             sfor<4>([&](auto I) {
-                const u32x4 fb = lds[(CV(S) * RT + row) * kStageChunks + ((2 * CV(I) + half) ^ (col & 7))];
+                const u32x4 fb = lds[(CV(S) * RT + row) * kStageChunks + ((2 * CV(I) + half) ^ row_key<kStageChunks>(col))];
                 acc = mma_step<OP, CV(I)>(fa[CV(S)][CV(I)], fb, acc, OP == kOpMx4 ? va[CV(S)] : 0u, vb);
             });
         });
@@ -730,6 +741,12 @@ __global__ void __launch_bounds__(512, rows_workgroups(OP, KS) * 2) layer_rows_k
     }
 }
 
+#ifndef LG_BIG
+#define LG_BIG 1
+#endif
+#ifndef LG_WN
+#define LG_WN 4
+#endif
 #ifndef LG_ROWS
 #define LG_ROWS 1
 #endif
@@ -753,11 +770,13 @@ hipError_t launch_layer_gemm(GemmArgs g, int n_cu, hipStream_t stream) {
         if constexpr (OP == kOpBf16) return launch_layer_rows<OP, 4, TA, DB, EPI>(g, n_cu, stream);
     }
     auto tiles = [&](int b) { return (uint64_t)((g.N + b - 1) / b) * (uint64_t)((g.M + b - 1) / b); };
-    const int b = tiles(128) >= (uint64_t)n_cu ? 128 : 64;
+    const int b = OP == kOpBf16 && tiles(256) >= LG_BIG * (uint64_t)n_cu ? 256 : tiles(128) >= (uint64_t)n_cu ? 128 : 64;
     g.tiles_n = (uint32_t)((g.N + b - 1) / b);
     g.tiles_m = (uint32_t)((g.M + b - 1) / b);
     const dim3 grid((g.tiles_n * g.tiles_m + 7) / 8 * 8);
-    if (b == 128) hipLaunchKernelGGL((layer_gemm_kernel<OP, 128, 128, 2, 2, TA, DA, DB, EPI>), grid, dim3(256), 0, stream, g);
+    if (b == 256) {
+        if constexpr (OP == kOpBf16) hipLaunchKernelGGL((layer_gemm_kernel<OP, 256, 256, LG_WN, 8 / LG_WN, TA, DA, DB, EPI>), grid, dim3(512), 0, stream, g);
+    } else if (b == 128) hipLaunchKernelGGL((layer_gemm_kernel<OP, 128, 128, 2, 2, TA, DA, DB, EPI>), grid, dim3(256), 0, stream, g);
     else hipLaunchKernelGGL((layer_gemm_kernel<OP, 64, 64, 2, 2, TA, DA, DB, EPI>), grid, dim3(256), 0, stream, g);
     return hipGetLastError();
 }

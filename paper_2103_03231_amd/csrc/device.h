@@ -44,6 +44,14 @@ __device__ __forceinline__ void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// Orders one wave's LDS accesses across its lanes: LDS executes a wave's
+// instructions in order, so only the compiler has to keep them in place.
+__device__ __forceinline__ void wave_lds_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // A barrier that waits for nothing but the other waves.  lds_barrier's release also
 // waits for every copy into LDS that is under way; where those of later stages are
 // to stay in flight, the caller waits for the ones that it needs, and its LDS reads

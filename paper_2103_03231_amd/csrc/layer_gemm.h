@@ -55,6 +55,7 @@ struct StageCopy {
     static_assert(ROWS % (8 * NW) == 0, "rows split evenly over the waves");
     static_assert(DIRECT || OP == kOpBf16, "microscaled rows are aligned");
     const uint8_t* row[DIRECT ? PER : 1];   // of this lane, in each copy
+    int64_t off[DIRECT ? 1 : PER];          // the same in values
     u32x4 held[DIRECT ? 1 : PER];
     Bf16Rows any;
     int64_t first;             // row of this lane in the wave's first copy
@@ -69,6 +70,8 @@ struct StageCopy {
             for (int i = 0; i < PER; ++i) row[i] = src.codes + row_of(i, rows) * src.ld;
         } else {
             any = Bf16Rows((const uint16_t*)src.codes, src.ld / 2, rows, K);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) off[i] = row_of(i, rows) * any.ld;
         }
     }
     // rows behind the last one repeat it: their results are not stored
@@ -86,7 +89,7 @@ struct StageCopy {
                 p = c * per_chunk < K ? p : (const uint8_t*)kZeroChunk;
                 __builtin_amdgcn_global_load_lds((const u32x4*)p, lds + (i * NW + wave) * 64, 16, 0, 0);
             } else {
-                held[i] = any.load(row_of(i, any.rows), c * 8);
+                held[i] = any.load_at(off[i] + c * 8, c * 8);
             }
         }
     }
@@ -106,7 +109,9 @@ struct StageCopy {
 // the stage is read by columns: a transposing read takes 64 bytes of eight rows at
 // once, and rows that follow each other start 64 bytes apart in the banks.
 template <int CHUNKS>
-__device__ __forceinline__ int column_slot(int m, int c) { return m * CHUNKS + (c ^ ((m & (CHUNKS >= 16 ? 3 : 1)) << 2)); }
+__device__ __forceinline__ int column_slot(int m, int c) {
+    return m * CHUNKS + (c ^ ((m & (CHUNKS >= 16 ? 3 : CHUNKS >= 8 ? 1 : 0)) << 2));
+}
 
 // The MFMA operand of 32 columns from column n on and 16 rows from row m on of
 // such a stage: lane l has column n + (l & 31), rows m + 8 (l >> 5) + (0..7).
@@ -134,6 +139,7 @@ struct ColumnCopy {
     Bf16Rows any;
     u32x4 held[DIRECT ? 1 : PER];
     int64_t begin, end;   // rows
+    int64_t off;          // of this lane's chunk in the first stage, in values
     int row, col, col0;   // of this lane in the wave's first copy; first column of the stage
     __device__ __forceinline__ void init(const uint16_t* p, int64_t ld, int64_t rows, int cols, int64_t begin_, int64_t end_,
                                          int col0_, int wave, int lane) {
@@ -146,17 +152,18 @@ struct ColumnCopy {
         static_assert((EACH * NW) % 4 == 0, "swizzle");
         col0 = col0_;
         col = col0_ + ((lane % CHUNKS) ^ (column_slot<CHUNKS>(row, 0) - row * CHUNKS)) * 8;
+        off = (begin + row) * ld + col;
     }
     __device__ __forceinline__ void issue(u32x4* lds, int stage, int wave) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int64_t m = begin + (int64_t)stage * ROWS + row + i * EACH * NW;
+            const int64_t first = (int64_t)stage * ROWS + i * EACH * NW, at = off + first * any.ld;
             if constexpr (DIRECT) {
-                const uint8_t* p = (const uint8_t*)(any.base + m * any.ld + col);
-                p = m < end && col < any.cols ? p : (const uint8_t*)kZeroChunk;
+                const uint8_t* p = (const uint8_t*)(any.base + at);
+                p = begin + first + row < end && col < any.cols ? p : (const uint8_t*)kZeroChunk;
                 __builtin_amdgcn_global_load_lds((const u32x4*)p, lds + (i * NW + wave) * 64, 16, 0, 0);
             } else {
-                held[i] = any.load(m < end ? m : end - 1, col);
+                held[i] = any.load_at(at, col);   // rows from `end` on are cleared afterwards
             }
         }
     }
@@ -741,15 +748,112 @@ __global__ void __launch_bounds__(512, rows_workgroups(OP, KS) * 2) layer_rows_k
     }
 }
 
-#ifndef LG_BIG
-#define LG_BIG 1
-#endif
-#ifndef LG_WN
-#define LG_WN 4
-#endif
-#ifndef LG_ROWS
-#define LG_ROWS 1
-#endif
+// Products with so few results that tiles would leave most compute units without
+// work: a workgroup takes 32 outputs of 32 batch rows, and its eight waves split the
+// terms, a stage each in turn, from memory into registers, and add up their parts
+// in LDS, in the waves' order.
+template <int OP, bool TA, int EPI>
+__global__ void __launch_bounds__(512, 2) layer_split_kernel(GemmArgs g) {
+    constexpr int NW = 8, stage_cols = OP == kOpBf16 ? 64 : 256;
+    using Out = Outgoing<EPI, 32, 32>;
+    __shared__ f32x4 part[NW][4][64];
+    __shared__ u32x4 out[Out::kSize];
+    __shared__ u32x4 terms[TA ? NW * 64 * 4 : 1];   // a wave's stage of transposed weights
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 31, half = lane >> 5;
+    const int n0 = (int)(blockIdx.x % g.tiles_n) * 32;
+    const int64_t m0 = (int64_t)(blockIdx.x / g.tiles_n) * 32;
+    const int stages = (g.K + stage_cols - 1) / stage_cols;
+    const int64_t ra = n0 + col < g.N ? n0 + col : g.N - 1, rb = m0 + col < g.M ? m0 + col : g.M - 1;
+    const Bf16Rows a((const uint16_t*)g.a.codes, g.a.ld / 2, TA ? g.K : g.N, TA ? g.N : g.K);
+    const Bf16Rows b((const uint16_t*)g.b.codes, g.b.ld / 2, g.M, g.K);
+    u32x4* const mine = terms + (TA ? wave * 64 * 4 : 0);
+
+    struct Held {
+        u32x4 a[4], b[4];
+        uint64_t sa, sb;
+    };
+    auto load = [&](Held& h, int stage) {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const int c = stage * kStageChunks + 2 * s + half;
+            if constexpr (OP == kOpBf16) {
+                h.b[s] = b.load(rb, c * 8);
+                if constexpr (!TA) h.a[s] = a.load(ra, c * 8);
+                // 16 terms by 32 outputs, a lane the quarter lane % 4 of a term
+                else h.a[s] = a.load_at((int64_t)(stage * 64 + s * 16 + lane / 4) * a.ld + n0 + lane % 4 * 8, n0 + lane % 4 * 8);
+            } else {
+                const uint8_t *pa = g.a.codes + ra * g.a.ld + c * 16, *pb = g.b.codes + rb * g.b.ld + c * 16;
+                h.a[s] = *(const u32x4*)(c * kMxBlock < g.K ? pa : (const uint8_t*)kZeroChunk);
+                h.b[s] = *(const u32x4*)(c * kMxBlock < g.K ? pb : (const uint8_t*)kZeroChunk);
+            }
+        }
+        if constexpr (OP == kOpMx4) {
+            const int at = stage * 8 * kMxBlock < g.K ? stage * 8 : 0;
+            h.sa = *(const uint64_t*)(g.a.scales + ra * g.a.ld_scales + at);
+            h.sb = *(const uint64_t*)(g.b.scales + rb * g.b.ld_scales + at);
+        }
+    };
+    f32x16 acc;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
+    auto multiply = [&](Held& h, int stage) {
+        if constexpr (OP == kOpBf16) {
+            if ((stage + 1) * stage_cols > g.K)
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    const int k = (stage * kStageChunks + 2 * s + half) * 8;
+                    h.b[s] = b.fix(h.b[s], rb, k);
+                    if constexpr (!TA) h.a[s] = a.fix(h.a[s], ra, k);
+                }
+            if constexpr (TA) {
+                const int n = n0 + lane % 4 * 8;
+                if (n0 + 32 > g.N || (stage + 1) * 64 > g.K)
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) {
+                        const int64_t term = stage * 64 + s * 16 + lane / 4;
+                        h.a[s] = term < g.K ? a.fix(h.a[s], term, n) : u32x4{0, 0, 0, 0};
+                    }
+#pragma unroll
+                for (int s = 0; s < 4; ++s) mine[s * 64 + lane] = h.a[s];
+                wave_lds_fence();
+#pragma unroll
+                for (int s = 0; s < 4; ++s) h.a[s] = __builtin_bit_cast(u32x4, read_columns<4>(mine, s * 16, 0, lane));
+                wave_lds_fence();
+            }
+        }
+        uint32_t va = 0, vb = 0;
+        if constexpr (OP == kOpMx4) {
+            va = pack_scales(h.sa, stage, g.K, half);
+            vb = pack_scales(h.sb, stage, g.K, half);
+        }
+        sfor<4>([&](auto S) { acc = mma_step<OP, CV(S)>(h.a[CV(S)], h.b[CV(S)], acc, va, vb); });
+    };
+    Held h0, h1;
+    if (wave < stages) load(h0, wave);
+    for (int s = wave; s < stages; s += 2 * NW) {
+        if (s + NW < stages) load(h1, s + NW);
+        multiply(h0, s);
+        if (s + 2 * NW < stages) load(h0, s + 2 * NW);
+        if (s + NW < stages) multiply(h1, s + NW);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) part[wave][q][lane] = f32x4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
+    lds_barrier();
+    if (wave > 0) return;
+    acc = bias_rows(g, n0, half);
+#pragma unroll
+    for (int w = 0; w < NW; ++w)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[4 * q + i] += part[w][q][lane][i];
+    Out::put(out, g, acc, load_mask<EPI>(g, m0, n0, lane), 0, 0, n0, lane);
+    wave_lds_fence();
+    Out::template store<64>(out, g, m0, n0, threadIdx.x);
+}
+
 template <int OP, int KS, bool TA, bool DB, int EPI>
 hipError_t launch_layer_rows(GemmArgs g, int n_cu, hipStream_t stream) {
     g.tiles_m = (uint32_t)(((int64_t)g.M + kRowsTile - 1) / kRowsTile);
@@ -764,19 +868,28 @@ template <int OP, bool TA, bool DA, bool DB, int EPI>
 hipError_t launch_layer_gemm(GemmArgs g, int n_cu, hipStream_t stream) {
     constexpr int stage_cols = OP == kOpBf16 ? 64 : 256;
     const int stages = (g.K + stage_cols - 1) / stage_cols;
-    if (LG_ROWS && g.N <= 256 && stages <= (OP == kOpMx4 ? 2 : 4) && (int64_t)g.M >= 64 * (int64_t)n_cu) {
+    if (g.N <= 256 && stages <= (OP == kOpMx4 ? 2 : 4) && (int64_t)g.M >= 64 * (int64_t)n_cu) {
         if (stages == 1) return launch_layer_rows<OP, 1, TA, DB, EPI>(g, n_cu, stream);
         if (stages == 2) return launch_layer_rows<OP, 2, TA, DB, EPI>(g, n_cu, stream);
         if constexpr (OP == kOpBf16) return launch_layer_rows<OP, 4, TA, DB, EPI>(g, n_cu, stream);
     }
     auto tiles = [&](int b) { return (uint64_t)((g.N + b - 1) / b) * (uint64_t)((g.M + b - 1) / b); };
-    const int b = OP == kOpBf16 && tiles(256) >= LG_BIG * (uint64_t)n_cu ? 256 : tiles(128) >= (uint64_t)n_cu ? 128 : 64;
+    // the largest tiles that leave every compute unit one
+    constexpr bool kBig = OP == kOpBf16 && DA && DB;
+    const bool big = kBig && tiles(256) >= (uint64_t)n_cu;
+    const bool split = 2 * tiles(64) <= (uint64_t)n_cu && stages >= 4;
+    const int b = big ? 256 : split ? 32 : tiles(128) >= (uint64_t)n_cu ? 128 : 64;
     g.tiles_n = (uint32_t)((g.N + b - 1) / b);
     g.tiles_m = (uint32_t)((g.M + b - 1) / b);
     const dim3 grid((g.tiles_n * g.tiles_m + 7) / 8 * 8);
-    if (b == 256) {
-        if constexpr (OP == kOpBf16) hipLaunchKernelGGL((layer_gemm_kernel<OP, 256, 256, LG_WN, 8 / LG_WN, TA, DA, DB, EPI>), grid, dim3(512), 0, stream, g);
-    } else if (b == 128) hipLaunchKernelGGL((layer_gemm_kernel<OP, 128, 128, 2, 2, TA, DA, DB, EPI>), grid, dim3(256), 0, stream, g);
+    if constexpr (kBig) {   // E2M1 ran slower on 256 x 256 (190 us for 8192 x 4096 x 4096, 143 us on 128 x 128)
+        if (b == 256) {
+            hipLaunchKernelGGL((layer_gemm_kernel<OP, 256, 256, 4, 2, TA, DA, DB, EPI>), grid, dim3(512), 0, stream, g);
+            return hipGetLastError();
+        }
+    }
+    if (b == 32) hipLaunchKernelGGL((layer_split_kernel<OP, TA, EPI>), dim3(g.tiles_n * g.tiles_m), dim3(512), 0, stream, g);
+    else if (b == 128) hipLaunchKernelGGL((layer_gemm_kernel<OP, 128, 128, 2, 2, TA, DA, DB, EPI>), grid, dim3(256), 0, stream, g);
     else hipLaunchKernelGGL((layer_gemm_kernel<OP, 64, 64, 2, 2, TA, DA, DB, EPI>), grid, dim3(256), 0, stream, g);
     return hipGetLastError();
 }

@@ -211,9 +211,13 @@ struct Bf16Rows {
     __device__ __forceinline__ Bf16Rows(const uint16_t* p, int64_t ld_, int64_t rows_, int cols_)
         : base(p), ld(ld_), rows(rows_), cols(cols_), last((rows_ - 1) * ld_ + cols_ - 8) {}
     // The chunk at column k of a row < rows; k may lie behind the last column.
-    __device__ __forceinline__ u32x4 load(int64_t row, int k) const {
-        if (last < 0) return Row8<uint16_t>::load_raw(base + row * ld, k, cols);   // fewer than 16 bytes
-        const int64_t at = row * ld + k;
+    __device__ __forceinline__ u32x4 load(int64_t row, int k) const { return load_at(row * ld + k, k); }
+    // The same by its offset in the matrix, which may lie behind its end.
+    __device__ __forceinline__ u32x4 load_at(int64_t at, int k) const {
+        if (last < 0) {   // fewer than 16 bytes
+            const int64_t row = at - k;
+            return row <= last + 8 - cols ? Row8<uint16_t>::load_raw(base + row, k, cols) : u32x4{0, 0, 0, 0};
+        }
         u32x4 v;
         __builtin_memcpy(&v, base + (at < last ? at : last), 16);
         return v;

@@ -85,14 +85,6 @@ struct Prec<kFP8> {
 
 // ------------------------------------------------------------------ LDS weight stream
 
-// Orders one wave's LDS accesses across its lanes: LDS executes a wave's
-// instructions in order, so only the compiler has to keep them in place.
-__device__ __forceinline__ void wave_lds_fence() {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
-}
-
 constexpr int kChunkVec = kChunkBytes / 16;  // u32x4 per chunk
 // LDS fragment reads in flight, in 1 KiB fragments.  Measured on 5 x 400 x
 // 400, N = 4: 12 ran 2 % faster than 3 with 32x32 hidden layers; with the 16x16

@@ -190,20 +190,31 @@ __global__ void __launch_bounds__(256, 2) weight_grad_kernel(GradArgs g) {
     }
 }
 
-// dW and db from the splits' parts, added in their order.
+// dW and db from the splits' parts: a workgroup adds up 32 values, eight threads a
+// value, each an eighth of the splits in their order, and then the eight sums.
 __global__ void __launch_bounds__(256) grad_sum_kernel(const float* dw_parts, const float* db_parts, int splits, int N,
                                                        int K, float* dw, int64_t lddw, float* db, int accumulate) {
+    __shared__ float part[8][32];
+    const int c = threadIdx.x & 31, eighth = threadIdx.x >> 5;
     const int64_t nk = (int64_t)N * K, total = (dw ? nk : 0) + (db ? N : 0);
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int from = splits * eighth / 8, to = splits * (eighth + 1) / 8;
+    for (int64_t i0 = (int64_t)blockIdx.x * 32; i0 < total; i0 += (int64_t)gridDim.x * 32) {
+        const int64_t i = i0 + c < total ? i0 + c : total - 1;
         const bool is_w = dw && i < nk;
-        const int64_t at = is_w ? i : i - (dw ? nk : 0);
-        const float* p = is_w ? dw_parts + at : db_parts + at;
-        const int64_t stride = is_w ? nk : N;
+        const int64_t at = is_w ? i : i - (dw ? nk : 0), stride = is_w ? nk : N;
+        const float* p = (is_w ? dw_parts : db_parts) + at;
         float s = 0.0f;
 #pragma unroll 8
-        for (int k = 0; k < splits; ++k) s += p[k * stride];
-        float* o = is_w ? dw + at / K * lddw + at % K : db + at;
-        *o = accumulate ? *o + s : s;
+        for (int k = from; k < to; ++k) s += p[k * stride];
+        part[eighth][c] = s;
+        __syncthreads();
+        if (eighth == 0 && i0 + c < total) {
+#pragma unroll
+            for (int e = 1; e < 8; ++e) s += part[e][c];
+            float* o = is_w ? dw + at / K * lddw + at % K : db + at;
+            *o = accumulate ? *o + s : s;
+        }
+        __syncthreads();
     }
 }
 
@@ -212,24 +223,18 @@ struct GradPlan {
     size_t parts;   // bytes
 };
 
-#ifndef GW_TK
-#define GW_TK 2
-#endif
-#ifndef GW_R
-#define GW_R 64
-#endif
-#ifndef GW_WG
-#define GW_WG 2
-#endif
-constexpr int kGradRows = GW_R;
+// Columns of a tile, in blocks per wave, and the batch rows of a stage; half of them
+// where dz, too, passes through registers.
+constexpr int kGradBlocks = 2, kGradRows = 64, kGradRowsAny = 32;
+
 // The batch is split until two workgroups per compute unit have work.
 GradPlan grad_plan(int64_t M, int N, int K, int n_cu) {
     GradPlan p;
     p.tiles_n = (N + kGradTileN - 1) / kGradTileN;
-    p.tiles_k = (K + 64 * GW_TK - 1) / (64 * GW_TK);
+    p.tiles_k = (K + 64 * kGradBlocks - 1) / (64 * kGradBlocks);
     const int64_t stages = (M + kGradRows - 1) / kGradRows;
     const int64_t tiles = (int64_t)p.tiles_n * p.tiles_k;
-    int64_t want = GW_WG * (int64_t)n_cu / tiles;
+    int64_t want = 2 * (int64_t)n_cu / tiles;
     want = want < 1 ? 1 : want > stages ? (stages < 1 ? 1 : stages) : want;
     const int64_t per = (stages + want - 1) / want;
     p.rows_per_split = (int)(per < 1 ? kGradRows : per * kGradRows);
@@ -301,14 +306,14 @@ hipError_t launch_train_linear_backward(const BackwardArgs& a, int n_cu, hipStre
         g.accumulate = direct ? a.accumulate : 0;
         const dim3 grid(((uint32_t)p.tiles_n * p.tiles_k * p.splits + 7) / 8 * 8);
         const bool copies = whole_chunks(MxIn{(const uint8_t*)a.dz, a.lddz * 2, nullptr, 0}, a.N);
-        if (copies && !a.x_bf16) hipLaunchKernelGGL((weight_grad_kernel<true, false, GW_TK, GW_R>), grid, dim3(256), 0, stream, g);
-        else if (copies) hipLaunchKernelGGL((weight_grad_kernel<true, true, GW_TK, GW_R>), grid, dim3(256), 0, stream, g);
-        else if (!a.x_bf16) hipLaunchKernelGGL((weight_grad_kernel<false, false, GW_TK, GW_R>), grid, dim3(256), 0, stream, g);
-        else hipLaunchKernelGGL((weight_grad_kernel<false, true, GW_TK, GW_R>), grid, dim3(256), 0, stream, g);
+        if (copies && !a.x_bf16) hipLaunchKernelGGL((weight_grad_kernel<true, false, kGradBlocks, kGradRows>), grid, dim3(256), 0, stream, g);
+        else if (copies) hipLaunchKernelGGL((weight_grad_kernel<true, true, kGradBlocks, kGradRows>), grid, dim3(256), 0, stream, g);
+        else if (!a.x_bf16) hipLaunchKernelGGL((weight_grad_kernel<false, false, kGradBlocks, kGradRowsAny>), grid, dim3(256), 0, stream, g);
+        else hipLaunchKernelGGL((weight_grad_kernel<false, true, kGradBlocks, kGradRowsAny>), grid, dim3(256), 0, stream, g);
         if ((e = hipGetLastError()) != hipSuccess || direct) return e;
     }
     const int64_t total = (int64_t)a.N * a.K + a.N;
-    const uint64_t wg = (uint64_t)((total + 255) / 256), most = (uint64_t)n_cu * 32;
+    const uint64_t wg = (uint64_t)((total + 31) / 32), most = (uint64_t)n_cu * 32;
     hipLaunchKernelGGL(grad_sum_kernel, dim3((uint32_t)(wg < most ? wg : most)), dim3(256), 0, stream, dw_parts, db_parts,
                        p.splits, a.N, a.K, a.dw, a.lddw, a.db, a.accumulate);
     return hipGetLastError();

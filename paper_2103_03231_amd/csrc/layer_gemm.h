@@ -750,85 +750,102 @@ __global__ void __launch_bounds__(512, rows_workgroups(OP, KS) * 2) layer_rows_k
 
 // Products with so few results that tiles would leave most compute units without
 // work: a workgroup takes 32 outputs of 32 batch rows, and its eight waves split the
-// terms, a stage each in turn, from memory into registers, and add up their parts
-// in LDS, in the waves' order.
+// terms, a stage each in turn, and add up their parts in LDS, in the waves' order.
+// A stage passes through a part of LDS that is the wave's own, so that its loads
+// cover eight rows' 128 bytes at once (whole cache lines) and no wave waits for
+// another.
 template <int OP, bool TA, int EPI>
 __global__ void __launch_bounds__(512, 2) layer_split_kernel(GemmArgs g) {
-    constexpr int NW = 8, stage_cols = OP == kOpBf16 ? 64 : 256;
+    constexpr int NW = 8, stage_cols = OP == kOpBf16 ? 64 : 256, kChunk = OP == kOpBf16 ? 8 : kMxBlock;
     using Out = Outgoing<EPI, 32, 32>;
     __shared__ f32x4 part[NW][4][64];
     __shared__ u32x4 out[Out::kSize];
-    __shared__ u32x4 terms[TA ? NW * 64 * 4 : 1];   // a wave's stage of transposed weights
+    __shared__ u32x4 stage_lds[NW][2][32 * kStageChunks];   // transposed weights: 64 terms of 4 chunks
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, half = lane >> 5;
     const int n0 = (int)(blockIdx.x % g.tiles_n) * 32;
     const int64_t m0 = (int64_t)(blockIdx.x / g.tiles_n) * 32;
     const int stages = (g.K + stage_cols - 1) / stage_cols;
-    const int64_t ra = n0 + col < g.N ? n0 + col : g.N - 1, rb = m0 + col < g.M ? m0 + col : g.M - 1;
     const Bf16Rows a((const uint16_t*)g.a.codes, g.a.ld / 2, TA ? g.K : g.N, TA ? g.N : g.K);
     const Bf16Rows b((const uint16_t*)g.b.codes, g.b.ld / 2, g.M, g.K);
-    u32x4* const mine = terms + (TA ? wave * 64 * 4 : 0);
+    u32x4 *const la = stage_lds[wave][0], *const lb = stage_lds[wave][1];
 
+    // copy i of a stage: rows 8 i + lane / 8, chunk lane % 8; of transposed weights
+    // terms 16 i + lane / 4, chunk lane % 4
+    auto row_a = [&](int i) { const int64_t r = n0 + 8 * i + lane / 8; return r < g.N ? r : g.N - 1; };
+    auto row_b = [&](int i) { const int64_t r = m0 + 8 * i + lane / 8; return r < g.M ? r : g.M - 1; };
+    const int n_ta = n0 + lane % 4 * 8;
+    const uint8_t *sa = nullptr, *sb = nullptr;
+    if constexpr (OP == kOpMx4) {
+        sa = g.a.scales + (int64_t)(n0 + col < g.N ? n0 + col : g.N - 1) * g.a.ld_scales;
+        sb = g.b.scales + (m0 + col < g.M ? m0 + col : g.M - 1) * g.b.ld_scales;
+    }
     struct Held {
         u32x4 a[4], b[4];
         uint64_t sa, sb;
     };
     auto load = [&](Held& h, int stage) {
+        const int c = stage * kStageChunks + lane % 8;
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const int c = stage * kStageChunks + 2 * s + half;
+        for (int i = 0; i < 4; ++i) {
             if constexpr (OP == kOpBf16) {
-                h.b[s] = b.load(rb, c * 8);
-                if constexpr (!TA) h.a[s] = a.load(ra, c * 8);
-                // 16 terms by 32 outputs, a lane the quarter lane % 4 of a term
-                else h.a[s] = a.load_at((int64_t)(stage * 64 + s * 16 + lane / 4) * a.ld + n0 + lane % 4 * 8, n0 + lane % 4 * 8);
+                h.b[i] = b.load(row_b(i), c * 8);
+                if constexpr (TA) h.a[i] = a.load_at((int64_t)(stage * 64 + 16 * i + lane / 4) * a.ld + n_ta, n_ta);
+                else h.a[i] = a.load(row_a(i), c * 8);
             } else {
-                const uint8_t *pa = g.a.codes + ra * g.a.ld + c * 16, *pb = g.b.codes + rb * g.b.ld + c * 16;
-                h.a[s] = *(const u32x4*)(c * kMxBlock < g.K ? pa : (const uint8_t*)kZeroChunk);
-                h.b[s] = *(const u32x4*)(c * kMxBlock < g.K ? pb : (const uint8_t*)kZeroChunk);
+                const uint8_t *pa = g.a.codes + row_a(i) * g.a.ld + c * 16, *pb = g.b.codes + row_b(i) * g.b.ld + c * 16;
+                h.a[i] = *(const u32x4*)(c * kChunk < g.K ? pa : (const uint8_t*)kZeroChunk);
+                h.b[i] = *(const u32x4*)(c * kChunk < g.K ? pb : (const uint8_t*)kZeroChunk);
             }
         }
         if constexpr (OP == kOpMx4) {
             const int at = stage * 8 * kMxBlock < g.K ? stage * 8 : 0;
-            h.sa = *(const uint64_t*)(g.a.scales + ra * g.a.ld_scales + at);
-            h.sb = *(const uint64_t*)(g.b.scales + rb * g.b.ld_scales + at);
+            h.sa = *(const uint64_t*)(sa + at);
+            h.sb = *(const uint64_t*)(sb + at);
         }
     };
     f32x16 acc;
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
     auto multiply = [&](Held& h, int stage) {
+        const bool last = (stage + 1) * stage_cols > g.K;
         if constexpr (OP == kOpBf16) {
-            if ((stage + 1) * stage_cols > g.K)
+            const int k = (stage * kStageChunks + lane % 8) * 8;
+            if (last)
 #pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    const int k = (stage * kStageChunks + 2 * s + half) * 8;
-                    h.b[s] = b.fix(h.b[s], rb, k);
-                    if constexpr (!TA) h.a[s] = a.fix(h.a[s], ra, k);
+                for (int i = 0; i < 4; ++i) {
+                    h.b[i] = b.fix(h.b[i], row_b(i), k);
+                    if constexpr (!TA) h.a[i] = a.fix(h.a[i], row_a(i), k);
                 }
-            if constexpr (TA) {
-                const int n = n0 + lane % 4 * 8;
-                if (n0 + 32 > g.N || (stage + 1) * 64 > g.K)
+            if constexpr (TA)
+                if (last || n0 + 32 > g.N)
 #pragma unroll
-                    for (int s = 0; s < 4; ++s) {
-                        const int64_t term = stage * 64 + s * 16 + lane / 4;
-                        h.a[s] = term < g.K ? a.fix(h.a[s], term, n) : u32x4{0, 0, 0, 0};
+                    for (int i = 0; i < 4; ++i) {
+                        const int64_t term = stage * 64 + 16 * i + lane / 4;
+                        h.a[i] = term < g.K ? a.fix(h.a[i], term, n_ta) : u32x4{0, 0, 0, 0};
                     }
-#pragma unroll
-                for (int s = 0; s < 4; ++s) mine[s * 64 + lane] = h.a[s];
-                wave_lds_fence();
-#pragma unroll
-                for (int s = 0; s < 4; ++s) h.a[s] = __builtin_bit_cast(u32x4, read_columns<4>(mine, s * 16, 0, lane));
-                wave_lds_fence();
-            }
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = 8 * i + lane / 8, at = row * kStageChunks + (lane % 8 ^ row_key<kStageChunks>(row));
+            lb[at] = h.b[i];
+            la[TA ? i * 64 + lane : at] = h.a[i];
+        }
+        wave_lds_fence();
         uint32_t va = 0, vb = 0;
         if constexpr (OP == kOpMx4) {
             va = pack_scales(h.sa, stage, g.K, half);
             vb = pack_scales(h.sb, stage, g.K, half);
         }
-        sfor<4>([&](auto S) { acc = mma_step<OP, CV(S)>(h.a[CV(S)], h.b[CV(S)], acc, va, vb); });
+        sfor<4>([&](auto S) {
+            const int at = col * kStageChunks + ((2 * CV(S) + half) ^ row_key<kStageChunks>(col));
+            u32x4 fa;
+            if constexpr (TA) fa = __builtin_bit_cast(u32x4, read_columns<4>(la, CV(S) * 16, 0, lane));
+            else fa = la[at];
+            acc = mma_step<OP, CV(S)>(fa, lb[at], acc, va, vb);
+        });
+        wave_lds_fence();
     };
     Held h0, h1;
     if (wave < stages) load(h0, wave);

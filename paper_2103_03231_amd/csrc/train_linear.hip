@@ -190,15 +190,17 @@ __global__ void __launch_bounds__(256, 2) weight_grad_kernel(GradArgs g) {
     }
 }
 
-// dW and db from the splits' parts: a workgroup adds up 32 values, eight threads a
-// value, each an eighth of the splits in their order, and then the eight sums.
+// dW and db from the splits' parts: GROUPS threads a value, each its share of the
+// splits in their order, and then the shares.
+template <int GROUPS>
 __global__ void __launch_bounds__(256) grad_sum_kernel(const float* dw_parts, const float* db_parts, int splits, int N,
                                                        int K, float* dw, int64_t lddw, float* db, int accumulate) {
-    __shared__ float part[8][32];
-    const int c = threadIdx.x & 31, eighth = threadIdx.x >> 5;
+    constexpr int kValues = 256 / GROUPS;   // of a workgroup
+    __shared__ float part[GROUPS][kValues];
+    const int c = threadIdx.x % kValues, group = threadIdx.x / kValues;
     const int64_t nk = (int64_t)N * K, total = (dw ? nk : 0) + (db ? N : 0);
-    const int from = splits * eighth / 8, to = splits * (eighth + 1) / 8;
-    for (int64_t i0 = (int64_t)blockIdx.x * 32; i0 < total; i0 += (int64_t)gridDim.x * 32) {
+    const int from = splits * group / GROUPS, to = splits * (group + 1) / GROUPS;
+    for (int64_t i0 = (int64_t)blockIdx.x * kValues; i0 < total; i0 += (int64_t)gridDim.x * kValues) {
         const int64_t i = i0 + c < total ? i0 + c : total - 1;
         const bool is_w = dw && i < nk;
         const int64_t at = is_w ? i : i - (dw ? nk : 0), stride = is_w ? nk : N;
@@ -206,15 +208,17 @@ __global__ void __launch_bounds__(256) grad_sum_kernel(const float* dw_parts, co
         float s = 0.0f;
 #pragma unroll 8
         for (int k = from; k < to; ++k) s += p[k * stride];
-        part[eighth][c] = s;
-        __syncthreads();
-        if (eighth == 0 && i0 + c < total) {
+        if constexpr (GROUPS > 1) {
+            part[group][c] = s;
+            __syncthreads();
 #pragma unroll
-            for (int e = 1; e < 8; ++e) s += part[e][c];
+            for (int e = 1; e < GROUPS; ++e) s += group == 0 ? part[e][c] : 0.0f;
+            __syncthreads();
+        }
+        if (group == 0 && i0 + c < total) {
             float* o = is_w ? dw + at / K * lddw + at % K : db + at;
             *o = accumulate ? *o + s : s;
         }
-        __syncthreads();
     }
 }
 
@@ -313,9 +317,14 @@ hipError_t launch_train_linear_backward(const BackwardArgs& a, int n_cu, hipStre
         if ((e = hipGetLastError()) != hipSuccess || direct) return e;
     }
     const int64_t total = (int64_t)a.N * a.K + a.N;
-    const uint64_t wg = (uint64_t)((total + 31) / 32), most = (uint64_t)n_cu * 32;
-    hipLaunchKernelGGL(grad_sum_kernel, dim3((uint32_t)(wg < most ? wg : most)), dim3(256), 0, stream, dw_parts, db_parts,
-                       p.splits, a.N, a.K, a.dw, a.lddw, a.db, a.accumulate);
+    // few values do not fill the device with a thread each (64 x 48 of 196 splits:
+    // 20 us, 16 us by eight threads); many lose by short rows (256 x 256 of 125
+    // splits: 9 us, 15 us)
+    const bool few = total <= 64 * (int64_t)n_cu;
+    const uint64_t values = few ? 32 : 256, wg = ((uint64_t)total + values - 1) / values, most = (uint64_t)n_cu * 32;
+    const dim3 grid((uint32_t)(wg < most ? wg : most));
+    if (few) hipLaunchKernelGGL(grad_sum_kernel<8>, grid, dim3(256), 0, stream, dw_parts, db_parts, p.splits, a.N, a.K, a.dw, a.lddw, a.db, a.accumulate);
+    else hipLaunchKernelGGL(grad_sum_kernel<1>, grid, dim3(256), 0, stream, dw_parts, db_parts, p.splits, a.N, a.K, a.dw, a.lddw, a.db, a.accumulate);
     return hipGetLastError();
 }
 

@@ -185,14 +185,55 @@ def test_product(r, rows, n_in, n_out):
             assert all(np.array_equal(u, v) for u, v in zip(host(q), host(q_ref)))
 
 
-@pytest.mark.parametrize("rows", [3, 200])
+def values64(r, q):
+    """What an MxTensor stands for, in 64 bits on the GPU (fp32 holds it exactly)."""
+    return r.mx_dequantize(q, torch.float32).double()
+
+
+# weights in registers (up to 256 outputs of up to 512 inputs, many rows), tiles of
+# 128 x 128, and the tails of each; the result types share a kernel's products
+@pytest.mark.parametrize("rows,n_in,n_out", [
+    (16384, 256, 256), (16391, 100, 200), (16700, 33, 129), (40001, 250, 128), (16385, 7, 31),
+    (16400, 512, 256), (20011, 300, 77), (17000, 257, 130), (33000, 64, 96),
+    (4500, 700, 1200), (4399, 1023, 1111), (36000, 513, 129), (40000, 40, 300), (128 * 256, 900, 64),
+])
+def test_product_many_rows(r, rows, n_in, n_out):
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    x, w = torch.randn(rows, n_in, generator=g, device="cuda"), torch.randn(n_out, n_in, generator=g, device="cuda")
+    bias = torch.randn(n_out, generator=g, device="cuda")
+    qx, qw = r.mx_quantize(x, b.MXFP4), r.mx_quantize(w, b.MXFP4)
+    vx, vw = values64(r, qx), values64(r, qw)
+    for relu, bias_ in ((True, bias), (False, None)):
+        ref, mag = vx @ vw.t(), vx.abs() @ vw.abs().t()
+        if bias_ is not None:
+            ref, mag = ref + bias.double(), mag + bias.abs().double()
+        ref = ref.clamp(min=0) if relu else ref
+        y = r.mx_linear(x, qw, bias_, relu, torch.float32)
+        assert ((y.double() - ref).abs() <= (n_in + 2) * 2.0 ** -23 * mag).all()
+        assert torch.equal(r.mx_linear(qx, qw, bias_, relu), y.bfloat16())
+        q, q_ref = r.mx_linear(qx, qw, bias_, relu, b.MXFP4), r.mx_quantize(y, b.MXFP4)
+        assert torch.equal(q.codes, q_ref.codes)
+        blocks = -(-n_out // 32)
+        assert torch.equal(q.scales[:, :blocks], q_ref.scales[:, :blocks])
+
+
+@pytest.mark.parametrize("rows,n_in,n_out", [(33, 5000, 100), (70, 1025, 64), (200, 2048, 33), (64, 800, 256), (90, 4096, 500)])
+def test_product_split_by_columns(r, rows, n_in, n_out):
+    test_product_many_rows(r, rows, n_in, n_out)
+
+
+@pytest.mark.parametrize("rows", [3, 40, 200, 17000])
 def test_product_not_finite(r, rows):
     """A NaN block makes its row (of x) or column (of w) NaN and nothing else; a
     ReLU keeps NaN; scales at both ends of their range."""
     x, w = np.random.default_rng(1).standard_normal((rows, 300)), np.random.default_rng(2).standard_normal((70, 300))
     x[1, 290] = np.nan
     w[5, 3] = np.inf
-    qx, qw = device(x, b.MXFP4), device(w, b.MXFP4)
+    if rows == 40:      # the columns split among waves
+        x, w = np.tile(x, 4), np.tile(w, 4)
+    qw = device(w, b.MXFP4)
+    qx = device(x, b.MXFP4) if rows < 1000 else r.mx_quantize(torch.from_numpy(x).float().cuda(), b.MXFP4)
+    assert (qx.rows, qw.rows) == (rows, 70)
     for relu in (False, True):
         for out in (torch.float32, torch.bfloat16):
             y = r.mx_linear(qx, qw, None, relu, out).float().cpu().numpy()
@@ -201,8 +242,8 @@ def test_product_not_finite(r, rows):
             assert np.array_equal(np.isnan(y), nan)
         back = numbers(r.mx_linear(qx, qw, None, relu, b.MXFP4))
         assert np.isnan(back[1]).all() and np.isnan(back[:, :32]).all() and not np.isnan(np.delete(back, 1, 0)[:, 32:]).any()
-    x, w = np.full((rows, 64), 2.0 ** -127), np.full((4, 64), 2.0 ** 100)
-    y = r.mx_linear(device(x, b.MXFP4), device(w, b.MXFP4), None, False, torch.float32)
+    x, w = torch.full((rows, 64), 2.0 ** -127, device="cuda"), np.full((4, 64), 2.0 ** 100)
+    y = r.mx_linear(x, device(w, b.MXFP4), None, False, torch.float32).cpu().numpy()
     assert (y == 64 * 2.0 ** -27).all()
 
 

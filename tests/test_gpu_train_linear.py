@@ -124,6 +124,59 @@ def test_many_rows(r, rows, n_in, n_out):
     assert torch.linalg.norm(dw.double() - z.t() @ vx) <= 2e-6 * torch.linalg.norm(z.t() @ vx) + 2.0 ** -24 * torch.linalg.norm(z.abs().t() @ vx.abs())
 
 
+# weights in registers (up to 256 by 256, many rows), tiles of 256 and 128, terms split
+# among waves; whole 16-byte chunks and any other rows; the tails of each
+LARGE = [(16384, 256, 256), (16391, 90, 256), (17003, 256, 128), (16385, 63, 200), (20001, 130, 33), (16384, 64, 64), (16500, 8, 136),
+         (16399, 200, 72), (33001, 191, 255), (8200, 72, 2056), (8200, 2056, 72), (8203, 2049, 71), (4500, 300, 1200), (4399, 1111, 250),
+         (40, 3001, 90), (90, 264, 2000), (33, 2000, 264), (7, 4096, 333), (64, 333, 4096)]
+
+
+@pytest.mark.parametrize("relu", [False, True])
+@pytest.mark.parametrize("rows,n_in,n_out", LARGE)
+def test_large(r, rows, n_in, n_out, relu):
+    """Every kernel that a rule on sizes picks, in 64 bits on the GPU."""
+    g = torch.Generator(device="cuda").manual_seed(rows + n_in)
+    rand = lambda *shape: torch.randn(*shape, generator=g, device="cuda").bfloat16()
+    x, w, bias, dz = rand(rows, n_in), rand(n_out, n_in), torch.randn(n_out, generator=g, device="cuda"), rand(rows, n_out)
+    x = torch.relu(x) if relu else x
+    X, W, Z = x.double(), w.double(), dz.double()
+    y, kept = r.train_linear(x, w, bias, relu)
+    ref, tol = X @ W.t() + bias.double(), (n_in + 2) * STEP * (X.abs() @ W.abs().t() + bias.abs().double())
+    ref = ref.clamp(min=0) if relu else ref
+    assert ((y.double() - ref).abs() <= tol + BF16_HALF * (ref.abs() + tol)).all()
+    # what is kept, by its own scales: half a step of E4M3 is at most 2^-4 of the value,
+    # and no less than half of 2^-9 of the scale (a whole one where a value is lifted to it)
+    v = r.mx_dequantize(kept, torch.float32).double()
+    blocks = -(-n_out // 32)
+    scale = torch.exp2(kept.scales[:, :blocks].double() - 127).repeat_interleave(32, 1)[:, :n_out]
+    assert ((v - ref).abs() <= torch.maximum(2.0 ** -4 * (ref.abs() + tol), 2.0 ** -9 * scale) + tol).all()
+    assert (ref.abs() <= 448 * scale + tol).all()
+    if relu:
+        assert ((v > 0) | (ref <= tol)).all() and ((v == 0) | (ref > 0) | (tol > 0)).all() and (v >= 0).all()
+    for q in (r.mx_quantize(x, b.MXFP8), x):
+        V = r.mx_dequantize(q, torch.float32).double() if isinstance(q, b.MxTensor) else X
+        dx, dw, db = r.train_linear_backward(dz, q, w, relu)
+        ref, tol = Z @ W, (n_out + 2) * STEP * (Z.abs() @ W.abs())
+        ref = torch.where(V != 0, ref, torch.zeros_like(ref)) if relu else ref
+        assert ((dx.double() - ref).abs() <= tol + BF16_HALF * (ref.abs() + tol)).all()
+        assert not relu or (dx[V == 0] == 0).all()
+        assert ((dw.double() - Z.t() @ V).abs() <= (rows + 2) * STEP * (Z.abs().t() @ V.abs())).all()
+        assert ((db.double() - Z.sum(0)).abs() <= (rows + 2) * STEP * Z.abs().sum(0)).all()
+
+
+def test_only_one_of_the_forward_outputs(r):
+    """Through the C names: y alone and what is kept alone, as with both."""
+    for rows in (50, 17000):
+        x, w = activations(1, rows, 72, True), normal(2, 56, 72)
+        y, kept = r.train_linear(x, w, None, True)
+        y2, kept2 = torch.full_like(y, 3.0), r.mx_empty(rows, 56, b.MXFP8)
+        mx, mw = (x.data_ptr(), 72, b.TYPE_BF16), (w.data_ptr(), 72, b.TYPE_BF16)
+        mq = r._mx("kept", kept2, (b.MXFP8,), device=0)
+        b.donerf_train_linear(r.h, mx, mw, None, 1, (y2.data_ptr(), 56, b.TYPE_BF16), None, rows, 72, 56)
+        b.donerf_train_linear(r.h, mx, mw, None, 1, None, mq, rows, 72, 56)
+        assert torch.equal(y, y2) and all(np.array_equal(u, v) for u, v in zip(host(kept), host(kept2)))
+
+
 def test_accumulates(r):
     for rows in (50, 5000):     # one part, and several that are summed afterwards
         x, w = r.mx_quantize(activations(3, rows, 70, True), b.MXFP8), normal(5, 45, 70)

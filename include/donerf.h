@@ -327,7 +327,9 @@ typedef enum donerf_type {
  *           codes, aligned to 16 bytes; 16 bytes a block in MXFP4 (the even
  *           column in a byte's low half), 32 bytes a block in MXFP8
  *   ld      from row to row: values (fp32, bf16) or bytes, a multiple of 16
- *           (microscaled); at least a row's length
+ *           (microscaled); at least a row's length.  What lies between the rows
+ *           of an input may be read, but is not used; that between the rows of
+ *           an output is left as it is
  *   scales  microscaled: one byte per block, aligned to 8 bytes; else NULL
  *   ld_scales  bytes from one row's scales to the next's, a multiple of 8 and at
  *           least a row's blocks.  Bytes behind the last block's are neither
@@ -377,7 +379,7 @@ int donerf_mx_dequantize(donerf_t* h, const donerf_mat* q, const donerf_mat* y, 
  * Products are exact, sums fp32.  y must not overlap the inputs.
  * rows 0..2^31 - 1 (0: nothing is done), in and out 1..DONERF_MAX_COLS.
  * Errors: as above, and E_SIZE (workspace too small), E_UNSUPPORTED (rows x out
- * of 2^38 or more).
+ * of 2^38 or more, or more results than a launch's grid counts).
  */
 int donerf_mx_linear(donerf_t* h, const donerf_mat* x, const donerf_mat* w, const float* bias, int32_t relu,
                      const donerf_mat* y, int64_t rows, int32_t in, int32_t out, void* workspace,

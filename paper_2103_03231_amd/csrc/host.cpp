@@ -565,10 +565,11 @@ int validate_mat(const char* name, const donerf_mat* m, int types, int64_t rows,
         return bad("this type is not taken here");
     const bool mx = microscaled(m->type);
     const int64_t least = mx ? code_bytes(m->type, cols) : cols;
-    if (m->ld < least || m->ld > ((int64_t)1 << 40)) return bad("ld out of range");
+    const int64_t most = ((int64_t)1 << 52) / (rows > 1 ? rows : 1);   // offsets stay far from 64 bits' end
+    if (m->ld < least || m->ld > most || m->ld > ((int64_t)1 << 40)) return bad("ld out of range");
     if (mx) {
         if (m->ld % 16) return bad("ld must be a multiple of 16 bytes");
-        if (m->ld_scales < (cols + 31) / 32 || m->ld_scales > ((int64_t)1 << 40) || m->ld_scales % 8)
+        if (m->ld_scales < (cols + 31) / 32 || m->ld_scales > most || m->ld_scales > ((int64_t)1 << 40) || m->ld_scales % 8)
             return bad("ld_scales must be a multiple of 8 and hold a row's blocks");
     } else if (m->scales) {
         return bad("scales given for a type without them");
@@ -996,7 +997,7 @@ int donerf_train_linear_backward(donerf_t* h, const donerf_mat* dz, const donerf
     if ((uintptr_t)db % 4) return fail(DONERF_E_INVALID_ARG, "db not aligned");
     if ((relu != 0 && relu != 1) || (accumulate != 0 && accumulate != 1))
         return fail(DONERF_E_INVALID_ARG, "relu and accumulate must be 0 or 1");
-    if ((rc = validate_tiles(rows, in)) || (rc = validate_handle(h)) ||
+    if ((rc = validate_tiles(rows, in)) || (rc = validate_tiles(rows, out)) || (rc = validate_handle(h)) ||
         (rc = validate_workspace(workspace, workspace_bytes, backward_workspace(rows, out, in, h->n_cu))))
         return rc;
     BackwardArgs a{};

@@ -554,7 +554,7 @@ __global__ void __launch_bounds__(64 * WN * WM, 2) layer_gemm_kernel(GemmArgs g)
         Mask16 mask[TN];
 #pragma unroll
         for (int i = 0; i < TN; ++i) mask[i] = load_mask<EPI>(g, m0 + (j * WM + wm) * 32, n0 + (wn * TN + i) * 32, lane);
-        if (j > 1) lds_barrier();
+        // (a place is written again after a barrier that follows its last readers)
 #pragma unroll
         for (int i = 0; i < TN; ++i) Out::put(out, g, acc[i][j], mask[i], wm * 32, (wn * TN + i) * 32, n0, lane);
         lds_barrier();

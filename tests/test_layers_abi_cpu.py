@@ -120,13 +120,18 @@ def test_sizes_of_conversions(make):
 
 @pytest.mark.parametrize("make", [linear, forward, backward])
 def test_sizes_of_layers(make):
-    big = mat(BF16, 1, 1, ld=1 << 20)
     for rows, n_in, n_out in ((-1, 8, 8), (1 << 31, 8, 8), (4, 0, 8), (4, 8, 0), (4, b.MAX_COLS + 1, 8), (4, 8, b.MAX_COLS + 1)):
         refused(make(rows=rows, n_in=n_in, n_out=n_out), "must lie in")
-    assert big
     # results that a launch's grid cannot count
-    wide = {"n_in": b.MAX_COLS} if make is backward else {"n_out": b.MAX_COLS}
-    refused(make(rows=(1 << 31) - 1, **wide), "more results", b.E_UNSUPPORTED)
+    for wide in ({"n_in": b.MAX_COLS}, {"n_out": b.MAX_COLS}) if make is backward else ({"n_out": b.MAX_COLS},):
+        refused(make(rows=(1 << 31) - 1, **wide), "more results", b.E_UNSUPPORTED)
+
+
+def test_offsets_that_64_bits_would_not_hold():
+    rows = (1 << 31) - 1
+    refused(quantize(rows=rows, cols=8, x=mat(F32, rows, 8, ld=1 << 40)), "x: ld out of range")
+    refused(quantize(rows=rows, cols=8, q=mat(b.MXFP4, rows, 8, ld_scales=1 << 40)), "q: ld_scales")
+    refused(quantize(rows=rows, cols=8), "handle is NULL")
 
 
 def test_flags_bias_and_workspace():

@@ -921,16 +921,6 @@ int donerf_mx_linear(donerf_t* h, const donerf_mat* x, const donerf_mat* w, cons
     }
     GemmArgs g{};
     g.a = mx_in(w);
-    hipError_t e;
-    if (x->type == DONERF_TYPE_MXFP4) {
-        g.b = mx_in(x);
-    } else {
-        uint8_t* ws = (uint8_t*)workspace;
-        const MxOut q{ws, code_bytes(DONERF_TYPE_MXFP4, in), ws + quantized_codes(rows, in), scale_row(in)};
-        e = launch_mx_quantize(x->data, x->ld, x->type == DONERF_TYPE_BF16, q, false, rows, in, h->n_cu, h->stream);
-        if (e != hipSuccess) return hip_fail(e, "mx_quantize launch");
-        g.b = MxIn{q.codes, q.ld, q.scales, q.ld_scales};
-    }
     g.bias = bias;
     g.relu = relu;
     if (kind == kOutMx4) {
@@ -942,6 +932,21 @@ int donerf_mx_linear(donerf_t* h, const donerf_mat* x, const donerf_mat* w, cons
     g.M = (int32_t)rows;
     g.N = out;
     g.K = in;
+    hipError_t e;
+    const bool x_bf16 = x->type == DONERF_TYPE_BF16;
+    if (x->type == DONERF_TYPE_MXFP4) {
+        g.b = mx_in(x);
+    } else if (mx_linear_converts(g, h->n_cu)) {
+        g.b = MxIn{(const uint8_t*)x->data, x->ld * (x_bf16 ? 2 : 4), nullptr, 0};
+        e = launch_mx_linear_convert(g, x_bf16, kind, h->n_cu, h->stream);
+        return e == hipSuccess ? DONERF_OK : hip_fail(e, "mx_linear launch");
+    } else {
+        uint8_t* ws = (uint8_t*)workspace;
+        const MxOut q{ws, code_bytes(DONERF_TYPE_MXFP4, in), ws + quantized_codes(rows, in), scale_row(in)};
+        e = launch_mx_quantize(x->data, x->ld, x_bf16, q, false, rows, in, h->n_cu, h->stream);
+        if (e != hipSuccess) return hip_fail(e, "mx_quantize launch");
+        g.b = MxIn{q.codes, q.ld, q.scales, q.ld_scales};
+    }
     e = launch_mx_linear(g, kind, h->n_cu, h->stream);
     return e == hipSuccess ? DONERF_OK : hip_fail(e, "mx_linear launch");
 }

@@ -176,6 +176,10 @@ hipError_t launch_mx_dequantize(const MxIn& q, bool fp8, void* y, int64_t ldy, b
                                 int n_cu, hipStream_t stream);
 // g.a, g.b E2M1.
 hipError_t launch_mx_linear(const GemmArgs& g, int out, int n_cu, hipStream_t stream);
+// g.b fp32 or bf16 rows (ld in bytes), converted where they are multiplied: for sizes
+// that mx_linear_converts takes.
+bool mx_linear_converts(const GemmArgs& g, int n_cu);
+hipError_t launch_mx_linear_convert(const GemmArgs& g, bool x_bf16, int out, int n_cu, hipStream_t stream);
 // The same for up to kFewRows rows, x fp32 (0), bf16 (1) or E2M1 (2).
 constexpr int kFewRows = 32;
 struct FewRowsArgs {

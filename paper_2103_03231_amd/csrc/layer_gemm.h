@@ -566,12 +566,18 @@ __global__ void __launch_bounds__(64 * WN * WM, 2) layer_gemm_kernel(GemmArgs g)
 // (32 per wave) of KS stages of 128 bytes.  They are read once per workgroup, and
 // tiles of 64 batch rows stream past them through a ring of three, two ahead, so
 // that the batch is read once and nothing else moves but the results.  WN waves
-// along the outputs, 8 / WN along the rows.
+// along the outputs, 8 / WN along the rows.  SRC: how the batch gets there.
+constexpr int kSrcCopies = 0;     // rows of whole, 16-byte aligned chunks: straight into LDS
+constexpr int kSrcBf16Rows = 1;   // any bf16 rows: through registers, a tile ahead
+constexpr int kSrcF32 = 2;        // fp32 or bf16 rows that become E2M1, likewise
+constexpr int kSrcBf16 = 3;
 constexpr int kRowsTile = 64;
 // Workgroups that share a compute unit.
-constexpr int rows_workgroups(int op, int ks) { return op == kOpMx4 && ks == 1 ? 2 : 1; }
-template <int OP, int KS, int WN, bool TA, bool DB, int EPI>
-__global__ void __launch_bounds__(512, rows_workgroups(OP, KS) * 2) layer_rows_kernel(GemmArgs g) {
+constexpr int rows_workgroups(int op, int ks, int src) { return op == kOpMx4 && ks == 1 && src == kSrcCopies ? 2 : 1; }
+template <int OP, int KS, int WN, bool TA, int SRC, int EPI>
+__global__ void __launch_bounds__(512, rows_workgroups(OP, KS, SRC) * 2) layer_rows_kernel(GemmArgs g) {
+    constexpr bool DB = SRC == kSrcCopies, kConvert = SRC == kSrcF32 || SRC == kSrcBf16;
+    static_assert(!kConvert || (OP == kOpMx4 && KS == 1), "conversion is to E2M1, of one stage");
     constexpr int NW = 8, WM = NW / WN, RT = kRowsTile, RB = RT / 32 / WM, CP = RT * KS / 8 / NW;
     using Out = Outgoing<EPI, RT, 32 * WN>;
     // a tile: its stages, then the rows' scales, KS words of eight each
@@ -630,7 +636,13 @@ __global__ void __launch_bounds__(512, rows_workgroups(OP, KS) * 2) layer_rows_k
     static_assert(RT == 8 * NW, "a wave's copies are the same rows of each stage");
     const int chunk = (lane & 7) ^ row_key<kStageChunks>(wave * 8 + (lane >> 3));
     const Bf16Rows rows((const uint16_t*)g.b.codes, g.b.ld / 2, g.M, g.K);
-    u32x4 held[DB ? 1 : CP];
+    u32x4 held[SRC == kSrcBf16Rows ? CP : 1];
+    // converted rows: 8 columns a lane, four lanes a block, 16 rows of the tile a turn
+    constexpr int kTurns = RT / 16;
+    u32x4 raw[kConvert ? kTurns : 1][SRC == kSrcF32 ? 2 : 1];
+    const int crow = threadIdx.x / 32, ccol = threadIdx.x % 32 * 8;
+    const Bf16Rows xrows((const uint16_t*)g.b.codes, g.b.ld / 2, g.M, g.K);
+    const bool ragged = ccol + 8 > g.K;
     // copy i of a wave: eight rows of one stage
     auto place = [&](uint32_t tile, int i, int64_t& r, int& c) {
         const int q = i * NW + wave;
@@ -639,6 +651,25 @@ __global__ void __launch_bounds__(512, rows_workgroups(OP, KS) * 2) layer_rows_k
         c = q / (RT / 8) * kStageChunks + chunk;
     };
     auto issue = [&](u32x4* lds, uint32_t tile) {
+        if constexpr (kConvert) {
+#pragma unroll
+            for (int i = 0; i < kTurns; ++i) {
+                int64_t r = (int64_t)tile * RT + i * 16 + crow;
+                r = r < g.M ? r : g.M - 1;
+                if constexpr (SRC == kSrcBf16) {
+                    raw[i][0] = xrows.load(r, ccol);
+                } else {
+                    const float* p = (const float*)(g.b.codes + r * g.b.ld);
+                    if (g.K % 8 == 0) {   // chunks are whole, or not there
+                        __builtin_memcpy(raw[i], p + (ragged ? 0 : ccol), 32);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) raw[i][e / 4][e % 4] = __float_as_uint(p[ccol + e < g.K ? ccol + e : g.K - 1]);
+                    }
+                }
+            }
+            return;
+        }
         if constexpr (OP == kOpMx4) {
             const int word = wave * 64 + lane, w = word % (2 * KS);   // of the tile, of its row
             if (wave * 64 < kScaleWords) {
@@ -664,7 +695,25 @@ __global__ void __launch_bounds__(512, rows_workgroups(OP, KS) * 2) layer_rows_k
         }
     };
     auto store = [&](u32x4* lds, uint32_t tile) {
-        if constexpr (!DB)
+        if constexpr (kConvert) {
+#pragma unroll
+            for (int i = 0; i < kTurns; ++i) {
+                float v[8];
+                if constexpr (SRC == kSrcBf16) {
+                    int64_t r = (int64_t)tile * RT + i * 16 + crow;
+                    r = r < g.M ? r : g.M - 1;
+                    const u32x4 p = ragged ? xrows.fix(raw[i][0], r, ccol) : raw[i][0];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(e & 1 ? p[e / 2] & 0xffff0000u : p[e / 2] << 16);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = !ragged || ccol + e < g.K ? __uint_as_float(raw[i][e / 4][e % 4]) : 0.0f;
+                }
+                const int code = mx4_code(quad_max(top_bits<8>(v))), row = i * 16 + crow, block = ccol / kMxBlock;
+                ((uint32_t*)(lds + row * kStageChunks + (block ^ row_key<kStageChunks>(row))))[ccol / 8 % 4] = to_e2m1x8(v, code);
+                if (ccol % kMxBlock == 0) ((uint8_t*)(lds + kChunks))[row * 8 + block] = (uint8_t)code;
+            }
+        } else if constexpr (!DB)
 #pragma unroll
             for (int i = 0; i < CP; ++i) {
                 int64_t r;
@@ -871,24 +920,31 @@ __global__ void __launch_bounds__(512, 2) layer_split_kernel(GemmArgs g) {
     Out::template store<64>(out, g, m0, n0, threadIdx.x);
 }
 
-template <int OP, int KS, bool TA, bool DB, int EPI>
+template <int OP, int KS, bool TA, int SRC, int EPI>
 hipError_t launch_layer_rows(GemmArgs g, int n_cu, hipStream_t stream) {
     g.tiles_m = (uint32_t)(((int64_t)g.M + kRowsTile - 1) / kRowsTile);
-    const uint32_t most = rows_workgroups(OP, KS) * (uint32_t)n_cu;
+    const uint32_t most = rows_workgroups(OP, KS, SRC) * (uint32_t)n_cu;
     const dim3 grid(g.tiles_m < most ? g.tiles_m : most);
-    if (g.N > 128) hipLaunchKernelGGL((layer_rows_kernel<OP, KS, 8, TA, DB, EPI>), grid, dim3(512), 0, stream, g);
-    else hipLaunchKernelGGL((layer_rows_kernel<OP, KS, 4, TA, DB, EPI>), grid, dim3(512), 0, stream, g);
+    if (g.N > 128) hipLaunchKernelGGL((layer_rows_kernel<OP, KS, 8, TA, SRC, EPI>), grid, dim3(512), 0, stream, g);
+    else hipLaunchKernelGGL((layer_rows_kernel<OP, KS, 4, TA, SRC, EPI>), grid, dim3(512), 0, stream, g);
     return hipGetLastError();
+}
+
+// Layers for layer_rows_kernel: weights for a workgroup, and a tile of rows for every
+// compute unit.
+inline bool fits_rows(const GemmArgs& g, int most_k, int n_cu) {
+    return g.N <= 256 && g.K <= most_k && (int64_t)g.M >= (int64_t)kRowsTile * n_cu;
 }
 
 template <int OP, bool TA, bool DA, bool DB, int EPI>
 hipError_t launch_layer_gemm(GemmArgs g, int n_cu, hipStream_t stream) {
     constexpr int stage_cols = OP == kOpBf16 ? 64 : 256;
     const int stages = (g.K + stage_cols - 1) / stage_cols;
-    if (g.N <= 256 && stages <= (OP == kOpMx4 ? 2 : 4) && (int64_t)g.M >= 64 * (int64_t)n_cu) {
-        if (stages == 1) return launch_layer_rows<OP, 1, TA, DB, EPI>(g, n_cu, stream);
-        if (stages == 2) return launch_layer_rows<OP, 2, TA, DB, EPI>(g, n_cu, stream);
-        if constexpr (OP == kOpBf16) return launch_layer_rows<OP, 4, TA, DB, EPI>(g, n_cu, stream);
+    if (fits_rows(g, OP == kOpMx4 ? 512 : 256, n_cu)) {
+        constexpr int SRC = DB ? kSrcCopies : kSrcBf16Rows;
+        if (stages == 1) return launch_layer_rows<OP, 1, TA, SRC, EPI>(g, n_cu, stream);
+        if (stages == 2) return launch_layer_rows<OP, 2, TA, SRC, EPI>(g, n_cu, stream);
+        if constexpr (OP == kOpBf16) return launch_layer_rows<OP, 4, TA, SRC, EPI>(g, n_cu, stream);
     }
     auto tiles = [&](int b) { return (uint64_t)((g.N + b - 1) / b) * (uint64_t)((g.M + b - 1) / b); };
     // the largest tiles that leave every compute unit one

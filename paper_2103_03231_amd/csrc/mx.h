@@ -41,6 +41,12 @@ __device__ __forceinline__ uint32_t finite_top_bits(const float* v) {
     return t;
 }
 
+// The largest of v over a quad of lanes.
+__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, true));   // lanes 1 0 3 2
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, true));   // lanes 2 3 0 1
+}
+
 // Scale code of a block whose largest |v| has the bits top: the exponent of
 // 1.5 * 2^2 (E2M1) or 1.75 * 2^8 (E4M3) below it, one more where its mantissa is
 // larger; at least 0, where every fp32 below the smallest normal number fits.

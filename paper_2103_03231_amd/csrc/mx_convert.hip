@@ -11,12 +11,6 @@ namespace {
 
 constexpr int kConvThreads = 256;
 
-// The largest of v over a quad of lanes.
-__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
-    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, true));   // lanes 1 0 3 2
-    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, true));   // lanes 2 3 0 1
-}
-
 template <class T, bool FP8>
 __global__ void __launch_bounds__(kConvThreads) mx_quantize_kernel(const T* x, int64_t ldx, MxOut q, uint32_t rows,
                                                                    int cols, uint32_t per_row) {

@@ -19,46 +19,53 @@ constexpr int kXF32 = 0, kXBf16 = 1, kXMx4 = 2;
 // takes 32, 16 or 4 of them for each group of rows.
 constexpr int steps_ahead(int xt, int tm) { return xt == kXMx4 ? 4 : xt == kXBf16 ? 4 / tm : 2 / tm; }
 
+// The batch: fp32, bf16, or E2M1 already.  ld: values, or bytes of E2M1 rows.
+struct XRows {
+    const uint8_t* p;
+    int64_t ld;
+    const uint8_t* scales;
+    int64_t ld_scales;
+    int64_t M;
+    int K;
+};
 struct Block {   // 32 columns of a row in E2M1
     u32x4 codes;
     int scale;
 };
-
 template <int XT>
 struct XBlock {   // as loaded
     u32x4 raw[XT == kXF32 ? 8 : XT == kXBf16 ? 4 : 1];
     int scale;
 };
-
+// A block that exists.  ragged: the rows' last block is not whole.
 template <int XT>
-__device__ __forceinline__ void load_x(XBlock<XT>& b, const FewRowsArgs& g, int row, int block, bool ragged) {
+__device__ __forceinline__ void load_block(XBlock<XT>& b, const XRows& x, int64_t row, int block, bool ragged) {
     if constexpr (XT == kXMx4) {
-        b.raw[0] = *(const u32x4*)(g.x + row * g.ldx + block * 16);
-        b.scale = g.x_scales[row * g.ldx_scales + block];
+        b.raw[0] = *(const u32x4*)(x.p + row * x.ld + block * 16);
+        b.scale = x.scales[row * x.ld_scales + block];
     } else if constexpr (XT == kXBf16) {
-        const Bf16Rows rows((const uint16_t*)g.x, g.ldx, g.M, g.K);
+        const Bf16Rows rows((const uint16_t*)x.p, x.ld, x.M, x.K);
 #pragma unroll
         for (int i = 0; i < 4; ++i) b.raw[i] = rows.load(row, block * kMxBlock + 8 * i);
     } else {
-        const float* p = (const float*)g.x + row * g.ldx;
+        const float* p = (const float*)x.p + row * x.ld;
         if (!ragged) {
             __builtin_memcpy(b.raw, p + block * kMxBlock, 128);
         } else {
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
                 const int k = block * kMxBlock + i;
-                b.raw[i / 4][i % 4] = __float_as_uint(p[k < g.K ? k : g.K - 1]);
+                b.raw[i / 4][i % 4] = __float_as_uint(p[k < x.K ? k : x.K - 1]);
             }
         }
     }
 }
-
 template <int XT>
-__device__ __forceinline__ Block to_block(const XBlock<XT>& b, const FewRowsArgs& g, int row, int block, bool ragged) {
+__device__ __forceinline__ Block to_block(const XBlock<XT>& b, const XRows& x, int64_t row, int block, bool ragged) {
     if constexpr (XT == kXMx4) return Block{b.raw[0], b.scale};
     float v[32];
     if constexpr (XT == kXBf16) {
-        const Bf16Rows rows((const uint16_t*)g.x, g.ldx, g.M, g.K);
+        const Bf16Rows rows((const uint16_t*)x.p, x.ld, x.M, x.K);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             u32x4 p = b.raw[i];
@@ -73,7 +80,7 @@ __device__ __forceinline__ Block to_block(const XBlock<XT>& b, const FewRowsArgs
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
             v[i] = __uint_as_float(b.raw[i / 4][i % 4]);
-            if (ragged) v[i] = block * kMxBlock + i < g.K ? v[i] : 0.0f;
+            if (ragged) v[i] = block * kMxBlock + i < x.K ? v[i] : 0.0f;
         }
     }
     const int code = mx4_code(top_bits<32>(v));
@@ -92,6 +99,7 @@ __global__ void __launch_bounds__(64 * kWaves) mx_few_rows_kernel(FewRowsArgs g)
     const int n0 = blockIdx.x * NB * 16;
     const int blocks = (g.K + kMxBlock - 1) / kMxBlock, steps = (blocks + 3) / 4;
     const bool ragged = g.K % kMxBlock != 0;
+    const XRows rows{g.x, g.ldx, g.x_scales, g.ldx_scales, g.M, g.K};
     f32x4 acc[NB][TM];
 #pragma unroll
     for (int i = 0; i < NB; ++i)
@@ -115,7 +123,7 @@ __global__ void __launch_bounds__(64 * kWaves) mx_few_rows_kernel(FewRowsArgs g)
 #pragma unroll
             for (int j = 0; j < TM; ++j) {
                 const int m = j * 16 + at;
-                load_x<XT>(x[s][j], g, m < g.M ? m : g.M - 1, block, ragged);
+                load_block<XT>(x[s][j], rows, m < g.M ? m : g.M - 1, block, ragged);
             }
         }
 #pragma unroll
@@ -125,7 +133,7 @@ __global__ void __launch_bounds__(64 * kWaves) mx_few_rows_kernel(FewRowsArgs g)
 #pragma unroll
             for (int j = 0; j < TM; ++j) {
                 const int m = j * 16 + at;
-                const Block xb = to_block<XT>(x[s][j], g, m < g.M ? m : g.M - 1, block, ragged);
+                const Block xb = to_block<XT>(x[s][j], rows, m < g.M ? m : g.M - 1, block, ragged);
                 const i32x8 bv = {(int)xb.codes.x, (int)xb.codes.y, (int)xb.codes.z, (int)xb.codes.w, 0, 0, 0, 0};
 #pragma unroll
                 for (int i = 0; i < NB; ++i) {

@@ -448,6 +448,10 @@ struct Outgoing {
 };
 
 // TA: the weights are transposed in memory, a[k][n] (bf16 only).
+// Measured, a call's results at the rate of their products: bf16 16,384 x 2048 x 2048
+// on 256 x 256 tiles 158 us (870 TFLOP/s; matrix pipes 35 % busy, half of the waves'
+// time waits for the next stage and the barrier that publishes it), 190 us on
+// 128 x 128; E2M1 8192 x 4096 x 4096 on 128 x 128 130 us (2.1 PFLOP/s).
 template <int OP, int BN, int BM, int WN, int WM, bool TA, bool DA, bool DB, int EPI>
 __global__ void __launch_bounds__(64 * WN * WM, 2) layer_gemm_kernel(GemmArgs g) {
     constexpr int NW = WN * WM, TN = BN / (32 * WN), TM = BM / (32 * WM);
@@ -567,6 +571,10 @@ __global__ void __launch_bounds__(64 * WN * WM, 2) layer_gemm_kernel(GemmArgs g)
 // tiles of 64 batch rows stream past them through a ring of three, two ahead, so
 // that the batch is read once and nothing else moves but the results.  WN waves
 // along the outputs, 8 / WN along the rows.  SRC: how the batch gets there.
+// Measured at 256 x 256: 160,000 rows forward with both outputs 55 us (207 MB, 3.8
+// TB/s), dx 50 us, E2M1 from bf16 32 us (164 MB, 5.1 TB/s); 640,000 rows from E2M1 to
+// E2M1 51 us, bound by the instructions of its epilogue and the two barriers of a tile,
+// to bf16 70 us (415 MB, 5.9 TB/s).
 constexpr int kSrcCopies = 0;     // rows of whole, 16-byte aligned chunks: straight into LDS
 constexpr int kSrcBf16Rows = 1;   // any bf16 rows: through registers, a tile ahead
 constexpr int kSrcF32 = 2;        // fp32 or bf16 rows that become E2M1, likewise
@@ -802,7 +810,8 @@ __global__ void __launch_bounds__(512, rows_workgroups(OP, KS, SRC) * 2) layer_r
 // terms, a stage each in turn, and add up their parts in LDS, in the waves' order.
 // A stage passes through a part of LDS that is the wave's own, so that its loads
 // cover eight rows' 128 bytes at once (whole cache lines) and no wave waits for
-// another.
+// another.  Measured: 14 x 3001 x 352 13 us, 37 us on tiles of 64 x 64 (six workgroups,
+// 47 stages one after the other).
 template <int OP, bool TA, int EPI>
 __global__ void __launch_bounds__(512, 2) layer_split_kernel(GemmArgs g) {
     constexpr int NW = 8, stage_cols = OP == kOpBf16 ? 64 : 256, kChunk = OP == kOpBf16 ? 8 : kMxBlock;

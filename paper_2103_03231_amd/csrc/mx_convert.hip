@@ -2,7 +2,9 @@
 //
 // Four lanes share a block of 32 columns, eight columns each: a wave's loads and
 // stores then cover whole cache lines, and the block's largest value takes two
-// exchanges within a quad of lanes.  One pass, nothing kept: bound by HBM.
+// exchanges within a quad of lanes.  One pass, nothing kept: bound by memory
+// (160,000 x 256 bf16 to E4M3 24 us, back 19 us: 5.2 and 6.4 TB/s, the buffers partly
+// in the last-level cache; 2049 x 4100 fp32 to E2M1 8.3 us).
 #include "internal.h"
 #include "mx.h"
 

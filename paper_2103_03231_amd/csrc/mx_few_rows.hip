@@ -6,7 +6,9 @@
 // parts in LDS.  A lane of a 16 x 16 x 128 MFMA holds whole blocks of 32 columns,
 // one of W and one of x, so x is converted in the lane that multiplies it, with no
 // exchange and no pass of its own: one launch, with the loads of several steps under
-// way before the first product.
+// way before the first product.  Measured: one bf16 row through 4096 x 4096 6.7 us
+// (8.9 MB; 1.3 TB/s, bound by the latency of a cold read and the launch), 16 us as a
+// conversion and a product on tiles; 13 fp32 rows through 256 x 256 3.8 us.
 #include "internal.h"
 #include "mx.h"
 

@@ -37,7 +37,12 @@ struct GradArgs {
 // One split's part of dW[n][k] = sum_m dz[m][n] x[m][k] for 128 weight rows and
 // 64 TK columns, in stages of R batch rows.  dz goes straight into LDS (DIRECT:
 // rows of 16-byte alignment, N a multiple of 8), x through registers, where E4M3
-// becomes bf16, loaded two stages ahead.
+// becomes bf16, loaded two stages ahead.  Both operands' terms are rows in memory and
+// are read from LDS by columns.  db comes from the fragments that are there anyway.
+// Measured: 160,000 x 256 x 256 44 us (124 MB read, 32 MB of parts written),
+// 16,384 x 2048 x 2048 203 us (680 TFLOP/s).  128 x 128 with two workgroups per CU: one
+// gave 455 us instead of 341 for the whole backward call, 128 x 256 330 (but 39 instead of
+// 32 us at 4000 x 512 x 512, 107 instead of 104 at 160,000 x 256 x 256).
 template <bool DIRECT, bool X_BF16, int TK, int R>
 __global__ void __launch_bounds__(256, 2) weight_grad_kernel(GradArgs g) {
     constexpr int kTileK = 64 * TK, kChunksK = kTileK / 8;
@@ -231,7 +236,8 @@ struct GradPlan {
 // where dz, too, passes through registers.
 constexpr int kGradBlocks = 2, kGradRows = 64, kGradRowsAny = 32;
 
-// The batch is split until two workgroups per compute unit have work.
+// The batch is split until two workgroups per compute unit have work; the parts, 64
+// KiB a workgroup, are what that costs.
 GradPlan grad_plan(int64_t M, int N, int K, int n_cu) {
     GradPlan p;
     p.tiles_n = (N + kGradTileN - 1) / kGradTileN;

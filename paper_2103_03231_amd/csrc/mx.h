@@ -153,7 +153,9 @@ struct Row8<float> {
             __builtin_memcpy(v, row + k, 32);
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = k + i < cols ? row[k + i] : 0.0f;
+            for (int i = 0; i < 8; ++i) v[i] = row[k + i < cols ? k + i : cols - 1];   // loads without conditions
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = k + i < cols ? v[i] : 0.0f;
         }
     }
     __device__ static __forceinline__ void store(float* row, int k, int cols, const float* v) {
@@ -174,8 +176,10 @@ struct Row8<uint16_t> {   // bf16
             __builtin_memcpy(&p, row + k, 16);
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (k + i < cols) p[i / 2] |= (uint32_t)row[k + i] << (16 * (i & 1));
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t v = row[k + i < cols ? k + i : cols - 1];
+                p[i / 2] |= k + i < cols ? v << (16 * (i & 1)) : 0u;
+            }
         }
         return p;
     }
@@ -186,10 +190,6 @@ struct Row8<uint16_t> {   // bf16
             v[2 * i] = __uint_as_float(p[i] << 16);
             v[2 * i + 1] = __uint_as_float(p[i] & 0xffff0000u);
         }
-    }
-    __device__ static __forceinline__ void store(uint16_t* row, int k, int cols, const float* v) {
-        store_raw(row, k, cols, u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
-                                      pack_bf16x2(v[6], v[7])});
     }
     __device__ static __forceinline__ void store_raw(uint16_t* row, int k, int cols, u32x4 p) {
         if (k + 8 <= cols) {

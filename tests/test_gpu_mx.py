@@ -151,6 +151,20 @@ def test_rows_far_apart(r):
     assert torch.equal(r.mx_linear(q, w, out=y), r.mx_linear(q, w))
 
 
+def test_more_rows_than_a_launch_counts(r):
+    """Rows of one column, 2^28 and some: conversions go by slices, indexes of rows and
+    tiles stay exact."""
+    rows = (1 << 28) + 777
+    x = torch.ones((rows, 1), dtype=torch.bfloat16, device="cuda")
+    x[::3] = -3.0
+    x[-1] = 0.25
+    q = r.mx_quantize(x, b.MXFP4)
+    assert torch.equal(r.mx_dequantize(q), x)
+    del q.codes
+    y = r.mx_linear(x, r.mx_quantize(torch.full((1, 1), 2.0, device="cuda"), b.MXFP4), torch.ones(1, device="cuda"))
+    assert torch.equal(y, 2 * x + 1)
+
+
 def bound(x, w, bias):
     return (x.shape[1] + 2) * 2.0 ** -23 * L.linear_magnitude(x, w, bias)
 

@@ -280,6 +280,23 @@ def test_rows_far_apart(r):
     assert all(torch.equal(u, v) for u, v in zip(ref, r.train_linear_backward(dz, b.MxTensor(codes, q.scales, 64, b.MXFP8), w, True)))
 
 
+def test_a_quarter_billion_rows(r):
+    """One column in and out: indexes of rows, tiles and parts stay exact."""
+    rows = (1 << 28) + 777
+    x = torch.ones((rows, 1), dtype=torch.bfloat16, device="cuda")
+    x[::3] = -3.0
+    x[-1] = 0.25
+    w = torch.full((1, 1), 2.0, dtype=torch.bfloat16, device="cuda")
+    y, none = r.train_linear(x, w, torch.ones(1, device="cuda"), keep=False)
+    assert none is None and torch.equal(y, 2 * x + 1)
+    dz = torch.zeros_like(x)
+    at = torch.tensor([0, 1, 5000, rows // 2, rows - 2, rows - 1], device="cuda")
+    dz[at] = 8.0
+    dx, dw, db = r.train_linear_backward(dz, x, w)
+    assert torch.equal(dx, 2 * dz) and db.item() == 48.0
+    assert dw.item() == (8 * x[at].double()).sum().item()
+
+
 def test_not_finite(r):
     """NaN and infinities reach the results that they belong to and no others."""
     x, w, dz = activations(1, 200, 70, True), normal(2, 40, 70), normal(3, 200, 40)

@@ -5,6 +5,7 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <string>
 #include <vector>
 
@@ -582,6 +583,35 @@ int validate_mat(const char* name, const donerf_mat* m, int types, int64_t rows,
     return DONERF_OK;
 }
 
+// Bytes that a validated matrix's rows take, from row to row `step` apart.
+struct Extent {
+    uintptr_t at;
+    int64_t rows, len, step;
+};
+Extent extent(const donerf_mat* m, int64_t rows, int32_t cols) {
+    const int64_t size = microscaled(m->type) ? 1 : m->type == DONERF_TYPE_FP32 ? 4 : 2;
+    const int64_t len = microscaled(m->type) ? code_bytes(m->type, cols) : cols * size;
+    return Extent{(uintptr_t)m->data, rows, len, m->ld * size};
+}
+// Whether two of them share memory.  Columns of one buffer side by side (rows
+// equally far apart) do not; rows of different strides count as their whole range.
+bool shared(const Extent& a, const Extent& b) {
+    if (a.rows < 1 || b.rows < 1) return false;
+    const uintptr_t end_a = a.at + (a.rows - 1) * a.step + a.len, end_b = b.at + (b.rows - 1) * b.step + b.len;
+    if (end_a <= b.at || end_b <= a.at) return false;
+    if (a.rows == 1 && b.rows == 1) return true;
+    if (a.step != b.step) return true;
+    const Extent &lo = a.at < b.at ? a : b, &hi = a.at < b.at ? b : a;
+    const int64_t off = (int64_t)((hi.at - lo.at) % (uintptr_t)a.step);
+    return off < lo.len || off + hi.len > a.step;
+}
+// The other checks, the handle's among them, come first.
+int validate_output(const char* name, const Extent& y, std::initializer_list<Extent> others) {
+    for (const Extent& o : others)
+        if (shared(y, o)) return fail(DONERF_E_INVALID_ARG, std::string(name) + " overlaps another matrix");
+    return DONERF_OK;
+}
+
 // Sizes of a layer operator.
 int validate_layer(int64_t rows, int32_t in, int32_t out) {
     if (rows < 0 || rows > INT32_MAX) return fail(DONERF_E_INVALID_ARG, "rows must lie in [0, 2^31)");
@@ -855,7 +885,8 @@ int donerf_mx_quantize(donerf_t* h, const donerf_mat* x, const donerf_mat* q, in
     g_err.clear();
     int rc = validate_layer(rows, cols, 1);
     if (rc || (rc = validate_mat("x", x, kF32Bit | kBf16Bit, rows, cols)) ||
-        (rc = validate_mat("q", q, kMx4Bit | kMx8Bit, rows, cols)) || (rc = validate_handle(h)))
+        (rc = validate_mat("q", q, kMx4Bit | kMx8Bit, rows, cols)) ||
+        (rc = validate_handle(h)) || (rc = validate_output("q", extent(q, rows, cols), {extent(x, rows, cols)})))
         return rc;
     const hipError_t e = launch_mx_quantize(x->data, x->ld, x->type == DONERF_TYPE_BF16, mx_out(q),
                                             q->type == DONERF_TYPE_MXFP8, rows, cols, h->n_cu, h->stream);
@@ -866,7 +897,8 @@ int donerf_mx_dequantize(donerf_t* h, const donerf_mat* q, const donerf_mat* y, 
     g_err.clear();
     int rc = validate_layer(rows, cols, 1);
     if (rc || (rc = validate_mat("q", q, kMx4Bit | kMx8Bit, rows, cols)) ||
-        (rc = validate_mat("y", y, kF32Bit | kBf16Bit, rows, cols)) || (rc = validate_handle(h)))
+        (rc = validate_mat("y", y, kF32Bit | kBf16Bit, rows, cols)) ||
+        (rc = validate_handle(h)) || (rc = validate_output("y", extent(y, rows, cols), {extent(q, rows, cols)})))
         return rc;
     const hipError_t e = launch_mx_dequantize(mx_in(q), q->type == DONERF_TYPE_MXFP8, y->data, y->ld,
                                               y->type == DONERF_TYPE_BF16, rows, cols, h->n_cu, h->stream);
@@ -893,7 +925,8 @@ int donerf_mx_linear(donerf_t* h, const donerf_mat* x, const donerf_mat* w, cons
     if (relu != 0 && relu != 1) return fail(DONERF_E_INVALID_ARG, "relu must be 0 or 1");
     if ((rc = validate_tiles(rows, out)) ||
         (rc = validate_workspace(workspace, workspace_bytes, donerf_mx_linear_workspace(x->type, rows, in))) ||
-        (rc = validate_handle(h)))
+        (rc = validate_handle(h)) ||
+        (rc = validate_output("y", extent(y, rows, out), {extent(x, rows, in), extent(w, out, in)})))
         return rc;
     if (rows == 0) return DONERF_OK;
     const int kind = y->type == DONERF_TYPE_MXFP4 ? kOutMx4 : y->type == DONERF_TYPE_BF16 ? kOutBf16 : kOutF32;
@@ -963,6 +996,11 @@ int donerf_train_linear(donerf_t* h, const donerf_mat* x, const donerf_mat* w, c
     if ((uintptr_t)bias % 4) return fail(DONERF_E_INVALID_ARG, "bias not aligned");
     if (relu != 0 && relu != 1) return fail(DONERF_E_INVALID_ARG, "relu must be 0 or 1");
     if ((rc = validate_tiles(rows, out)) || (rc = validate_handle(h))) return rc;
+    const Extent ex = extent(x, rows, in), ew = extent(w, out, in);
+    if ((y && (rc = validate_output("y", extent(y, rows, out), {ex, ew}))) ||
+        (kept && (rc = validate_output("kept", extent(kept, rows, out), {ex, ew}))) ||
+        (y && kept && (rc = validate_output("kept", extent(kept, rows, out), {extent(y, rows, out)}))))
+        return rc;
     if (rows == 0) return DONERF_OK;
     GemmArgs g{};
     g.a = bf16_in(w);
@@ -1004,6 +1042,12 @@ int donerf_train_linear_backward(donerf_t* h, const donerf_mat* dz, const donerf
         return fail(DONERF_E_INVALID_ARG, "relu and accumulate must be 0 or 1");
     if ((rc = validate_tiles(rows, in)) || (rc = validate_tiles(rows, out)) || (rc = validate_handle(h)) ||
         (rc = validate_workspace(workspace, workspace_bytes, backward_workspace(rows, out, in, h->n_cu))))
+        return rc;
+    const Extent ez = extent(dz, rows, out), ex = extent(x, rows, in);
+    if ((dx && (rc = validate_output("dx", extent(dx, rows, in), {ez, ex, extent(w, out, in)}))) ||
+        (dw && (rc = validate_output("dw", extent(dw, out, in), {ez, ex}))) ||
+        (dw && w && (rc = validate_output("dw", extent(dw, out, in), {extent(w, out, in)}))) ||
+        (dw && dx && (rc = validate_output("dw", extent(dw, out, in), {extent(dx, rows, in)}))))
         return rc;
     BackwardArgs a{};
     a.dz = (const uint16_t*)dz->data;

@@ -390,3 +390,46 @@ def test_replays_from_a_graph(r):
         torch.cuda.synchronize()
         assert all(torch.equal(u, v) for u, v in zip(other, ref))
     del g
+
+
+def raw(m):
+    """An argument of the C ABI from a 2-D tensor or an MxTensor."""
+    if isinstance(m, b.MxTensor):
+        return m.codes.data_ptr(), m.codes.stride(0), m.format, m.scales.data_ptr(), m.scales.stride(0)
+    return m.data_ptr(), m.stride(0), b.TYPE_FP32 if m.dtype == torch.float32 else b.TYPE_BF16
+
+
+def test_outputs_that_overlap_are_refused(r):
+    x, w = torch.randn(40, 64, device="cuda"), r.mx_quantize(torch.randn(64, 64, device="cuda"), b.MXFP4)
+    x0 = x.clone()
+    buf = torch.randn(50, 64, device="cuda")
+    q = r.mx_quantize(x, b.MXFP4)
+    spare = r.mx_empty(40, 64, b.MXFP4)
+    on_x = b.MxTensor(x.view(torch.uint8)[:, :32], spare.scales, 64, b.MXFP4)
+    on_w = b.MxTensor(w.codes[:40], spare.scales, 64, b.MXFP4)
+    for call in (lambda: r.mx_linear(x, w, out=x), lambda: r.mx_linear(buf[:40], w, out=buf[10:]), lambda: r.mx_linear(buf[10:], w, out=buf[:40]),
+                 lambda: r.mx_linear(buf[39:], w, out=buf[:40][29:]), lambda: r.mx_linear(q, w, out=q), lambda: r.mx_linear(x, w, out=on_w),
+                 lambda: b.donerf_mx_quantize(r.h, raw(x), raw(on_x), 40, 64),
+                 lambda: b.donerf_mx_dequantize(r.h, raw(on_x), raw(x), 40, 64)):
+        with pytest.raises(b.DonerfError, match="overlaps another matrix"):
+            call()
+    torch.cuda.synchronize()
+    assert torch.equal(x, x0)
+
+
+def test_neighbours_in_one_buffer(r):
+    """Rows behind each other and columns side by side share nothing."""
+    w = r.mx_quantize(torch.randn(64, 64, device="cuda"), b.MXFP4)
+    for rows in (5, 100):
+        buf = torch.randn(2 * rows, 64, device="cuda")
+        want = r.mx_linear(buf[:rows], w, out=torch.float32)
+        assert torch.equal(r.mx_linear(buf[:rows], w, out=buf[rows:]), want)
+        for x_first in (True, False):
+            buf = torch.randn(rows, 128, device="cuda")
+            x, y = (buf[:, :64], buf[:, 64:]) if x_first else (buf[:, 64:], buf[:, :64])
+            x0 = x.clone()
+            want = r.mx_linear(x0, w, out=torch.float32)
+            assert torch.equal(r.mx_linear(x, w, out=y), want) and torch.equal(x, x0)
+        buf = torch.randn(rows, 128, device="cuda")
+        with pytest.raises(b.DonerfError, match="overlaps another matrix"):
+            r.mx_linear(buf[:, :64], w, out=buf[:, 63:127])

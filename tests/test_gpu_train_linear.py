@@ -430,3 +430,26 @@ def test_replays_from_a_graph(r):
         assert all(torch.equal(u, v) for u, v in zip(work(other), ref))
     del graphs
     other.close()
+
+
+def test_outputs_that_overlap_are_refused(r):
+    bf = lambda rows: torch.randn(256, 64, device="cuda").bfloat16()[:rows]   # with room for every matrix below
+    x, w, dz, y = bf(40), bf(64), bf(40), bf(40)
+    dw, db = torch.zeros(64, 64, device="cuda"), torch.zeros(64, device="cuda")
+    kept = r.mx_empty(40, 64, b.MXFP8)
+    raw = lambda t: (t.data_ptr(), t.stride(0), b.TYPE_FP32 if t.dtype == torch.float32 else b.TYPE_BF16)
+    mx = lambda at: (at.data_ptr(), 64, b.MXFP8, kept.scales.data_ptr(), kept.scales.stride(0))
+    need = b.donerf_train_linear_backward_workspace(r.h, 40, 64, 64)
+    ws = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+    forward = lambda y, k: b.donerf_train_linear(r.h, raw(x), raw(w), None, 0, y, k, 40, 64, 64)
+    backward = lambda dx, dw: b.donerf_train_linear_backward(r.h, raw(dz), raw(x), 0, raw(w), dx, dw, db.data_ptr(), 0, 40, 64, 64,
+                                                             ws.data_ptr(), ws.numel())
+    before = [t.clone() for t in (x, w, dz, y)]
+    for call in (lambda: forward(raw(x), None), lambda: forward(raw(w), None), lambda: forward(raw(y), mx(y)), lambda: forward(None, mx(x)),
+                 lambda: backward(raw(dz), None), lambda: backward(raw(x), None), lambda: backward(raw(w), raw(dw)),
+                 lambda: backward(raw(y), (y.data_ptr(), 64, b.TYPE_FP32)), lambda: backward(None, (w.data_ptr(), 64, b.TYPE_FP32)),
+                 lambda: backward(None, (dz.data_ptr(), 64, b.TYPE_FP32))):
+        with pytest.raises(b.DonerfError, match="overlaps another matrix"):
+            call()
+    torch.cuda.synchronize()
+    assert all(torch.equal(t, u) for t, u in zip((x, w, dz, y), before))

@@ -334,10 +334,11 @@ typedef enum donerf_type {
  *   ld_scales  bytes from one row's scales to the next's, a multiple of 8 and at
  *           least a row's blocks.  Bytes behind the last block's are neither
  *           used nor written
- * An output whose data share memory with those of another matrix of its call is
- * refused (E_INVALID_ARG).
- * Columns of one buffer side by side share none if their rows are equally far
- * apart; with different strides the whole range from first to last row counts.
+ * What a call writes (an output's data and scales, db, the workspace as far as it
+ * is needed) may share memory with nothing else that the call is given; a call in
+ * which it does is refused (E_INVALID_ARG).  Columns of one buffer side by
+ * side share none if their rows are equally far apart; with different strides the
+ * whole range from first to last row counts.
  * Both directions of every conversion treat a block the same way: its scale is
  * the smallest power of two, 2^-127 or more, that holds its largest value as an
  * element (6 or 448 times the scale), and elements are rounded to the nearest,

@@ -5,7 +5,6 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
-#include <initializer_list>
 #include <string>
 #include <vector>
 
@@ -583,16 +582,11 @@ int validate_mat(const char* name, const donerf_mat* m, int types, int64_t rows,
     return DONERF_OK;
 }
 
-// Bytes that a validated matrix's rows take, from row to row `step` apart.
+// Bytes that rows of `len` take, `step` apart.
 struct Extent {
     uintptr_t at;
     int64_t rows, len, step;
 };
-Extent extent(const donerf_mat* m, int64_t rows, int32_t cols) {
-    const int64_t size = microscaled(m->type) ? 1 : m->type == DONERF_TYPE_FP32 ? 4 : 2;
-    const int64_t len = microscaled(m->type) ? code_bytes(m->type, cols) : cols * size;
-    return Extent{(uintptr_t)m->data, rows, len, m->ld * size};
-}
 // Whether two of them share memory.  Columns of one buffer side by side (rows
 // equally far apart) do not; rows of different strides count as their whole range.
 bool shared(const Extent& a, const Extent& b) {
@@ -600,17 +594,53 @@ bool shared(const Extent& a, const Extent& b) {
     const uintptr_t end_a = a.at + (a.rows - 1) * a.step + a.len, end_b = b.at + (b.rows - 1) * b.step + b.len;
     if (end_a <= b.at || end_b <= a.at) return false;
     if (a.rows == 1 && b.rows == 1) return true;
-    if (a.step != b.step) return true;
+    const int64_t step = a.rows == 1 ? b.step : a.step;   // a single row has none of its own
+    if (b.rows > 1 && b.step != step) return true;
     const Extent &lo = a.at < b.at ? a : b, &hi = a.at < b.at ? b : a;
-    const int64_t off = (int64_t)((hi.at - lo.at) % (uintptr_t)a.step);
-    return off < lo.len || off + hi.len > a.step;
+    const int64_t off = (int64_t)((hi.at - lo.at) % (uintptr_t)step);
+    return off < lo.len || off + hi.len > step;
 }
-// The other checks, the handle's among them, come first.
-int validate_output(const char* name, const Extent& y, std::initializer_list<Extent> others) {
-    for (const Extent& o : others)
-        if (shared(y, o)) return fail(DONERF_E_INVALID_ARG, std::string(name) + " overlaps another matrix");
-    return DONERF_OK;
-}
+
+// All memory that a call reads and writes, validated already: matrices (their scales
+// are a range of their own), vectors and the workspace.  Absent ones take none.
+class Ranges {
+  public:
+    Ranges& reads(const donerf_mat* m, int64_t rows, int32_t cols) { return add(nullptr, m, rows, cols); }
+    Ranges& writes(const char* name, const donerf_mat* m, int64_t rows, int32_t cols) { return add(name, m, rows, cols); }
+    Ranges& reads(const void* p, size_t bytes) { return add(nullptr, p, bytes); }
+    Ranges& writes(const char* name, const void* p, size_t bytes) { return add(name, p, bytes); }
+    // What is written shares memory with nothing else of the call.  Callers have
+    // made all other checks, the handle's among them.
+    int validate() const {
+        for (int i = 0; i < n_; ++i)
+            for (int j = 0; name_[i] && j < n_; ++j)
+                if (j != i && shared(at_[i], at_[j]))
+                    return fail(DONERF_E_INVALID_ARG, std::string(name_[i]) + " overlaps another matrix or buffer of the call");
+        return DONERF_OK;
+    }
+
+  private:
+    Ranges& add(const char* name, const donerf_mat* m, int64_t rows, int32_t cols) {
+        if (!m) return *this;
+        const bool mx = microscaled(m->type);
+        const int64_t size = mx ? 1 : m->type == DONERF_TYPE_FP32 ? 4 : 2;
+        push(name, Extent{(uintptr_t)m->data, rows, mx ? code_bytes(m->type, cols) : cols * size, m->ld * size});
+        if (mx) push(name, Extent{(uintptr_t)m->scales, rows, (cols + 31) / 32, m->ld_scales});
+        return *this;
+    }
+    Ranges& add(const char* name, const void* p, size_t bytes) {
+        if (p && bytes) push(name, Extent{(uintptr_t)p, 1, (int64_t)bytes, (int64_t)bytes});
+        return *this;
+    }
+    void push(const char* name, const Extent& e) {
+        name_[n_] = name;
+        at_[n_++] = e;
+    }
+    static constexpr int kMost = 12;   // of one call: five matrices with scales, two more
+    const char* name_[kMost];          // null: read only
+    Extent at_[kMost];
+    int n_ = 0;
+};
 
 // Sizes of a layer operator.
 int validate_layer(int64_t rows, int32_t in, int32_t out) {
@@ -886,7 +916,7 @@ int donerf_mx_quantize(donerf_t* h, const donerf_mat* x, const donerf_mat* q, in
     int rc = validate_layer(rows, cols, 1);
     if (rc || (rc = validate_mat("x", x, kF32Bit | kBf16Bit, rows, cols)) ||
         (rc = validate_mat("q", q, kMx4Bit | kMx8Bit, rows, cols)) ||
-        (rc = validate_handle(h)) || (rc = validate_output("q", extent(q, rows, cols), {extent(x, rows, cols)})))
+        (rc = validate_handle(h)) || (rc = Ranges().writes("q", q, rows, cols).reads(x, rows, cols).validate()))
         return rc;
     const hipError_t e = launch_mx_quantize(x->data, x->ld, x->type == DONERF_TYPE_BF16, mx_out(q),
                                             q->type == DONERF_TYPE_MXFP8, rows, cols, h->n_cu, h->stream);
@@ -898,7 +928,7 @@ int donerf_mx_dequantize(donerf_t* h, const donerf_mat* q, const donerf_mat* y, 
     int rc = validate_layer(rows, cols, 1);
     if (rc || (rc = validate_mat("q", q, kMx4Bit | kMx8Bit, rows, cols)) ||
         (rc = validate_mat("y", y, kF32Bit | kBf16Bit, rows, cols)) ||
-        (rc = validate_handle(h)) || (rc = validate_output("y", extent(y, rows, cols), {extent(q, rows, cols)})))
+        (rc = validate_handle(h)) || (rc = Ranges().writes("y", y, rows, cols).reads(q, rows, cols).validate()))
         return rc;
     const hipError_t e = launch_mx_dequantize(mx_in(q), q->type == DONERF_TYPE_MXFP8, y->data, y->ld,
                                               y->type == DONERF_TYPE_BF16, rows, cols, h->n_cu, h->stream);
@@ -923,10 +953,11 @@ int donerf_mx_linear(donerf_t* h, const donerf_mat* x, const donerf_mat* w, cons
         return rc;
     if ((uintptr_t)bias % 4) return fail(DONERF_E_INVALID_ARG, "bias not aligned");
     if (relu != 0 && relu != 1) return fail(DONERF_E_INVALID_ARG, "relu must be 0 or 1");
-    if ((rc = validate_tiles(rows, out)) ||
-        (rc = validate_workspace(workspace, workspace_bytes, donerf_mx_linear_workspace(x->type, rows, in))) ||
+    const size_t need = donerf_mx_linear_workspace(x->type, rows, in);
+    if ((rc = validate_tiles(rows, out)) || (rc = validate_workspace(workspace, workspace_bytes, need)) ||
         (rc = validate_handle(h)) ||
-        (rc = validate_output("y", extent(y, rows, out), {extent(x, rows, in), extent(w, out, in)})))
+        (rc = Ranges().writes("y", y, rows, out).writes("workspace", workspace, need).reads(x, rows, in)
+                  .reads(w, out, in).reads(bias, (size_t)out * sizeof(float)).validate()))
         return rc;
     if (rows == 0) return DONERF_OK;
     const int kind = y->type == DONERF_TYPE_MXFP4 ? kOutMx4 : y->type == DONERF_TYPE_BF16 ? kOutBf16 : kOutF32;
@@ -996,10 +1027,8 @@ int donerf_train_linear(donerf_t* h, const donerf_mat* x, const donerf_mat* w, c
     if ((uintptr_t)bias % 4) return fail(DONERF_E_INVALID_ARG, "bias not aligned");
     if (relu != 0 && relu != 1) return fail(DONERF_E_INVALID_ARG, "relu must be 0 or 1");
     if ((rc = validate_tiles(rows, out)) || (rc = validate_handle(h))) return rc;
-    const Extent ex = extent(x, rows, in), ew = extent(w, out, in);
-    if ((y && (rc = validate_output("y", extent(y, rows, out), {ex, ew}))) ||
-        (kept && (rc = validate_output("kept", extent(kept, rows, out), {ex, ew}))) ||
-        (y && kept && (rc = validate_output("kept", extent(kept, rows, out), {extent(y, rows, out)}))))
+    if ((rc = Ranges().writes("y", y, rows, out).writes("kept", kept, rows, out).reads(x, rows, in).reads(w, out, in)
+                  .reads(bias, (size_t)out * sizeof(float)).validate()))
         return rc;
     if (rows == 0) return DONERF_OK;
     GemmArgs g{};
@@ -1040,14 +1069,11 @@ int donerf_train_linear_backward(donerf_t* h, const donerf_mat* dz, const donerf
     if ((uintptr_t)db % 4) return fail(DONERF_E_INVALID_ARG, "db not aligned");
     if ((relu != 0 && relu != 1) || (accumulate != 0 && accumulate != 1))
         return fail(DONERF_E_INVALID_ARG, "relu and accumulate must be 0 or 1");
-    if ((rc = validate_tiles(rows, in)) || (rc = validate_tiles(rows, out)) || (rc = validate_handle(h)) ||
-        (rc = validate_workspace(workspace, workspace_bytes, backward_workspace(rows, out, in, h->n_cu))))
-        return rc;
-    const Extent ez = extent(dz, rows, out), ex = extent(x, rows, in);
-    if ((dx && (rc = validate_output("dx", extent(dx, rows, in), {ez, ex, extent(w, out, in)}))) ||
-        (dw && (rc = validate_output("dw", extent(dw, out, in), {ez, ex}))) ||
-        (dw && w && (rc = validate_output("dw", extent(dw, out, in), {extent(w, out, in)}))) ||
-        (dw && dx && (rc = validate_output("dw", extent(dw, out, in), {extent(dx, rows, in)}))))
+    if ((rc = validate_tiles(rows, in)) || (rc = validate_tiles(rows, out)) || (rc = validate_handle(h))) return rc;
+    const size_t need = backward_workspace(rows, out, in, h->n_cu);
+    if ((rc = validate_workspace(workspace, workspace_bytes, need)) ||
+        (rc = Ranges().writes("dx", dx, rows, in).writes("dw", dw, out, in).writes("db", db, (size_t)out * sizeof(float))
+                  .writes("workspace", workspace, need).reads(dz, rows, out).reads(x, rows, in).reads(w, out, in).validate()))
         return rc;
     BackwardArgs a{};
     a.dz = (const uint16_t*)dz->data;

@@ -658,9 +658,13 @@ int validate_handle(const donerf_t* h) {
     if (dev != h->device) return fail(DONERF_E_DEVICE, "the current device is not the handle's");
     return DONERF_OK;
 }
-// A product's tiles, 128 x 128 or more wherever there are many, in the 32-bit grid.
+// A product's tiles, 128 x 128 or more wherever there are many, in the 32-bit grid:
+// workgroups of 256 threads, a multiple of eight of them.  (Up to 256 columns that
+// many rows fit into memory only with few inputs, for the kernel that walks over
+// its tiles with a workgroup or two per compute unit.)
 int validate_tiles(int64_t rows, int32_t cols) {
-    if (rows * (int64_t)cols >= (int64_t)1 << 38 || ((rows + 127) / 128) * ((cols + 127) / 128) >= 1 << 24)
+    const int64_t tiles = ((rows + 127) / 128) * ((cols + 127) / 128), most = (int64_t)1 << 24;
+    if (rows * (int64_t)cols >= (int64_t)1 << 38 || tiles >= most || (cols > 256 && (tiles + 7) / 8 * 8 >= most))
         return fail(DONERF_E_UNSUPPORTED, "more results than a launch takes");
     return DONERF_OK;
 }

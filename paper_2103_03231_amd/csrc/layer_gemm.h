@@ -580,18 +580,33 @@ constexpr int kSrcBf16Rows = 1;   // any bf16 rows: through registers, a tile ah
 constexpr int kSrcF32 = 2;        // fp32 or bf16 rows that become E2M1, likewise
 constexpr int kSrcBf16 = 3;
 constexpr int kRowsTile = 64;
-// Workgroups that share a compute unit.
-constexpr int rows_workgroups(int op, int ks, int src) { return op == kOpMx4 && ks == 1 && src == kSrcCopies ? 2 : 1; }
+// LDS: a tile's stages, then its rows' scales, KS words of eight each, or a stage of
+// transposed weights, three times; and the results.
+constexpr int kLdsPerCu = 160 * 1024;
+template <int OP, int KS, int WN, bool TA, int EPI>
+struct RowsLds {
+    static constexpr int kChunks = kRowsTile * KS * kStageChunks, kScaleWords = OP == kOpMx4 ? kRowsTile * KS * 2 : 0;
+    static constexpr int kTile = kChunks + kScaleWords / 4, kRing = TA ? 64 * 32 : 0;
+    static constexpr int kSlot = kTile > kRing ? kTile : kRing;
+    static constexpr int kBytes = (3 * kSlot + Outgoing<EPI, kRowsTile, 32 * WN>::kSize) * 16;
+};
+// Workgroups that share a compute unit: two where a tile's batch is small and copied,
+// if LDS holds them.  fp32 results of more than 128 outputs take 64 KiB of it: a grid
+// of two workgroups per unit there, half of which waited for the other half, took 11.1
+// us for 20,000 x 256 x 256 and 17.3 for 50,000; a grid of one takes 9.1 and 15.0.
 template <int OP, int KS, int WN, bool TA, int SRC, int EPI>
-__global__ void __launch_bounds__(512, rows_workgroups(OP, KS, SRC) * 2) layer_rows_kernel(GemmArgs g) {
+constexpr int rows_workgroups() {
+    return OP == kOpMx4 && KS == 1 && SRC == kSrcCopies && 2 * RowsLds<OP, KS, WN, TA, EPI>::kBytes <= kLdsPerCu ? 2 : 1;
+}
+template <int OP, int KS, int WN, bool TA, int SRC, int EPI, int WGS = rows_workgroups<OP, KS, WN, TA, SRC, EPI>()>
+__global__ void __launch_bounds__(512, WGS * 2) layer_rows_kernel(GemmArgs g) {
     constexpr bool DB = SRC == kSrcCopies, kConvert = SRC == kSrcF32 || SRC == kSrcBf16;
     static_assert(!kConvert || (OP == kOpMx4 && KS == 1), "conversion is to E2M1, of one stage");
     constexpr int NW = 8, WM = NW / WN, RT = kRowsTile, RB = RT / 32 / WM, CP = RT * KS / 8 / NW;
     using Out = Outgoing<EPI, RT, 32 * WN>;
-    // a tile: its stages, then the rows' scales, KS words of eight each
-    constexpr int kChunks = RT * KS * kStageChunks, kScaleWords = OP == kOpMx4 ? RT * KS * 2 : 0;
-    constexpr int kRing = TA ? 64 * 32 : 0;   // a stage of transposed weights passes through, too
-    constexpr int kSlot = kChunks + kScaleWords / 4 > kRing ? kChunks + kScaleWords / 4 : kRing;
+    using Lds = RowsLds<OP, KS, WN, TA, EPI>;
+    constexpr int kChunks = Lds::kChunks, kScaleWords = Lds::kScaleWords, kSlot = Lds::kSlot;
+    static_assert(WGS * Lds::kBytes <= kLdsPerCu, "workgroups that share a compute unit share its LDS");
     __shared__ u32x4 ring0[kSlot], ring1[kSlot], ring2[kSlot];
     __shared__ u32x4 out[Out::kSize];
     const int lane = threadIdx.x & 63;
@@ -929,13 +944,17 @@ __global__ void __launch_bounds__(512, 2) layer_split_kernel(GemmArgs g) {
     Out::template store<64>(out, g, m0, n0, threadIdx.x);
 }
 
-template <int OP, int KS, bool TA, int SRC, int EPI>
-hipError_t launch_layer_rows(GemmArgs g, int n_cu, hipStream_t stream) {
+template <int OP, int KS, int WN, bool TA, int SRC, int EPI>
+void launch_rows_of(GemmArgs g, int n_cu, hipStream_t stream) {
     g.tiles_m = (uint32_t)(((int64_t)g.M + kRowsTile - 1) / kRowsTile);
-    const uint32_t most = rows_workgroups(OP, KS, SRC) * (uint32_t)n_cu;
+    const uint32_t most = rows_workgroups<OP, KS, WN, TA, SRC, EPI>() * (uint32_t)n_cu;
     const dim3 grid(g.tiles_m < most ? g.tiles_m : most);
-    if (g.N > 128) hipLaunchKernelGGL((layer_rows_kernel<OP, KS, 8, TA, SRC, EPI>), grid, dim3(512), 0, stream, g);
-    else hipLaunchKernelGGL((layer_rows_kernel<OP, KS, 4, TA, SRC, EPI>), grid, dim3(512), 0, stream, g);
+    hipLaunchKernelGGL((layer_rows_kernel<OP, KS, WN, TA, SRC, EPI>), grid, dim3(512), 0, stream, g);
+}
+template <int OP, int KS, bool TA, int SRC, int EPI>
+hipError_t launch_layer_rows(const GemmArgs& g, int n_cu, hipStream_t stream) {
+    if (g.N > 128) launch_rows_of<OP, KS, 8, TA, SRC, EPI>(g, n_cu, stream);
+    else launch_rows_of<OP, KS, 4, TA, SRC, EPI>(g, n_cu, stream);
     return hipGetLastError();
 }
 

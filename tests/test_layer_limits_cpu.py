@@ -1,8 +1,13 @@
-"""The layer operators' limit on results, at the edge: what is refused as such and
-what is taken (and, without a handle, gets as far as the handle)."""
+"""The layer operators' limits: on results, at the edge (what is refused as such, and
+what is taken and, without a handle, gets as far as the handle), and on what the
+workgroups of a compute unit share, read from the library's code object."""
+import re
+import struct
+
 import pytest
 
 from paper_2103_03231_amd import binding as b
+from test_code_object import LDS_PER_CU, _gfx950_code_objects, _sections
 from test_layers_abi_cpu import backward, forward, linear, mat, refused
 
 
@@ -22,3 +27,27 @@ def test_results_of_a_launch(tiles_m, tiles_n, taken):
             refused(call, "handle is NULL")
         else:
             refused(call, "more results", b.E_UNSUPPORTED)
+
+
+# layer_rows_kernel<OP, KS, WN, TA, SRC, EPI, workgroups of a compute unit>
+ROWS = re.compile(r"17layer_rows_kernelILi\dELi\dELi\dELb\dELi\dELi\dELi(\d)EEEv")
+SIMDS, VGPRS, WAVES = 4, 512, 8        # of a compute unit, of a SIMD's lane, of a workgroup
+
+
+def test_workgroups_that_a_launch_counts_on_share_a_compute_unit():
+    seen = {1: 0, 2: 0}
+    for co in _gfx950_code_objects(b.LIB_PATH):
+        secs, raw = _sections(co)
+        symbols, names = secs[".symtab"], secs[".strtab"]
+        for i in range(symbols[5] // 24):
+            st_name, _, _, st_shndx, st_value, _ = struct.unpack_from("<IBBHQQ", co, symbols[4] + 24 * i)
+            name = co[names[4] + st_name:co.index(b"\0", names[4] + st_name)].decode()
+            if not name.endswith(".kd") or "layer_rows_kernel" not in name:
+                continue
+            kd = co[raw[st_shndx][4] + (st_value - raw[st_shndx][3]):][:64]
+            lds, = struct.unpack_from("<I", kd, 0)
+            vgprs = 8 * ((struct.unpack_from("<I", kd, 48)[0] & 63) + 1)      # accumulators among them
+            count = int(ROWS.search(name).group(1))
+            assert count * lds <= LDS_PER_CU and count * WAVES * vgprs <= SIMDS * VGPRS, (name, lds, vgprs)
+            seen[count] += 1
+    assert seen[1] > 0 and seen[2] > 0, seen

@@ -1,0 +1,268 @@
+"""Every kernel of the layer operators on whole numbers, whose products and sums
+fp32 holds: results are the reference's rounded once, bit for bit, whatever the order
+of the sums, so a term that is lost, doubled or read from elsewhere shows.  Sizes
+reach each kernel that a rule on sizes picks; matrices are whole, cut out of wider ones
+at aligned addresses (rows of 16-byte chunks still), or at odd ones; NaN lies between
+the rows of inputs, and what lies around outputs is as it was afterwards.
+
+Whole numbers of at most 2^24 are exact in fp32.  The largest sums here: 150,001
+terms of at most 2 x 4, and 5000 of at most 6 x 6."""
+import pytest
+import torch
+
+from paper_2103_03231_amd import binding as b
+from paper_2103_03231_amd import inputs
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+LAYOUTS = ["whole", "aligned", "odd"]
+
+
+@pytest.fixture(scope="module")
+def r():
+    r = b.Renderer(b.Config(), inputs.make_weights(128, 0))
+    yield r
+    r.close()
+
+
+def generator(*key):
+    return torch.Generator(device="cuda").manual_seed(hash(key) % (1 << 31))
+
+
+def ints(g, most, *shape):
+    return torch.randint(-most, most + 1, shape, generator=g, device="cuda").to(BF16)
+
+
+def fours(g, *shape):
+    """Whole numbers that E2M1 holds at every scale that their block may get."""
+    table = torch.tensor([-6, -4, -3, -2, -1, 0, 1, 2, 3, 4, 6], dtype=F32, device="cuda")
+    return table[torch.randint(0, 11, shape, generator=g, device="cuda")]
+
+
+# ---------------------------------------------------------------- matrices and what surrounds them
+
+def room(rows, cols, dtype, layout, fill):
+    """(all of it, the matrix in it)"""
+    if layout == "whole":
+        m = torch.full((rows, cols), fill, dtype=dtype, device="cuda")
+        return m, m
+    if layout == "aligned":      # 16-byte chunks stay whole where cols holds whole ones
+        big = torch.full((rows + 2, -(-cols // 8) * 8 + 24), fill, dtype=dtype, device="cuda")
+        return big, big[1:1 + rows, 8:8 + cols]
+    big = torch.full(((rows + 3) * (cols + 37) + 1,), fill, dtype=dtype, device="cuda")[1:].view(rows + 3, cols + 37)
+    return big, big[1:1 + rows, 3:3 + cols]
+
+
+def placed(t, layout):
+    m = room(*t.shape, t.dtype, layout, float("nan"))[1]
+    return m.copy_(t)
+
+
+def mx_room(rows, cols, kind, layout, fill):
+    """(codes and scales with what surrounds them, the MxTensor in them)"""
+    blocks = -(-cols // 32)
+    wide, wide_s = blocks * (16 if kind == b.MXFP4 else 32), -(-blocks // 8) * 8
+    around = 0 if layout == "whole" else 1
+    codes = torch.full((rows + 2 * around, wide + 48 * around), fill, dtype=torch.uint8, device="cuda")
+    scales = torch.full((rows + 2 * around, wide_s + 16 * around), fill, dtype=torch.uint8, device="cuda")
+    q = b.MxTensor(codes[around:around + rows, 16 * around:16 * around + wide], scales[around:around + rows, 8 * around:8 * around + wide_s], cols, kind)
+    return (codes, scales), q
+
+
+def mx_placed(q, layout):
+    """The same matrix with NaN around it, in what fills its rows of scales up, too."""
+    m = mx_room(q.rows, q.cols, q.format, layout, 255)[1]
+    blocks = -(-q.cols // 32)
+    m.codes.copy_(q.codes)
+    m.scales[:, :blocks] = q.scales[:, :blocks]
+    return m
+
+
+def raw(m):
+    """An argument of the C names."""
+    if m is None:
+        return None
+    if isinstance(m, b.MxTensor):
+        return m.codes.data_ptr(), m.codes.stride(0), m.format, m.scales.data_ptr(), m.scales.stride(0)
+    return m.data_ptr(), max(m.stride(0), m.shape[1]), b.TYPE_FP32 if m.dtype == F32 else b.TYPE_BF16
+
+
+def same(got, ref):
+    """Equal, NaN where the reference has NaN."""
+    return torch.equal(got.isnan(), ref.isnan()) and torch.equal(got.nan_to_num(0.0, posinf=float("inf"), neginf=-float("inf")),
+                                                                 ref.nan_to_num(0.0, posinf=float("inf"), neginf=-float("inf")))
+
+
+def same_mx(got, ref):
+    """The same codes and scales; an element's NaN may have either sign."""
+    blocks = -(-ref.cols // 32)
+    wide = blocks * (16 if ref.format == b.MXFP4 else 32)
+    u, v = got.codes[:, :wide], ref.codes[:, :wide]
+    if ref.format == b.MXFP8:
+        u, v = (torch.where((t & 127) == 127, torch.full_like(t, 127), t) for t in (u, v))
+    return torch.equal(got.scales[:, :blocks], ref.scales[:, :blocks]) and torch.equal(u, v)
+
+
+def untouched(big, m, fill):
+    """Only m was written in `big`."""
+    m.fill_(fill)
+    return bool((big == fill).all())
+
+
+def mx_untouched(big, q, fill):
+    q.codes.fill_(fill)
+    q.scales[:, :-(-q.cols // 32)] = fill
+    return all(bool((t == fill).all()) for t in big)
+
+
+# ---------------------------------------------------------------- training layers
+
+def forward_case(r, rows, n_in, n_out, relu, layout, planted, outputs=(("y", "kept"),)):
+    g = generator(rows, n_in, n_out, relu)
+    x, w, bias = ints(g, 4, rows, n_in), ints(g, 3, n_out, n_in), ints(g, 8, n_out).float()
+    if planted:
+        x[rows - 1, n_in - 1], w[n_out - 1, 0] = float("nan"), float("inf")
+    ref = (x.double() @ w.double().t() + bias.double()).float() + 0.0
+    if relu:
+        ref = torch.where(ref <= 0, torch.zeros_like(ref), ref)
+    kept_ref = r.mx_quantize(ref, b.MXFP8)
+    x, w = placed(x, layout), placed(w, layout)
+    for names in outputs:
+        big, y = room(rows, n_out, BF16, layout, 5.0) if "y" in names else (None, None)
+        mx_big, kept = mx_room(rows, n_out, b.MXFP8, layout, 9) if "kept" in names else (None, None)
+        b.donerf_train_linear(r.h, raw(x), raw(w), bias.data_ptr(), int(relu), raw(y), raw(kept), rows, n_in, n_out)
+        if y is not None:
+            assert same(y, ref.to(BF16)), names
+            assert untouched(big, y, 5.0)
+        if kept is not None:
+            assert same_mx(kept, kept_ref), names
+            assert mx_untouched(mx_big, kept, 9)
+
+
+def backward_case(r, rows, n_in, n_out, relu, layout, planted, kinds=("mxfp8", "bf16")):
+    g = generator(rows, n_in, n_out, relu, 1)
+    x, w, dz = ints(g, 4, rows, n_in), ints(g, 3, n_out, n_in), ints(g, 2, rows, n_out)
+    x = torch.relu(x) if relu else x
+    if planted:
+        x[rows - 1, n_in - 1], w[n_out - 1, 0], dz[rows - 1, n_out // 2] = float("nan"), float("inf"), float("inf")
+    X, W, Z = x.double(), w.double(), dz.double()
+    dx_ref, dw_ref, db_ref = Z @ W, (Z.t() @ X).float(), Z.sum(0).float()
+    dx_ref = (torch.where(X != 0, dx_ref, torch.zeros_like(dx_ref)) if relu else dx_ref).to(BF16)
+    dz, w = placed(dz, layout), placed(w, layout)
+    need = b.donerf_train_linear_backward_workspace(r.h, rows, n_in, n_out)
+    for kind in kinds:
+        q = mx_placed(r.mx_quantize(x, b.MXFP8), layout) if kind == "mxfp8" else placed(x, layout)
+        big, dx = room(rows, n_in, BF16, layout, 5.0)
+        big_w, dw = room(n_out, n_in, F32, layout, 5.0)
+        db, ws = torch.full((n_out + 2,), 5.0, device="cuda"), torch.full((need + 64,), 5, dtype=torch.uint8, device="cuda")
+        b.donerf_train_linear_backward(r.h, raw(dz), raw(q), int(relu), raw(w), raw(dx), raw(dw), db[1:].data_ptr(), 0, rows, n_in, n_out,
+                                       ws.data_ptr(), need)
+        assert same(dw, dw_ref), kind
+        assert same(db[1:-1], db_ref), kind
+        assert same(dx, dx_ref), kind
+        assert untouched(big, dx, 5.0) and untouched(big_w, dw, 5.0) and db[0] == 5 and db[-1] == 5 and bool((ws[need:] == 5).all())
+
+
+# terms split among waves, tiles of 64, 128 and 256, weights in registers (both widths,
+# one to four stages of terms), for y and dx; dW from one part and from many, of one
+# stage and of several
+TRAIN = [(1, 1, 1), (5, 8, 8), (33, 72, 40), (70, 333, 130), (64, 336, 4096), (3000, 90, 256), (3001, 256, 90), (2500, 128, 384),
+         (16391, 90, 250), (16391, 90, 120), (16385, 40, 100), (16400, 256, 200), (20001, 130, 33), (17003, 64, 256), (33001, 191, 255), (16500, 8, 136),
+         (4500, 300, 1200), (4504, 304, 1200), (4500, 1200, 304), (8203, 2049, 71), (8200, 72, 2056), (8200, 2056, 72)]
+
+
+@pytest.mark.parametrize("planted", [False, True])
+@pytest.mark.parametrize("relu", [False, True])
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("rows,n_in,n_out", TRAIN)
+def test_forward(r, rows, n_in, n_out, layout, relu, planted):
+    forward_case(r, rows, n_in, n_out, relu, layout, planted)
+
+
+@pytest.mark.parametrize("planted", [False, True])
+@pytest.mark.parametrize("relu", [False, True])
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("rows,n_in,n_out", TRAIN)
+def test_backward(r, rows, n_in, n_out, layout, relu, planted):
+    backward_case(r, rows, n_in, n_out, relu, layout, planted)
+
+
+# Weights in registers past batches so long that every workgroup's ring of three tiles
+# turns, with copies and stores of other tiles under way: 150,001 rows are nine tiles of
+# 64 a workgroup, or four and a half where two share one of 256 compute units.
+LONG = 150001
+
+
+@pytest.mark.parametrize("n_out", [128, 256, 100, 200])
+@pytest.mark.parametrize("n_in", [64, 128, 256, 184, 63])
+def test_forward_of_a_long_batch(r, n_in, n_out):
+    forward_case(r, LONG, n_in, n_out, True, "whole", False, (("y", "kept"), ("y",), ("kept",)))
+
+
+@pytest.mark.parametrize("relu", [False, True])
+@pytest.mark.parametrize("n_in", [128, 256, 104, 199])
+@pytest.mark.parametrize("n_out", [64, 128, 256, 184, 63])
+def test_backward_of_a_long_batch(r, n_in, n_out, relu):
+    backward_case(r, LONG, n_in, n_out, relu, "whole", False)
+
+
+def test_splits_of_every_length(r):
+    """dW where the batch's parts are of one stage, of several and of an odd number of
+    them, the last part and the last stage short."""
+    for rows in (63, 64, 65, 127, 129, 191, 193, 320, 5000, 32 * 1024 + 1, 100003):
+        for n_in, n_out in ((64, 48), (40, 130), (300, 520)):
+            backward_case(r, rows, n_in, n_out, False, "whole", False)
+
+
+# ---------------------------------------------------------------- products in 4 bits
+
+def mx_case(r, rows, n_in, n_out, relu, layout, planted):
+    g = generator(rows, n_in, n_out, relu, 2)
+    x, w, bias = fours(g, rows, n_in), fours(g, n_out, n_in), ints(g, 8, n_out).float()
+    X, W = x.double(), w.double()
+    if planted:      # a block with either is NaN
+        x[rows - 1, n_in - 1], w[n_out - 1, 0] = float("nan"), float("inf")
+        if rows > 1:
+            x[rows // 2, 0] = -float("inf")
+            X[rows // 2] = float("nan")
+        X[rows - 1], W[n_out - 1] = float("nan"), float("nan")
+    ref = (X @ W.t() + bias.double()).float() + 0.0
+    ref = torch.where(ref <= 0, torch.zeros_like(ref), ref) if relu else ref
+    q_ref = r.mx_quantize(ref, b.MXFP4)
+    qw, qx = mx_placed(r.mx_quantize(w, b.MXFP4), layout), mx_placed(r.mx_quantize(x, b.MXFP4), layout)
+    for m in (placed(x, layout), placed(x.to(BF16), layout), qx):
+        kind = raw(m)[2]
+        need = b.donerf_mx_linear_workspace(kind, rows, n_in)
+        ws = torch.full((need + 64,), 5, dtype=torch.uint8, device="cuda")
+        for out in (F32, BF16, b.MXFP4):
+            big, y = mx_room(rows, n_out, b.MXFP4, layout, 9) if out == b.MXFP4 else room(rows, n_out, out, layout, 5.0)
+            b.donerf_mx_linear(r.h, raw(m), raw(qw), bias.data_ptr(), int(relu), raw(y), rows, n_in, n_out, ws.data_ptr(), need)
+            if out == b.MXFP4:
+                assert same_mx(y, q_ref), (kind, out)
+                assert mx_untouched(big, y, 9)
+            else:
+                assert same(y, ref.to(out)), (kind, out)
+                assert untouched(big, y, 5.0)
+        assert bool((ws[need:] == 5).all())
+
+
+# a few rows (one and two groups of 16, one and several turns of the waves), terms split
+# among waves, tiles of 64 and 128, weights in registers (converted on the way, one and
+# two stages, both widths)
+MX = [(1, 1, 1), (1, 4096, 257), (3, 100, 40), (13, 300, 70), (16, 5000, 33), (17, 128, 16), (32, 2080, 100), (33, 700, 40), (70, 1025, 64),
+      (90, 4096, 500), (200, 300, 300), (1021, 283, 100), (3000, 64, 640), (16384, 256, 256), (16391, 100, 200), (16400, 512, 129),
+      (16385, 7, 31), (20011, 300, 77), (4500, 700, 1200), (36000, 513, 129)]
+
+
+@pytest.mark.parametrize("planted", [False, True])
+@pytest.mark.parametrize("relu", [False, True])
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("rows,n_in,n_out", MX)
+def test_mx_linear(r, rows, n_in, n_out, layout, relu, planted):
+    mx_case(r, rows, n_in, n_out, relu, layout, planted)
+
+
+@pytest.mark.parametrize("n_out", [128, 256, 100, 200])
+@pytest.mark.parametrize("n_in", [256, 512, 100, 300])
+def test_mx_linear_of_a_long_batch(r, n_in, n_out):
+    mx_case(r, LONG, n_in, n_out, True, "whole", False)

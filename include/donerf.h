@@ -416,7 +416,9 @@ int donerf_train_linear(donerf_t* h, const donerf_mat* x, const donerf_mat* w, c
  *   x     rows x in: what the forward pass of the layer before kept (MXFP8), or
  *         BF16 (a network's input)
  *   relu  1: x is a ReLU's output, and dx is the gradient of that ReLU's input:
- *         0 where x is zero.  0: dx is the gradient of x
+ *         0 where x is zero, in MXFP8 where its element is, whatever the block's
+ *         scale (a zero of a block whose scale is NaN stops the gradient, too,
+ *         though x reads as NaN there).  0: dx is the gradient of x
  *   w     out x in, BF16; may be NULL without dx
  *   dx    rows x in, BF16, or NULL
  *   dw    out x in, FP32, or NULL

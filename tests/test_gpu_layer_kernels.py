@@ -266,3 +266,19 @@ def test_mx_linear(r, rows, n_in, n_out, layout, relu, planted):
 @pytest.mark.parametrize("n_in", [256, 512, 100, 300])
 def test_mx_linear_of_a_long_batch(r, n_in, n_out):
     mx_case(r, LONG, n_in, n_out, True, "whole", False)
+
+
+@pytest.mark.parametrize("rows,n_in,n_out", [(70, 64, 333), (300, 90, 72), (16400, 256, 200), (8200, 2056, 72)])
+def test_elements_tell_what_a_relu_let_through(r, rows, n_in, n_out):
+    """Also in blocks whose scale is NaN, very small or very large; -0 is a
+    zero.  dW is NaN where such a block's columns meet any row of it."""
+    g = generator(rows, n_in, n_out, 3)
+    x, w, dz = torch.relu(ints(g, 4, rows, n_in)), ints(g, 3, n_out, n_in), ints(g, 2, rows, n_out)
+    q = r.mx_quantize(x, b.MXFP8)
+    q.codes[::3] |= torch.where(q.codes[::3] == 0, 128, 0).to(torch.uint8)
+    q.scales[0], q.scales[1] = 0, 200
+    q.scales[rows - 1, 0] = 255
+    dx, dw, _ = r.train_linear_backward(dz, q, w, True)
+    ref = (dz.double() @ w.double()).to(BF16)
+    assert same(dx, torch.where(x > 0, ref, torch.zeros_like(ref)))
+    assert bool(dw[:, :32].isnan().all()) and not bool(dw[:, 32:].isnan().any())

@@ -662,11 +662,12 @@ int validate_handle(const donerf_t* h) {
 // workgroups of 256 threads, a multiple of eight of them.  (Up to 256 columns that
 // many rows fit into memory only with few inputs, for the kernel that walks over
 // its tiles with a workgroup or two per compute unit.)
-int validate_tiles(int64_t rows, int32_t cols) {
+bool fits_launch(int64_t rows, int32_t cols) {
     const int64_t tiles = ((rows + 127) / 128) * ((cols + 127) / 128), most = (int64_t)1 << 24;
-    if (rows * (int64_t)cols >= (int64_t)1 << 38 || tiles >= most || (cols > 256 && (tiles + 7) / 8 * 8 >= most))
-        return fail(DONERF_E_UNSUPPORTED, "more results than a launch takes");
-    return DONERF_OK;
+    return rows * (int64_t)cols < (int64_t)1 << 38 && tiles < most && (cols <= 256 || (tiles + 7) / 8 * 8 < most);
+}
+int validate_tiles(int64_t rows, int32_t cols) {
+    return fits_launch(rows, cols) ? DONERF_OK : fail(DONERF_E_UNSUPPORTED, "more results than a launch takes");
 }
 
 int validate_workspace(const void* p, size_t have, size_t need) {
@@ -1054,6 +1055,7 @@ int donerf_train_linear(donerf_t* h, const donerf_mat* x, const donerf_mat* w, c
 
 size_t donerf_train_linear_backward_workspace(const donerf_t* h, int64_t rows, int32_t in, int32_t out) {
     if (!h || rows < 0 || rows > INT32_MAX || in < 1 || in > DONERF_MAX_COLS || out < 1 || out > DONERF_MAX_COLS) return 0;
+    if (!fits_launch(rows, in) || !fits_launch(rows, out)) return 0;
     return backward_workspace(rows, out, in, h->n_cu);
 }
 

@@ -112,3 +112,15 @@ def test_neighbours_are_taken(r):
     b.donerf_train_linear_backward(r.h, (dz.data_ptr(), OUT, BF), (x.data_ptr(), IN, BF), 0, None, None, (at, IN, F32), at + 4 * OUT * IN, 0,
                                    200, IN, OUT, at + 4 * (OUT * IN + OUT), need)
     assert torch.equal(flat[:OUT * IN].view(OUT, IN), ref[1]) and torch.equal(flat[OUT * IN:OUT * IN + OUT], ref[2]) and flat[-1] == 7
+
+
+def test_sizes_that_are_refused_need_no_workspace(r):
+    """What donerf_train_linear_backward refuses for its size, though its columns and
+    rows alone lie in their ranges."""
+    most = b.MAX_COLS
+    for rows, n_in, n_out in (((1 << 31) - 1, most, most), ((1 << 31) - 1, most, 1), ((1 << 31) - 1, 1, most), (1 << 22, most, 8), (1 << 22, 8, most),
+                              (-1, 8, 8), (8, 0, 8), (8, 8, most + 1)):
+        assert b.donerf_train_linear_backward_workspace(r.h, rows, n_in, n_out) == 0, (rows, n_in, n_out)
+    # taken: more tiles than the chip holds workgroups make one part, a single tile many
+    need = lambda *size: b.donerf_train_linear_backward_workspace(r.h, *size)
+    assert need((1 << 22) - 128, 8, most) == 0 < need(1 << 21, 8, 8) and need(1 << 21, 8, 8) % (4 * (8 * 8 + 8)) == 0

@@ -380,7 +380,8 @@ int donerf_mx_dequantize(donerf_t* h, const donerf_mat* q, const donerf_mat* y, 
  *   relu  0: act is the identity; 1: max(z, 0), NaN kept
  *   y     rows x out: FP32, BF16 or MXFP4 (converted from the fp32 results)
  *   workspace  device, 16-byte aligned, at least donerf_mx_linear_workspace(...)
- *         bytes, the call's own until it is done; may be NULL if that is 0
+ *         bytes, the call's own until it is done (for some sizes unused: the query
+ *         does not know `out`); may be NULL if that is 0
  * Products are exact, sums fp32.  y must not overlap the inputs.
  * rows 0..2^31 - 1 (0: nothing is done), in and out 1..DONERF_MAX_COLS.
  * Errors: as above, and E_SIZE (workspace too small), E_UNSUPPORTED (rows x out

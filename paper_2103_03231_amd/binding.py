@@ -340,7 +340,9 @@ class Renderer:
         return out
 
     # ---- layer operators.  Matrices are 2-D tensors with unit column stride (any row
-    # stride); they and the current stream must be those of the handle.
+    # stride); they and the current stream must be those of the handle.  Nothing is
+    # recorded for autograd, also where a tensor requires its gradient: gradients come
+    # from train_linear_backward.
 
     # Checks are written for few attribute reads: on small calls they are most
     # of the time.
@@ -484,7 +486,8 @@ class Renderer:
 
     def train_linear(self, x, w, bias=None, relu=False, keep=True):
         """A layer's forward pass (donerf_train_linear): x (rows, in) and w (out,
-        in) bf16 -> (y (rows, out) bf16, the same in MXFP8 or None without keep)."""
+        in) bf16 -> (y (rows, out) bf16, the same in MXFP8 or None without keep).
+        y has no autograd history: its gradient is train_linear_backward's dz."""
         t, dev = self.torch, self._bind()
         bf16 = (t.bfloat16,)
         mx, mw = self._rows("x", x, bf16, None, dev), self._rows("w", w, bf16, None, dev)

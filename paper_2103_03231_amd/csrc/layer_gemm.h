@@ -6,7 +6,9 @@
 // 128 bytes of every row (64 bf16 or 256 E2M1 columns).  In LDS a row's eight
 // 16-byte chunks are permuted (row_key), so that reads of one chunk of sixteen rows
 // meet all 64 banks.  Two such stages alternate in two arrays: the copy of one runs
-// while the other is multiplied.
+// while the other is multiplied, but not within an E2M1 workgroup, where a stage's
+// scales are loaded behind the next stage's copies and arrive after them: there only
+// the other workgroup of the compute unit multiplies meanwhile.
 //
 // The weights are the MFMA's A operand and the batch its B operand, so a lane's
 // accumulators are 16 of a block's 32 outputs of one batch row, which it shares
@@ -449,9 +451,10 @@ struct Outgoing {
 
 // TA: the weights are transposed in memory, a[k][n] (bf16 only).
 // Measured, a call's results at the rate of their products: bf16 16,384 x 2048 x 2048
-// on 256 x 256 tiles 158 us (870 TFLOP/s; matrix pipes 35 % busy, half of the waves'
-// time waits for the next stage and the barrier that publishes it), 190 us on
-// 128 x 128; E2M1 8192 x 4096 x 4096 on 128 x 128 130 us (2.1 PFLOP/s).
+// on 256 x 256 tiles 150 us forward (920 TFLOP/s) and 158 us dx (870 TFLOP/s; matrix
+// pipes 35 % busy, half of the waves' time waits for the next stage and the barrier
+// that publishes it), dx 190 us on 128 x 128; E2M1 8192 x 4096 x 4096 on 128 x 128 129
+// us (2.1 PFLOP/s; a stage's scales wait for the next one's copies, see above).
 template <int OP, int BN, int BM, int WN, int WM, bool TA, bool DA, bool DB, int EPI>
 __global__ void __launch_bounds__(64 * WN * WM, 2) layer_gemm_kernel(GemmArgs g) {
     constexpr int NW = WN * WM, TN = BN / (32 * WN), TM = BM / (32 * WM);
@@ -573,8 +576,11 @@ __global__ void __launch_bounds__(64 * WN * WM, 2) layer_gemm_kernel(GemmArgs g)
 // along the outputs, 8 / WN along the rows.  SRC: how the batch gets there.
 // Measured at 256 x 256: 160,000 rows forward with both outputs 55 us (207 MB, 3.8
 // TB/s), dx 50 us, E2M1 from bf16 32 us (164 MB, 5.1 TB/s); 640,000 rows from E2M1 to
-// E2M1 51 us, bound by the instructions of its epilogue and the two barriers of a tile,
-// to bf16 70 us (415 MB, 5.9 TB/s).
+// E2M1 51 us (174 MB, 3.4 TB/s), to bf16 70 us (415 MB, 5.9 TB/s).  What bounds E2M1 to
+// E2M1 is in part that one of the three unrolled steps waits for all copies under way
+// before it reads its tile (the compiler's wait: it does not tell the ring's slots
+// apart there), so that the ring drains on every third tile; the epilogue's
+// instructions and the two barriers of a tile are the rest.
 constexpr int kSrcCopies = 0;     // rows of whole, 16-byte aligned chunks: straight into LDS
 constexpr int kSrcBf16Rows = 1;   // any bf16 rows: through registers, a tile ahead
 constexpr int kSrcF32 = 2;        // fp32 or bf16 rows that become E2M1, likewise
@@ -983,7 +989,7 @@ hipError_t launch_layer_gemm(GemmArgs g, int n_cu, hipStream_t stream) {
     g.tiles_n = (uint32_t)((g.N + b - 1) / b);
     g.tiles_m = (uint32_t)((g.M + b - 1) / b);
     const dim3 grid((g.tiles_n * g.tiles_m + 7) / 8 * 8);
-    if constexpr (kBig) {   // E2M1 ran slower on 256 x 256 (190 us for 8192 x 4096 x 4096, 143 us on 128 x 128)
+    if constexpr (kBig) {   // E2M1 runs slower on 256 x 256 (165 us for 8192 x 4096 x 4096, 129 us on 128 x 128)
         if (b == 256) {
             hipLaunchKernelGGL((layer_gemm_kernel<OP, 256, 256, 4, 2, TA, DA, DB, EPI>), grid, dim3(512), 0, stream, g);
             return hipGetLastError();

@@ -7,8 +7,19 @@
 // one of W and one of x, so x is converted in the lane that multiplies it, with no
 // exchange and no pass of its own: one launch, with the loads of several steps under
 // way before the first product.  Measured: one bf16 row through 4096 x 4096 6.7 us
-// (8.9 MB; 1.3 TB/s, bound by the latency of a cold read and the launch), 16 us as a
-// conversion and a product on tiles; 13 fp32 rows through 256 x 256 3.8 us.
+// (8.9 MB; 1.3 TB/s, bound by the latency of a cold read and the launch); 13 fp32 rows
+// through 256 x 256 3.8 us.
+//
+// The rule that takes it is on rows alone, so that up to 32 of them need no workspace.
+// Against a conversion and a product (in a graph of calls, on four weights in turn, bf16
+// rows / fp32 rows, us; these two launches come to the same for both):
+//                    1 row          8 rows         16 rows        32 rows
+//     256 x 256       3.4/3.1  4.9   3.4/3.2  5.0   3.5/3.5  5.3   4.3/3.9  5.4
+//    1024 x 1024      4.7/4.2  5.6   5.8/5.5  5.9   7.2/6.7  6.0   7.2/6.8  6.0
+//    4096 x 4096      6.7/7.6  7.7   7.6/9.6  7.9   8.9/12.4 8.1  13.2/19.3 8.4
+//    4096 -> 16,384  20.2/23.8 18.2 24.0/32.1 18.5 29.2/43.0 18.7 46.5/70.5 19.0
+// Every workgroup reads and converts all of x again, which costs more than a second
+// launch from about 16 rows of 1024 columns, 8 of 4096, or 16,384 outputs on.
 #include "internal.h"
 #include "mx.h"
 

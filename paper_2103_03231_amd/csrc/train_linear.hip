@@ -37,10 +37,12 @@ struct GradArgs {
 // One split's part of dW[n][k] = sum_m dz[m][n] x[m][k] for 128 weight rows and
 // 64 TK columns, in stages of R batch rows.  dz goes straight into LDS (DIRECT:
 // rows of 16-byte alignment, N a multiple of 8), x through registers, where E4M3
-// becomes bf16, loaded two stages ahead.  Both operands' terms are rows in memory and
-// are read from LDS by columns.  db comes from the fragments that are there anyway.
+// becomes bf16.  x is loaded a stage before it is stored, but with a lead of one stage's
+// products only: the wait for dz's copies, which ends a stage, waits for it too.  Both
+// operands' terms are rows in memory and are read from LDS by columns.  db comes from
+// the fragments that are there anyway.
 // Measured: 160,000 x 256 x 256 44 us (124 MB read, 32 MB of parts written),
-// 16,384 x 2048 x 2048 203 us (680 TFLOP/s).  128 x 128 with two workgroups per CU: one
+// 16,384 x 2048 x 2048 199 us (690 TFLOP/s).  128 x 128 with two workgroups per CU: one
 // gave 455 us instead of 341 for the whole backward call, 128 x 256 330 (but 39 instead of
 // 32 us at 4000 x 512 x 512, 107 instead of 104 at 160,000 x 256 x 256).
 template <bool DIRECT, bool X_BF16, int TK, int R>
@@ -138,7 +140,7 @@ __global__ void __launch_bounds__(256, 2) weight_grad_kernel(GradArgs g) {
         });
     };
     // Stage s is multiplied while dz of s + 1 is copied, x of s + 1 stands in
-    // `now` and x of s + 2 is loaded into `later`.
+    // `now` and x of s + 2 is loaded into `later` (all of it has arrived at the end).
     auto step = [&](u32x4* zs, u32x4* zn, u32x4* xs, u32x4* xn, Held& now, Held& later, int s) {
         const bool more = s + 1 < stages;
         if (more) z.issue(zn, s + 1, wave);

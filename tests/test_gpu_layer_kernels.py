@@ -6,7 +6,7 @@ at aligned addresses (rows of 16-byte chunks still), or at odd ones; NaN lies be
 the rows of inputs, and what lies around outputs is as it was afterwards.
 
 Whole numbers of at most 2^24 are exact in fp32.  The largest sums here: 150,001
-terms of at most 2 x 4, and 5000 of at most 6 x 6."""
+terms of at most 2 x 4, and 65,536 of at most 6 x 6."""
 import pytest
 import torch
 
@@ -41,6 +41,10 @@ def fours(g, *shape):
 
 # ---------------------------------------------------------------- matrices and what surrounds them
 
+def far_pitch(rows):
+    return (1 << 33) // rows // 16 * 16
+
+
 def room(rows, cols, dtype, layout, fill):
     """(all of it, the matrix in it)"""
     if layout == "whole":
@@ -49,6 +53,11 @@ def room(rows, cols, dtype, layout, fill):
     if layout == "aligned":      # 16-byte chunks stay whole where cols holds whole ones
         big = torch.full((rows + 2, -(-cols // 8) * 8 + 24), fill, dtype=dtype, device="cuda")
         return big, big[1:1 + rows, 8:8 + cols]
+    if layout.startswith("far"):     # 8 GiB from the first row to the last; "far odd": rows not of whole chunks
+        size = dtype.itemsize
+        pitch = far_pitch(rows) // size + (layout == "far odd")
+        m = torch.empty(pitch * (rows - 1) + cols, dtype=dtype, device="cuda").as_strided((rows, cols), (pitch, 1))
+        return m.fill_(fill), m
     big = torch.full(((rows + 3) * (cols + 37) + 1,), fill, dtype=dtype, device="cuda")[1:].view(rows + 3, cols + 37)
     return big, big[1:1 + rows, 3:3 + cols]
 
@@ -62,6 +71,10 @@ def mx_room(rows, cols, kind, layout, fill):
     """(codes and scales with what surrounds them, the MxTensor in them)"""
     blocks = -(-cols // 32)
     wide, wide_s = blocks * (16 if kind == b.MXFP4 else 32), -(-blocks // 8) * 8
+    if layout.startswith("far"):
+        pitch = far_pitch(rows)
+        codes, scales = (torch.empty(pitch * (rows - 1) + w, dtype=torch.uint8, device="cuda").as_strided((rows, w), (pitch, 1)) for w in (wide, wide_s))
+        return (codes.fill_(fill), scales.fill_(fill)[:, :blocks]), b.MxTensor(codes, scales, cols, kind)
     around = 0 if layout == "whole" else 1
     codes = torch.full((rows + 2 * around, wide + 48 * around), fill, dtype=torch.uint8, device="cuda")
     scales = torch.full((rows + 2 * around, wide_s + 16 * around), fill, dtype=torch.uint8, device="cuda")
@@ -282,3 +295,28 @@ def test_elements_tell_what_a_relu_let_through(r, rows, n_in, n_out):
     ref = (dz.double() @ w.double()).to(BF16)
     assert same(dx, torch.where(x > 0, ref, torch.zeros_like(ref)))
     assert bool(dw[:, :32].isnan().all()) and not bool(dw[:, 32:].isnan().any())
+
+
+# a row's offset passes 32 bits, in bytes and in values, in every matrix of the call
+@pytest.mark.parametrize("layout", ["far", "far odd"])
+@pytest.mark.parametrize("rows,n_in,n_out", [(70, 333, 130), (3000, 90, 256), (16391, 90, 250), (16400, 256, 200), (4504, 304, 1200), (4500, 1200, 304),
+                                             (8200, 72, 2056), (8200, 2056, 72)])
+def test_rows_far_apart(r, rows, n_in, n_out, layout):
+    forward_case(r, rows, n_in, n_out, True, layout, False)
+    backward_case(r, rows, n_in, n_out, True, layout, False)
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("rows,n_in,n_out", [(17, 128, 40), (70, 1025, 64), (3000, 64, 640), (16391, 100, 200), (16400, 512, 129), (4500, 700, 1200)])
+def test_mx_rows_far_apart(r, rows, n_in, n_out):
+    mx_case(r, rows, n_in, n_out, True, "far", False)
+    torch.cuda.empty_cache()
+
+
+# the most columns that are taken
+@pytest.mark.parametrize("rows,narrow", [(1, 33), (5, 40), (40, 33), (200, 64)])
+def test_the_widest_layers(r, rows, narrow):
+    for n_in, n_out in ((b.MAX_COLS, narrow), (narrow, b.MAX_COLS), (b.MAX_COLS - 1, narrow), (narrow, b.MAX_COLS - 1)):
+        forward_case(r, rows, n_in, n_out, True, "whole", True)
+        backward_case(r, rows, n_in, n_out, True, "whole", True)
+        mx_case(r, rows, n_in, n_out, True, "whole", True)

@@ -315,19 +315,21 @@ typedef enum donerf_type {
     DONERF_TYPE_BF16 = 1,
     DONERF_TYPE_MXFP4 = 2, /* microscaled E2M1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and
                               their negatives)                                */
-    DONERF_TYPE_MXFP8 = 3  /* microscaled E4M3 (largest value 448)            */
+    DONERF_TYPE_MXFP8 = 3, /* microscaled E4M3 (largest value 448)            */
+    DONERF_TYPE_INT32 = 4, /* whole numbers: ids, classes                     */
+    DONERF_TYPE_INT64 = 5
 } donerf_type;
 
 /*
- * A matrix in device memory.  fp32 and bf16: rows of values, at least `cols`
- * apart.  Microscaled: a row's columns form blocks of 32, the last one filled
+ * A matrix in device memory.  fp32, bf16 and whole numbers: rows of values, at least
+ * `cols` apart.  Microscaled: a row's columns form blocks of 32, the last one filled
  * up with zeros, and the values of a block are its elements times its scale
  * 2^(c - 127), c one byte, 255 for NaN (OCP Microscaling Formats v1.0).
- *   data    fp32, bf16: aligned to the type's size.  Microscaled: the elements'
+ *   data    aligned to the type's size.  Microscaled: the elements'
  *           codes, aligned to 16 bytes; 16 bytes a block in MXFP4 (the even
  *           column in a byte's low half), 32 bytes a block in MXFP8
- *   ld      from row to row: values (fp32, bf16) or bytes, a multiple of 16
- *           (microscaled); at least a row's length.  What lies between the rows
+ *   ld      from row to row: values, or bytes, a multiple of 16 (microscaled);
+ *           at least a row's length.  What lies between the rows
  *           of an input may be read, but is not used; that between the rows of
  *           an output is left as it is
  *   scales  microscaled: one byte per block, aligned to 8 bytes; else NULL
@@ -439,6 +441,127 @@ int donerf_train_linear_backward(donerf_t* h, const donerf_mat* dz, const donerf
 /* Bytes of workspace on the handle's device: 0 where none is needed (a few rows),
    and for sizes that are refused. */
 size_t donerf_train_linear_backward_workspace(const donerf_t* h, int64_t rows, int32_t in, int32_t out);
+
+/* ------------------------------------------------------------------------
+ * What stands around the layers in training: the norm between two of them, the
+ * lookup of learned rows (a code per view, a vector per token) at a network's input,
+ * and the loss at its end where a larger network's best classes are the target.
+ * They take and leave memory, streams and graphs as the layer operators do.
+ * ------------------------------------------------------------------------ */
+
+/*
+ * Layer norm: of each row of x its mean m and r = 1 / sqrt(v + eps), v the mean of
+ * (x - m)^2; y = act((x - m) r weight + bias), and kept, the same values (before
+ * their rounding to y's type) in MXFP8 for the backward pass of the layer that
+ * reads them.
+ *   x      rows x cols, FP32 or BF16
+ *   weight, bias  device, cols fp32 each, or NULL for ones and zeros
+ *   eps    finite, at least 1e-30
+ *   relu   0 or 1, as in donerf_mx_linear
+ *   y      rows x cols, FP32 or BF16, or NULL
+ *   kept   rows x cols, MXFP8, or NULL; one of the two at least
+ *   stats  device, rows x 2 fp32, aligned to 8 bytes: m and r, for the backward pass
+ * Sums and stats are fp32.  Where a row's squares do not fit fp32, r is 0.
+ * rows 0..2^31 - 1 (0: nothing is done), cols 1..DONERF_MAX_COLS.
+ * Errors: E_INVALID_ARG (NULL handle, x or stats, a size, type, alignment or value
+ * that the above rules out, an output that shares memory), E_DEVICE, E_HIP.
+ */
+int donerf_train_norm(donerf_t* h, const donerf_mat* x, const float* weight, const float* bias, float eps, int32_t relu,
+                      const donerf_mat* y, const donerf_mat* kept, float* stats, int64_t rows, int32_t cols);
+
+/*
+ * Its backward pass, from the gradient dz of z = (x - m) r weight + bias (what
+ * donerf_train_linear_backward leaves as dx with `relu`, where y was rectified).
+ * With xh = (x - m) r and g = dz weight:
+ *   dx = r (g - mean(g) - xh mean(g xh)), dw = the sum over the rows of dz xh,
+ *   db = that of dz.
+ *   dz     rows x cols, FP32 or BF16
+ *   x      rows x cols, FP32 or BF16, or what the layer before kept of it (MXFP8)
+ *   relu   1: x is a ReLU's output, and dx is the gradient of that ReLU's input:
+ *          0 where x is zero, in MXFP8 where its element is, whatever the block's
+ *          scale.  0: dx is the gradient of x
+ *   weight device, cols fp32, or NULL for ones
+ *   stats  what the forward pass wrote
+ *   dx     rows x cols, FP32 or BF16, or NULL
+ *   dw, db device, cols fp32 each, or NULL; one of the three at least
+ *   accumulate  0: dw and db are written; 1: they are added to
+ *   workspace   device, 16-byte aligned, donerf_train_norm_backward_workspace(...)
+ *          bytes at least, the call's own until it is done; not needed without dw
+ *          and db
+ * fp32 sums; the same call gives the same bits.  With rows = 0, dw and db are zero
+ * (or stay, with accumulate).
+ * Sizes and errors: as above, and E_SIZE (workspace too small).
+ */
+int donerf_train_norm_backward(donerf_t* h, const donerf_mat* dz, const donerf_mat* x, int32_t relu, const float* weight,
+                               const float* stats, const donerf_mat* dx, float* dw, float* db, int32_t accumulate,
+                               int64_t rows, int32_t cols, void* workspace, size_t workspace_bytes);
+
+/* Bytes of workspace on the handle's device: 0 where none is needed (a few rows),
+   and for sizes that are refused. */
+size_t donerf_train_norm_backward_workspace(const donerf_t* h, int64_t rows, int32_t cols);
+
+/*
+ * y_i = scale table[ids_i], row by row; zeros where ids_i is not in 0..n - 1.
+ *   table  n x cols, FP32 or BF16
+ *   ids    rows x 1, INT32 or INT64
+ *   y      rows x cols, FP32 or BF16
+ * rows 0..2^31 - 1, n 1..2^31 - 1, cols 1..DONERF_MAX_COLS.
+ * Errors: as for donerf_train_norm.
+ */
+int donerf_train_embedding(donerf_t* h, const donerf_mat* table, const donerf_mat* ids, float scale, const donerf_mat* y,
+                           int64_t rows, int64_t n, int32_t cols);
+
+/*
+ * The table's gradient: its row v is scale times the sum of dy_i over the i with
+ * ids_i = v, zero where there is none.  Rows of dy whose id is not in 0..n - 1 count
+ * nowhere.
+ *   dy      rows x cols, FP32 or BF16
+ *   dtable  n x cols, FP32
+ *   accumulate  0: dtable is written; 1: it is added to, and rows without an id stay
+ *           as they are
+ *   workspace   device, 16-byte aligned,
+ *           donerf_train_embedding_backward_workspace(...) bytes at least, the call's
+ *           own until it is done
+ * Rows are summed in fp32 in an order that the sizes and ids alone give: the same call
+ * gives the same bits.  With rows = 0, dtable is zero (or stays, with accumulate).
+ * Sizes and errors: as above, and E_SIZE (workspace too small).
+ */
+int donerf_train_embedding_backward(donerf_t* h, const donerf_mat* dy, const donerf_mat* ids, float scale,
+                                    const donerf_mat* dtable, int32_t accumulate, int64_t rows, int64_t n, int32_t cols,
+                                    void* workspace, size_t workspace_bytes);
+
+/* Bytes of workspace: 0 where none is needed, and for sizes that are refused. */
+size_t donerf_train_embedding_backward_workspace(const donerf_t* h, int64_t rows, int64_t n, int32_t cols);
+
+/* Most entries of a teacher's row. */
+#define DONERF_MAX_TOP 128
+
+/*
+ * Distillation from a teacher's top logits: with p the softmax of teacher /
+ * temperature over a row's entries and q that of x / temperature over its classes,
+ *   loss_i = w_i temperature^2 sum_e p_e (log p_e - log q_{c_e}),
+ *   dx = the gradient of the losses' sum: w_i temperature (q_j - sum of p_e over
+ *        the entries e of class j).
+ *   x        rows x cols, FP32 or BF16: the student's logits, -inf for classes that
+ *            are masked
+ *   classes  rows x k, INT32 or INT64: the entries' classes.  An entry whose class is
+ *            not in 0..cols - 1 is not given: it may hold anything.  A class may come
+ *            twice: each is an entry of its own
+ *   teacher  rows x k, FP32 or BF16: their logits
+ *   row_weight  device, rows fp32, or NULL for ones
+ *   temperature 2^-16..2^16
+ *   loss     device, rows fp32, or NULL
+ *   dx       rows x cols, FP32 or BF16, or NULL; one of the two at least
+ * A row of weight 0, without a given entry above -inf or without a class above -inf
+ * has no loss and no gradient (0), whatever else it holds.  A class of probability 0
+ * that an entry asks for makes the loss infinite; NaN and +inf make it NaN.
+ * fp32 arithmetic.  rows 0..2^31 - 1 (0: nothing is done), cols 1..DONERF_MAX_COLS,
+ * k 1..DONERF_MAX_TOP.
+ * Errors: as for donerf_train_norm.
+ */
+int donerf_train_distill(donerf_t* h, const donerf_mat* x, const donerf_mat* classes, const donerf_mat* teacher,
+                         const float* row_weight, float temperature, float* loss, const donerf_mat* dx, int64_t rows,
+                         int32_t cols, int32_t k);
 
 /* The device and the stream that a handle's work goes to; each may be NULL. */
 int donerf_get_stream(const donerf_t* h, int32_t* device, void** stream);

@@ -39,7 +39,10 @@ TYPE_FP32 = 0
 TYPE_BF16 = 1
 MXFP4 = 2
 MXFP8 = 3
+TYPE_INT32 = 4
+TYPE_INT64 = 5
 MAX_COLS = 65536
+MAX_TOP = 128
 
 # Every function include/donerf.h declares.
 EXPORTS = ("donerf_weight_count", "donerf_create", "donerf_destroy", "donerf_set_stream",
@@ -47,7 +50,9 @@ EXPORTS = ("donerf_weight_count", "donerf_create", "donerf_destroy", "donerf_set
            "donerf_debug_plan", "donerf_debug_topn", "donerf_debug_bins", "donerf_debug_mfma_peak",
            "donerf_mx_quantize", "donerf_mx_dequantize", "donerf_mx_linear", "donerf_mx_linear_workspace",
            "donerf_train_linear", "donerf_train_linear_backward", "donerf_train_linear_backward_workspace",
-           "donerf_get_stream", "donerf_status_str", "donerf_last_error")
+           "donerf_train_norm", "donerf_train_norm_backward", "donerf_train_norm_backward_workspace",
+           "donerf_train_embedding", "donerf_train_embedding_backward", "donerf_train_embedding_backward_workspace",
+           "donerf_train_distill", "donerf_get_stream", "donerf_status_str", "donerf_last_error")
 
 
 class DonerfLibraryMissing(RuntimeError):
@@ -142,6 +147,20 @@ def lib():
         L.donerf_train_linear_backward.restype = ctypes.c_int
         L.donerf_train_linear_backward_workspace.argtypes = [vp, i64, i32, i32]
         L.donerf_train_linear_backward_workspace.restype = sz
+        f32 = ctypes.c_float
+        L.donerf_train_norm.argtypes = [vp, mat, vp, vp, f32, i32, mat, mat, vp, i64, i32]
+        L.donerf_train_norm.restype = ctypes.c_int
+        L.donerf_train_norm_backward.argtypes = [vp, mat, mat, i32, vp, vp, mat, vp, vp, i32, i64, i32, vp, sz]
+        L.donerf_train_norm_backward.restype = ctypes.c_int
+        L.donerf_train_norm_backward_workspace.argtypes = [vp, i64, i32]
+        L.donerf_train_norm_backward_workspace.restype = sz
+        L.donerf_train_embedding.argtypes, L.donerf_train_embedding.restype = [vp, mat, mat, f32, mat, i64, i64, i32], ctypes.c_int
+        L.donerf_train_embedding_backward.argtypes = [vp, mat, mat, f32, mat, i32, i64, i64, i32, vp, sz]
+        L.donerf_train_embedding_backward.restype = ctypes.c_int
+        L.donerf_train_embedding_backward_workspace.argtypes = [vp, i64, i64, i32]
+        L.donerf_train_embedding_backward_workspace.restype = sz
+        L.donerf_train_distill.argtypes = [vp, mat, mat, mat, vp, f32, vp, mat, i64, i32, i32]
+        L.donerf_train_distill.restype = ctypes.c_int
         L.donerf_get_stream.argtypes = [vp, ctypes.POINTER(i32), ctypes.POINTER(vp)]
         L.donerf_get_stream.restype = ctypes.c_int
         L.donerf_status_str.argtypes, L.donerf_status_str.restype = [ctypes.c_int], ctypes.c_char_p
@@ -242,7 +261,7 @@ def donerf_debug_bins(h, n_bins):
 
 
 def _mat(m):
-    """A matrix argument: None, or (data, ld, type) of fp32 and bf16 rows, or
+    """A matrix argument: None, or (data, ld, type) of rows of values, or
     (data, ld, type, scales, ld_scales) of microscaled ones, addresses as integers."""
     if m is None:
         return None
@@ -279,6 +298,39 @@ def donerf_train_linear_backward(h, dz, x, relu, w, dx, dw, db_ptr, accumulate, 
                                  workspace_ptr=None, workspace_bytes=0) -> None:
     _check(lib().donerf_train_linear_backward(h, _mat(dz), _mat(x), relu, _mat(w), _mat(dx), _mat(dw), db_ptr,
                                               accumulate, rows, n_in, n_out, workspace_ptr, workspace_bytes))
+
+
+def donerf_train_norm(h, x, weight_ptr, bias_ptr, eps, relu, y, kept, stats_ptr, rows, cols) -> None:
+    _check(lib().donerf_train_norm(h, _mat(x), weight_ptr, bias_ptr, eps, relu, _mat(y), _mat(kept), stats_ptr, rows, cols))
+
+
+def donerf_train_norm_backward_workspace(h, rows, cols) -> int:
+    return lib().donerf_train_norm_backward_workspace(h, rows, cols)
+
+
+def donerf_train_norm_backward(h, dz, x, relu, weight_ptr, stats_ptr, dx, dw_ptr, db_ptr, accumulate, rows, cols,
+                               workspace_ptr=None, workspace_bytes=0) -> None:
+    _check(lib().donerf_train_norm_backward(h, _mat(dz), _mat(x), relu, weight_ptr, stats_ptr, _mat(dx), dw_ptr, db_ptr,
+                                            accumulate, rows, cols, workspace_ptr, workspace_bytes))
+
+
+def donerf_train_embedding(h, table, ids, scale, y, rows, n, cols) -> None:
+    _check(lib().donerf_train_embedding(h, _mat(table), _mat(ids), scale, _mat(y), rows, n, cols))
+
+
+def donerf_train_embedding_backward_workspace(h, rows, n, cols) -> int:
+    return lib().donerf_train_embedding_backward_workspace(h, rows, n, cols)
+
+
+def donerf_train_embedding_backward(h, dy, ids, scale, dtable, accumulate, rows, n, cols, workspace_ptr=None,
+                                    workspace_bytes=0) -> None:
+    _check(lib().donerf_train_embedding_backward(h, _mat(dy), _mat(ids), scale, _mat(dtable), accumulate, rows, n, cols,
+                                                 workspace_ptr, workspace_bytes))
+
+
+def donerf_train_distill(h, x, classes, teacher, row_weight_ptr, temperature, loss_ptr, dx, rows, cols, k) -> None:
+    _check(lib().donerf_train_distill(h, _mat(x), _mat(classes), _mat(teacher), row_weight_ptr, temperature, loss_ptr,
+                                      _mat(dx), rows, cols, k))
 
 
 def donerf_get_stream(h):
@@ -339,7 +391,7 @@ class Renderer:
         donerf_targets(self.h, depth.data_ptr(), P, H, W, K, Z, out.data_ptr())
         return out
 
-    # ---- layer operators.  Matrices are 2-D tensors with unit column stride (any row
+    # ---- layer operators, and those around the layers.  Matrices are 2-D tensors with unit column stride (any row
     # stride); they and the current stream must be those of the handle.  Nothing is
     # recorded for autograd, also where a tensor requires its gradient: gradients come
     # from train_linear_backward.
@@ -375,7 +427,30 @@ class Renderer:
             ld = cols
         if step != 1 and cols > 1 or ld < cols:
             raise ValueError(f"{name}: columns must be adjacent and rows must not overlap")
-        return x.data_ptr(), ld, TYPE_FP32 if x.dtype is t.float32 else TYPE_BF16, None, 0
+        d = x.dtype
+        return x.data_ptr(), ld, (TYPE_FP32 if d is t.float32 else TYPE_BF16 if d is t.bfloat16 else
+                                  TYPE_INT32 if d is t.int32 else TYPE_INT64), None, 0
+
+    def _ids(self, ids, device):
+        """A vector of whole numbers, of any stride, as a matrix argument of one column."""
+        t = self.torch
+        if not isinstance(ids, t.Tensor) or ids.dtype not in (t.int32, t.int64) or ids.dim() != 1:
+            raise ValueError("ids must be a 1-D tensor of torch.int32 or torch.int64")
+        if ids.get_device() != device:
+            raise ValueError("ids must be on the handle's device")
+        n = ids.shape[0]
+        ld = ids.stride(0) if n > 1 else 1
+        if ld < 1:
+            raise ValueError("ids must not share memory with each other")
+        return ids.data_ptr(), ld, TYPE_INT32 if ids.dtype is t.int32 else TYPE_INT64, None, 0
+
+    def _out(self, out, default):
+        """The type of a new result."""
+        t = self.torch
+        out = out or default
+        if out is not t.bfloat16 and out is not t.float32:
+            raise ValueError("out must be torch.bfloat16 or torch.float32")
+        return out
 
     def _mx(self, name, q, formats, shape=None, device=None):
         t = self.torch
@@ -528,6 +603,101 @@ class Renderer:
         donerf_train_linear_backward(self.h, mz, mx, 1 if relu else 0, mw, mdx, mdw, pdb, 1 if add else 0,
                                      rows, n_in, n_out, ws.data_ptr() if need else None, need)
         return dx, dw, db
+
+    def train_norm(self, x, weight=None, bias=None, eps=1e-5, relu=False, keep=True, out=None):
+        """Layer norm's forward pass (donerf_train_norm): x (rows, cols) fp32 or
+        bf16; weight and bias (cols) fp32 -> (y in torch.bfloat16 or `out`, the
+        same in MXFP8 or None without keep, stats (rows, 2) for the backward pass)."""
+        t, dev = self.torch, self._bind()
+        mx = self._rows("x", x, (t.float32, t.bfloat16), None, dev)
+        rows, cols = x.shape
+        pw, pb = self._vector("weight", weight, cols, dev), self._vector("bias", bias, cols, dev)
+        y, my = self._new(rows, cols, self._out(out, t.bfloat16), dev)
+        kept, mk = self._mx_new(rows, cols, MXFP8, dev) if keep else (None, None)
+        stats = t.empty((rows, 2), dtype=t.float32, device=dev)
+        donerf_train_norm(self.h, mx, pw, pb, eps, 1 if relu else 0, my, mk, stats.data_ptr(), rows, cols)
+        return y, kept, stats
+
+    def train_norm_backward(self, dz, x, stats, weight=None, relu=False, need_dx=True, dw=None, db=None, out=None):
+        """Its backward pass (donerf_train_norm_backward): dz (rows, cols) fp32 or
+        bf16; x as the forward pass had it, or in MXFP8, `relu` where it came out of a
+        ReLU; stats from the forward pass -> (dx in torch.bfloat16 or `out`, or None,
+        dw (cols) fp32, db (cols) fp32).  Where dw and db are given, they are added to."""
+        t, dev = self.torch, self._bind()
+        mz = self._rows("dz", dz, (t.float32, t.bfloat16), None, dev)
+        rows, cols = dz.shape
+        mx = (self._mx("x", x, (MXFP8,), (rows, cols), dev) if isinstance(x, MxTensor)
+              else self._rows("x", x, (t.float32, t.bfloat16), (rows, cols), dev))
+        if not (isinstance(stats, t.Tensor) and stats.dtype is t.float32 and stats.get_device() == dev
+                and stats.shape == (rows, 2) and stats.is_contiguous()):
+            raise ValueError(f"stats must be a contiguous float32 tensor of {(rows, 2)} on the handle's device")
+        pw = self._vector("weight", weight, cols, dev)
+        add = dw is not None
+        if add != (db is not None):
+            raise ValueError("dw and db are given together or not at all")
+        if not add:
+            dw, db = t.empty(cols, dtype=t.float32, device=dev), t.empty(cols, dtype=t.float32, device=dev)
+        pdw, pdb = self._vector("dw", dw, cols, dev), self._vector("db", db, cols, dev)
+        dx, mdx = self._new(rows, cols, self._out(out, t.bfloat16), dev) if need_dx else (None, None)
+        need = donerf_train_norm_backward_workspace(self.h, rows, cols)
+        ws = self._workspace(need, dev)
+        donerf_train_norm_backward(self.h, mz, mx, 1 if relu else 0, pw, stats.data_ptr(), mdx, pdw, pdb, 1 if add else 0,
+                                   rows, cols, ws.data_ptr() if need else None, need)
+        return dx, dw, db
+
+    def train_embedding(self, table, ids, scale=1.0, out=None):
+        """scale table[ids], zeros for ids outside the table (donerf_train_embedding):
+        table (n, cols) fp32 or bf16, ids (rows) int32 or int64 -> (rows, cols) in
+        torch.bfloat16 or `out`."""
+        t, dev = self.torch, self._bind()
+        mt = self._rows("table", table, (t.float32, t.bfloat16), None, dev)
+        mi = self._ids(ids, dev)
+        (n, cols), rows = table.shape, ids.shape[0]
+        y, my = self._new(rows, cols, self._out(out, t.bfloat16), dev)
+        donerf_train_embedding(self.h, mt, mi, scale, my, rows, n, cols)
+        return y
+
+    def train_embedding_backward(self, dy, ids, n, scale=1.0, dtable=None):
+        """The gradient of a table of n rows (donerf_train_embedding_backward): dy
+        (rows, cols) fp32 or bf16, ids (rows) int32 or int64 -> (n, cols) fp32.  Where
+        dtable is given, it is added to."""
+        t, dev = self.torch, self._bind()
+        md = self._rows("dy", dy, (t.float32, t.bfloat16), None, dev)
+        mi = self._ids(ids, dev)
+        rows, cols = dy.shape
+        if ids.shape[0] != rows:
+            raise ValueError(f"dy has {rows} rows and ids {ids.shape[0]}")
+        add = dtable is not None
+        if add:
+            mt = self._rows("dtable", dtable, (t.float32,), (n, cols), dev)
+        elif 1 <= n < 1 << 31:
+            dtable, mt = self._new(n, cols, t.float32, dev)
+        else:
+            raise ValueError("n must lie in [1, 2^31)")
+        need = donerf_train_embedding_backward_workspace(self.h, rows, n, cols)
+        ws = self._workspace(need, dev)
+        donerf_train_embedding_backward(self.h, md, mi, scale, mt, 1 if add else 0, rows, n, cols, ws.data_ptr() if need else None,
+                                        need)
+        return dtable
+
+    def train_distill(self, x, classes, teacher, temperature=1.0, row_weight=None, need_dx=True, out=None):
+        """Distillation from a teacher's top logits (donerf_train_distill): x (rows,
+        classes) fp32 or bf16, the student's logits; classes (rows, k) int32 or int64
+        and teacher (rows, k) fp32 or bf16, the teacher's entries; row_weight (rows)
+        fp32 -> (each row's loss (rows) fp32, the gradient of their sum in
+        torch.bfloat16 or `out`, or None)."""
+        t, dev = self.torch, self._bind()
+        mx = self._rows("x", x, (t.float32, t.bfloat16), None, dev)
+        mc = self._rows("classes", classes, (t.int32, t.int64), None, dev)
+        (rows, cols), k = x.shape, classes.shape[1]
+        mt = self._rows("teacher", teacher, (t.float32, t.bfloat16), (rows, k), dev)
+        if classes.shape[0] != rows:
+            raise ValueError(f"x has {rows} rows and classes {classes.shape[0]}")
+        pw = self._vector("row_weight", row_weight, rows, dev)
+        loss = t.empty(rows, dtype=t.float32, device=dev)
+        dx, mdx = self._new(rows, cols, self._out(out, t.bfloat16), dev) if need_dx else (None, None)
+        donerf_train_distill(self.h, mx, mc, mt, pw, temperature, loss.data_ptr(), mdx, rows, cols, k)
+        return loss, dx
 
     def mfma_peak(self, workgroups, iters):
         """Enqueue the register-fed MFMA loop in the handle's precision;

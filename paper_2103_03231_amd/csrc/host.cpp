@@ -555,13 +555,18 @@ int64_t code_bytes(int type, int32_t cols) {
 }
 
 constexpr int kF32Bit = 1 << DONERF_TYPE_FP32, kBf16Bit = 1 << DONERF_TYPE_BF16, kMx4Bit = 1 << DONERF_TYPE_MXFP4,
-              kMx8Bit = 1 << DONERF_TYPE_MXFP8;
+              kMx8Bit = 1 << DONERF_TYPE_MXFP8, kI32Bit = 1 << DONERF_TYPE_INT32, kI64Bit = 1 << DONERF_TYPE_INT64;
+
+// Bytes of a value of a type that is not microscaled.
+int64_t value_bytes(int type) {
+    return type == DONERF_TYPE_INT64 ? 8 : type == DONERF_TYPE_BF16 ? 2 : 4;
+}
 
 // Checks one matrix argument against the types (bits) that its place takes.
 int validate_mat(const char* name, const donerf_mat* m, int types, int64_t rows, int32_t cols) {
     auto bad = [&](const char* what) { return fail(DONERF_E_INVALID_ARG, std::string(name) + ": " + what); };
     if (!m) return bad("NULL");
-    if (m->type < DONERF_TYPE_FP32 || m->type > DONERF_TYPE_MXFP8 || !(types & (1 << m->type)))
+    if (m->type < DONERF_TYPE_FP32 || m->type > DONERF_TYPE_INT64 || !(types & (1 << m->type)))
         return bad("this type is not taken here");
     const bool mx = microscaled(m->type);
     const int64_t least = mx ? code_bytes(m->type, cols) : cols;
@@ -576,7 +581,7 @@ int validate_mat(const char* name, const donerf_mat* m, int types, int64_t rows,
     }
     if (rows == 0) return DONERF_OK;   // no row, no memory
     if (!m->data || (mx && !m->scales)) return bad("NULL buffer");
-    const uintptr_t align = mx ? 16 : m->type == DONERF_TYPE_FP32 ? 4 : 2;
+    const uintptr_t align = mx ? 16 : (uintptr_t)value_bytes(m->type);
     if ((uintptr_t)m->data % align || (mx && (uintptr_t)m->scales % 8))
         return bad("buffer not aligned");
     return DONERF_OK;
@@ -623,7 +628,7 @@ class Ranges {
     Ranges& add(const char* name, const donerf_mat* m, int64_t rows, int32_t cols) {
         if (!m) return *this;
         const bool mx = microscaled(m->type);
-        const int64_t size = mx ? 1 : m->type == DONERF_TYPE_FP32 ? 4 : 2;
+        const int64_t size = mx ? 1 : value_bytes(m->type);
         push(name, Extent{(uintptr_t)m->data, rows, mx ? code_bytes(m->type, cols) : cols * size, m->ld * size});
         if (mx) push(name, Extent{(uintptr_t)m->scales, rows, (cols + 31) / 32, m->ld_scales});
         return *this;
@@ -679,6 +684,16 @@ int validate_workspace(const void* p, size_t have, size_t need) {
     return DONERF_OK;
 }
 
+int validate_vector(const char* name, const void* p, uintptr_t align) {
+    return (uintptr_t)p % align == 0 ? DONERF_OK : fail(DONERF_E_INVALID_ARG, std::string(name) + " not aligned");
+}
+// Rows of a table.
+int validate_table(int64_t n) {
+    return n >= 1 && n <= INT32_MAX ? DONERF_OK : fail(DONERF_E_INVALID_ARG, "table rows must lie in [1, 2^31)");
+}
+
+RowsOut rows_out(const donerf_mat* m) { return RowsOut{m->data, m->ld, m->type == DONERF_TYPE_BF16}; }
+IntRows int_rows(const donerf_mat* m) { return IntRows{m->data, m->ld, m->type == DONERF_TYPE_INT64}; }
 MxIn mx_in(const donerf_mat* m) { return MxIn{(const uint8_t*)m->data, m->ld, m->scales, m->ld_scales}; }
 MxOut mx_out(const donerf_mat* m) { return MxOut{(uint8_t*)m->data, m->ld, m->scales, m->ld_scales}; }
 // bf16 rows, ld in bytes.
@@ -1105,6 +1120,185 @@ int donerf_train_linear_backward(donerf_t* h, const donerf_mat* dz, const donerf
     a.workspace = (uint8_t*)workspace;
     const hipError_t e = launch_train_linear_backward(a, h->n_cu, h->stream);
     return e == hipSuccess ? DONERF_OK : hip_fail(e, "train_linear_backward launch");
+}
+
+int donerf_train_norm(donerf_t* h, const donerf_mat* x, const float* weight, const float* bias, float eps, int32_t relu,
+                      const donerf_mat* y, const donerf_mat* kept, float* stats, int64_t rows, int32_t cols) {
+    g_err.clear();
+    int rc = validate_layer(rows, cols, 1);
+    if (rc || (rc = validate_mat("x", x, kF32Bit | kBf16Bit, rows, cols)) ||
+        (y && (rc = validate_mat("y", y, kF32Bit | kBf16Bit, rows, cols))) ||
+        (kept && (rc = validate_mat("kept", kept, kMx8Bit, rows, cols))) ||
+        (rc = validate_vector("weight", weight, 4)) || (rc = validate_vector("bias", bias, 4)) ||
+        (rc = validate_vector("stats", stats, 8)))
+        return rc;
+    if (rows > 0 && !stats) return fail(DONERF_E_INVALID_ARG, "stats is NULL");
+    if (!y && !kept) return fail(DONERF_E_INVALID_ARG, "neither y nor kept is given");
+    if (!(eps >= 1e-30f && eps <= 3e38f)) return fail(DONERF_E_INVALID_ARG, "eps must be finite and at least 1e-30");
+    if (relu != 0 && relu != 1) return fail(DONERF_E_INVALID_ARG, "relu must be 0 or 1");
+    const size_t vec = (size_t)cols * sizeof(float);
+    if ((rc = validate_handle(h)) ||
+        (rc = Ranges().writes("y", y, rows, cols).writes("kept", kept, rows, cols).writes("stats", stats, (size_t)rows * 8)
+                  .reads(x, rows, cols).reads(weight, vec).reads(bias, vec).validate()))
+        return rc;
+    if (rows == 0) return DONERF_OK;
+    NormArgs a{};
+    a.x = x->data;
+    a.ldx = x->ld;
+    a.w = weight;
+    a.b = bias;
+    a.eps = eps;
+    a.relu = relu;
+    if (y) a.y = rows_out(y);
+    if (kept) a.q = mx_out(kept);
+    a.stats = stats;
+    a.rows = (uint32_t)rows;
+    a.cols = cols;
+    a.inv_cols = 1.0f / (float)cols;
+    const hipError_t e = launch_train_norm(a, x->type == DONERF_TYPE_BF16, h->n_cu, h->stream);
+    return e == hipSuccess ? DONERF_OK : hip_fail(e, "train_norm launch");
+}
+
+size_t donerf_train_norm_backward_workspace(const donerf_t* h, int64_t rows, int32_t cols) {
+    if (!h || rows < 0 || rows > INT32_MAX || cols < 1 || cols > DONERF_MAX_COLS) return 0;
+    return norm_backward_workspace(rows, cols, h->n_cu);
+}
+
+int donerf_train_norm_backward(donerf_t* h, const donerf_mat* dz, const donerf_mat* x, int32_t relu, const float* weight,
+                               const float* stats, const donerf_mat* dx, float* dw, float* db, int32_t accumulate,
+                               int64_t rows, int32_t cols, void* workspace, size_t workspace_bytes) {
+    g_err.clear();
+    int rc = validate_layer(rows, cols, 1);
+    if (rc || (rc = validate_mat("dz", dz, kF32Bit | kBf16Bit, rows, cols)) ||
+        (rc = validate_mat("x", x, kF32Bit | kBf16Bit | kMx8Bit, rows, cols)) ||
+        (dx && (rc = validate_mat("dx", dx, kF32Bit | kBf16Bit, rows, cols))) ||
+        (rc = validate_vector("weight", weight, 4)) || (rc = validate_vector("stats", stats, 8)) ||
+        (rc = validate_vector("dw", dw, 4)) || (rc = validate_vector("db", db, 4)))
+        return rc;
+    if (rows > 0 && !stats) return fail(DONERF_E_INVALID_ARG, "stats is NULL");
+    if (!dx && !dw && !db) return fail(DONERF_E_INVALID_ARG, "no gradient is asked for");
+    if ((relu != 0 && relu != 1) || (accumulate != 0 && accumulate != 1))
+        return fail(DONERF_E_INVALID_ARG, "relu and accumulate must be 0 or 1");
+    if ((rc = validate_handle(h))) return rc;
+    const size_t need = dw || db ? norm_backward_workspace(rows, cols, h->n_cu) : 0, vec = (size_t)cols * sizeof(float);
+    if ((rc = validate_workspace(workspace, workspace_bytes, need)) ||
+        (rc = Ranges().writes("dx", dx, rows, cols).writes("dw", dw, vec).writes("db", db, vec)
+                  .writes("workspace", workspace, need).reads(dz, rows, cols).reads(x, rows, cols).reads(weight, vec)
+                  .reads(stats, (size_t)rows * 8).validate()))
+        return rc;
+    NormBackwardArgs a{};
+    a.dz = dz->data;
+    a.lddz = dz->ld;
+    a.x = mx_in(x);
+    a.relu = relu;
+    a.w = weight;
+    a.stats = stats;
+    if (dx) a.dx = rows_out(dx);
+    a.dw = dw;
+    a.db = db;
+    a.accumulate = accumulate;
+    a.rows = (uint32_t)rows;
+    a.cols = cols;
+    a.inv_cols = 1.0f / (float)cols;
+    const int kind = x->type == DONERF_TYPE_FP32 ? kRowsF32 : x->type == DONERF_TYPE_BF16 ? kRowsBf16 : kRowsMx8;
+    const hipError_t e = launch_train_norm_backward(a, kind, dz->type == DONERF_TYPE_BF16, workspace, h->n_cu, h->stream);
+    return e == hipSuccess ? DONERF_OK : hip_fail(e, "train_norm_backward launch");
+}
+
+int donerf_train_embedding(donerf_t* h, const donerf_mat* table, const donerf_mat* ids, float scale, const donerf_mat* y,
+                           int64_t rows, int64_t n, int32_t cols) {
+    g_err.clear();
+    int rc = validate_layer(rows, cols, 1);
+    if (rc || (rc = validate_table(n)) || (rc = validate_mat("table", table, kF32Bit | kBf16Bit, n, cols)) ||
+        (rc = validate_mat("ids", ids, kI32Bit | kI64Bit, rows, 1)) ||
+        (rc = validate_mat("y", y, kF32Bit | kBf16Bit, rows, cols)) || (rc = validate_handle(h)) ||
+        (rc = Ranges().writes("y", y, rows, cols).reads(table, n, cols).reads(ids, rows, 1).validate()))
+        return rc;
+    if (rows == 0) return DONERF_OK;
+    EmbeddingArgs a{};
+    a.table = table->data;
+    a.ldt = table->ld;
+    a.ids = int_rows(ids);
+    a.scale = scale;
+    a.y = rows_out(y);
+    a.rows = rows;
+    a.n = n;
+    a.cols = cols;
+    const hipError_t e = launch_train_embedding(a, table->type == DONERF_TYPE_BF16, h->n_cu, h->stream);
+    return e == hipSuccess ? DONERF_OK : hip_fail(e, "train_embedding launch");
+}
+
+size_t donerf_train_embedding_backward_workspace(const donerf_t* h, int64_t rows, int64_t n, int32_t cols) {
+    if (!h || rows < 0 || rows > INT32_MAX || n < 1 || n > INT32_MAX || cols < 1 || cols > DONERF_MAX_COLS) return 0;
+    return embedding_backward_workspace(rows, n, cols);
+}
+
+int donerf_train_embedding_backward(donerf_t* h, const donerf_mat* dy, const donerf_mat* ids, float scale,
+                                    const donerf_mat* dtable, int32_t accumulate, int64_t rows, int64_t n, int32_t cols,
+                                    void* workspace, size_t workspace_bytes) {
+    g_err.clear();
+    int rc = validate_layer(rows, cols, 1);
+    if (rc || (rc = validate_table(n)) || (rc = validate_mat("dy", dy, kF32Bit | kBf16Bit, rows, cols)) ||
+        (rc = validate_mat("ids", ids, kI32Bit | kI64Bit, rows, 1)) || (rc = validate_mat("dtable", dtable, kF32Bit, n, cols)))
+        return rc;
+    if (accumulate != 0 && accumulate != 1) return fail(DONERF_E_INVALID_ARG, "accumulate must be 0 or 1");
+    const size_t need = embedding_backward_workspace(rows, n, cols);
+    if ((rc = validate_workspace(workspace, workspace_bytes, need)) || (rc = validate_handle(h)) ||
+        (rc = Ranges().writes("dtable", dtable, n, cols).writes("workspace", workspace, need).reads(dy, rows, cols)
+                  .reads(ids, rows, 1).validate()))
+        return rc;
+    EmbeddingGradArgs a{};
+    a.dy = dy->data;
+    a.lddy = dy->ld;
+    a.scale = scale;
+    a.dtable = (float*)dtable->data;
+    a.lddt = dtable->ld;
+    a.accumulate = accumulate;
+    a.rows = rows;
+    a.n = n;
+    a.cols = cols;
+    const hipError_t e = launch_train_embedding_backward(a, int_rows(ids), dy->type == DONERF_TYPE_BF16, workspace, h->n_cu, h->stream);
+    return e == hipSuccess ? DONERF_OK : hip_fail(e, "train_embedding_backward launch");
+}
+
+int donerf_train_distill(donerf_t* h, const donerf_mat* x, const donerf_mat* classes, const donerf_mat* teacher,
+                         const float* row_weight, float temperature, float* loss, const donerf_mat* dx, int64_t rows,
+                         int32_t cols, int32_t k) {
+    g_err.clear();
+    int rc = validate_layer(rows, cols, 1);
+    if (rc) return rc;
+    if (k < 1 || k > DONERF_MAX_TOP) return fail(DONERF_E_INVALID_ARG, "entries must lie in [1, 128]");
+    if ((rc = validate_mat("x", x, kF32Bit | kBf16Bit, rows, cols)) ||
+        (rc = validate_mat("classes", classes, kI32Bit | kI64Bit, rows, k)) ||
+        (rc = validate_mat("teacher", teacher, kF32Bit | kBf16Bit, rows, k)) ||
+        (dx && (rc = validate_mat("dx", dx, kF32Bit | kBf16Bit, rows, cols))) ||
+        (rc = validate_vector("row_weight", row_weight, 4)) || (rc = validate_vector("loss", loss, 4)))
+        return rc;
+    if (!loss && !dx) return fail(DONERF_E_INVALID_ARG, "neither loss nor dx is given");
+    if (!(temperature >= 0x1p-16f && temperature <= 0x1p16f))
+        return fail(DONERF_E_INVALID_ARG, "temperature must lie in [2^-16, 2^16]");
+    const size_t vec = (size_t)rows * sizeof(float);
+    if ((rc = validate_handle(h)) ||
+        (rc = Ranges().writes("dx", dx, rows, cols).writes("loss", loss, vec).reads(x, rows, cols).reads(classes, rows, k)
+                  .reads(teacher, rows, k).reads(row_weight, vec).validate()))
+        return rc;
+    if (rows == 0) return DONERF_OK;
+    DistillArgs a{};
+    a.x = x->data;
+    a.ldx = x->ld;
+    a.classes = int_rows(classes);
+    a.teacher = FloatRows{teacher->data, teacher->ld, teacher->type == DONERF_TYPE_BF16};
+    a.weight = row_weight;
+    a.temp = temperature;
+    a.inv_temp = (float)(1.0 / (double)temperature);
+    a.log2e_over_t = (float)(1.4426950408889634 / (double)temperature);
+    a.loss = loss;
+    if (dx) a.dx = rows_out(dx);
+    a.rows = (uint32_t)rows;
+    a.cols = cols;
+    a.k = k;
+    const hipError_t e = launch_train_distill(a, x->type == DONERF_TYPE_BF16, h->n_cu, h->stream);
+    return e == hipSuccess ? DONERF_OK : hip_fail(e, "train_distill launch");
 }
 
 int donerf_get_stream(const donerf_t* h, int32_t* device, void** stream) {

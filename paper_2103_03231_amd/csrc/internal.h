@@ -224,4 +224,132 @@ struct BackwardArgs {
 size_t backward_workspace(int64_t M, int N, int K, int n_cu);
 hipError_t launch_train_linear_backward(const BackwardArgs& a, int n_cu, hipStream_t stream);
 
+// ---- operators around the layers: layer norm (train_norm.hip), lookup
+// (train_embedding.hip), distillation loss (train_distill.hip).
+
+// Rows of whole numbers, 32 or 64 bits (wide) each.
+struct IntRows {
+    const void* p;
+    int64_t ld;
+    int32_t wide;
+    __device__ __forceinline__ int64_t at(int64_t row, int col) const {
+        const int64_t i = row * ld + col;
+        return wide ? ((const int64_t*)p)[i] : (int64_t)((const int32_t*)p)[i];
+    }
+};
+// Rows of fp32 or bf16 numbers, read one at a time.
+struct FloatRows {
+    const void* p;
+    int64_t ld;
+    int32_t bf16;
+    __device__ __forceinline__ float at(int64_t row, int col) const {
+        const int64_t i = row * ld + col;
+        return bf16 ? __uint_as_float((uint32_t)((const uint16_t*)p)[i] << 16) : ((const float*)p)[i];
+    }
+};
+
+// Rows of fp32 or bf16 results; rows.h stores them.
+struct RowsOut {
+    void* base;
+    int64_t ld;
+    int32_t bf16;
+};
+
+// Types of rows that kernels are built for.
+constexpr int kRowsF32 = 0, kRowsBf16 = 1, kRowsMx8 = 2;
+
+struct NormArgs {
+    const void* x;           // fp32 or bf16
+    int64_t ldx;
+    const float* w;          // cols, or null
+    const float* b;          // cols, or null
+    float eps;
+    int32_t relu;
+    RowsOut y;               // base null without it
+    MxOut q;                 // E4M3, or codes null
+    float* stats;            // rows x (mean, 1 / standard deviation)
+    uint32_t rows;
+    int32_t cols;
+    float inv_cols;
+};
+hipError_t launch_train_norm(const NormArgs& a, bool x_bf16, int n_cu, hipStream_t stream);
+
+struct NormBackwardArgs {
+    const void* dz;          // fp32 or bf16
+    int64_t lddz;
+    MxIn x;                  // ld in values (fp32, bf16) or bytes (E4M3)
+    int32_t relu;            // x is a ReLU's output
+    const float* w;          // cols, or null
+    const float* stats;
+    RowsOut dx;              // base null without it
+    float* dw;               // cols, or null
+    float* db;               // cols, or null
+    int32_t accumulate;
+    uint32_t rows;
+    int32_t cols;
+    float inv_cols;
+    float* parts;            // set by the launch: each workgroup's dw and db, or null
+};
+size_t norm_backward_workspace(int64_t rows, int cols, int n_cu);
+hipError_t launch_train_norm_backward(const NormBackwardArgs& a, int x_type, bool dz_bf16, void* workspace, int n_cu,
+                                      hipStream_t stream);
+
+struct EmbeddingArgs {
+    const void* table;       // n x cols, fp32 or bf16
+    int64_t ldt;
+    IntRows ids;
+    float scale;
+    RowsOut y;
+    int64_t rows, n;
+    int32_t cols;
+};
+hipError_t launch_train_embedding(const EmbeddingArgs& a, bool table_bf16, int n_cu, hipStream_t stream);
+
+// One pass of the sort of rows by their ids.
+constexpr int kSortBits = 10;   // most bits of a pass
+struct SortPass {
+    IntRows ids;             // what the first pass makes its keys of
+    const uint32_t* keys_in; // null in the first pass
+    const uint32_t* rows_in; // null in the first pass
+    uint32_t* keys_out;
+    uint32_t* rows_out;
+    uint32_t* counts;        // bins x tiles
+    uint32_t* totals;        // bins
+    uint32_t rows, tile;     // keys, and those of a workgroup
+    int64_t n;
+    int32_t shift, bits;
+};
+struct EmbeddingGradArgs {
+    const void* dy;          // rows x cols, fp32 or bf16
+    int64_t lddy;
+    float scale;
+    float* dtable;           // n x cols
+    int64_t lddt;
+    int32_t accumulate;
+    int64_t rows, n;
+    int32_t cols;
+    const uint32_t* keys;    // set by the launch: sorted ids, and their rows
+    const uint32_t* order;
+    float* ends;             // sums of runs that cross the parts' ends
+    uint32_t part;           // sorted rows of a part
+};
+size_t embedding_backward_workspace(int64_t rows, int64_t n, int cols);
+hipError_t launch_train_embedding_backward(EmbeddingGradArgs a, const IntRows& ids, bool dy_bf16, void* workspace, int n_cu,
+                                           hipStream_t stream);
+
+constexpr int kMostEntries = 128;   // of a teacher's row (include/donerf.h DONERF_MAX_TOP)
+struct DistillArgs {
+    const void* x;           // fp32 or bf16
+    int64_t ldx;
+    IntRows classes;
+    FloatRows teacher;
+    const float* weight;     // rows, or null
+    float temp, inv_temp, log2e_over_t;
+    float* loss;             // rows, or null
+    RowsOut dx;              // base null without it
+    uint32_t rows;
+    int32_t cols, k;
+};
+hipError_t launch_train_distill(const DistillArgs& a, bool x_bf16, int n_cu, hipStream_t stream);
+
 }  // namespace donerf

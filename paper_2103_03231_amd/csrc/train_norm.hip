@@ -1,0 +1,480 @@
+// train_norm.hip - layer norm over a row's columns, forward and backward.
+//
+//   forward   m = mean(x), r = 1/sqrt(mean((x - m)^2) + eps), z = (x - m) r w + b,
+//             y = act(z): one pass, the row in registers between its sums.  The
+//             first sum's mean is off by its roundings; the differences to it give
+//             what it lacks, so that rows far from zero, or of one value, are exact.
+//   backward  with xh = (x - m) r and g = dz w:
+//             dx = r (g - mean(g) - xh mean(g xh)), dw = sum over rows of dz xh,
+//             db = that of dz: each workgroup adds up dw and db of its rows in
+//             registers, and a second launch adds the workgroups' parts.
+#include "rows.h"
+
+namespace donerf {
+namespace {
+
+// ---------------------------------------------------------------- forward
+
+// w and b at a chunk's columns, or at a lane's single one.
+__device__ __forceinline__ void affine_at(const NormArgs& a, const Columns& c, int k, float* w, float* b) {
+    const RowsIn<float> ws(a.w, 0, a.cols), bs(a.b, 0, a.cols);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = 1.0f, b[i] = 0.0f;
+    if (a.w) ws.load(0, k).values(w);
+    if (a.b) bs.load(0, k).values(b);
+}
+
+template <class T, int L, int C, bool KEEP>
+__global__ void __launch_bounds__(row_threads(L)) norm_kernel(NormArgs a) {
+    constexpr int kGroups = row_threads(L) / L;
+    constexpr bool kHeld = C <= 2;   // w and b in registers, too
+    __shared__ typename RowReduce<L, 1>::Lds lds;
+    RowReduce<L, 1> reduce(&lds);
+    const int lane = threadIdx.x % L, group = threadIdx.x / L;
+    const RowsIn<T> x((const T*)a.x, a.ldx, a.cols);
+    const Columns& c = x.c;
+    float w[kHeld ? C : 1][8], b[kHeld ? C : 1][8];
+    if constexpr (kHeld)
+#pragma unroll
+        for (int j = 0; j < C; ++j) affine_at(a, c, 8 * (lane + L * j), w[j], b[j]);
+    auto act = [&](float z) { return a.relu ? __builtin_elementwise_maximum(z, 0.0f) : z; };
+    // the same number of rows for every wave: sums over a workgroup's waves need them all
+    for (uint32_t r0 = blockIdx.x * kGroups; r0 < a.rows; r0 += gridDim.x * kGroups) {
+        const bool live = r0 + group < a.rows;
+        const int64_t row = live ? r0 + group : a.rows - 1;
+        Raw<T> raw[C];
+#pragma unroll
+        for (int j = 0; j < C; ++j) raw[j] = x.load(row, 8 * (lane + L * j));
+        float one = 0.0f;
+        if (c.any_single()) one = x.load_single(row, lane);
+        auto total = [&](auto f) {   // of f over the row's values
+            float sum = c.has_single(lane) ? f(one) : 0.0f;
+#pragma unroll
+            for (int j = 0; j < C; ++j) {
+                if (c.has(8 * (lane + L * j))) {
+                    float v[8];
+                    raw[j].values(v);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) sum += f(v[i]);
+                }
+                raw[j].hold();
+            }
+            return reduce.template one<Add>(sum) * a.inv_cols;
+        };
+        const float first = total([](float v) { return v; });
+        const float mean = first + total([&](float v) { return v - first; });
+        const float var = total([&](float v) { return (v - mean) * (v - mean); });
+        const float r = __builtin_amdgcn_rsqf(var + a.eps);
+        if (!live) continue;   // behind the last sum of this row
+        if (lane == 0) *(f32x2*)(a.stats + 2 * row) = f32x2{mean, r};
+        float tail[8];   // kept values: the chunk that is not whole, by the lane whose turn it is
+        if constexpr (KEEP) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) tail[i] = 0.0f;
+            if (c.any_single() && lane == c.whole / 8 % L)
+#pragma unroll
+                for (int i = 0; i < 7; ++i) {
+                    const int k = c.whole + i < a.cols ? c.whole + i : a.cols - 1;
+                    const float xh = (value_of(x.base[row * x.ld + k]) - mean) * r;
+                    const float z = act(__builtin_fmaf(xh, a.w ? a.w[k] : 1.0f, a.b ? a.b[k] : 0.0f));
+                    tail[i] = c.whole + i < a.cols ? z : 0.0f;
+                }
+        }
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+            const int k = 8 * (lane + L * j);
+            float v[8];
+            raw[j].values(v);
+            float wj[8], bj[8];
+            if constexpr (!kHeld) affine_at(a, c, k, wj, bj);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                v[i] = act(__builtin_fmaf((v[i] - mean) * r, kHeld ? w[kHeld ? j : 0][i] : wj[i], kHeld ? b[kHeld ? j : 0][i] : bj[i]));
+            if (a.y.base && c.has(k)) store8(a.y, row, k, v);
+            if constexpr (KEEP) {
+                if (!c.has(k))
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = k == c.whole ? tail[i] : 0.0f;
+                store_mx8(a.q, row, k, a.cols, v);
+            }
+        }
+        if (c.has_single(lane) && a.y.base) {
+            const int k = c.single(lane);
+            store1(a.y, row, k, act(__builtin_fmaf((one - mean) * r, a.w ? a.w[k] : 1.0f, a.b ? a.b[k] : 0.0f)));
+        }
+    }
+}
+
+// ---------------------------------------------------------------- backward
+
+// x of type X: float, uint16_t (bf16) or uint8_t (E4M3).
+template <class X>
+struct NormInput : RowsIn<X> {
+    __device__ __forceinline__ explicit NormInput(const NormBackwardArgs& a) : RowsIn<X>((const X*)a.x.codes, a.x.ld, a.cols) {}
+};
+template <>
+struct NormInput<uint8_t> : Mx8In {
+    __device__ __forceinline__ explicit NormInput(const NormBackwardArgs& a) : Mx8In(a.x, a.cols) {}
+};
+
+// A result of one workgroup alone, or its part of one.
+struct NormSums {
+    float* w;
+    float* b;
+    bool add;
+    __device__ __forceinline__ explicit NormSums(const NormBackwardArgs& a)
+        : w(a.parts ? a.parts + (int64_t)blockIdx.x * 2 * a.cols : a.dw), b(a.parts ? w + a.cols : a.db), add(!a.parts && a.accumulate) {}
+    __device__ __forceinline__ void put(float* out, int k, float v) const {
+        if (out) out[k] = add ? out[k] + v : v;
+    }
+};
+
+template <class X, class Z, int L, int C>
+__global__ void __launch_bounds__(row_threads(L)) norm_backward_kernel(NormBackwardArgs a) {
+    constexpr int kGroups = row_threads(L) / L;
+    __shared__ typename RowReduce<L, 2>::Lds lds;
+    __shared__ float parts[kGroups > 1 ? 16 * row_threads(L) : 1];
+    RowReduce<L, 2> reduce(&lds);
+    const int lane = threadIdx.x % L, group = threadIdx.x / L;
+    const NormInput<X> x(a);
+    const RowsIn<Z> dz((const Z*)a.dz, a.lddz, a.cols);
+    const Columns& c = dz.c;
+    const RowsIn<float> ws(a.w, 0, a.cols);
+    float dw[C][8], db[C][8], w[C][8];
+    float dw1 = 0.0f, db1 = 0.0f, w1 = 1.0f;   // of the single column
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dw[j][i] = 0.0f, db[j][i] = 0.0f, w[j][i] = 1.0f;
+        if (a.w) ws.load(0, 8 * (lane + L * j)).values(w[j]);
+    }
+    if (a.w) w1 = ws.load_single(0, lane);
+    for (uint32_t r0 = blockIdx.x * kGroups; r0 < a.rows; r0 += gridDim.x * kGroups) {
+        const bool live = r0 + group < a.rows;
+        const int64_t row = live ? r0 + group : a.rows - 1;
+        typename NormInput<X>::Held xr[C];
+        Raw<Z> zr[C];
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+            xr[j] = x.load(row, 8 * (lane + L * j));
+            zr[j] = dz.load(row, 8 * (lane + L * j));
+        }
+        const f32x2 st = *(const f32x2*)(a.stats + 2 * row);
+        const float mean = st[0], r = st[1];
+        float v1 = 0.0f, z1 = 0.0f, s[2] = {0.0f, 0.0f};
+        if (c.any_single()) {
+            v1 = x.load_single(row, lane);
+            z1 = dz.load_single(row, lane);
+            if (live && c.has_single(lane)) {
+                const float xh = (v1 - mean) * r, g = z1 * w1;
+                s[0] = g;
+                s[1] = g * xh;
+                dw1 = __builtin_fmaf(z1, xh, dw1);
+                db1 += z1;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+            if (live && c.has(8 * (lane + L * j))) {
+                float v[8], z[8];
+                xr[j].values(v);
+                zr[j].values(z);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float xh = (v[i] - mean) * r, g = z[i] * w[j][i];
+                    s[0] += g;
+                    s[1] = __builtin_fmaf(g, xh, s[1]);
+                    dw[j][i] = __builtin_fmaf(z[i], xh, dw[j][i]);
+                    db[j][i] += z[i];
+                }
+            }
+            xr[j].hold();
+            zr[j].hold();
+        }
+        reduce.template all<Add>(s);
+        if (!a.dx.base || !live) continue;
+        const float one = s[0] * a.inv_cols, two = s[1] * a.inv_cols;
+        auto grad = [&](float v, float z, float wk) {
+            const float xh = (v - mean) * r;
+            return r * __builtin_fmaf(-xh, two, __builtin_fmaf(z, wk, -one));
+        };
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+            const int k = 8 * (lane + L * j);
+            if (!c.has(k)) continue;
+            float v[8], z[8];
+            xr[j].values(v);
+            zr[j].values(z);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[i] = a.relu && is_zero(xr[j], v, i) ? 0.0f : grad(v[i], z[i], w[j][i]);
+            store8(a.dx, row, k, z);
+        }
+        if (c.has_single(lane))
+            store1(a.dx, row, c.single(lane), a.relu && x.single_is_zero(v1, row, lane) ? 0.0f : grad(v1, z1, w1));
+    }
+    if (!a.parts && !a.dw && !a.db) return;
+    const NormSums out(a);
+    if constexpr (kGroups > 1) {
+        static_assert(C == 1);
+        // the row groups' sums in their order; a lane's two parts by turns
+        auto join = [&](auto N, auto value, auto column) {
+            constexpr int n = CV(N);
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < n; ++i) {
+                parts[group * 16 * L + 2 * (n * lane + i)] = value(i, 0);
+                parts[group * 16 * L + 2 * (n * lane + i) + 1] = value(i, 1);
+            }
+            __syncthreads();
+            for (int t = threadIdx.x; t < 2 * n * L; t += row_threads(L)) {
+                const int k = column(t / 2);
+                if (k < 0) continue;
+                float sum = parts[t];
+#pragma unroll
+                for (int g = 1; g < kGroups; ++g) sum += parts[g * 16 * L + t];
+                out.put(t % 2 ? +out.b : +out.w, k, sum);
+            }
+        };
+        join(std::integral_constant<int, 8>{}, [&](int i, int b) { return b ? +db[0][i] : +dw[0][i]; }, [&](int t) { return t < c.whole ? t : -1; });
+        if (c.any_single())
+            join(std::integral_constant<int, 1>{}, [&](int, int b) { return b ? +db1 : +dw1; }, [&](int t) { return c.has_single(t) ? c.whole + t : -1; });
+    } else {
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+            const int k = 8 * (lane + L * j);
+            if (!c.has(k)) continue;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                out.put(out.w, k + i, dw[j][i]);
+                out.put(out.b, k + i, db[j][i]);
+            }
+        }
+        if (c.has_single(lane)) {
+            out.put(out.w, c.single(lane), dw1);
+            out.put(out.b, c.single(lane), db1);
+        }
+    }
+}
+
+// Rows that registers do not hold: dx, read once for their sums and once for itself.
+template <class X, class Z>
+__global__ void __launch_bounds__(1024) norm_backward_wide_kernel(NormBackwardArgs a) {
+    constexpr int L = 1024;
+    __shared__ typename RowReduce<L, 2>::Lds lds;
+    RowReduce<L, 2> reduce(&lds);
+    const NormInput<X> x(a);
+    const RowsIn<Z> dz((const Z*)a.dz, a.lddz, a.cols);
+    const Columns& c = dz.c;
+    const RowsIn<float> ws(a.w, 0, a.cols);
+    const int lane = threadIdx.x;
+    for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const f32x2 st = *(const f32x2*)(a.stats + 2 * (int64_t)row);
+        const float mean = st[0], r = st[1];
+        float s[2] = {0.0f, 0.0f}, v[8], z[8], w[8] = {1, 1, 1, 1, 1, 1, 1, 1}, v1 = 0.0f, z1 = 0.0f, w1 = 1.0f;
+        if (c.has_single(lane)) {
+            v1 = x.load_single(row, lane);
+            z1 = dz.load_single(row, lane);
+            if (a.w) w1 = ws.load_single(0, lane);
+            s[0] = z1 * w1;
+            s[1] = z1 * w1 * ((v1 - mean) * r);
+        }
+        for (int k = 8 * lane; c.has(k); k += 8 * L) {
+            x.load(row, k).values(v);
+            dz.load(row, k).values(z);
+            if (a.w) ws.load(0, k).values(w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float g = z[i] * w[i];
+                s[0] += g;
+                s[1] = __builtin_fmaf(g, (v[i] - mean) * r, s[1]);
+            }
+        }
+        reduce.template all<Add>(s);
+        const float one = s[0] * a.inv_cols, two = s[1] * a.inv_cols;
+        auto grad = [&](float vk, float zk, float wk) {
+            const float xh = (vk - mean) * r;
+            return r * __builtin_fmaf(-xh, two, __builtin_fmaf(zk, wk, -one));
+        };
+        for (int k = 8 * lane; c.has(k); k += 8 * L) {
+            const auto xr = x.load(row, k);
+            xr.values(v);
+            dz.load(row, k).values(z);
+            if (a.w) ws.load(0, k).values(w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[i] = a.relu && is_zero(xr, v, i) ? 0.0f : grad(v[i], z[i], w[i]);
+            store8(a.dx, row, k, z);
+        }
+        if (c.has_single(lane))
+            store1(a.dx, row, c.single(lane), a.relu && x.single_is_zero(v1, row, lane) ? 0.0f : grad(v1, z1, w1));
+    }
+}
+
+// Their dw and db: 2048 columns (blockIdx.y) over a share of the rows.
+template <class X, class Z>
+__global__ void __launch_bounds__(256) norm_columns_kernel(NormBackwardArgs a) {
+    const NormInput<X> x(a);
+    const RowsIn<Z> dz((const Z*)a.dz, a.lddz, a.cols);
+    const Columns& c = dz.c;
+    const NormSums out(a);
+    const int t = (int)(blockIdx.y * 256 + threadIdx.x), k = 8 * t;
+    if (c.has(k)) {
+        float dw[8], db[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dw[i] = 0.0f, db[i] = 0.0f;
+        for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+            const f32x2 st = *(const f32x2*)(a.stats + 2 * (int64_t)row);
+            float v[8], z[8];
+            x.load(row, k).values(v);
+            dz.load(row, k).values(z);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                dw[i] = __builtin_fmaf(z[i], (v[i] - st[0]) * st[1], dw[i]);
+                db[i] += z[i];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            out.put(out.w, k + i, dw[i]);
+            out.put(out.b, k + i, db[i]);
+        }
+    }
+    if (c.has_single(t)) {
+        float dw = 0.0f, db = 0.0f;
+        for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+            const f32x2 st = *(const f32x2*)(a.stats + 2 * (int64_t)row);
+            const float z = dz.load_single(row, t);
+            dw = __builtin_fmaf(z, (x.load_single(row, t) - st[0]) * st[1], dw);
+            db += z;
+        }
+        out.put(out.w, c.single(t), dw);
+        out.put(out.b, c.single(t), db);
+    }
+}
+
+// Sums of n parts of 2 cols values (dw, then db), 16 columns a workgroup, 64 threads each.
+__global__ void __launch_bounds__(1024) norm_parts_kernel(const float* parts, uint32_t n, int cols, float* dw, float* db,
+                                                          int accumulate) {
+    __shared__ float lds[64][17];
+    const int c = threadIdx.x % 16, slice = threadIdx.x / 16;
+    const int64_t at = (int64_t)blockIdx.x * 16 + c;
+    float sum = 0.0f;
+    if (at < 2 * cols)
+        for (uint32_t p = slice; p < n; p += 64) sum += parts[p * (int64_t)(2 * cols) + at];
+    lds[slice][c] = sum;
+    __syncthreads();
+    if (threadIdx.x >= 16 || at >= 2 * cols) return;
+    sum = lds[0][c];
+    for (int s = 1; s < 64; ++s) sum += lds[s][c];
+    float* const out = at < cols ? dw : db;
+    const int64_t k = at < cols ? at : at - cols;
+    if (out) out[k] = accumulate ? out[k] + sum : sum;
+}
+
+__global__ void __launch_bounds__(256) norm_zero_kernel(float* dw, float* db, int cols) {
+    const int k = blockIdx.x * 256 + threadIdx.x;
+    if (k >= cols) return;
+    if (dw) dw[k] = 0.0f;
+    if (db) db[k] = 0.0f;
+}
+
+// ---------------------------------------------------------------- launches
+
+template <class T, int L, int C>
+hipError_t forward_launch(const NormArgs& a, int n_cu, hipStream_t stream) {
+    constexpr uint32_t groups = row_threads(L) / L;
+    const uint32_t need = (a.rows + groups - 1) / groups, full = (uint32_t)n_cu * (2048 / row_threads(L));
+    const dim3 grid(need < full ? need : full), threads(row_threads(L));
+    if (a.q.codes) hipLaunchKernelGGL((norm_kernel<T, L, C, true>), grid, threads, 0, stream, a);
+    else hipLaunchKernelGGL((norm_kernel<T, L, C, false>), grid, threads, 0, stream, a);
+    return hipGetLastError();
+}
+template <class T>
+hipError_t forward_by_width(const NormArgs& a, int n_cu, hipStream_t s) {
+    const int c = a.cols;
+    return c <= 64 ? forward_launch<T, 8, 1>(a, n_cu, s) : c <= 128 ? forward_launch<T, 16, 1>(a, n_cu, s)
+         : c <= 256 ? forward_launch<T, 32, 1>(a, n_cu, s) : c <= 512 ? forward_launch<T, 64, 1>(a, n_cu, s)
+         : c <= 1024 ? forward_launch<T, 64, 2>(a, n_cu, s) : c <= 2048 ? forward_launch<T, 64, 4>(a, n_cu, s)
+         : c <= 4096 ? forward_launch<T, 256, 2>(a, n_cu, s) : c <= 8192 ? forward_launch<T, 256, 4>(a, n_cu, s)
+         : c <= 16384 ? forward_launch<T, 512, 4>(a, n_cu, s) : c <= 32768 ? forward_launch<T, 1024, 4>(a, n_cu, s)
+         : forward_launch<T, 1024, 8>(a, n_cu, s);
+}
+
+// Lanes of a row in the backward pass, 0 for rows that registers do not hold.
+int backward_lanes(int cols) {
+    int lanes = 8;
+    while (lanes < 1024 && 8 * lanes < cols) lanes *= 2;
+    return cols <= 16 * 1024 ? lanes : 0;
+}
+// Workgroups of the backward pass: each leaves a part of dw and db.
+uint32_t backward_groups(int64_t rows, int cols, int n_cu) {
+    const int lanes = backward_lanes(cols);
+    const int64_t per = lanes ? row_threads(lanes) / lanes : 1;
+    const int64_t need = (rows + per - 1) / per;
+    const int64_t most = lanes ? (int64_t)n_cu * 1024 / row_threads(lanes) : n_cu;
+    if (need <= 4) return need ? 1 : 0;
+    return (uint32_t)(need < most ? need : most);
+}
+
+template <class X, class Z, int L, int C>
+void backward_kernel(const NormBackwardArgs& a, uint32_t wg, hipStream_t s) {
+    hipLaunchKernelGGL((norm_backward_kernel<X, Z, L, C>), dim3(wg), dim3(row_threads(L)), 0, s, a);
+}
+template <class X, class Z>
+hipError_t backward_by_width(NormBackwardArgs a, float* workspace, int n_cu, hipStream_t s) {
+    const uint32_t wg = backward_groups(a.rows, a.cols, n_cu);
+    const bool sums = a.dw || a.db;
+    a.parts = sums && wg > 1 ? workspace : nullptr;
+    switch (backward_lanes(a.cols)) {
+        case 8: backward_kernel<X, Z, 8, 1>(a, wg, s); break;
+        case 16: backward_kernel<X, Z, 16, 1>(a, wg, s); break;
+        case 32: backward_kernel<X, Z, 32, 1>(a, wg, s); break;
+        case 64: backward_kernel<X, Z, 64, 1>(a, wg, s); break;
+        case 128: backward_kernel<X, Z, 128, 1>(a, wg, s); break;
+        case 256: backward_kernel<X, Z, 256, 1>(a, wg, s); break;
+        case 512: backward_kernel<X, Z, 512, 1>(a, wg, s); break;
+        case 1024:
+            if (a.cols <= 8192) backward_kernel<X, Z, 1024, 1>(a, wg, s);
+            else backward_kernel<X, Z, 1024, 2>(a, wg, s);
+            break;
+        default:
+            if (a.dx.base) {
+                const uint32_t full = (uint32_t)n_cu * 2;
+                hipLaunchKernelGGL((norm_backward_wide_kernel<X, Z>), dim3(a.rows < full ? a.rows : full), dim3(1024), 0, s, a);
+            }
+            if (sums)
+                hipLaunchKernelGGL((norm_columns_kernel<X, Z>), dim3(wg, (a.cols + 2047) / 2048), dim3(256), 0, s, a);
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !a.parts) return e;
+    hipLaunchKernelGGL(norm_parts_kernel, dim3((2 * a.cols + 15) / 16), dim3(1024), 0, s, a.parts, wg, a.cols, a.dw, a.db, a.accumulate);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_train_norm(const NormArgs& a, bool x_bf16, int n_cu, hipStream_t stream) {
+    return x_bf16 ? forward_by_width<uint16_t>(a, n_cu, stream) : forward_by_width<float>(a, n_cu, stream);
+}
+
+size_t norm_backward_workspace(int64_t rows, int cols, int n_cu) {
+    const uint32_t wg = backward_groups(rows, cols, n_cu);
+    return wg > 1 ? (size_t)wg * 2 * (size_t)cols * sizeof(float) : 0;
+}
+
+hipError_t launch_train_norm_backward(const NormBackwardArgs& a, int x_type, bool dz_bf16, void* workspace, int n_cu,
+                                      hipStream_t stream) {
+    if (a.rows == 0) {
+        if (a.accumulate || (!a.dw && !a.db)) return hipSuccess;
+        hipLaunchKernelGGL(norm_zero_kernel, dim3((a.cols + 255) / 256), dim3(256), 0, stream, a.dw, a.db, a.cols);
+        return hipGetLastError();
+    }
+    float* const ws = (float*)workspace;
+    if (x_type == kRowsF32)
+        return dz_bf16 ? backward_by_width<float, uint16_t>(a, ws, n_cu, stream) : backward_by_width<float, float>(a, ws, n_cu, stream);
+    if (x_type == kRowsBf16)
+        return dz_bf16 ? backward_by_width<uint16_t, uint16_t>(a, ws, n_cu, stream)
+                       : backward_by_width<uint16_t, float>(a, ws, n_cu, stream);
+    return dz_bf16 ? backward_by_width<uint8_t, uint16_t>(a, ws, n_cu, stream) : backward_by_width<uint8_t, float>(a, ws, n_cu, stream);
+}
+
+}  // namespace donerf

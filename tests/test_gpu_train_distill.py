@@ -1,0 +1,234 @@
+"""The distillation loss and its gradient against the oracle, through the public entry
+points.
+
+With A = |x - max| / T and B = |t - max| / T, an exponential is off by 3u (u = 2^-24) of
+its argument from the difference, the scale and the product, and by a step, 2u, of its
+own; a sum by below 100 roundings (64 values of a lane, 7 single ones, 6 exchanges, 16
+waves).  Results below 2^-126 may become zero.  bf16 gradients are off by half a bf16
+step more."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import training_oracle as O
+from paper_2103_03231_amd import binding as b
+from paper_2103_03231_amd import inputs
+
+pytestmark = pytest.mark.gpu
+U, SUM, LEAST = 2.0 ** -24, 100 * 2.0 ** -24, 2.0 ** -126
+HALF = {torch.float32: 0.0, torch.bfloat16: torch.finfo(torch.bfloat16).eps / 2}
+F32, BF16 = torch.float32, torch.bfloat16
+INF = float("inf")
+
+
+@pytest.fixture(scope="module")
+def r():
+    r = b.Renderer(b.Config(), inputs.make_weights(128, 0))
+    yield r
+    r.close()
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+def inputs_of(seed, rows, cols, k, dtype=F32, kind=torch.int64, pad=0, masked=False, twice=False):
+    """(x, classes, teacher, row_weight): a teacher near the student; masked: classes of -inf, entries that are not given, rows
+    without weight; twice: classes that come more than once."""
+    g = torch.Generator().manual_seed(seed)
+    x = 2 * torch.randn(rows, cols + pad, generator=g)
+    near = x[:, :cols] + torch.randn(rows, cols, generator=g)
+    if twice or k > cols:
+        classes = torch.randint(0, max(1, cols // 2), (rows, k), generator=g)
+        t = near.gather(1, classes) + torch.randn(rows, k, generator=g)
+    else:
+        t, classes = torch.topk(near, k, dim=1)
+    weight = torch.rand(rows, generator=g) + 0.5
+    if masked:
+        off = (torch.rand(rows, cols, generator=g) < 0.3).scatter(1, classes, False)
+        x[:, :cols][off] = -INF
+        lost = torch.arange(k) >= (torch.rand(rows, 1, generator=g) * (k + 1)).floor()
+        classes = torch.where(lost, torch.tensor([-1, cols, -5, 1 << 30])[torch.randint(0, 4, (rows, k), generator=g)], classes)
+        t = torch.where(lost, torch.tensor([float("nan"), INF, -INF, 0.0])[torch.randint(0, 4, (rows, k), generator=g)], t)
+        t = torch.where((torch.rand(rows, k, generator=g) < 0.1) & ~lost, -INF, t)
+        weight = torch.where(torch.rand(rows, generator=g) < 0.2, 0.0, weight)
+    return x.to(dtype).cuda()[:, :cols], classes.to(kind).cuda(), t.cuda(), weight.cuda()
+
+
+def bounds(x, classes, t, temp, weight):
+    """(of the loss, of dx) without a final rounding."""
+    rows, cols = x.shape
+    bl, bd = np.zeros(rows), np.zeros(x.shape)
+    for i in range(rows):
+        given = (classes[i] >= 0) & (classes[i] < cols)
+        c, v = classes[i][given], t[i][given]
+        if weight[i] == 0 or not (v > -np.inf).any() or not (x[i] > -np.inf).any():
+            continue
+        A, B = (x[i].max() - x[i]) / temp, (v.max() - v) / temp
+        q, p = np.exp(-A), np.exp(-B)
+        lq, lp = np.log(q.sum()), np.log(p.sum())
+        q, p = q / q.sum(), p / p.sum()
+        fa, fb = np.where(np.isfinite(A), A, 0.0), np.where(np.isfinite(B), B, 0.0)
+        of_sum_q, of_sum_p = 4 * U * (q * fa).sum() + SUM + 3 * U, 4 * U * (p * fb).sum() + SUM + 3 * U
+        rel_q, rel_p = 4 * U * fa + of_sum_q + 4 * U, 4 * U * fb + of_sum_p + 4 * U
+        term = fa[c] + fb + lq + lp
+        bl[i] = abs(weight[i]) * temp ** 2 * ((p * ((rel_p + SUM + 8 * U) * term + 4 * U * (fa[c] + fb))).sum() + of_sum_q + of_sum_p + 6 * U * (lq + lp))
+        bd[i] = abs(weight[i]) * temp * ((rel_q + 4 * U) * q + LEAST)
+        np.add.at(bd[i], c, abs(weight[i]) * temp * ((rel_p + (len(c) + 4) * U) * p + LEAST))
+    return bl, bd
+
+
+def check(r, x, classes, t, weight, temp, out=BF16):
+    w = np.ones(len(x)) if weight is None else f64(weight)
+    vx, vc, vt = f64(x), classes.cpu().numpy(), f64(t)
+    ref_l, ref_d = O.distill(vx, vc, vt, temp, w)
+    bl, bd = bounds(vx, vc, vt, temp, w)
+    loss, dx = r.train_distill(x, classes, t, temperature=temp, row_weight=weight, out=out)
+    assert dx.dtype is out and loss.dtype is F32
+    assert (np.abs(f64(loss) - ref_l) <= bl + U * np.abs(ref_l)).all(), np.abs(f64(loss) - ref_l).max()
+    assert (np.abs(f64(dx) - ref_d) <= bd + HALF[out] * (np.abs(ref_d) + bd)).all(), np.abs(f64(dx) - ref_d).max()
+    assert (f64(loss)[bl == 0] == 0).all() and (f64(dx)[bl == 0] == 0).all()
+    loss2, dx2 = r.train_distill(x, classes, t, temperature=temp, row_weight=weight, out=out)
+    assert torch.equal(loss, loss2) and torch.equal(dx, dx2)              # the same bits
+    loss3, none = r.train_distill(x, classes, t, temperature=temp, row_weight=weight, need_dx=False)
+    assert none is None and torch.equal(loss, loss3)
+
+
+SIZES = [(1, 1, 1), (2, 2, 2), (5, 7, 3), (1, 8, 8), (40, 9, 4), (33, 31, 1), (70, 64, 16), (300, 100, 4), (1000, 128, 4), (65, 129, 5), (257, 192, 7),
+         (30, 256, 128), (20, 283, 33), (19, 512, 64), (9, 1000, 10), (7, 1024, 100), (5, 2048, 128), (4, 2055, 65), (3, 4096, 64), (2, 5001, 128),
+         (3, 8192, 1), (2, 16384, 128), (2, 16390, 7), (2, 32000, 64), (1, 32768, 128), (2, 40001, 50), (1, 65536, 128), (1, 65535, 3)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,cols,k", SIZES)
+def test_loss_and_gradient(r, rows, cols, k, dtype):
+    x, c, t, w = inputs_of(rows + cols, rows, cols, k, dtype)
+    check(r, x, c, t, None, 1.0, F32)
+    check(r, x, c, t.bfloat16(), w, 2.0)
+    x, c, t, w = inputs_of(rows + cols + 1, rows, cols, k, dtype, torch.int32, pad=3, masked=True)
+    check(r, x, c, t, w, 0.5, F32)
+    x, c, t, w = inputs_of(rows + cols + 2, rows, cols, k, dtype, torch.int32, pad=1, twice=True)
+    check(r, x, c, t, w, 4.0)
+
+
+@pytest.mark.parametrize("rows,cols,k", [(20001, 128, 4), (9000, 64, 16), (3000, 1000, 20), (700, 9000, 40), (600, 33000, 64)])
+def test_many_rows(r, rows, cols, k):
+    """More rows than workgroups, in 64 bits on the GPU."""
+    x, c, t, w = inputs_of(3, rows, cols, k, BF16)
+    loss, dx = r.train_distill(x, c, t, 2.0, w, out=F32)
+    log_q, log_p = torch.log_softmax(x.double() / 2, 1), torch.log_softmax(t.double() / 2, 1)
+    ref = 4 * w.double() * (log_p.exp() * (log_p - log_q.gather(1, c))).sum(1)
+    grad = 2 * w.double()[:, None] * log_q.exp().scatter_add(1, c, -log_p.exp())
+    # arguments are below 20 and logarithms below 15: the bounds above with 4 * 20 + 100 + 8 and (4 * 20 + 200 + 16) * 2 * 35 roundings
+    assert ((loss.double() - ref).abs() <= 4 * w * 21000 * U).all()
+    big = log_q.exp().scatter_add(1, c, log_p.exp())
+    assert ((dx.double() - grad).abs() <= 2 * w[:, None] * (400 * U * big + LEAST)).all()
+
+
+def test_gradient_against_differences(r):
+    x, c, t, w = inputs_of(1, 3, 21, 5)
+    _, dx = r.train_distill(x, c, t, 1.5, w, out=F32)
+    vx, step = f64(x), 1e-5
+    for i in np.ndindex(vx.shape):
+        up, down = vx.copy(), vx.copy()
+        up[i] += step
+        down[i] -= step
+        slope = (O.distill(up, c.cpu().numpy(), f64(t), 1.5, f64(w))[0].sum() - O.distill(down, c.cpu().numpy(), f64(t), 1.5, f64(w))[0].sum()) / (2 * step)
+        assert abs(float(dx[i]) - slope) <= 1e-6       # fp32's parts in 10^7 of values below 3, and the step's square
+
+
+def test_rows_without_anything_to_learn(r):
+    nan = float("nan")
+    for cols in (5, 70, 700, 5000):
+        x, c, t, _ = inputs_of(2, 6, cols, 3)
+        w = torch.ones(6, device="cuda")
+        c[0], t[0] = torch.tensor([-1, cols, 1 << 40]), nan        # no entry given
+        t[1] = -INF                                                # none above -inf
+        x[2] = -INF                                                # no class left
+        w[3], x[3], t[3] = 0.0, nan, nan                           # no weight
+        for out in (F32, BF16):
+            loss, dx = r.train_distill(x, c, t, 2.0, w, out=out)
+            assert (loss[:4] == 0).all() and (dx[:4] == 0).all() and (loss[4:] > 0).all() and (dx[4:] != 0).any(1).all()
+
+
+def test_infinities_and_nan(r):
+    nan = float("nan")
+    for cols in (6, 90, 3000):
+        x, c, t, _ = inputs_of(4, 6, cols, 2)
+        x[0, c[0, 1]] = -INF      # an entry of a class without probability
+        x[1, 0] = nan
+        x[2, cols - 1] = INF
+        t[3, 1] = nan
+        t[4, 0] = INF
+        loss, dx = r.train_distill(x, c, t, out=F32)
+        assert loss[0] == INF and torch.isfinite(dx[0]).all() and dx[0, c[0, 1]] < 0
+        assert torch.isnan(loss[1:5]).all() and torch.isnan(dx[1]).all() and torch.isnan(dx[2]).all()
+        assert torch.isnan(dx[3].gather(0, c[3])).all() and torch.isnan(dx[4].gather(0, c[4])).all()
+        assert torch.isfinite(loss[5]) and torch.isfinite(dx[5]).all()
+
+
+def test_masks_of_the_lowest_value(r):
+    """Logits of the type's lowest value act as -inf beside others, and as any equal values among themselves."""
+    for dtype in (F32, BF16):
+        for temp in (0.25, 1.0, 3.0):
+            x, c, t, _ = inputs_of(6, 4, 50, 3, dtype)
+            off = torch.ones_like(x, dtype=torch.bool).scatter(1, c, False) & (torch.arange(50, device="cuda") % 2 == 0)
+            low = torch.where(off, torch.finfo(dtype).min, x)
+            for u, v in zip(r.train_distill(low, c, t, temp, out=F32), r.train_distill(torch.where(off, -INF, x), c, t, temp, out=F32)):
+                assert torch.equal(u, v)
+            low[:] = torch.finfo(dtype).min
+            for u, v in zip(r.train_distill(low, c, t, temp, out=F32), r.train_distill(torch.zeros_like(x), c, t, temp, out=F32)):
+                assert torch.equal(u, v)
+            t[0] = torch.tensor([1.0, torch.finfo(F32).min, torch.finfo(F32).min])
+            gone = t.clone()
+            gone[0, 1:] = -INF
+            for u, v in zip(r.train_distill(x, c, t, temp, out=F32), r.train_distill(x, c, gone, temp, out=F32)):
+                assert torch.equal(u, v)
+
+
+def test_what_lies_between_the_rows_stays(r):
+    rows, cols, k = 37, 45, 4
+    x, c, t, w = inputs_of(1, rows, cols, k)
+    loss, dx = r.train_distill(x, c, t, 1.0, w, out=F32)
+    for dtype, kind in ((F32, b.TYPE_FP32), (BF16, b.TYPE_BF16)):
+        wide = torch.full((rows, cols + 3), 7.0, dtype=dtype, device="cuda")
+        b.donerf_train_distill(r.h, (x.data_ptr(), cols, b.TYPE_FP32), (c.data_ptr(), k, b.TYPE_INT64), (t.data_ptr(), k, b.TYPE_FP32), w.data_ptr(), 1.0,
+                               None, (wide.data_ptr(), cols + 3, kind), rows, cols, k)
+        assert torch.equal(wide[:, :cols], dx.to(dtype)) and (wide[:, cols:] == 7).all()
+
+
+def test_no_rows(r):
+    loss, dx = r.train_distill(torch.empty(0, 5, device="cuda"), torch.empty(0, 2, dtype=torch.int32, device="cuda"), torch.empty(0, 2, device="cuda"))
+    assert loss.shape == (0,) and dx.shape == (0, 5)
+
+
+def test_a_render_as_teacher(r):
+    """A larger oracle's dumped classes and scores are entries as they are."""
+    out = r.render(inputs.make_poses([0]), 24, 20, 4, debug=True)
+    scores, bins = out["scores"].view(-1, 128), out["bins"].view(-1, 4)
+    x = scores + torch.randn(scores.shape, generator=torch.Generator().manual_seed(1)).cuda()
+    check(r, x, bins, scores.gather(1, bins.long()), None, 2.0, F32)
+
+
+def test_refusals(r):
+    x, c, t, w = inputs_of(1, 6, 20, 3)
+    for call in (lambda: r.train_distill(x.half(), c, t), lambda: r.train_distill(x, c.float(), t), lambda: r.train_distill(x, c, t.double()),
+                 lambda: r.train_distill(x, c[:5], t[:5]), lambda: r.train_distill(x, c, t[:, :2]), lambda: r.train_distill(x, c.cpu(), t),
+                 lambda: r.train_distill(x, c, t, row_weight=w[:5]), lambda: r.train_distill(x, c, t, row_weight=w.double()),
+                 lambda: r.train_distill(x, c[:, 0], t), lambda: r.train_distill(x.t(), c, t), lambda: r.train_distill(x, c, t, out=torch.float16)):
+        with pytest.raises(ValueError):
+            call()
+    for temp in (0.0, -1.0, float("nan"), 1e9):
+        with pytest.raises(b.DonerfError, match="temperature"):
+            r.train_distill(x, c, t, temp)
+    with pytest.raises(b.DonerfError, match="entries"):
+        r.train_distill(x, c.repeat(1, 43), t.repeat(1, 43))
+    with pytest.raises(b.DonerfError, match="dx overlaps"):
+        b.donerf_train_distill(r.h, (x.data_ptr(), 20, b.TYPE_FP32), (c.data_ptr(), 3, b.TYPE_INT64), (t.data_ptr(), 3, b.TYPE_FP32), None, 1.0, None,
+                               (x.data_ptr(), 20, b.TYPE_FP32), 6, 20, 3)
+    with pytest.raises(b.DonerfError, match="loss overlaps"):
+        b.donerf_train_distill(r.h, (x.data_ptr(), 20, b.TYPE_FP32), (c.data_ptr(), 3, b.TYPE_INT64), (t.data_ptr(), 3, b.TYPE_FP32), None, 1.0, t.data_ptr(),
+                               None, 6, 20, 3)
+    with torch.cuda.stream(torch.cuda.Stream()):
+        with pytest.raises(ValueError, match="stream"):
+            r.train_distill(x, c, t)

@@ -1,0 +1,180 @@
+"""Lookup of learned rows and its gradient against the oracle, through the public
+entry points.
+
+A lookup is one product and one rounding: its bits are known.  A gradient's row is a
+sum in fp32 of as many rows as have its id, with one product behind it: off by at most
+(their number + 2) roundings of u = 2^-24 of the terms' summed magnitudes."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import training_oracle as O
+from paper_2103_03231_amd import binding as b
+from paper_2103_03231_amd import inputs
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+@pytest.fixture(scope="module")
+def r():
+    r = b.Renderer(b.Config(), inputs.make_weights(128, 0))
+    yield r
+    r.close()
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+def normal(seed, rows, cols, dtype, pad=0):
+    return torch.randn(rows, cols + pad, generator=torch.Generator().manual_seed(seed)).to(dtype).cuda()[:, :cols]
+
+
+def ids_of(seed, rows, n, spread, dtype=torch.int64, step=1):
+    """Ids on every `step`th place of a buffer."""
+    g = torch.Generator().manual_seed(seed)
+    if spread == "even":
+        v = torch.randint(0, n, (rows,), generator=g)
+    elif spread == "same":
+        v = torch.full((rows,), n // 2)
+    elif spread == "none":
+        v = torch.full((rows,), -1)
+    elif spread == "runs":     # long runs of few ids, in order
+        v = torch.sort(torch.randint(0, max(1, min(n, 5)), (rows,), generator=g)).values
+    else:                      # few rows often, and ids of no row: below, just behind, far behind
+        v = (torch.exp(torch.rand(rows, generator=g).double() * np.log(n + 1)) - 1).long().clamp(max=n - 1)
+        lost = torch.tensor([-1, n, -(1 << 31), (1 << 31) - 1] + ([1 << 40, (1 << 32) + 1, -(1 << 62)] if dtype is torch.int64 else []))
+        v = torch.where(torch.rand(rows, generator=g) < 0.1, lost[torch.randint(0, len(lost), (rows,), generator=g)], v)
+    wide = torch.zeros(rows * step, dtype=dtype)
+    wide[::step] = v.to(dtype)
+    return wide.cuda()[::step]
+
+
+SIZES = [(1, 1, 1), (1, 5, 8), (3, 7, 7), (40, 3, 9), (100, 1, 64), (33, 70, 33), (257, 100, 100), (64, 1000, 130), (500, 40, 257), (1000, 1023, 64),
+         (1000, 1024, 63), (300, 5000, 520), (31, 12, 1031), (4097, 300, 16), (20, 9, 4099), (3, 2, 65536), (9000, 70000, 5), (5000, 37, 256)]
+
+
+@pytest.mark.parametrize("rows,n,cols", SIZES)
+def test_lookup(r, rows, n, cols):
+    for seed, (dtype, out, kind, spread, pad, step) in enumerate([
+            (F32, F32, torch.int64, "tokens", 0, 1), (F32, BF16, torch.int32, "even", 3, 2), (BF16, BF16, torch.int64, "same", 1, 3),
+            (BF16, F32, torch.int32, "tokens", 0, 1)]):
+        table, ids = normal(seed, n, cols, dtype, pad), ids_of(seed, rows, n, spread, kind, step)
+        y = r.train_embedding(table, ids, scale=1.7, out=out)
+        given = (ids >= 0) & (ids < n)
+        ref = torch.where(given[:, None], table[ids.long().clamp(0, n - 1)].float() * torch.tensor(1.7, device="cuda"), 0.0).to(out)
+        assert y.dtype is out and torch.equal(y, ref)
+
+
+def check_gradient(r, dy, ids, n, scale=0.75):
+    got = r.train_embedding_backward(dy, ids, n, scale)
+    ref, mag = O.lookup_grad(f64(dy), ids.cpu().numpy(), n, scale), O.lookup_grad(np.abs(f64(dy)), ids.cpu().numpy(), n, scale)
+    v = ids.cpu().numpy()
+    count = np.bincount(v[(v >= 0) & (v < n)], minlength=n)
+    assert (np.abs(f64(got) - ref) <= ((count + 2) * U)[:, None] * mag).all()
+    assert torch.equal(got, r.train_embedding_backward(dy, ids, n, scale))      # the same bits
+    before = torch.randn(n, dy.shape[1] + 2, generator=torch.Generator().manual_seed(1)).cuda()
+    wide = before.clone()
+    assert r.train_embedding_backward(dy, ids, n, scale, dtable=wide[:, :-2]).data_ptr() == wide.data_ptr()
+    assert torch.equal(wide[:, -2:], before[:, -2:]) and torch.equal(wide[count == 0], before[count == 0])
+    # added in one rounding, to the sum of the same bits
+    assert torch.equal(wide[:, :-2], before[:, :-2] + got)
+
+
+@pytest.mark.parametrize("spread", ["even", "same", "none", "runs", "tokens"])
+@pytest.mark.parametrize("rows,n,cols", SIZES)
+def test_gradient(r, rows, n, cols, spread):
+    check_gradient(r, normal(1, rows, cols, BF16, 3 if rows % 2 else 0), ids_of(2, rows, n, spread, torch.int32), n)
+    check_gradient(r, normal(3, rows, cols, F32, 1 if rows % 2 else 0), ids_of(4, rows, n, spread, torch.int64, 2), n)
+
+
+@pytest.mark.parametrize("rows,n,cols,spread", [(160001, 120, 40, "even"), (50000, 1, 256, "same"), (70000, 32000, 72, "tokens"), (100000, 3, 31, "runs"),
+                                                (300000, 1 << 20, 8, "even"), (140000, (1 << 20) + 5, 4, "tokens")])
+def test_many_rows(r, rows, n, cols, spread):
+    """Several tiles of the sort and parts of the sums, in 64 bits on the GPU."""
+    for dtype in (BF16, F32):
+        dy, ids = normal(1, rows, cols, dtype), ids_of(2, rows, n, spread, torch.int64)
+        got = r.train_embedding_backward(dy, ids, n, 2.0)
+        safe = torch.where((ids >= 0) & (ids < n), ids, n)
+        ref = torch.zeros(n + 1, cols, dtype=torch.float64, device="cuda").index_add_(0, safe, dy.double())[:-1] * 2
+        mag = torch.zeros(n + 1, cols, dtype=torch.float64, device="cuda").index_add_(0, safe, dy.double().abs())[:-1] * 2
+        count = torch.bincount(safe, minlength=n + 1)[:-1, None]
+        assert ((got.double() - ref).abs() <= (count + 2) * U * mag).all()
+        # a run's parts are short: 64 roundings in a row of half a step, each at full size
+        assert torch.linalg.norm(got.double() - ref) <= 64 * U * torch.linalg.norm(mag)
+        assert torch.equal(got, r.train_embedding_backward(dy, ids, n, 2.0))
+
+
+def test_rows_are_summed_in_their_order_whatever_the_ids(r):
+    """Whole numbers, whose sums are exact in any order: every row is counted once."""
+    rows, n = 30011, 517
+    dy = torch.randint(-8, 9, (rows, 24), generator=torch.Generator().manual_seed(3)).float().cuda()
+    for spread in ("even", "runs", "tokens", "same"):
+        ids = ids_of(5, rows, n, spread)
+        safe = torch.where((ids >= 0) & (ids < n), ids, n)
+        ref = torch.zeros(n + 1, 24, device="cuda").index_add_(0, safe, dy)[:-1]
+        assert torch.equal(r.train_embedding_backward(dy, ids, n), ref)
+
+
+def test_rows_without_an_id_may_hold_anything(r):
+    dy = normal(1, 500, 70, F32)
+    ids = ids_of(2, 500, 30, "tokens")
+    lost = (ids < 0) | (ids >= 30)
+    assert lost.any()
+    ref = r.train_embedding_backward(dy, ids, 30)
+    dy[lost] = float("nan")
+    assert torch.equal(r.train_embedding_backward(dy, ids, 30), ref)
+    # NaN of a token stays in its row
+    at = int(ids[~lost][0])
+    dy[torch.nonzero(~lost)[0, 0], 5] = float("nan")
+    got = r.train_embedding_backward(dy, ids, 30)
+    assert torch.isnan(got[at, 5]) and int(torch.isnan(got).sum()) == 1
+    table = normal(3, 30, 70, F32)
+    table[0] = float("inf")      # what a clamped id would read
+    assert (r.train_embedding(table, ids, out=F32)[lost] == 0).all()
+
+
+def test_no_rows(r):
+    ids = torch.empty(0, dtype=torch.int64, device="cuda")
+    assert r.train_embedding(normal(1, 4, 6, F32), ids).shape == (0, 6)
+    assert torch.equal(r.train_embedding_backward(torch.empty(0, 6, device="cuda"), ids, 4), torch.zeros(4, 6, device="cuda"))
+    keep = torch.ones(4, 6, device="cuda")
+    assert (r.train_embedding_backward(torch.empty(0, 6, device="cuda"), ids, 4, dtable=keep) == 1).all()
+
+
+def test_what_lies_between_the_rows_stays(r):
+    rows, n, cols = 90, 20, 21
+    table, ids, dy = normal(1, n, cols, F32), ids_of(2, rows, n, "even", torch.int32), normal(3, rows, cols, F32)
+    for dtype, kind in ((F32, b.TYPE_FP32), (BF16, b.TYPE_BF16)):
+        wide = torch.full((rows, cols + 3), 7.0, dtype=dtype, device="cuda")
+        b.donerf_train_embedding(r.h, (table.data_ptr(), cols, b.TYPE_FP32), (ids.data_ptr(), 1, b.TYPE_INT32), 1.0, (wide.data_ptr(), cols + 3, kind),
+                                 rows, n, cols)
+        assert torch.equal(wide[:, :cols], r.train_embedding(table, ids, out=dtype)) and (wide[:, cols:] == 7).all()
+    need = b.donerf_train_embedding_backward_workspace(r.h, rows, n, cols)
+    ws = torch.full((need + 64,), 5, dtype=torch.uint8, device="cuda")
+    wide = torch.full((n, cols + 3), 7.0, device="cuda")
+    b.donerf_train_embedding_backward(r.h, (dy.data_ptr(), cols, b.TYPE_FP32), (ids.data_ptr(), 1, b.TYPE_INT32), 1.0, (wide.data_ptr(), cols + 3, b.TYPE_FP32),
+                                      0, rows, n, cols, ws.data_ptr(), need)
+    assert torch.equal(wide[:, :cols], r.train_embedding_backward(dy, ids, n)) and (wide[:, cols:] == 7).all() and (ws[need:] == 5).all()
+
+
+def test_refusals(r):
+    table, ids, dy = normal(1, 5, 8, F32), ids_of(1, 6, 5, "even"), normal(2, 6, 8, F32)
+    for call in (lambda: r.train_embedding(table.half(), ids), lambda: r.train_embedding(table, ids.float()), lambda: r.train_embedding(table, ids.cpu()),
+                 lambda: r.train_embedding(table, ids[None]), lambda: r.train_embedding(table, ids[:1].expand(6)), lambda: r.train_embedding(table.t(), ids),
+                 lambda: r.train_embedding(table, ids, out=torch.float16), lambda: r.train_embedding_backward(dy, ids[:5], 5),
+                 lambda: r.train_embedding_backward(dy, ids, 0), lambda: r.train_embedding_backward(dy, ids, 1 << 31),
+                 lambda: r.train_embedding_backward(dy, ids, 5, dtable=table.bfloat16()), lambda: r.train_embedding_backward(dy, ids, 6, dtable=table)):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(b.DonerfError, match="dtable overlaps"):
+        r.train_embedding_backward(dy, ids, 5, dtable=dy[:5])
+    with pytest.raises(b.DonerfError, match="y overlaps"):
+        b.donerf_train_embedding(r.h, (table.data_ptr(), 8, b.TYPE_FP32), (ids.data_ptr(), 1, b.TYPE_INT64), 1.0, (ids.data_ptr(), 8, b.TYPE_FP32), 6, 5, 8)
+    with pytest.raises(b.DonerfError, match="table rows"):
+        b.donerf_train_embedding(r.h, (table.data_ptr(), 8, b.TYPE_FP32), (ids.data_ptr(), 1, b.TYPE_INT64), 1.0, (dy.data_ptr(), 8, b.TYPE_FP32), 6, 0, 8)
+    with torch.cuda.stream(torch.cuda.Stream()):
+        with pytest.raises(ValueError, match="stream"):
+            r.train_embedding(table, ids)

@@ -305,6 +305,13 @@ struct EmbeddingArgs {
 };
 hipError_t launch_train_embedding(const EmbeddingArgs& a, bool table_bf16, int n_cu, hipStream_t stream);
 
+// Rows [begin, end) of a table of zeros.
+struct ZeroFill {
+    float* table;
+    int64_t ld;
+    int32_t cols;
+    int64_t begin, end;
+};
 // One pass of the sort of rows by their ids.
 constexpr int kSortBits = 10;   // most bits of a pass
 struct SortPass {
@@ -313,11 +320,12 @@ struct SortPass {
     const uint32_t* rows_in; // null in the first pass
     uint32_t* keys_out;
     uint32_t* rows_out;
-    uint32_t* counts;        // bins x tiles
+    uint32_t* counts;        // tiles x bins
     uint32_t* totals;        // bins
-    uint32_t rows, tile;     // keys, and those of a workgroup
+    uint32_t rows, tile, tiles;   // keys, those of a workgroup, workgroups
     int64_t n;
     int32_t shift, bits;
+    int32_t scanned;         // counts are those of the tiles before, totals theirs
 };
 struct EmbeddingGradArgs {
     const void* dy;          // rows x cols, fp32 or bf16
@@ -328,12 +336,13 @@ struct EmbeddingGradArgs {
     int32_t accumulate;
     int64_t rows, n;
     int32_t cols;
-    const uint32_t* keys;    // set by the launch: sorted ids, and their rows
+    const uint32_t* keys;    // set by the launch, as the rest: sorted ids, and their rows
     const uint32_t* order;
     float* ends;             // sums of runs that cross the parts' ends
     uint32_t part;           // sorted rows of a part
+    uint32_t slabs;          // workgroups that sum, where one launch does all
 };
-size_t embedding_backward_workspace(int64_t rows, int64_t n, int cols);
+size_t embedding_backward_workspace(int64_t rows, int64_t n, int cols, int n_cu);
 hipError_t launch_train_embedding_backward(EmbeddingGradArgs a, const IntRows& ids, bool dy_bf16, void* workspace, int n_cu,
                                            hipStream_t stream);
 

@@ -35,138 +35,304 @@ __global__ void __launch_bounds__(256) embedding_kernel(EmbeddingArgs a) {
     }
 }
 
+// ---------------------------------------------------------------- zeros
+
+constexpr int kThreads = 1024;        // of the gradient's workgroups
+constexpr int kWaves = kThreads / 64;
+
+// Zeros into rows [begin, end), but for those whose flag is set (by row - begin).
+__device__ __forceinline__ void fill_rows(const ZeroFill& z, int64_t begin, int64_t end, const uint32_t* flags) {
+    // 4 columns a lane; a row's lanes a power of two, up to a wave
+    int bits = 0;
+    while (bits < 6 && 4 << bits < z.cols) ++bits;
+    const int lane = threadIdx.x & ((1 << bits) - 1), per = kThreads >> bits;
+    const int quads = z.cols & ~3;
+    const float zero[4] = {0, 0, 0, 0};
+    for (int64_t row = begin + (threadIdx.x >> bits); row < end; row += per) {
+        const uint32_t f = (uint32_t)(row - begin);
+        if (flags && flags[f / 32] >> f % 32 & 1) continue;
+        float* const to = z.table + row * z.ld;
+        for (int k = 4 * lane; k < quads; k += 4 << bits) __builtin_memcpy(to + k, zero, 16);
+        for (int k = quads + lane; k < z.cols; k += 1 << bits) to[k] = 0.0f;
+    }
+}
+// The share of workgroup `at` of `all` in the rows of a fill.
+__device__ __forceinline__ void fill_share(const ZeroFill& z, uint32_t at, uint32_t all) {
+    const int64_t n = z.end - z.begin;
+    fill_rows(z, z.begin + n * at / all, z.begin + n * (at + 1) / all, nullptr);
+}
+
 // ---------------------------------------------------------------- sort
 
-constexpr int kSortThreads = 256;
-constexpr int kSortWaves = kSortThreads / 64;
-constexpr int kSortItems = 16;                            // of a thread in one step of its tile
-constexpr int kSortStep = kSortThreads * kSortItems;
 constexpr int kMostBins = 1 << kSortBits;
 
-// The key that a pass reads: the first one makes it of the ids, n for those without a row.
+// The key of an id: n for those without a row.
+__device__ __forceinline__ uint32_t key_of(int64_t id, int64_t n) { return id >= 0 && id < n ? (uint32_t)id : (uint32_t)n; }
+// The key that a pass reads.
 __device__ __forceinline__ uint32_t sort_key(const SortPass& s, uint32_t i) {
-    if (s.keys_in) return s.keys_in[i];
-    const int64_t id = s.ids.at(i, 0);
-    return id >= 0 && id < s.n ? (uint32_t)id : (uint32_t)s.n;
+    return s.keys_in ? s.keys_in[i] : key_of(s.ids.at(i, 0), s.n);
 }
 
-// counts[bin][tile]: the keys of each tile by their digit.
-__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(SortPass s) {
+// One more in each live lane's bin.  Lanes that agree, as sorted or repeated ids
+// do, add once: the same address is served lane by lane.
+__device__ __forceinline__ void count_bin(uint32_t* bins, uint32_t bin, bool live) {
+    const uint64_t all = __ballot(live);
+    if (all == 0) return;
+    const int leader = __ffsll((unsigned long long)all) - 1;
+    const uint32_t first = __builtin_amdgcn_readlane(bin, leader);
+    if (__ballot(live && bin == first) == all) {
+        if ((threadIdx.x & 63) == leader) atomicAdd(&bins[first], (uint32_t)__popcll(all));
+    } else if (live) {
+        atomicAdd(&bins[bin], 1u);
+    }
+}
+
+// counts[tile][bin]: the keys of each tile by their digit.
+__global__ void __launch_bounds__(kThreads) sort_count_kernel(SortPass s, ZeroFill z) {
     __shared__ uint32_t bins[kMostBins];
+    if (blockIdx.x >= s.tiles) return fill_share(z, blockIdx.x - s.tiles, gridDim.x - s.tiles);
     const uint32_t n_bins = 1u << s.bits;
-    for (uint32_t b = threadIdx.x; b < n_bins; b += kSortThreads) bins[b] = 0;
+    for (uint32_t b = threadIdx.x; b < n_bins; b += kThreads) bins[b] = 0;
     __syncthreads();
     const uint32_t first = blockIdx.x * s.tile, end = s.rows - first < s.tile ? s.rows : first + s.tile;
-    for (uint32_t i = first + threadIdx.x; i < end; i += kSortThreads)
-        atomicAdd(&bins[sort_key(s, i) >> s.shift & (n_bins - 1)], 1u);
+    for (uint32_t i0 = first; i0 < end; i0 += kThreads) {
+        const uint32_t i = i0 + threadIdx.x;
+        const bool live = i < end;
+        count_bin(bins, (live ? sort_key(s, i) : 0) >> s.shift & (n_bins - 1), live);
+    }
     __syncthreads();
-    for (uint32_t b = threadIdx.x; b < n_bins; b += kSortThreads) s.counts[(size_t)b * gridDim.x + blockIdx.x] = bins[b];
+    for (uint32_t b = threadIdx.x; b < n_bins; b += kThreads) s.counts[((size_t)blockIdx.x << s.bits) + b] = bins[b];
 }
 
-// The sum of v over a workgroup's threads before this one, and all of them.
-template <int THREADS>
-__device__ __forceinline__ uint32_t scan_before(uint32_t v, uint32_t* lds, uint32_t& total) {
+// 64 bins a workgroup: counts become the keys of the bin in the tiles before, a wave a
+// share of the tiles.
+__global__ void __launch_bounds__(kThreads) sort_scan_kernel(SortPass s) {
+    __shared__ uint32_t sums[kWaves][64];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    uint32_t x = v;
+    const uint32_t bin = blockIdx.x * 64 + lane, per = (s.tiles + kWaves - 1) / kWaves;
+    const uint32_t t0 = wave * per, t1 = t0 + per < s.tiles ? t0 + per : s.tiles;
+    const bool live = bin < 1u << s.bits;
+    uint32_t sum = 0;
+    if (live)
+        for (uint32_t t = t0; t < t1; ++t) sum += s.counts[((size_t)t << s.bits) + bin];
+    sums[wave][lane] = sum;
+    __syncthreads();
+    uint32_t run = 0, total = 0;
+    for (int w = 0; w < kWaves; ++w) {
+        if (w < wave) run += sums[w][lane];
+        total += sums[w][lane];
+    }
+    if (!live) return;
+    for (uint32_t t = t0; t < t1; ++t) {
+        uint32_t* const at = s.counts + ((size_t)t << s.bits) + bin;
+        const uint32_t v = *at;
+        *at = run;
+        run += v;
+    }
+    if (wave == 0) s.totals[bin] = total;
+}
+
+// LDS of a workgroup that puts keys in order.
+struct SortLds {
+    uint32_t at[kMostBins];               // where the next key of each bin goes
+    uint32_t before[kMostBins];
+    uint16_t waves[kWaves][kMostBins];    // keys of each wave, then of the waves before
+    uint32_t sums[kWaves];
+};
+
+// at[b] becomes the sum of totals before bin b, and before[b].
+template <class Lds>
+__device__ __forceinline__ void bin_starts(Lds& l, uint32_t total, uint32_t before, uint32_t n_bins) {
+    // a thread a bin: kMostBins of them at most
+    static_assert(kMostBins <= kThreads);
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    uint32_t x = total;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
         const uint32_t o = __shfl_up(x, d, 64);
         if (lane >= d) x += o;
     }
-    if (lane == 63) lds[wave] = x;
+    if (lane == 63) l.sums[wave] = x;
     __syncthreads();
-    uint32_t before = 0;
-    total = 0;
+    uint32_t run = 0;
 #pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) {
-        if (w < wave) before += lds[w];
-        total += lds[w];
-    }
+    for (int w = 0; w < kWaves; ++w)
+        if (w < wave) run += l.sums[w];
+    if (threadIdx.x < n_bins) l.at[threadIdx.x] = run + x - total + before;
     __syncthreads();
-    return before + x - v;
 }
 
-// A workgroup per bin: counts become the keys of the bin in the tiles before.
-__global__ void __launch_bounds__(kSortThreads) sort_scan_kernel(SortPass s, uint32_t tiles) {
-    __shared__ uint32_t lds[kSortWaves];
-    uint32_t* const row = s.counts + (size_t)blockIdx.x * tiles;
-    uint32_t sum = 0;
-    for (uint32_t t0 = 0; t0 < tiles; t0 += kSortThreads) {
-        const uint32_t t = t0 + threadIdx.x;
-        const uint32_t v = t < tiles ? row[t] : 0;
-        uint32_t total;
-        const uint32_t before = scan_before<kSortThreads>(v, lds, total);
-        if (t < tiles) row[t] = sum + before;
-        sum += total;
+// Where a workgroup's next kThreads keys go, one a thread (those of live threads);
+// at[] moves on.  Keys of one bin keep their order.
+__device__ __forceinline__ uint32_t place_keys(SortLds& l, uint32_t bin, bool live, int bits) {
+    const uint32_t n_bins = 1u << bits;
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    for (uint32_t b = threadIdx.x; b < kWaves << bits; b += kThreads) l.waves[b >> bits][b & (n_bins - 1)] = 0;
+    __syncthreads();
+    uint64_t same = __ballot(live);   // the live lanes with this lane's bin
+    for (int b = 0; b < bits; ++b) {
+        const uint64_t ones = __ballot(bin >> b & 1);
+        same &= bin >> b & 1 ? ones : ~ones;
     }
-    if (threadIdx.x == 0) s.totals[blockIdx.x] = sum;
+    const uint32_t rank = (uint32_t)__popcll(same & ((1ull << lane) - 1));
+    if (live && rank == 0) l.waves[wave][bin] = (uint16_t)__popcll(same);
+    __syncthreads();
+    if (threadIdx.x < n_bins) {
+        uint32_t run = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const uint32_t v = l.waves[w][threadIdx.x];
+            l.waves[w][threadIdx.x] = (uint16_t)run;
+            run += v;
+        }
+        l.before[threadIdx.x] = run;
+    }
+    __syncthreads();
+    const uint32_t to = live ? l.at[bin] + l.waves[wave][bin] + rank : 0;
+    __syncthreads();
+    if (threadIdx.x < n_bins) l.at[threadIdx.x] += l.before[threadIdx.x];
+    return to;   // at[] is read behind the next call's barriers
 }
 
 // Moves a tile's keys and rows to their places.
-__global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(SortPass s) {
-    __shared__ uint32_t at[kMostBins];                  // where the tile's next key of each bin goes
-    __shared__ uint32_t waves[kSortWaves][kMostBins];   // keys of each wave, then of the waves before
-    __shared__ uint32_t lds[kSortWaves];
+__global__ void __launch_bounds__(kThreads) sort_scatter_kernel(SortPass s, ZeroFill z) {
+    __shared__ SortLds l;
+    if (blockIdx.x >= s.tiles) return fill_share(z, blockIdx.x - s.tiles, gridDim.x - s.tiles);
+    const uint32_t n_bins = 1u << s.bits, bin = threadIdx.x;
+    const uint32_t first = blockIdx.x * s.tile, end = s.rows - first < s.tile ? s.rows : first + s.tile;
+    // the first step's, on their way early
+    const uint32_t i1 = first + threadIdx.x < end ? first + threadIdx.x : end - 1;
+    uint32_t key = sort_key(s, i1), row = s.rows_in ? s.rows_in[i1] : i1;
+    uint32_t total = 0, before = 0;   // keys of this thread's bin: all, and those of the tiles before
+    if (s.scanned) {
+        if (bin < n_bins) total = s.totals[bin], before = s.counts[((size_t)blockIdx.x << s.bits) + bin];
+    } else {
+        for (uint32_t b = threadIdx.x; b < n_bins; b += kThreads) l.at[b] = l.before[b] = 0;
+        __syncthreads();
+        const uint32_t per = kThreads >> s.bits, b = threadIdx.x & (n_bins - 1);   // tiles at a time
+        constexpr int kTogether = 16;
+        for (uint32_t t0 = threadIdx.x >> s.bits; t0 < s.tiles; t0 += kTogether * per) {
+            uint32_t v[kTogether];
+#pragma unroll
+            for (int j = 0; j < kTogether; ++j) {
+                const uint32_t t = t0 + j * per < s.tiles ? t0 + j * per : 0;
+                v[j] = s.counts[((size_t)t << s.bits) + b];
+            }
+#pragma unroll
+            for (int j = 0; j < kTogether; ++j) {
+                const uint32_t t = t0 + j * per;
+                total += t < s.tiles ? v[j] : 0;
+                before += t < blockIdx.x ? v[j] : 0;
+            }
+        }
+        atomicAdd(&l.at[b], total);
+        atomicAdd(&l.before[b], before);
+        __syncthreads();
+        if (bin < n_bins) {
+            before = l.before[bin];
+            total = l.at[bin];
+        }
+        __syncthreads();
+    }
+    bin_starts(l, total, before, n_bins);
+    for (uint32_t i0 = first; i0 < end; i0 += kThreads) {
+        const uint32_t i = i0 + threadIdx.x;
+        const bool live = i < end;
+        if (i0 > first && live) {
+            key = sort_key(s, i);
+            row = s.rows_in ? s.rows_in[i] : i;
+        }
+        const uint32_t to = place_keys(l, key >> s.shift & (n_bins - 1), live, s.bits);
+        if (live) {
+            s.keys_out[to] = key;
+            s.rows_out[to] = row;
+        }
+    }
+}
+
+// All passes of up to ITEMS keys a thread, by one workgroup in LDS; the others write
+// zeros meanwhile.  Waves take consecutive keys and count their own.
+template <int ITEMS>
+struct SortAllLds {
+    uint32_t at[kMostBins];
+    uint16_t waves[kWaves][kMostBins];   // keys of each wave, then of the waves before
+    uint32_t sums[kWaves];
+    uint32_t keys[ITEMS * kThreads];
+    uint16_t rows[ITEMS * kThreads];
+};
+template <int ITEMS>
+__global__ void __launch_bounds__(kThreads) sort_all_kernel(SortPass s, ZeroFill z, int passes) {
+    static_assert(ITEMS * kThreads <= 65536);
+    __shared__ SortAllLds<ITEMS> l;
+    if (blockIdx.x > 0) return fill_share(z, blockIdx.x - 1, gridDim.x - 1);
     const uint32_t n_bins = 1u << s.bits;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    uint32_t sum = 0;
-    for (uint32_t b0 = 0; b0 < n_bins; b0 += kSortThreads) {
-        const uint32_t b = b0 + threadIdx.x;
-        const uint32_t v = b < n_bins ? s.totals[b] : 0;
-        uint32_t total;
-        const uint32_t before = scan_before<kSortThreads>(v, lds, total);
-        if (b < n_bins) at[b] = sum + before + s.counts[(size_t)b * gridDim.x + blockIdx.x];
-        sum += total;
+    const uint32_t at0 = wave * ITEMS * 64 + lane;   // the first of this lane's places, 64 apart
+    uint32_t key[ITEMS], row[ITEMS], rank[ITEMS];
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j) {
+        row[j] = at0 + 64 * j;
+        key[j] = sort_key(s, row[j] < s.rows ? row[j] : s.rows - 1);
     }
-    const uint32_t first = blockIdx.x * s.tile, end = s.rows - first < s.tile ? s.rows : first + s.tile;
-    // steps of kSortStep keys: a wave takes consecutive ones, 64 at a time
-    for (uint32_t step = first; step < end; step += kSortStep) {
-        for (uint32_t b = threadIdx.x; b < kSortWaves * n_bins; b += kSortThreads) waves[b / n_bins][b % n_bins] = 0;
+#pragma unroll 1
+    for (int p = 0; p < passes; ++p) {
+        const int shift = p * s.bits;
+        for (uint32_t b = threadIdx.x; b < kWaves << s.bits; b += kThreads) l.waves[b >> s.bits][b & (n_bins - 1)] = 0;
         __syncthreads();
-        uint32_t key[kSortItems], rank[kSortItems];
+        // (conditions on places are asked anew at every step: held ones fill the registers)
+        auto steps = [&](auto f) {
+            uint32_t at = at0;
+            asm volatile("" : "+v"(at));
 #pragma unroll
-        for (int j = 0; j < kSortItems; ++j) {
-            const uint32_t i = step + (wave * kSortItems + j) * 64 + lane;
-            key[j] = i < end ? sort_key(s, i) : 0;
-        }
-#pragma unroll
-        for (int j = 0; j < kSortItems; ++j) {
-            const bool live = step + (wave * kSortItems + j) * 64 + lane < end;
-            const uint32_t bin = key[j] >> s.shift & (n_bins - 1);
-            uint64_t same = __ballot(live);   // the live lanes with this lane's digit
+            for (int j = 0; j < ITEMS; ++j) {
+                f(j, at);
+                at += 64;
+                asm volatile("" : "+v"(at));
+            }
+        };
+        steps([&](int j, uint32_t at) {
+            const uint32_t bin = key[j] >> shift & (n_bins - 1);
+            const bool live = at < s.rows;
+            uint64_t same = __ballot(live);   // the live lanes with this lane's bin
+#pragma unroll 1
             for (int b = 0; b < s.bits; ++b) {
                 const uint64_t ones = __ballot(bin >> b & 1);
                 same &= bin >> b & 1 ? ones : ~ones;
             }
             const uint32_t before = (uint32_t)__popcll(same & ((1ull << lane) - 1));
-            const uint32_t seen = live ? waves[wave][bin] : 0;
+            const uint32_t seen = l.waves[wave][bin];
             wave_lds_fence();
-            if (live && before == 0) waves[wave][bin] = seen + (uint32_t)__popcll(same);
+            if (live && before == 0) l.waves[wave][bin] = (uint16_t)(seen + __popcll(same));
             wave_lds_fence();
             rank[j] = seen + before;
-        }
+        });
         __syncthreads();
-        for (uint32_t b = threadIdx.x; b < n_bins; b += kSortThreads) {
-            uint32_t run = at[b];
+        uint32_t total = 0;
+        if (threadIdx.x < n_bins)
 #pragma unroll
-            for (int w = 0; w < kSortWaves; ++w) {
-                const uint32_t v = waves[w][b];
-                waves[w][b] = run;
-                run += v;
+            for (int w = 0; w < kWaves; ++w) {
+                const uint32_t v = l.waves[w][threadIdx.x];
+                l.waves[w][threadIdx.x] = (uint16_t)total;
+                total += v;
             }
-            at[b] = run;
-        }
+        bin_starts(l, total, 0, n_bins);
+        steps([&](int j, uint32_t at) {
+            if (at >= s.rows) return;
+            const uint32_t bin = key[j] >> shift & (n_bins - 1), to = l.at[bin] + l.waves[wave][bin] + rank[j];
+            l.keys[to] = key[j];
+            l.rows[to] = (uint16_t)row[j];
+        });
         __syncthreads();
+        steps([&](int j, uint32_t at) {
+            key[j] = l.keys[at];   // what lies behind the last one is not used
+            row[j] = l.rows[at];
+        });
+    }
 #pragma unroll
-        for (int j = 0; j < kSortItems; ++j) {
-            const uint32_t i = step + (wave * kSortItems + j) * 64 + lane;
-            if (i < end) {
-                const uint32_t to = waves[wave][key[j] >> s.shift & (n_bins - 1)] + rank[j];
-                s.keys_out[to] = key[j];
-                s.rows_out[to] = s.rows_in ? s.rows_in[i] : i;
-            }
-        }
-        __syncthreads();
+    for (int j = 0; j < ITEMS; ++j) {
+        if (at0 + 64 * j >= s.rows) continue;
+        s.keys_out[at0 + 64 * j] = key[j];
+        s.rows_out[at0 + 64 * j] = row[j];
     }
 }
 
@@ -175,36 +341,28 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(SortPass s) 
 // Rows of a part are read this many at a time.
 constexpr int kAhead = 8;
 
-// Parts of `part` sorted rows; a run of one id that lies within one is the result, one
-// that comes from the part before leaves its sum in ends[2 p], one that goes on into
-// the next part in ends[2 p + 1].
-template <class T, int L>
-__global__ void __launch_bounds__(256) embedding_sum_kernel(EmbeddingGradArgs a) {
-    const int lane = threadIdx.x % L;
-    const int64_t p = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
-    const int k = 8 * (int)(blockIdx.y * L + lane);
-    const RowsIn<T> dy((const T*)a.dy, a.lddy, a.cols);
+// Sums sorted rows [first, end) of dy at this lane's 8 columns from k on (c.has(k)) and its
+// single column (if `single`).  Each run of one id that lies within them is left as the
+// result; one that comes from before, or goes on, is put by end(0, ...) or end(1, ...).
+template <class T, class Keys, class End>
+__device__ __forceinline__ void sum_runs(const EmbeddingGradArgs& a, const RowsIn<T>& dy, const Keys& keys, const Keys& order, uint32_t first,
+                                         uint32_t end, int k, int lane, bool single, End put_end) {
     const Columns& c = dy.c;
-    const bool single = blockIdx.y == 0 && c.has_single(lane);
-    if (p * a.part >= a.rows || !(c.has(k) || single)) return;
-    const uint32_t first = (uint32_t)(p * a.part), end = a.rows - first < a.part ? a.rows : first + a.part;
-    uint32_t cur = a.keys[first];
-    bool from_before = first > 0 && a.keys[first - 1] == cur;
+    uint32_t cur = keys[first];
+    bool from_before = first > 0 && keys[first - 1] == cur;
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0}, sum1 = 0.0f;
     auto leave = [&](bool goes_on) {
         if (cur >= a.n) return;   // rows without an id
-        const bool part = from_before || goes_on;
-        float* const to = part ? a.ends + (2 * p + (from_before ? 0 : 1)) * a.cols : a.dtable + cur * a.lddt;
-        const float scale = part ? 1.0f : a.scale;
-        const bool add = !part && a.accumulate;
+        if (from_before || goes_on) return put_end(from_before ? 0 : 1, sum, sum1);
+        float* const to = a.dtable + cur * a.lddt;
         if (c.has(k)) {
             float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-            if (add) __builtin_memcpy(v, to + k, 32);
+            if (a.accumulate) __builtin_memcpy(v, to + k, 32);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += sum[i] * scale;
+            for (int i = 0; i < 8; ++i) v[i] += sum[i] * a.scale;
             __builtin_memcpy(to + k, v, 32);
         }
-        if (single) to[c.single(lane)] = (add ? to[c.single(lane)] : 0.0f) + sum1 * scale;
+        if (single) to[c.single(lane)] = (a.accumulate ? to[c.single(lane)] : 0.0f) + sum1 * a.scale;
     };
     for (uint32_t i0 = first; i0 < end; i0 += kAhead) {
         uint32_t key[kAhead], row[kAhead];
@@ -213,8 +371,8 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(EmbeddingGradArgs a)
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
             const uint32_t i = i0 + j < end ? i0 + j : end - 1;
-            key[j] = a.keys[i];
-            row[j] = a.order[i];
+            key[j] = keys[i];
+            row[j] = order[i];
         }
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
@@ -239,47 +397,201 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(EmbeddingGradArgs a)
             sum1 += one[j];
         }
     }
-    leave(end < a.rows && a.keys[end] == cur);
+    leave(end < a.rows && keys[end] == cur);
 }
 
-// Joins a run that begins in part blockIdx.x and goes on: 64 columns a workgroup, 16
-// threads each.
-__global__ void __launch_bounds__(1024) embedding_join_kernel(EmbeddingGradArgs a) {
-    __shared__ float lds[16][64];
-    const int64_t p = blockIdx.x, first = p * a.part, end = first + a.part;
-    if (end >= a.rows) return;
-    const uint32_t cur = a.keys[end - 1];
-    if (cur >= a.n || a.keys[end] != cur) return;                                  // none goes on
-    if (first > 0 && a.keys[first] == cur && a.keys[first - 1] == cur) return;     // it began before
-    const int group = threadIdx.x / 64, k = (int)(blockIdx.y * 64 + threadIdx.x % 64);
-    float sum = 0.0f;
-    if (k < a.cols) {
-        if (group == 0) sum = a.ends[(2 * p + 1) * a.cols + k];
-        for (int64_t q = p + 1 + group; q * a.part < a.rows && a.keys[q * a.part] == cur; q += 16) sum += a.ends[2 * q * a.cols + k];
-    }
-    lds[group][threadIdx.x % 64] = sum;
-    __syncthreads();
-    if (group > 0 || k >= a.cols) return;
-#pragma unroll
-    for (int g = 1; g < 16; ++g) sum += lds[g][threadIdx.x];
-    float* const to = a.dtable + cur * a.lddt + k;
-    *to = (a.accumulate ? *to : 0.0f) + sum * a.scale;
-}
-
-template <int L>
-__global__ void __launch_bounds__(256) embedding_zero_kernel(EmbeddingGradArgs a) {
-    constexpr int kGroups = 256 / L;
+// Parts of `part` sorted rows, 8 L columns a workgroup: what comes from the part before is
+// left in ends[2 p], what goes on into the next one in ends[2 p + 1].
+template <class T, int L>
+__global__ void __launch_bounds__(256) embedding_sum_kernel(EmbeddingGradArgs a) {
     const int lane = threadIdx.x % L;
-    const Columns c(a.cols);
-    const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    for (int64_t row = (int64_t)blockIdx.x * kGroups + threadIdx.x / L; row < a.n; row += (int64_t)gridDim.x * kGroups) {
-        float* const to = a.dtable + row * a.lddt;
-        for (int k = 8 * lane; c.has(k); k += 8 * L) __builtin_memcpy(to + k, zero, 32);
-        if (c.has_single(lane)) to[c.single(lane)] = 0.0f;
+    const int64_t p = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
+    const int k = 8 * (int)(blockIdx.y * L + lane);
+    const RowsIn<T> dy((const T*)a.dy, a.lddy, a.cols);
+    const Columns& c = dy.c;
+    const bool single = blockIdx.y == 0 && c.has_single(lane);
+    if (p * a.part >= a.rows || !(c.has(k) || single)) return;
+    const uint32_t first = (uint32_t)(p * a.part), end = (uint32_t)a.rows - first < a.part ? (uint32_t)a.rows : first + a.part;
+    sum_runs(a, dy, a.keys, a.order, first, end, k, lane, single, [&](int which, const float* sum, float sum1) {
+        float* const to = a.ends + (2 * p + which) * a.cols;
+        if (c.has(k)) __builtin_memcpy(to + k, sum, 32);
+        if (single) to[c.single(lane)] = sum1;
+    });
+}
+
+// Joins the runs that begin in 16 parts, a wave each, and go on: 256 columns a workgroup.
+// Runs of more than kLongRun parts are summed by all waves together.
+constexpr int kLongRun = 8;
+__global__ void __launch_bounds__(kThreads) embedding_join_kernel(EmbeddingGradArgs a) {
+    __shared__ int64_t long_first[kWaves], long_last[kWaves];   // parts of a long run, or 0, 0
+    __shared__ float lds[kWaves][256];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int64_t p = (int64_t)blockIdx.x * kWaves + wave, parts = (a.rows + a.part - 1) / a.part;
+    const int k = (int)(blockIdx.y * 256) + 4 * lane;
+    int64_t last = p;   // the run's last part
+    if (p + 1 < parts) {
+        const int64_t first = p * a.part, end = first + a.part;
+        // loaded together, whether they are asked for or not
+        const uint32_t cur = a.keys[end - 1], next = a.keys[end], head = a.keys[first], before = a.keys[first > 0 ? first - 1 : 0];
+        const bool starts = cur < a.n && next == cur && !(first > 0 && head == cur && before == cur);
+        while (starts) {
+            const int64_t q = last + 1 + lane;
+            const uint64_t same = __ballot(q < parts && a.keys[q * a.part] == cur);
+            const int n = same == ~0ull ? 64 : __ffsll((unsigned long long)~same) - 1;
+            last += n;
+            if (n < 64) break;
+        }
     }
+    // adds ends[2 q] for q in [begin, end), every step-th
+    auto add = [&](float* sum, int64_t begin, int64_t end, int step) {
+        const float* from = a.ends + 2 * begin * a.cols + k;
+        const int64_t stride = 2 * (int64_t)step * a.cols;
+        int n = (int)((end - begin + step - 1) / step);
+        if (k + 4 <= a.cols) {
+            for (; n >= 2; n -= 2) {
+                float v[2][4];
+#pragma unroll
+                for (int j = 0; j < 2; ++j, from += stride) __builtin_memcpy(v[j], from, 16);
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum[i] += v[j][i];
+            }
+        }
+        for (; n > 0; --n, from += stride)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (k + i < a.cols) sum[i] += from[i];
+    };
+    auto begin_sum = [&](float* sum, int64_t part) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] = k + i < a.cols ? a.ends[(2 * part + 1) * a.cols + k + i] : 0.0f;
+    };
+    auto finish = [&](const float* sum, int64_t part) {
+        float* const to = a.dtable + (int64_t)a.keys[(part + 1) * a.part - 1] * a.lddt + k;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (k + i < a.cols) to[i] = (a.accumulate ? to[i] : 0.0f) + sum[i] * a.scale;
+    };
+    const bool is_long = last - p > kLongRun;
+    if (lane == 0) long_first[wave] = is_long ? p : 0, long_last[wave] = is_long ? last : 0;
+    if (last > p && !is_long) {
+        float sum[4];
+        begin_sum(sum, p);
+        add(sum, p + 1, last + 1, 1);
+        finish(sum, p);
+    }
+    __syncthreads();
+    for (int w = 0; w < kWaves; ++w) {   // the same for all waves
+        if (long_last[w] == 0) continue;
+        float sum[4] = {0, 0, 0, 0};
+        if (wave == 0) begin_sum(sum, long_first[w]);
+        add(sum, long_first[w] + 1 + wave, long_last[w] + 1, kWaves);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) lds[wave][4 * lane + i] = sum[i];
+        __syncthreads();
+        if (wave == 0) {
+            for (int v = 1; v < kWaves; ++v)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[i] += lds[v][4 * lane + i];
+            finish(sum, long_first[w]);
+        }
+        __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------- all at once
+
+// Up to kThreads rows in one launch.  Workgroups below a.slabs take 64 columns each: they
+// sort the ids in LDS and sum the rows in parts of `part`, ends in LDS, too.  The others
+// write zeros into the table's rows that have no id.
+constexpr int kSmallLanes = 8, kSmallGroups = kThreads / kSmallLanes;
+struct SmallLds {
+    union {
+        SortLds sort;
+        float ends[kSmallGroups][2][8 * kSmallLanes];
+        uint32_t flags[kMostBins];
+    };
+    float ends1[kSmallGroups][2][8];   // of the single columns
+    uint32_t keys[kThreads], order[kThreads];
+};
+template <class T>
+__global__ void __launch_bounds__(kThreads) embedding_small_kernel(EmbeddingGradArgs a, IntRows ids, ZeroFill z, int passes, int bits) {
+    __shared__ SmallLds l;
+    const int t = threadIdx.x;
+    const uint32_t rows = (uint32_t)a.rows;
+    const bool live = t < (int)rows;
+    uint32_t key = live ? key_of(ids.at(t, 0), a.n) : 0;
+    if (blockIdx.x >= a.slabs) {
+        // 32 rows a word of flags
+        const uint32_t at = blockIdx.x - a.slabs, all = gridDim.x - a.slabs;
+        const int64_t begin = a.n * at / all, end = a.n * (at + 1) / all;
+        for (int64_t v0 = begin; v0 < end; v0 += 32 * kMostBins) {
+            const int64_t v1 = v0 + 32 * kMostBins < end ? v0 + 32 * kMostBins : end;
+            for (int w = t; w < kMostBins; w += kThreads) l.flags[w] = 0;
+            __syncthreads();
+            if (live && key >= v0 && key < v1) atomicOr(&l.flags[(uint32_t)(key - v0) / 32], 1u << (uint32_t)(key - v0) % 32);
+            __syncthreads();
+            fill_rows(z, v0, v1, l.flags);
+            __syncthreads();
+        }
+        return;
+    }
+    uint32_t row = t;
+    for (int p = 0; p < passes; ++p) {
+        const uint32_t n_bins = 1u << bits, bin = key >> (p * bits) & (n_bins - 1);
+        if (t < (int)n_bins) l.sort.before[t] = 0;
+        __syncthreads();
+        count_bin(l.sort.before, bin, live);
+        __syncthreads();
+        const uint32_t total = t < (int)n_bins ? l.sort.before[t] : 0;
+        bin_starts(l.sort, total, 0, n_bins);
+        const uint32_t to = place_keys(l.sort, bin, live, bits);
+        if (live) l.keys[to] = key, l.order[to] = row;
+        __syncthreads();
+        if (live) key = l.keys[t], row = l.order[t];
+        __syncthreads();
+    }
+    const int lane = t % kSmallLanes, group = t / kSmallLanes;
+    const int k = 8 * (int)(blockIdx.x * kSmallLanes + lane);
+    const RowsIn<T> dy((const T*)a.dy, a.lddy, a.cols);
+    const Columns& c = dy.c;
+    const bool single = blockIdx.x == 0 && c.has_single(lane);
+    const uint32_t first = group * a.part;
+    if (first < rows && (c.has(k) || single)) {
+        const uint32_t end = rows - first < a.part ? rows : first + a.part;
+        sum_runs(a, dy, l.keys, l.order, first, end, k, lane, single, [&](int which, const float* sum, float sum1) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) l.ends[group][which][8 * lane + i] = sum[i];
+            if (single) l.ends1[group][which][lane] = sum1;
+        });
+    }
+    __syncthreads();
+    // a group joins the run that begins in its part and goes on
+    const uint32_t end = first + a.part;
+    if (end >= rows || !(c.has(k) || single)) return;
+    const uint32_t cur = l.keys[end - 1];
+    if (cur >= a.n || l.keys[end] != cur || (first > 0 && l.keys[first] == cur && l.keys[first - 1] == cur)) return;
+    float sum[8], sum1 = single ? l.ends1[group][1][lane] : 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] = l.ends[group][1][8 * lane + i];
+    for (uint32_t q = group + 1; q * a.part < rows && l.keys[q * a.part] == cur; ++q) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += l.ends[q][0][8 * lane + i];
+        if (single) sum1 += l.ends1[q][0][lane];
+    }
+    float* const to = a.dtable + cur * a.lddt;
+    if (c.has(k))
+#pragma unroll
+        for (int i = 0; i < 8; ++i) to[k + i] = (a.accumulate ? to[k + i] : 0.0f) + sum[i] * a.scale;
+    if (single) to[c.single(lane)] = (a.accumulate ? to[c.single(lane)] : 0.0f) + sum1 * a.scale;
 }
 
 // ---------------------------------------------------------------- launches
+
+// Rows that one workgroup sorts by itself, and counts of all tiles that each tile's
+// workgroup adds up by itself.
+constexpr int64_t kMostSortedAtOnce = 4 * kThreads, kMostTileCounts = 65536;
 
 template <class T, int L>
 hipError_t lookup_launch(const EmbeddingArgs& a, int n_cu, hipStream_t s) {
@@ -297,24 +609,36 @@ hipError_t lookup_by_width(const EmbeddingArgs& a, int n_cu, hipStream_t s) {
 // How the gradient's rows are sorted and summed, and where its workspace's parts are.
 struct GradPlan {
     int passes, bits;        // of the sort
-    uint32_t tile, tiles;    // keys of a workgroup
+    bool at_once;            // by one workgroup
+    uint32_t tile, tiles;    // else: keys of a workgroup
+    int scanned;             // the tiles' counts are added up in a launch of their own
+    int lanes;               // of a row in the sums
     uint32_t part, parts;    // sorted rows of a sum
     size_t keys[2], order[2], counts, totals, ends, bytes;
 };
-GradPlan grad_plan(int64_t rows, int64_t n, int cols) {
+GradPlan grad_plan(int64_t rows, int64_t n, int cols, int n_cu) {
     GradPlan p{};
     int bits = 1;
     while (bits < 32 && ((int64_t)1 << bits) <= n) ++bits;   // keys 0..n
     p.passes = (bits + kSortBits - 1) / kSortBits;
     p.bits = (bits + p.passes - 1) / p.passes;
+    if (rows <= kThreads) {
+        p.part = (uint32_t)((rows + kSmallGroups - 1) / kSmallGroups);
+        return p;            // all at once, without a workspace
+    }
     auto cut = [&](int64_t least, int64_t most_parts) {
         const int64_t per = (rows + most_parts - 1) / most_parts;
-        const int64_t v = per < least ? least : (per + least - 1) / least * least;
-        return (uint32_t)v;
+        return (uint32_t)(per < least ? least : (per + least - 1) / least * least);
     };
-    p.tile = cut(kSortStep, 8192);
+    p.tile = cut(kThreads, 2048);
     p.tiles = (uint32_t)((rows + p.tile - 1) / p.tile);
-    p.part = cut(32, 65536);
+    p.at_once = rows <= kMostSortedAtOnce;
+    p.scanned = (int64_t)p.tiles << p.bits > kMostTileCounts;
+    p.lanes = cols <= 64 ? 8 : cols <= 128 ? 16 : cols <= 256 ? 32 : 64;
+    // parts of 8 rows at least, and so many that their waves fill the chip
+    const int64_t slabs = (cols + 8 * p.lanes - 1) / (8 * p.lanes), waves = (int64_t)n_cu * 16 * 64 / p.lanes / slabs;
+    p.part = cut(kAhead, waves < 1024 ? 1024 : waves);
+    if (p.part > 32 && rows <= 32 * 65536) p.part = 32;
     p.parts = (uint32_t)((rows + p.part - 1) / p.part);
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -322,22 +646,15 @@ GradPlan grad_plan(int64_t rows, int64_t n, int cols) {
         at += (bytes + 15) / 16 * 16;
         return here;
     };
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < (p.passes > 1 && !p.at_once ? 2 : 1); ++i) {
         p.keys[i] = take((size_t)rows * 4);
         p.order[i] = take((size_t)rows * 4);
     }
-    p.counts = take(((size_t)p.tiles << p.bits) * 4);
-    p.totals = take(((size_t)1 << p.bits) * 4);
+    if (!p.at_once) p.counts = take(((size_t)p.tiles << p.bits) * 4);
+    if (!p.at_once && p.scanned) p.totals = take(((size_t)1 << p.bits) * 4);
     p.ends = take((size_t)p.parts * 2 * (size_t)cols * 4);
     p.bytes = at;
     return p;
-}
-
-template <int L>
-hipError_t zero_launch(const EmbeddingGradArgs& a, int n_cu, hipStream_t s) {
-    const int64_t need = (a.n + 256 / L - 1) / (256 / L), full = (int64_t)n_cu * 32;
-    hipLaunchKernelGGL((embedding_zero_kernel<L>), dim3((uint32_t)(need < full ? need : full)), dim3(256), 0, s, a);
-    return hipGetLastError();
 }
 
 template <class T, int L>
@@ -346,13 +663,20 @@ hipError_t sum_launch(const EmbeddingGradArgs& a, uint32_t parts, hipStream_t s)
     hipLaunchKernelGGL((embedding_sum_kernel<T, L>), dim3((parts + 256 / L - 1) / (256 / L), slabs), dim3(256), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || parts < 2) return e;
-    hipLaunchKernelGGL(embedding_join_kernel, dim3(parts - 1, (uint32_t)((a.cols + 63) / 64)), dim3(1024), 0, s, a);
+    hipLaunchKernelGGL(embedding_join_kernel, dim3((parts + kWaves - 1) / kWaves, (uint32_t)((a.cols + 255) / 256)), dim3(kThreads), 0, s, a);
     return hipGetLastError();
 }
 template <class T>
-hipError_t sum_by_width(const EmbeddingGradArgs& a, uint32_t parts, hipStream_t s) {
-    return a.cols <= 64 ? sum_launch<T, 8>(a, parts, s) : a.cols <= 128 ? sum_launch<T, 16>(a, parts, s)
-         : a.cols <= 256 ? sum_launch<T, 32>(a, parts, s) : sum_launch<T, 64>(a, parts, s);
+hipError_t sum_by_width(const EmbeddingGradArgs& a, const GradPlan& p, hipStream_t s) {
+    return p.lanes == 8 ? sum_launch<T, 8>(a, p.parts, s) : p.lanes == 16 ? sum_launch<T, 16>(a, p.parts, s)
+         : p.lanes == 32 ? sum_launch<T, 32>(a, p.parts, s) : sum_launch<T, 64>(a, p.parts, s);
+}
+
+// Workgroups that write zeros into n rows.
+uint32_t fill_groups(int64_t n, int cols, int n_cu) {
+    const int64_t need = (n * cols + 16383) / 16384;   // 64 KB each, or more
+    const int64_t most = (int64_t)n_cu * 2;
+    return (uint32_t)(need < 1 ? 1 : need < most ? need : most);
 }
 
 }  // namespace
@@ -361,17 +685,21 @@ hipError_t launch_train_embedding(const EmbeddingArgs& a, bool table_bf16, int n
     return table_bf16 ? lookup_by_width<uint16_t>(a, n_cu, stream) : lookup_by_width<float>(a, n_cu, stream);
 }
 
-size_t embedding_backward_workspace(int64_t rows, int64_t n, int cols) { return rows ? grad_plan(rows, n, cols).bytes : 0; }
+size_t embedding_backward_workspace(int64_t rows, int64_t n, int cols, int n_cu) { return grad_plan(rows, n, cols, n_cu).bytes; }
 
 hipError_t launch_train_embedding_backward(EmbeddingGradArgs a, const IntRows& ids, bool dy_bf16, void* workspace, int n_cu,
                                            hipStream_t stream) {
-    if (!a.accumulate) {
-        const hipError_t e = a.cols <= 64 ? zero_launch<8>(a, n_cu, stream) : a.cols <= 256 ? zero_launch<32>(a, n_cu, stream)
-                                                                                           : zero_launch<256>(a, n_cu, stream);
-        if (e != hipSuccess) return e;
+    if (a.rows == 0 && a.accumulate) return hipSuccess;
+    const GradPlan p = grad_plan(a.rows, a.n, a.cols, n_cu);
+    ZeroFill z{a.dtable, a.lddt, a.cols, 0, a.n};
+    a.part = p.part;
+    if (a.rows <= kThreads) {
+        a.slabs = a.rows ? (uint32_t)((a.cols + 8 * kSmallLanes - 1) / (8 * kSmallLanes)) : 0;
+        const dim3 grid(a.slabs + (a.accumulate ? 0 : fill_groups(a.n, a.cols, n_cu)));
+        if (dy_bf16) hipLaunchKernelGGL((embedding_small_kernel<uint16_t>), grid, dim3(kThreads), 0, stream, a, ids, z, p.passes, p.bits);
+        else hipLaunchKernelGGL((embedding_small_kernel<float>), grid, dim3(kThreads), 0, stream, a, ids, z, p.passes, p.bits);
+        return hipGetLastError();
     }
-    if (a.rows == 0) return hipSuccess;
-    const GradPlan p = grad_plan(a.rows, a.n, a.cols);
     uint8_t* const ws = (uint8_t*)workspace;
     SortPass s{};
     s.ids = ids;
@@ -379,25 +707,44 @@ hipError_t launch_train_embedding_backward(EmbeddingGradArgs a, const IntRows& i
     s.n = a.n;
     s.bits = p.bits;
     s.tile = p.tile;
+    s.tiles = p.tiles;
+    s.scanned = p.scanned;
     s.counts = (uint32_t*)(ws + p.counts);
     s.totals = (uint32_t*)(ws + p.totals);
-    for (int i = 0; i < p.passes; ++i) {
+    // the zeros are written beside the sort, whose launches leave most of the chip idle
+    const int launches = p.at_once ? 1 : 2 * p.passes;
+    int launch = 0;
+    auto share = [&] {
+        z.begin = a.n * launch / launches;
+        z.end = a.n * (launch + 1) / launches;
+        ++launch;
+        return a.accumulate ? 0 : fill_groups(z.end - z.begin, a.cols, n_cu);
+    };
+    hipError_t e = hipSuccess;
+    for (int i = 0; i < (p.at_once ? 1 : p.passes) && e == hipSuccess; ++i) {
         s.shift = i * p.bits;
         s.keys_out = (uint32_t*)(ws + p.keys[i % 2]);
         s.rows_out = (uint32_t*)(ws + p.order[i % 2]);
-        hipLaunchKernelGGL(sort_count_kernel, dim3(p.tiles), dim3(kSortThreads), 0, stream, s);
-        hipLaunchKernelGGL(sort_scan_kernel, dim3(1u << p.bits), dim3(kSortThreads), 0, stream, s, p.tiles);
-        hipLaunchKernelGGL(sort_scatter_kernel, dim3(p.tiles), dim3(kSortThreads), 0, stream, s);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
+        const dim3 threads(kThreads);
+        if (p.at_once) {
+            const dim3 grid(1 + share());
+            hipLaunchKernelGGL((sort_all_kernel<4>), grid, threads, 0, stream, s, z, p.passes);
+        } else {
+            const dim3 counters(p.tiles + share());
+            hipLaunchKernelGGL(sort_count_kernel, counters, threads, 0, stream, s, z);
+            if (p.scanned) hipLaunchKernelGGL(sort_scan_kernel, dim3(((1u << p.bits) + 63) / 64), threads, 0, stream, s);
+            const dim3 movers(p.tiles + share());
+            hipLaunchKernelGGL(sort_scatter_kernel, movers, threads, 0, stream, s, z);
+        }
+        e = hipGetLastError();
         s.keys_in = s.keys_out;
         s.rows_in = s.rows_out;
     }
+    if (e != hipSuccess) return e;
     a.keys = s.keys_in;
     a.order = s.rows_in;
     a.ends = (float*)(ws + p.ends);
-    a.part = p.part;
-    return dy_bf16 ? sum_by_width<uint16_t>(a, p.parts, stream) : sum_by_width<float>(a, p.parts, stream);
+    return dy_bf16 ? sum_by_width<uint16_t>(a, p, stream) : sum_by_width<float>(a, p, stream);
 }
 
 }  // namespace donerf

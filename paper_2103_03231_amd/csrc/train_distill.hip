@@ -1,134 +1,181 @@
 // train_distill.hip - distillation from a teacher's top logits, loss and gradient.
 //
 //   p = softmax of t / T over a row's given entries, q = softmax of x / T over its
-//   classes, loss = w T^2 sum_k p_k (log p_k - log q_{c_k}),
-//   dx_j = w T (q_j - sum of p_k over the k with c_k = j).
+//   classes, loss = w T^2 sum_e p_e (log p_e - log q_{c_e}),
+//   dx_j = w T (q_j - sum of p_e over the e with c_e = j).
 //
-// One pass over x: a row stays in registers between its maximum, its sum and the
-// gradient.  Differences to the maximum are taken before they are scaled, so that
-// logits of the type's lowest value are as good a mask as -inf.  The entries' few
-// columns are written a second time, behind the rest of their row.
+// One pass over x: a row's exponentials stay in registers between their sum and the
+// gradient, and the next row is loaded over the logits that they were made of.  The
+// entries' few columns are written a second time, behind the rest of their row and by
+// the wave that wrote that: a wave's stores to one address keep their order.
 #include "rows.h"
 
 namespace donerf {
 namespace {
 
 constexpr uint32_t kNegInfBits = 0xff800000u;
+constexpr float kLn2 = 0.693147180559945f;
+
+// A row's entries in LDS, k each: classes (-1: not given), logits, which become
+// powers 2^((t - max) / (T ln 2)), and the powers of their classes' own logits.
+struct Entries {
+    int32_t* cls;
+    float* power;
+    float* own;
+};
 
 template <class T, int L, int C>
 __global__ void __launch_bounds__(row_threads(L)) distill_kernel(DistillArgs a) {
     constexpr int kGroups = row_threads(L) / L;
-    __shared__ typename RowReduce<L, 1>::Lds lds;
-    extern __shared__ uint32_t entries[];   // of each row: k classes, then k probabilities
-    RowReduce<L, 1> reduce(&lds);
+    constexpr bool kAhead = C <= 4;  // rows of which registers hold two, in part
+    constexpr int kTurns = L > 64 ? 2 : 1;
+    __shared__ typename RowReduce<L, 2>::Lds lds;
+    __shared__ uint8_t owners[kGroups * 8 * L * C];   // a byte a column: one of the entries of that class
+    extern __shared__ uint32_t room[];
+    RowReduce<L, 2> reduce(&lds);
     const int lane = threadIdx.x % L, group = threadIdx.x / L;
-    int32_t* const cls = (int32_t*)entries + group * 2 * a.k;
-    float* const prob = (float*)(cls + a.k);
+    // In two places by turns, where a row's waves are several: one that is a row ahead
+    // writes to the other.
+    int turn = 0;
+    uint8_t* const owner = owners + group * 8 * L * C;
     const RowsIn<T> x((const T*)a.x, a.ldx, a.cols);
     const Columns& c = x.c;
     const float neg_inf = __uint_as_float(kNegInfBits);
-    auto fence = [] {
-        if constexpr (L > 64) __syncthreads();
-        else wave_lds_fence();
-    };
-    for (uint32_t r0 = blockIdx.x * kGroups; r0 < a.rows; r0 += gridDim.x * kGroups) {
-        const bool live = r0 + group < a.rows;
-        const int64_t row = live ? r0 + group : a.rows - 1;
-        Raw<T> raw[C];
+    // what a row begins with: its chunks, its single column, its lane's first entry and its weight
+    Raw<T> raw[C];
+    float one, t0, weight;
+    int64_t c0;
+    auto load = [&](int64_t row) {
 #pragma unroll
         for (int j = 0; j < C; ++j) raw[j] = x.load(row, 8 * (lane + L * j));
-        float one = neg_inf;
-        if (c.any_single()) one = x.load_single(row, lane);
-        // the teacher's entries: their maximum, then their sum
-        float top_t = neg_inf;
+        one = c.any_single() ? x.load_single(row, lane) : 0.0f;
+        const int e = lane < a.k ? lane : a.k - 1;
+        c0 = a.classes.at(row, e);
+        t0 = a.teacher.at(row, e);
+        weight = a.weight ? a.weight[row] : 1.0f;
+    };
+    auto row_of = [&](uint32_t r0) { return (int64_t)(r0 + group < a.rows ? r0 + group : a.rows - 1); };
+    const uint32_t step = gridDim.x * kGroups;
+    uint32_t r0 = blockIdx.x * kGroups;
+    if (kAhead) load(row_of(r0));
+    // the same number of rows for every wave: sums over a workgroup's waves need them all
+    for (; r0 < a.rows; r0 += step) {
+        const bool live = r0 + group < a.rows;
+        const int64_t row = row_of(r0);
+        if (!kAhead) load(row);
+        uint32_t* const place = room + (group * kTurns + turn) * 3 * a.k;
+        const Entries en{(int32_t*)place, (float*)place + a.k, (float*)place + 2 * a.k};
+        turn ^= kTurns - 1;
+        // maxima of the logits and of the entries
+        float m[2] = {c.has_single(lane) ? one : neg_inf, neg_inf};
+        one = m[0];
         for (int e = lane; e < a.k; e += L) {
-            const int64_t at = a.classes.at(row, e);
+            const int64_t at = e == lane ? c0 : a.classes.at(row, e);
             const bool given = at >= 0 && at < a.cols;
-            const float t = given ? a.teacher.at(row, e) : neg_inf;
-            cls[e] = given ? (int32_t)at : -1;
-            prob[e] = t;
-            top_t = Max::of(top_t, t);
+            const float t = e == lane ? t0 : a.teacher.at(row, e);
+            en.cls[e] = given ? (int32_t)at : -1;
+            en.power[e] = given ? t : neg_inf;
+            m[1] = Max::of(m[1], en.power[e]);
         }
-        top_t = reduce.template one<Max>(top_t);
-        float sum_t = 0.0f;
-        for (int e = lane; e < a.k; e += L) {
-            const float t = prob[e] == neg_inf ? neg_inf : prob[e] - top_t;
-            const float p = __builtin_amdgcn_exp2f(t * a.log2e_over_t);
-            sum_t += p;
-        }
-        sum_t = reduce.template one<Add>(sum_t);
-        if (!c.has_single(lane)) one = neg_inf;
-        float top = one;
 #pragma unroll
         for (int j = 0; j < C; ++j) {
             if (!c.has(8 * (lane + L * j))) raw[j].fill(kNegInfBits);
             float v[8];
             raw[j].values(v);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) top = Max::of(top, v[i]);
+            for (int i = 0; i < 8; i += 2) m[0] = Max::of(Max::of(m[0], v[i]), v[i + 1]);
             raw[j].hold();
         }
-        top = reduce.template one<Max>(top);
-        auto power = [&](float v) { return __builtin_amdgcn_exp2f((v - top) * a.log2e_over_t); };
-        float sum = power(one);
+        reduce.template all<Max>(m);
+        const float top = m[0], top_t = m[1], w = weight;
+        // nothing to learn: no weight, no entry, no class
+        const bool empty = w == 0.0f || top_t == neg_inf || top == neg_inf;
+        // v / (T ln 2) less the maximum's, in one rounding; the maximum's own is the same in
+        // every power of the row and in the loss.  Far from zero, where it is a part of 1 and
+        // more, differences first.
+        const float base = top * a.log2e_over_t;
+        const bool far = !(__builtin_fabsf(base) < 1048576.0f);
+        auto exponent = [&](float v) { return far ? (v - top) * a.log2e_over_t : __builtin_fmaf(v, a.log2e_over_t, -base); };
+        float e1 = __builtin_amdgcn_exp2f(exponent(one));
+        float p[C][8], s[2] = {e1, 0.0f};
+        if (far) {   // rare, and then for all lanes of a row
+#pragma unroll
+            for (int j = 0; j < C; ++j) {
+                raw[j].values(p[j]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) p[j][i] = __builtin_amdgcn_exp2f((p[j][i] - top) * a.log2e_over_t);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < C; ++j) {
+                raw[j].values(p[j]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) p[j][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[j][i], a.log2e_over_t, -base));
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < C; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[0] += p[j][i];
+        float logit = 0.0f;   // the sum of p (t - x) / (T ln 2), each less its maximum
+        float from = 0.0f;    // of the first entry's class
+        if (lane < a.k) from = value_of(x.base[row * x.ld + (en.cls[lane] < 0 ? 0 : en.cls[lane])]);
+        if (kAhead && r0 + step < a.rows) load(row_of(r0 + step));
+        bool twice = false;
+        for (int e = lane; e < a.k; e += L) {
+            const float t = en.power[e];
+            const int at = en.cls[e];
+            const float d = (t - top_t) * a.log2e_over_t;
+            const float pe = t == neg_inf ? 0.0f : __builtin_amdgcn_exp2f(d);
+            s[1] += pe;
+            const float xe = e == lane ? from : value_of(x.base[row * x.ld + (at < 0 ? 0 : at)]);
+            const float ex = exponent(xe);
+            if (at >= 0 && pe != 0.0f) logit += pe * (d - ex);
+            en.power[e] = pe;
+            en.own[e] = __builtin_amdgcn_exp2f(ex);
+            if (at >= 0) owner[at] = (uint8_t)e;
+        }
+        reduce.template all<Add>(s);
+        const float inv = 1.0f / s[0], inv_t = 1.0f / s[1], scale = w * a.temp;
+        wave_lds_fence();   // the entries' powers and owners are there (behind the sums' barrier, too)
+        // classes that come twice: all but one of their entries find another in their place
+        for (int e = lane; e < a.k; e += L) twice |= en.cls[e] >= 0 && owner[en.cls[e]] != (uint8_t)e;
+        float l[2] = {logit, twice ? 1.0f : 0.0f};
+        reduce.template all<Add>(l);
+        twice = l[1] > 0.0f;   // the same for a row's lanes
+        if (lane == 0 && live && a.loss) {
+            const float loss = l[0] * inv_t * kLn2 + (logf(s[0]) - logf(s[1]));
+            a.loss[row] = empty ? 0.0f : loss * w * a.temp * a.temp;
+        }
+        if (!a.dx.base || !live) continue;
+        const float factor = inv * scale;
 #pragma unroll
         for (int j = 0; j < C; ++j) {
-            float v[8];
-            raw[j].values(v);
+            const int k = 8 * (lane + L * j);
+            if (!c.has(k)) continue;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum += power(v[i]);
-            raw[j].hold();
+            for (int i = 0; i < 8; ++i) p[j][i] = empty ? 0.0f : p[j][i] * factor;
+            store8(a.dx, row, k, p[j]);
         }
-        sum = reduce.template one<Add>(sum);
-        const float weight = a.weight ? a.weight[row] : 1.0f;
-        // nothing to learn: no weight, no entry, no class
-        const bool empty = weight == 0.0f || top_t == neg_inf || top == neg_inf;
-        const float inv_sum = 1.0f / sum, inv_t = 1.0f / sum_t, log_ratio = logf(sum) - logf(sum_t);
-        float loss = 0.0f;
-        for (int e = lane; e < a.k; e += L) {
-            if (cls[e] < 0) continue;
-            const float t = prob[e];
-            const float p = __builtin_amdgcn_exp2f((t - top_t) * a.log2e_over_t) * inv_t;
-            const float xc = value_of(x.base[row * x.ld + cls[e]]);
-            if (!(p == 0.0f)) loss += p * (((t - top_t) - (xc - top)) * a.inv_temp + log_ratio);
-            prob[e] = p;
+        if (c.has_single(lane)) store1(a.dx, row, c.single(lane), empty ? 0.0f : e1 * factor);
+        if (empty) continue;
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        constexpr int kLanes = L < 64 ? L : 64;
+        for (int e = lane % kLanes; e < a.k; e += kLanes) {
+            const int at = en.cls[e];
+            if (at < 0) continue;
+            // the lane that stored this column
+            const int by = at < c.whole ? at / 8 % L : at - c.whole;
+            if (L > 64 && by / 64 != lane / 64) continue;
+            float pe = en.power[e];
+            if (twice) {
+                pe = 0.0f;
+                for (int f = 0; f < a.k; ++f) pe += en.cls[f] == at ? en.power[f] : 0.0f;
+            }
+            store1(a.dx, row, at, (en.own[e] * inv - pe * inv_t) * scale);
         }
-        loss = reduce.template one<Add>(loss);
-        fence();
-        if (live && lane == 0 && a.loss) a.loss[row] = empty ? 0.0f : loss * weight * a.temp * a.temp;
-        if (a.dx.base) {
-            const float scale = weight * a.temp;
-            if (live) {
-#pragma unroll
-                for (int j = 0; j < C; ++j) {
-                    const int k = 8 * (lane + L * j);
-                    if (!c.has(k)) continue;
-                    float v[8];
-                    raw[j].values(v);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = empty ? 0.0f : power(v[i]) * inv_sum * scale;
-                    store8(a.dx, row, k, v);
-                }
-                if (c.has_single(lane)) store1(a.dx, row, c.single(lane), empty ? 0.0f : power(one) * inv_sum * scale);
-            }
-            // the entries' columns, behind the stores that they overwrite
-            if constexpr (L > 64) {
-                __syncthreads();
-            } else {
-                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-            }
-            for (int e = lane; e < a.k; e += L) {
-                const int at = cls[e];
-                if (at < 0 || empty || !live) continue;
-                float p = 0.0f;
-                for (int f = 0; f < a.k; ++f)
-                    if (cls[f] == at) p += prob[f];
-                store1(a.dx, row, at, (power(value_of(x.base[row * x.ld + at])) * inv_sum - p) * scale);
-            }
-        }
-        fence();   // the next row's entries come into the same place
     }
 }
 
@@ -136,18 +183,20 @@ template <class T, int L, int C>
 hipError_t distill_launch(const DistillArgs& a, int n_cu, hipStream_t s) {
     constexpr uint32_t groups = row_threads(L) / L;
     const uint32_t need = (a.rows + groups - 1) / groups, full = (uint32_t)n_cu * (2048 / row_threads(L));
-    hipLaunchKernelGGL((distill_kernel<T, L, C>), dim3(need < full ? need : full), dim3(row_threads(L)), groups * 8 * a.k, s, a);
+    hipLaunchKernelGGL((distill_kernel<T, L, C>), dim3(need < full ? need : full), dim3(row_threads(L)), groups * (L > 64 ? 24 : 12) * a.k, s, a);
     return hipGetLastError();
 }
 template <class T>
 hipError_t distill_by_width(const DistillArgs& a, int n_cu, hipStream_t s) {
     const int c = a.cols;
-    return c <= 64 ? distill_launch<T, 8, 1>(a, n_cu, s) : c <= 128 ? distill_launch<T, 16, 1>(a, n_cu, s)
-         : c <= 256 ? distill_launch<T, 32, 1>(a, n_cu, s) : c <= 512 ? distill_launch<T, 64, 1>(a, n_cu, s)
-         : c <= 1024 ? distill_launch<T, 64, 2>(a, n_cu, s) : c <= 2048 ? distill_launch<T, 64, 4>(a, n_cu, s)
-         : c <= 4096 ? distill_launch<T, 256, 2>(a, n_cu, s) : c <= 8192 ? distill_launch<T, 256, 4>(a, n_cu, s)
-         : c <= 16384 ? distill_launch<T, 512, 4>(a, n_cu, s) : c <= 32768 ? distill_launch<T, 1024, 4>(a, n_cu, s)
-         : distill_launch<T, 1024, 8>(a, n_cu, s);
+    // rows of single columns, up to 7, have 8 lanes at least
+    if (c <= 128 && c % 8 == 0)
+        return c <= 64 ? distill_launch<T, 4, 2>(a, n_cu, s) : distill_launch<T, 4, 4>(a, n_cu, s);
+    return c <= 64 ? distill_launch<T, 8, 1>(a, n_cu, s) : c <= 128 ? distill_launch<T, 8, 2>(a, n_cu, s) : c <= 256 ? distill_launch<T, 8, 4>(a, n_cu, s)
+         : c <= 512 ? distill_launch<T, 16, 4>(a, n_cu, s) : c <= 1024 ? distill_launch<T, 32, 4>(a, n_cu, s)
+         : c <= 2048 ? distill_launch<T, 64, 4>(a, n_cu, s) : c <= 4096 ? distill_launch<T, 128, 4>(a, n_cu, s)
+         : c <= 8192 ? distill_launch<T, 256, 4>(a, n_cu, s) : c <= 16384 ? distill_launch<T, 512, 4>(a, n_cu, s)
+         : c <= 32768 ? distill_launch<T, 1024, 4>(a, n_cu, s) : distill_launch<T, 1024, 8>(a, n_cu, s);
 }
 
 }  // namespace

@@ -181,9 +181,9 @@ __device__ __forceinline__ float lanes_all(float v) {
 // Over the L lanes of a row, N values at once.  Rows of several waves meet in LDS,
 // in two places by turns: a wave that is a call ahead writes to the other one, and
 // cannot be two ahead.
-template <int L, int N>
+template <int L, int N, int THREADS = row_threads(L)>
 struct RowReduce {
-    static constexpr int kWaves = L > 64 ? row_threads(L) / 64 : 0;
+    static constexpr int kWaves = L > 64 ? THREADS / 64 : 0;
     struct Lds {
         float v[2][N][kWaves > 0 ? kWaves : 1];
     };

@@ -27,7 +27,9 @@ struct Entries {
 template <class T, int L, int C>
 __global__ void __launch_bounds__(row_threads(L)) distill_kernel(DistillArgs a) {
     constexpr int kGroups = row_threads(L) / L;
-    constexpr bool kAhead = C <= 4;  // rows of which registers hold two, in part
+    // Registers hold a row's powers and the next row's logits; of the widest rows the
+    // logits alone, and the powers are made twice.
+    constexpr bool kAhead = C <= 4;
     constexpr int kTurns = L > 64 ? 2 : 1;
     __shared__ typename RowReduce<L, 2>::Lds lds;
     __shared__ uint8_t owners[kGroups * 8 * L * C];   // a byte a column: one of the entries of that class
@@ -97,26 +99,30 @@ __global__ void __launch_bounds__(row_threads(L)) distill_kernel(DistillArgs a) 
         const bool far = !(__builtin_fabsf(base) < 1048576.0f);
         auto exponent = [&](float v) { return far ? (v - top) * a.log2e_over_t : __builtin_fmaf(v, a.log2e_over_t, -base); };
         float e1 = __builtin_amdgcn_exp2f(exponent(one));
-        float p[C][8], s[2] = {e1, 0.0f};
-        if (far) {   // rare, and then for all lanes of a row
+        float p[kAhead ? C : 1][8], s[2] = {e1, 0.0f};
+        auto powers = [&](const Raw<T>& r, float* v) {
+            r.values(v);
+            if (far) {   // rare, and then for all lanes of a row
 #pragma unroll
-            for (int j = 0; j < C; ++j) {
-                raw[j].values(p[j]);
+                for (int i = 0; i < 8; ++i) v[i] = __builtin_amdgcn_exp2f((v[i] - top) * a.log2e_over_t);
+            } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) p[j][i] = __builtin_amdgcn_exp2f((p[j][i] - top) * a.log2e_over_t);
+                for (int i = 0; i < 8; ++i) v[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(v[i], a.log2e_over_t, -base));
             }
-        } else {
+        };
 #pragma unroll
-            for (int j = 0; j < C; ++j) {
-                raw[j].values(p[j]);
+        for (int j = 0; j < C; ++j) {
+            float v[8];
+            powers(raw[j], v);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) p[j][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[j][i], a.log2e_over_t, -base));
+            for (int i = 0; i < 8; ++i) s[0] += v[i];
+            if constexpr (kAhead) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) p[j][i] = v[i];
+            } else {
+                raw[j].hold();
             }
         }
-#pragma unroll
-        for (int j = 0; j < C; ++j)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s[0] += p[j][i];
         float logit = 0.0f;   // the sum of p (t - x) / (T ln 2), each less its maximum
         float from = 0.0f;    // of the first entry's class
         if (lane < a.k) from = value_of(x.base[row * x.ld + (en.cls[lane] < 0 ? 0 : en.cls[lane])]);
@@ -153,9 +159,16 @@ __global__ void __launch_bounds__(row_threads(L)) distill_kernel(DistillArgs a) 
         for (int j = 0; j < C; ++j) {
             const int k = 8 * (lane + L * j);
             if (!c.has(k)) continue;
+            float v[8];
+            if constexpr (kAhead) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) p[j][i] = empty ? 0.0f : p[j][i] * factor;
-            store8(a.dx, row, k, p[j]);
+                for (int i = 0; i < 8; ++i) v[i] = p[j][i];
+            } else {
+                powers(raw[j], v);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = empty ? 0.0f : v[i] * factor;
+            store8(a.dx, row, k, v);
         }
         if (c.has_single(lane)) store1(a.dx, row, c.single(lane), empty ? 0.0f : e1 * factor);
         if (empty) continue;

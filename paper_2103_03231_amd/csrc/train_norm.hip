@@ -129,12 +129,16 @@ struct NormSums {
     }
 };
 
+// Threads of a workgroup of the backward pass.
+constexpr int backward_threads(int L) { return L > 512 ? L : 512; }
+
 template <class X, class Z, int L, int C>
-__global__ void __launch_bounds__(row_threads(L)) norm_backward_kernel(NormBackwardArgs a) {
-    constexpr int kGroups = row_threads(L) / L;
-    __shared__ typename RowReduce<L, 2>::Lds lds;
-    __shared__ float parts[kGroups > 1 ? 16 * row_threads(L) : 1];
-    RowReduce<L, 2> reduce(&lds);
+__global__ void __launch_bounds__(backward_threads(L), 4) norm_backward_kernel(NormBackwardArgs a) {
+    constexpr int kThreads = backward_threads(L), kGroups = kThreads / L;
+    typedef RowReduce<L, 2, kThreads> Reduce;
+    __shared__ typename Reduce::Lds lds;
+    __shared__ float parts[kGroups > 1 ? 8 * kThreads : 1];
+    Reduce reduce(&lds);
     const int lane = threadIdx.x % L, group = threadIdx.x / L;
     const NormInput<X> x(a);
     const RowsIn<Z> dz((const Z*)a.dz, a.lddz, a.cols);
@@ -161,17 +165,18 @@ __global__ void __launch_bounds__(row_threads(L)) norm_backward_kernel(NormBackw
         }
         const f32x2 st = *(const f32x2*)(a.stats + 2 * row);
         const float mean = st[0], r = st[1];
-        float v1 = 0.0f, z1 = 0.0f, s[2] = {0.0f, 0.0f};
+        float v1 = 0.0f, z1 = 0.0f;
         if (c.any_single()) {
             v1 = x.load_single(row, lane);
             z1 = dz.load_single(row, lane);
-            if (live && c.has_single(lane)) {
-                const float xh = (v1 - mean) * r, g = z1 * w1;
-                s[0] = g;
-                s[1] = g * xh;
-                dw1 = __builtin_fmaf(z1, xh, dw1);
-                db1 += z1;
-            }
+        }
+        float s[2] = {0.0f, 0.0f};
+        if (live && c.has_single(lane)) {
+            const float xh = (v1 - mean) * r, g = z1 * w1;
+            s[0] = g;
+            s[1] = g * xh;
+            dw1 = __builtin_fmaf(z1, xh, dw1);
+            db1 += z1;
         }
 #pragma unroll
         for (int j = 0; j < C; ++j) {
@@ -215,29 +220,36 @@ __global__ void __launch_bounds__(row_threads(L)) norm_backward_kernel(NormBackw
     if (!a.parts && !a.dw && !a.db) return;
     const NormSums out(a);
     if constexpr (kGroups > 1) {
-        static_assert(C == 1);
-        // the row groups' sums in their order; a lane's two parts by turns
-        auto join = [&](auto N, auto value, auto column) {
-            constexpr int n = CV(N);
-            __syncthreads();
+        // the row groups' sums in their order, 8 columns of each lane at a time
+        auto join = [&](const float (&v)[8], float* to, int k0) {
 #pragma unroll
-            for (int i = 0; i < n; ++i) {
-                parts[group * 16 * L + 2 * (n * lane + i)] = value(i, 0);
-                parts[group * 16 * L + 2 * (n * lane + i) + 1] = value(i, 1);
-            }
+            for (int i = 0; i < 8; ++i) parts[group * 8 * L + 8 * lane + i] = v[i];
             __syncthreads();
-            for (int t = threadIdx.x; t < 2 * n * L; t += row_threads(L)) {
-                const int k = column(t / 2);
-                if (k < 0) continue;
+            for (int t = threadIdx.x; t < 8 * L; t += kThreads) {
                 float sum = parts[t];
-#pragma unroll
-                for (int g = 1; g < kGroups; ++g) sum += parts[g * 16 * L + t];
-                out.put(t % 2 ? +out.b : +out.w, k, sum);
+                for (int g = 1; g < kGroups; ++g) sum += parts[g * 8 * L + t];
+                if (c.has(k0 + t)) out.put(to, k0 + t, sum);
             }
+            __syncthreads();
         };
-        join(std::integral_constant<int, 8>{}, [&](int i, int b) { return b ? +db[0][i] : +dw[0][i]; }, [&](int t) { return t < c.whole ? t : -1; });
-        if (c.any_single())
-            join(std::integral_constant<int, 1>{}, [&](int, int b) { return b ? +db1 : +dw1; }, [&](int t) { return c.has_single(t) ? c.whole + t : -1; });
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+            join(dw[j], out.w, 8 * L * j);
+            join(db[j], out.b, 8 * L * j);
+        }
+        if (c.any_single()) {
+            parts[2 * threadIdx.x] = dw1;
+            parts[2 * threadIdx.x + 1] = db1;
+            __syncthreads();
+            if (group == 0 && c.has_single(lane)) {
+                for (int g = 1; g < kGroups; ++g) {
+                    dw1 += parts[2 * (g * L + lane)];
+                    db1 += parts[2 * (g * L + lane) + 1];
+                }
+                out.put(out.w, c.single(lane), dw1);
+                out.put(out.b, c.single(lane), db1);
+            }
+        }
     } else {
 #pragma unroll
         for (int j = 0; j < C; ++j) {
@@ -321,6 +333,7 @@ __global__ void __launch_bounds__(256) norm_columns_kernel(NormBackwardArgs a) {
         float dw[8], db[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) dw[i] = 0.0f, db[i] = 0.0f;
+#pragma unroll 4
         for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
             const f32x2 st = *(const f32x2*)(a.stats + 2 * (int64_t)row);
             float v[8], z[8];
@@ -354,17 +367,22 @@ __global__ void __launch_bounds__(256) norm_columns_kernel(NormBackwardArgs a) {
 // Sums of n parts of 2 cols values (dw, then db), 16 columns a workgroup, 64 threads each.
 __global__ void __launch_bounds__(1024) norm_parts_kernel(const float* parts, uint32_t n, int cols, float* dw, float* db,
                                                           int accumulate) {
-    __shared__ float lds[64][17];
+    __shared__ float lds[16][16];
     const int c = threadIdx.x % 16, slice = threadIdx.x / 16;
     const int64_t at = (int64_t)blockIdx.x * 16 + c;
     float sum = 0.0f;
     if (at < 2 * cols)
+#pragma unroll 8
         for (uint32_t p = slice; p < n; p += 64) sum += parts[p * (int64_t)(2 * cols) + at];
-    lds[slice][c] = sum;
+    // a wave's four slices, then the waves
+    sum += __shfl_xor(sum, 16, 64);
+    sum += __shfl_xor(sum, 32, 64);
+    if (threadIdx.x % 64 < 16) lds[slice / 4][c] = sum;
     __syncthreads();
     if (threadIdx.x >= 16 || at >= 2 * cols) return;
     sum = lds[0][c];
-    for (int s = 1; s < 64; ++s) sum += lds[s][c];
+#pragma unroll
+    for (int w = 1; w < 16; ++w) sum += lds[w][c];
     float* const out = at < cols ? dw : db;
     const int64_t k = at < cols ? at : at - cols;
     if (out) out[k] = accumulate ? out[k] + sum : sum;
@@ -399,25 +417,27 @@ hipError_t forward_by_width(const NormArgs& a, int n_cu, hipStream_t s) {
          : forward_launch<T, 1024, 8>(a, n_cu, s);
 }
 
-// Lanes of a row in the backward pass, 0 for rows that registers do not hold.
+// Lanes of a row in the backward pass, of 16 columns each, 0 for rows that registers do
+// not hold.
 int backward_lanes(int cols) {
     int lanes = 8;
-    while (lanes < 1024 && 8 * lanes < cols) lanes *= 2;
+    while (lanes < 1024 && 16 * lanes < cols) lanes *= 2;
     return cols <= 16 * 1024 ? lanes : 0;
 }
 // Workgroups of the backward pass: each leaves a part of dw and db.
 uint32_t backward_groups(int64_t rows, int cols, int n_cu) {
     const int lanes = backward_lanes(cols);
-    const int64_t per = lanes ? row_threads(lanes) / lanes : 1;
+    const int64_t per = lanes ? backward_threads(lanes) / lanes : 16;
     const int64_t need = (rows + per - 1) / per;
-    const int64_t most = lanes ? (int64_t)n_cu * 1024 / row_threads(lanes) : n_cu;
-    if (need <= 4) return need ? 1 : 0;
+    // two workgroups of 512 threads a compute unit, eight of 256 where they share columns
+    const int64_t most = lanes ? (int64_t)n_cu * 1024 / backward_threads(lanes) : (int64_t)n_cu * 8 / ((cols + 2047) / 2048) + 1;
+    if (need <= 2) return need ? 1 : 0;
     return (uint32_t)(need < most ? need : most);
 }
 
 template <class X, class Z, int L, int C>
 void backward_kernel(const NormBackwardArgs& a, uint32_t wg, hipStream_t s) {
-    hipLaunchKernelGGL((norm_backward_kernel<X, Z, L, C>), dim3(wg), dim3(row_threads(L)), 0, s, a);
+    hipLaunchKernelGGL((norm_backward_kernel<X, Z, L, C>), dim3(wg), dim3(backward_threads(L)), 0, s, a);
 }
 template <class X, class Z>
 hipError_t backward_by_width(NormBackwardArgs a, float* workspace, int n_cu, hipStream_t s) {
@@ -425,17 +445,14 @@ hipError_t backward_by_width(NormBackwardArgs a, float* workspace, int n_cu, hip
     const bool sums = a.dw || a.db;
     a.parts = sums && wg > 1 ? workspace : nullptr;
     switch (backward_lanes(a.cols)) {
-        case 8: backward_kernel<X, Z, 8, 1>(a, wg, s); break;
-        case 16: backward_kernel<X, Z, 16, 1>(a, wg, s); break;
-        case 32: backward_kernel<X, Z, 32, 1>(a, wg, s); break;
-        case 64: backward_kernel<X, Z, 64, 1>(a, wg, s); break;
-        case 128: backward_kernel<X, Z, 128, 1>(a, wg, s); break;
-        case 256: backward_kernel<X, Z, 256, 1>(a, wg, s); break;
-        case 512: backward_kernel<X, Z, 512, 1>(a, wg, s); break;
-        case 1024:
-            if (a.cols <= 8192) backward_kernel<X, Z, 1024, 1>(a, wg, s);
-            else backward_kernel<X, Z, 1024, 2>(a, wg, s);
-            break;
+        case 8: backward_kernel<X, Z, 8, 2>(a, wg, s); break;
+        case 16: backward_kernel<X, Z, 16, 2>(a, wg, s); break;
+        case 32: backward_kernel<X, Z, 32, 2>(a, wg, s); break;
+        case 64: backward_kernel<X, Z, 64, 2>(a, wg, s); break;
+        case 128: backward_kernel<X, Z, 128, 2>(a, wg, s); break;
+        case 256: backward_kernel<X, Z, 256, 2>(a, wg, s); break;
+        case 512: backward_kernel<X, Z, 512, 2>(a, wg, s); break;
+        case 1024: backward_kernel<X, Z, 1024, 2>(a, wg, s); break;
         default:
             if (a.dx.base) {
                 const uint32_t full = (uint32_t)n_cu * 2;

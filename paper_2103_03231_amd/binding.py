@@ -485,14 +485,14 @@ class Renderer:
 
     def _new(self, rows, cols, dtype, device):
         """A new matrix and itself as an argument."""
-        y = self.torch.empty((rows, cols), dtype=dtype, device=device)
+        y = self.torch.empty_strided((rows, cols), (cols, 1), dtype=dtype, device=device)   # cheaper than empty
         return y, (y.data_ptr(), cols, TYPE_FP32 if dtype is self.torch.float32 else TYPE_BF16, None, 0)
 
     def _mx_new(self, rows, cols, format, device):
-        empty, u8 = self.torch.empty, self.torch.uint8
+        empty, u8 = self.torch.empty_strided, self.torch.uint8
         blocks = (cols + 31) // 32
         ld, ld_s = blocks * (16 if format == MXFP4 else 32), (blocks + 7) // 8 * 8
-        q = MxTensor(empty((rows, ld), dtype=u8, device=device), empty((rows, ld_s), dtype=u8, device=device), cols, format)
+        q = MxTensor(empty((rows, ld), (ld, 1), dtype=u8, device=device), empty((rows, ld_s), (ld_s, 1), dtype=u8, device=device), cols, format)
         return q, (q.codes.data_ptr(), ld, format, q.scales.data_ptr(), ld_s)
 
     def _workspace(self, n, device):
@@ -614,7 +614,7 @@ class Renderer:
         pw, pb = self._vector("weight", weight, cols, dev), self._vector("bias", bias, cols, dev)
         y, my = self._new(rows, cols, self._out(out, t.bfloat16), dev)
         kept, mk = self._mx_new(rows, cols, MXFP8, dev) if keep else (None, None)
-        stats = t.empty((rows, 2), dtype=t.float32, device=dev)
+        stats = t.empty_strided((rows, 2), (2, 1), dtype=t.float32, device=dev)
         donerf_train_norm(self.h, mx, pw, pb, eps, 1 if relu else 0, my, mk, stats.data_ptr(), rows, cols)
         return y, kept, stats
 

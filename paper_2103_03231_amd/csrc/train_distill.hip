@@ -202,8 +202,9 @@ hipError_t distill_launch(const DistillArgs& a, int n_cu, hipStream_t s) {
 template <class T>
 hipError_t distill_by_width(const DistillArgs& a, int n_cu, hipStream_t s) {
     const int c = a.cols;
-    // rows of single columns, up to 7, have 8 lanes at least
-    if (c <= 128 && c % 8 == 0)
+    // rows of single columns, up to 7, have 8 lanes at least; with more lanes a workgroup has
+    // fewer rows, whose entries fit into 48 KB of LDS
+    if (c <= 128 && c % 8 == 0 && a.k <= 64)
         return c <= 64 ? distill_launch<T, 4, 2>(a, n_cu, s) : distill_launch<T, 4, 4>(a, n_cu, s);
     return c <= 64 ? distill_launch<T, 8, 1>(a, n_cu, s) : c <= 128 ? distill_launch<T, 8, 2>(a, n_cu, s) : c <= 256 ? distill_launch<T, 8, 4>(a, n_cu, s)
          : c <= 512 ? distill_launch<T, 16, 4>(a, n_cu, s) : c <= 1024 ? distill_launch<T, 32, 4>(a, n_cu, s)

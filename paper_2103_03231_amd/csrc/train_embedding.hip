@@ -420,81 +420,102 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(EmbeddingGradArgs a)
 }
 
 // Joins the runs that begin in 16 parts, a wave each, and go on: 256 columns a workgroup.
-// Runs of more than kLongRun parts are summed by all waves together.
+// Runs of more than kLongRun further parts are summed by all waves together.
 constexpr int kLongRun = 8;
 __global__ void __launch_bounds__(kThreads) embedding_join_kernel(EmbeddingGradArgs a) {
-    __shared__ int64_t long_first[kWaves], long_last[kWaves];   // parts of a long run, or 0, 0
+    __shared__ int64_t first_of[kWaves], last_of[kWaves];   // parts of each wave's run, and its id
+    __shared__ uint32_t id_of[kWaves], longs;
     __shared__ float lds[kWaves][256];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int64_t p = (int64_t)blockIdx.x * kWaves + wave, parts = (a.rows + a.part - 1) / a.part;
     const int k = (int)(blockIdx.y * 256) + 4 * lane;
+    const bool four = k + 4 <= a.cols;
+    if (threadIdx.x == 0) longs = 0;
     int64_t last = p;   // the run's last part
+    uint32_t cur = 0;
     if (p + 1 < parts) {
         const int64_t first = p * a.part, end = first + a.part;
         // loaded together, whether they are asked for or not
-        const uint32_t cur = a.keys[end - 1], next = a.keys[end], head = a.keys[first], before = a.keys[first > 0 ? first - 1 : 0];
-        const bool starts = cur < a.n && next == cur && !(first > 0 && head == cur && before == cur);
-        while (starts) {
-            const int64_t q = last + 1 + lane;
-            const uint64_t same = __ballot(q < parts && a.keys[q * a.part] == cur);
-            const int n = same == ~0ull ? 64 : __ffsll((unsigned long long)~same) - 1;
-            last += n;
-            if (n < 64) break;
+        const int64_t q1 = p + 1 + lane;
+        const uint32_t next = a.keys[end], head = a.keys[first], before = a.keys[first > 0 ? first - 1 : 0];
+        const uint32_t ahead = a.keys[(q1 < parts ? q1 : parts - 1) * a.part];
+        cur = a.keys[end - 1];
+        if (cur < a.n && next == cur && !(first > 0 && head == cur && before == cur)) {
+            uint64_t same = __ballot(q1 < parts && ahead == cur);
+            while (same == ~0ull) {
+                last += 64;
+                const int64_t q = last + 1 + lane;
+                same = __ballot(q < parts && a.keys[q * a.part] == cur);
+            }
+            last += __ffsll((unsigned long long)~same) - 1;
         }
     }
-    // adds ends[2 q] for q in [begin, end), every step-th
-    auto add = [&](float* sum, int64_t begin, int64_t end, int step) {
-        const float* from = a.ends + 2 * begin * a.cols + k;
-        const int64_t stride = 2 * (int64_t)step * a.cols;
-        int n = (int)((end - begin + step - 1) / step);
-        if (k + 4 <= a.cols) {
-            for (; n >= 2; n -= 2) {
-                float v[2][4];
+    auto load = [&](float* v, int64_t q, int which) {
+        const float* const from = a.ends + (2 * q + which) * a.cols + k;
+        if (four) {
+            __builtin_memcpy(v, from, 16);
+        } else {
 #pragma unroll
-                for (int j = 0; j < 2; ++j, from += stride) __builtin_memcpy(v[j], from, 16);
+            for (int i = 0; i < 4; ++i) v[i] = k + i < a.cols ? from[i] : 0.0f;
+        }
+    };
+    // adds the beginnings of parts from, from + step, ..., up to `to`, kLongRun at a time
+    auto add = [&](float* sum, int64_t from, int64_t to, int step) {
+        for (; from <= to; from += kLongRun * step) {
+            float v[kLongRun][4];
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < kLongRun; ++j)
+                if (from + j * step <= to) load(v[j], from + j * step, 0);
+#pragma unroll
+            for (int j = 0; j < kLongRun; ++j)
+                if (from + j * step <= to)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) sum[i] += v[j][i];
-            }
         }
-        for (; n > 0; --n, from += stride)
+    };
+    auto finish = [&](const float* sum, uint32_t id) {
+        float* const to = a.dtable + id * a.lddt + k;
+        float v[4] = {0, 0, 0, 0};
+        if (a.accumulate)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = k + i < a.cols ? to[i] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] += sum[i] * a.scale;
+        if (four) {
+            __builtin_memcpy(to, v, 16);
+        } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (k + i < a.cols) sum[i] += from[i];
+                if (k + i < a.cols) to[i] = v[i];
+        }
     };
-    auto begin_sum = [&](float* sum, int64_t part) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i] = k + i < a.cols ? a.ends[(2 * part + 1) * a.cols + k + i] : 0.0f;
-    };
-    auto finish = [&](const float* sum, int64_t part) {
-        float* const to = a.dtable + (int64_t)a.keys[(part + 1) * a.part - 1] * a.lddt + k;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (k + i < a.cols) to[i] = (a.accumulate ? to[i] : 0.0f) + sum[i] * a.scale;
-    };
-    const bool is_long = last - p > kLongRun;
-    if (lane == 0) long_first[wave] = is_long ? p : 0, long_last[wave] = is_long ? last : 0;
-    if (last > p && !is_long) {
+    __syncthreads();
+    if (last - p > kLongRun) {
+        if (lane == 0) {
+            first_of[wave] = p, last_of[wave] = last, id_of[wave] = cur;
+            atomicOr(&longs, 1u << wave);
+        }
+    } else if (last > p) {
         float sum[4];
-        begin_sum(sum, p);
-        add(sum, p + 1, last + 1, 1);
-        finish(sum, p);
+        load(sum, p, 1);
+        add(sum, p + 1, last, 1);
+        finish(sum, cur);
     }
     __syncthreads();
-    for (int w = 0; w < kWaves; ++w) {   // the same for all waves
-        if (long_last[w] == 0) continue;
+    for (uint32_t left = longs; left; left &= left - 1) {   // the same for all waves
+        const int w = __ffs(left) - 1;
         float sum[4] = {0, 0, 0, 0};
-        if (wave == 0) begin_sum(sum, long_first[w]);
-        add(sum, long_first[w] + 1 + wave, long_last[w] + 1, kWaves);
+        if (wave == 0) load(sum, first_of[w], 1);
+        add(sum, first_of[w] + 1 + wave, last_of[w], kWaves);
 #pragma unroll
         for (int i = 0; i < 4; ++i) lds[wave][4 * lane + i] = sum[i];
         __syncthreads();
         if (wave == 0) {
+#pragma unroll
             for (int v = 1; v < kWaves; ++v)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) sum[i] += lds[v][4 * lane + i];
-            finish(sum, long_first[w]);
+            finish(sum, id_of[w]);
         }
         __syncthreads();
     }

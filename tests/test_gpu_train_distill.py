@@ -95,7 +95,7 @@ def check(r, x, classes, t, weight, temp, out=BF16):
 
 
 SIZES = [(1, 1, 1), (2, 2, 2), (5, 7, 3), (1, 8, 8), (40, 9, 4), (33, 31, 1), (70, 64, 16), (300, 100, 4), (1000, 128, 4), (65, 129, 5), (257, 192, 7),
-         (30, 256, 128), (20, 283, 33), (19, 512, 64), (9, 1000, 10), (7, 1024, 100), (5, 2048, 128), (4, 2055, 65), (3, 4096, 64), (2, 5001, 128),
+         (30, 256, 128), (300, 128, 128), (200, 64, 100), (100, 8, 64), (90, 24, 65), (20, 283, 33), (19, 512, 64), (9, 1000, 10), (7, 1024, 100), (5, 2048, 128), (4, 2055, 65), (3, 4096, 64), (2, 5001, 128),
          (3, 8192, 1), (2, 16384, 128), (2, 16390, 7), (2, 32000, 64), (1, 32768, 128), (2, 40001, 50), (1, 65536, 128), (1, 65535, 3)]
 
 

@@ -1230,7 +1230,7 @@ int donerf_train_embedding(donerf_t* h, const donerf_mat* table, const donerf_ma
 
 size_t donerf_train_embedding_backward_workspace(const donerf_t* h, int64_t rows, int64_t n, int32_t cols) {
     if (!h || rows < 0 || rows > INT32_MAX || n < 1 || n > INT32_MAX || cols < 1 || cols > DONERF_MAX_COLS) return 0;
-    return embedding_backward_workspace(rows, n, cols, h->n_cu);
+    return embedding_backward_workspace(rows, n, cols);
 }
 
 int donerf_train_embedding_backward(donerf_t* h, const donerf_mat* dy, const donerf_mat* ids, float scale,
@@ -1242,9 +1242,8 @@ int donerf_train_embedding_backward(donerf_t* h, const donerf_mat* dy, const don
         (rc = validate_mat("ids", ids, kI32Bit | kI64Bit, rows, 1)) || (rc = validate_mat("dtable", dtable, kF32Bit, n, cols)))
         return rc;
     if (accumulate != 0 && accumulate != 1) return fail(DONERF_E_INVALID_ARG, "accumulate must be 0 or 1");
-    if ((rc = validate_handle(h))) return rc;
-    const size_t need = embedding_backward_workspace(rows, n, cols, h->n_cu);
-    if ((rc = validate_workspace(workspace, workspace_bytes, need)) ||
+    const size_t need = embedding_backward_workspace(rows, n, cols);
+    if ((rc = validate_workspace(workspace, workspace_bytes, need)) || (rc = validate_handle(h)) ||
         (rc = Ranges().writes("dtable", dtable, n, cols).writes("workspace", workspace, need).reads(dy, rows, cols)
                   .reads(ids, rows, 1).validate()))
         return rc;

@@ -342,7 +342,7 @@ struct EmbeddingGradArgs {
     uint32_t part;           // sorted rows of a part
     uint32_t slabs;          // workgroups that sum, where one launch does all
 };
-size_t embedding_backward_workspace(int64_t rows, int64_t n, int cols, int n_cu);
+size_t embedding_backward_workspace(int64_t rows, int64_t n, int cols);
 hipError_t launch_train_embedding_backward(EmbeddingGradArgs a, const IntRows& ids, bool dy_bf16, void* workspace, int n_cu,
                                            hipStream_t stream);
 

@@ -8,6 +8,7 @@
 // gradient, and the next row is loaded over the logits that they were made of.  The
 // entries' few columns are written a second time, behind the rest of their row and by
 // the wave that wrote that: a wave's stores to one address keep their order.
+#include "../../include/donerf.h"
 #include "rows.h"
 
 namespace donerf {
@@ -27,9 +28,6 @@ struct Entries {
 template <class T, int L, int C>
 __global__ void __launch_bounds__(row_threads(L)) distill_kernel(DistillArgs a) {
     constexpr int kGroups = row_threads(L) / L;
-    // Registers hold a row's powers and the next row's logits; of the widest rows the
-    // logits alone, and the powers are made twice.
-    constexpr bool kAhead = C <= 4;
     constexpr int kTurns = L > 64 ? 2 : 1;
     __shared__ typename RowReduce<L, 2>::Lds lds;
     __shared__ uint8_t owners[kGroups * 8 * L * C];   // a byte a column: one of the entries of that class
@@ -59,12 +57,11 @@ __global__ void __launch_bounds__(row_threads(L)) distill_kernel(DistillArgs a) 
     auto row_of = [&](uint32_t r0) { return (int64_t)(r0 + group < a.rows ? r0 + group : a.rows - 1); };
     const uint32_t step = gridDim.x * kGroups;
     uint32_t r0 = blockIdx.x * kGroups;
-    if (kAhead) load(row_of(r0));
+    load(row_of(r0));
     // the same number of rows for every wave: sums over a workgroup's waves need them all
     for (; r0 < a.rows; r0 += step) {
         const bool live = r0 + group < a.rows;
         const int64_t row = row_of(r0);
-        if (!kAhead) load(row);
         uint32_t* const place = room + (group * kTurns + turn) * 3 * a.k;
         const Entries en{(int32_t*)place, (float*)place + a.k, (float*)place + 2 * a.k};
         turn ^= kTurns - 1;
@@ -99,34 +96,30 @@ __global__ void __launch_bounds__(row_threads(L)) distill_kernel(DistillArgs a) 
         const bool far = !(__builtin_fabsf(base) < 1048576.0f);
         auto exponent = [&](float v) { return far ? (v - top) * a.log2e_over_t : __builtin_fmaf(v, a.log2e_over_t, -base); };
         float e1 = __builtin_amdgcn_exp2f(exponent(one));
-        float p[kAhead ? C : 1][8], s[2] = {e1, 0.0f};
-        auto powers = [&](const Raw<T>& r, float* v) {
-            r.values(v);
-            if (far) {   // rare, and then for all lanes of a row
+        float p[C][8], s[2] = {e1, 0.0f};
+        if (far) {   // rare, and then for all lanes of a row
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = __builtin_amdgcn_exp2f((v[i] - top) * a.log2e_over_t);
-            } else {
+            for (int j = 0; j < C; ++j) {
+                raw[j].values(p[j]);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(v[i], a.log2e_over_t, -base));
+                for (int i = 0; i < 8; ++i) p[j][i] = __builtin_amdgcn_exp2f((p[j][i] - top) * a.log2e_over_t);
             }
-        };
+        } else {
 #pragma unroll
-        for (int j = 0; j < C; ++j) {
-            float v[8];
-            powers(raw[j], v);
+            for (int j = 0; j < C; ++j) {
+                raw[j].values(p[j]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s[0] += v[i];
-            if constexpr (kAhead) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) p[j][i] = v[i];
-            } else {
-                raw[j].hold();
+                for (int i = 0; i < 8; ++i) p[j][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[j][i], a.log2e_over_t, -base));
             }
         }
+#pragma unroll
+        for (int j = 0; j < C; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[0] += p[j][i];
         float logit = 0.0f;   // the sum of p (t - x) / (T ln 2), each less its maximum
         float from = 0.0f;    // of the first entry's class
         if (lane < a.k) from = value_of(x.base[row * x.ld + (en.cls[lane] < 0 ? 0 : en.cls[lane])]);
-        if (kAhead && r0 + step < a.rows) load(row_of(r0 + step));
+        if (r0 + step < a.rows) load(row_of(r0 + step));
         bool twice = false;
         for (int e = lane; e < a.k; e += L) {
             const float t = en.power[e];
@@ -159,16 +152,9 @@ __global__ void __launch_bounds__(row_threads(L)) distill_kernel(DistillArgs a) 
         for (int j = 0; j < C; ++j) {
             const int k = 8 * (lane + L * j);
             if (!c.has(k)) continue;
-            float v[8];
-            if constexpr (kAhead) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = p[j][i];
-            } else {
-                powers(raw[j], v);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = empty ? 0.0f : v[i] * factor;
-            store8(a.dx, row, k, v);
+            for (int i = 0; i < 8; ++i) p[j][i] = empty ? 0.0f : p[j][i] * factor;
+            store8(a.dx, row, k, p[j]);
         }
         if (c.has_single(lane)) store1(a.dx, row, c.single(lane), empty ? 0.0f : e1 * factor);
         if (empty) continue;
@@ -192,11 +178,118 @@ __global__ void __launch_bounds__(row_threads(L)) distill_kernel(DistillArgs a) 
     }
 }
 
+// Rows that registers do not hold, by a workgroup each: read three times, from the
+// caches but for the first.
+template <class T>
+__global__ void __launch_bounds__(1024) distill_wide_kernel(DistillArgs a) {
+    constexpr int L = 1024;
+    __shared__ typename RowReduce<L, 2>::Lds lds;
+    __shared__ uint8_t owner[DONERF_MAX_COLS];   // a byte a column: one of the entries of that class
+    __shared__ int32_t cls[kMostEntries];
+    __shared__ float power[kMostEntries], own[kMostEntries];
+    RowReduce<L, 2> reduce(&lds);
+    const int lane = threadIdx.x;
+    const RowsIn<T> x((const T*)a.x, a.ldx, a.cols);
+    const Columns& c = x.c;
+    const float neg_inf = __uint_as_float(kNegInfBits);
+    for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const float w = a.weight ? a.weight[row] : 1.0f;
+        float one = c.has_single(lane) ? x.load_single(row, lane) : neg_inf, t = neg_inf;
+        int64_t at = -1;
+        if (lane < a.k) {
+            at = a.classes.at(row, lane);
+            if (at < 0 || at >= a.cols) at = -1;
+            else t = a.teacher.at(row, lane);
+        }
+        auto chunks = [&](auto f) {
+            int k = 8 * lane;
+            for (; c.has(k + 24 * L); k += 32 * L) {   // four at a time
+                Raw<T> r[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) r[j] = x.load(row, k + 8 * L * j);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) f(k + 8 * L * j, r[j]);
+            }
+            for (; c.has(k); k += 8 * L) f(k, x.load(row, k));
+        };
+        float m[2] = {one, t};
+        chunks([&](int, const Raw<T>& r) {
+            float v[8];
+            r.values(v);
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) m[0] = Max::of(Max::of(m[0], v[i]), v[i + 1]);
+        });
+        reduce.template all<Max>(m);
+        const float top = m[0], top_t = m[1];
+        const bool empty = w == 0.0f || top_t == neg_inf || top == neg_inf;
+        auto exponent = [&](float v) { return (v - top) * a.log2e_over_t; };
+        const float e1 = __builtin_amdgcn_exp2f(exponent(one));
+        float s[2] = {e1, 0.0f};
+        chunks([&](int, const Raw<T>& r) {
+            float v[8];
+            r.values(v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[0] += __builtin_amdgcn_exp2f(exponent(v[i]));
+        });
+        float logit = 0.0f;
+        if (lane < a.k) {
+            const float d = (t - top_t) * a.log2e_over_t, p = t == neg_inf ? 0.0f : __builtin_amdgcn_exp2f(d);
+            const float ex = exponent(value_of(x.base[row * x.ld + (at < 0 ? 0 : at)]));
+            s[1] = p;
+            if (at >= 0 && p != 0.0f) logit = p * (d - ex);
+            cls[lane] = (int32_t)at;
+            power[lane] = p;
+            own[lane] = __builtin_amdgcn_exp2f(ex);
+            if (at >= 0) owner[at] = (uint8_t)lane;
+        }
+        reduce.template all<Add>(s);
+        const float inv = 1.0f / s[0], inv_t = 1.0f / s[1], scale = w * a.temp;
+        // whether a class comes twice: all but one of its entries find another in their place
+        float l[2] = {logit, lane < a.k && at >= 0 && owner[at] != (uint8_t)lane ? 1.0f : 0.0f};
+        reduce.template all<Add>(l);
+        if (lane == 0 && a.loss) {
+            const float loss = l[0] * inv_t * kLn2 + (logf(s[0]) - logf(s[1]));
+            a.loss[row] = empty ? 0.0f : loss * w * a.temp * a.temp;
+        }
+        if (a.dx.base) {
+            const float factor = inv * scale;
+            chunks([&](int k, const Raw<T>& r) {
+                float v[8];
+                r.values(v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = empty ? 0.0f : __builtin_amdgcn_exp2f(exponent(v[i])) * factor;
+                store8(a.dx, row, k, v);
+            });
+            if (c.has_single(lane)) store1(a.dx, row, c.single(lane), empty ? 0.0f : e1 * factor);
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            for (int e = lane % 64; e < a.k && !empty; e += 64) {
+                const int to = cls[e], by = to < c.whole ? to / 8 % L : to - c.whole;   // the lane that stored this column
+                if (to < 0 || by / 64 != lane / 64) continue;
+                float p = power[e];
+                if (l[1] > 0.0f) {
+                    p = 0.0f;
+                    for (int f = 0; f < a.k; ++f) p += cls[f] == to ? power[f] : 0.0f;
+                }
+                store1(a.dx, row, to, (own[e] * inv - p * inv_t) * scale);
+            }
+        }
+        lds_barrier();   // the next row's entries come into the same place
+    }
+}
+
 template <class T, int L, int C>
 hipError_t distill_launch(const DistillArgs& a, int n_cu, hipStream_t s) {
     constexpr uint32_t groups = row_threads(L) / L;
     const uint32_t need = (a.rows + groups - 1) / groups, full = (uint32_t)n_cu * (2048 / row_threads(L));
     hipLaunchKernelGGL((distill_kernel<T, L, C>), dim3(need < full ? need : full), dim3(row_threads(L)), groups * (L > 64 ? 24 : 12) * a.k, s, a);
+    return hipGetLastError();
+}
+template <class T>
+hipError_t distill_wide(const DistillArgs& a, int n_cu, hipStream_t s) {
+    const uint32_t full = (uint32_t)n_cu * 2;
+    hipLaunchKernelGGL((distill_wide_kernel<T>), dim3(a.rows < full ? a.rows : full), dim3(1024), 0, s, a);
     return hipGetLastError();
 }
 template <class T>
@@ -210,7 +303,7 @@ hipError_t distill_by_width(const DistillArgs& a, int n_cu, hipStream_t s) {
          : c <= 512 ? distill_launch<T, 16, 4>(a, n_cu, s) : c <= 1024 ? distill_launch<T, 32, 4>(a, n_cu, s)
          : c <= 2048 ? distill_launch<T, 64, 4>(a, n_cu, s) : c <= 4096 ? distill_launch<T, 128, 4>(a, n_cu, s)
          : c <= 8192 ? distill_launch<T, 256, 4>(a, n_cu, s) : c <= 16384 ? distill_launch<T, 512, 4>(a, n_cu, s)
-         : c <= 32768 ? distill_launch<T, 1024, 4>(a, n_cu, s) : distill_launch<T, 1024, 8>(a, n_cu, s);
+         : c <= 32768 ? distill_launch<T, 1024, 4>(a, n_cu, s) : distill_wide<T>(a, n_cu, s);
 }
 
 }  // namespace

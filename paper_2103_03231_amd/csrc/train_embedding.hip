@@ -441,13 +441,16 @@ __global__ void __launch_bounds__(kThreads) embedding_join_kernel(EmbeddingGradA
         const uint32_t ahead = a.keys[(q1 < parts ? q1 : parts - 1) * a.part];
         cur = a.keys[end - 1];
         if (cur < a.n && next == cur && !(first > 0 && head == cur && before == cur)) {
-            uint64_t same = __ballot(q1 < parts && ahead == cur);
-            while (same == ~0ull) {
-                last += 64;
-                const int64_t q = last + 1 + lane;
-                same = __ballot(q < parts && a.keys[q * a.part] == cur);
+            const uint64_t same = __ballot(q1 < parts && ahead == cur);
+            last += same == ~0ull ? 64 : __ffsll((unsigned long long)~same) - 1;
+            // a run of more: 64 places of the rest at a time, a 64th of it left each time
+            for (int64_t rest = parts - 1 - last; same == ~0ull && rest > 0;) {
+                const int64_t step = (rest + 63) / 64, q = last + (lane + 1) * step;
+                const uint64_t more = __ballot(q < parts && a.keys[(q < parts ? q : parts - 1) * a.part] == cur);
+                const int n = more == ~0ull ? 64 : __ffsll((unsigned long long)~more) - 1;
+                last += n * step;
+                rest = step - 1 < parts - 1 - last ? step - 1 : parts - 1 - last;
             }
-            last += __ffsll((unsigned long long)~same) - 1;
         }
     }
     auto load = [&](float* v, int64_t q, int which) {
@@ -637,7 +640,7 @@ struct GradPlan {
     uint32_t part, parts;    // sorted rows of a sum
     size_t keys[2], order[2], counts, totals, ends, bytes;
 };
-GradPlan grad_plan(int64_t rows, int64_t n, int cols, int n_cu) {
+GradPlan grad_plan(int64_t rows, int64_t n, int cols) {
     GradPlan p{};
     int bits = 1;
     while (bits < 32 && ((int64_t)1 << bits) <= n) ++bits;   // keys 0..n
@@ -656,10 +659,11 @@ GradPlan grad_plan(int64_t rows, int64_t n, int cols, int n_cu) {
     p.at_once = rows <= kMostSortedAtOnce;
     p.scanned = (int64_t)p.tiles << p.bits > kMostTileCounts;
     p.lanes = cols <= 64 ? 8 : cols <= 128 ? 16 : cols <= 256 ? 32 : 64;
-    // parts of 8 rows at least, and so many that their waves fill the chip
-    const int64_t slabs = (cols + 8 * p.lanes - 1) / (8 * p.lanes), waves = (int64_t)n_cu * 16 * 64 / p.lanes / slabs;
-    p.part = cut(kAhead, waves < 1024 ? 1024 : waves);
-    if (p.part > 32 && rows <= 32 * 65536) p.part = 32;
+    // 2048 parts of 8 to 32 rows: fewer leave the chip idle, more take long to join.  Beyond 2
+    // million rows, 65,536 longer ones.
+    p.part = cut(kAhead, 2048);
+    if (p.part > 32) p.part = 32;
+    if (rows > 32 * 65536) p.part = cut(kAhead, 65536);
     p.parts = (uint32_t)((rows + p.part - 1) / p.part);
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -706,12 +710,12 @@ hipError_t launch_train_embedding(const EmbeddingArgs& a, bool table_bf16, int n
     return table_bf16 ? lookup_by_width<uint16_t>(a, n_cu, stream) : lookup_by_width<float>(a, n_cu, stream);
 }
 
-size_t embedding_backward_workspace(int64_t rows, int64_t n, int cols, int n_cu) { return grad_plan(rows, n, cols, n_cu).bytes; }
+size_t embedding_backward_workspace(int64_t rows, int64_t n, int cols) { return grad_plan(rows, n, cols).bytes; }
 
 hipError_t launch_train_embedding_backward(EmbeddingGradArgs a, const IntRows& ids, bool dy_bf16, void* workspace, int n_cu,
                                            hipStream_t stream) {
     if (a.rows == 0 && a.accumulate) return hipSuccess;
-    const GradPlan p = grad_plan(a.rows, a.n, a.cols, n_cu);
+    const GradPlan p = grad_plan(a.rows, a.n, a.cols);
     ZeroFill z{a.dtable, a.lddt, a.cols, 0, a.n};
     a.part = p.part;
     if (a.rows <= kThreads) {

@@ -127,6 +127,19 @@ struct NormSums {
     __device__ __forceinline__ void put(float* out, int k, float v) const {
         if (out) out[k] = add ? out[k] + v : v;
     }
+    __device__ __forceinline__ void put8(float* out, int k, const float (&v)[8]) const {
+        if (!out) return;
+        float s[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] = v[i];
+        if (add) {
+            float old[8];
+            __builtin_memcpy(old, out + k, 32);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[i] = old[i] + v[i];
+        }
+        __builtin_memcpy(out + k, s, 32);
+    }
 };
 
 // Threads of a workgroup of the backward pass.
@@ -255,11 +268,8 @@ __global__ void __launch_bounds__(backward_threads(L), 4) norm_backward_kernel(N
         for (int j = 0; j < C; ++j) {
             const int k = 8 * (lane + L * j);
             if (!c.has(k)) continue;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                out.put(out.w, k + i, dw[j][i]);
-                out.put(out.b, k + i, db[j][i]);
-            }
+            out.put8(out.w, k, dw[j]);
+            out.put8(out.b, k, db[j]);
         }
         if (c.has_single(lane)) {
             out.put(out.w, c.single(lane), dw1);
@@ -345,11 +355,8 @@ __global__ void __launch_bounds__(256) norm_columns_kernel(NormBackwardArgs a) {
                 db[i] += z[i];
             }
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            out.put(out.w, k + i, dw[i]);
-            out.put(out.b, k + i, db[i]);
-        }
+        out.put8(out.w, k, dw);
+        out.put8(out.b, k, db);
     }
     if (c.has_single(t)) {
         float dw = 0.0f, db = 0.0f;
@@ -364,22 +371,22 @@ __global__ void __launch_bounds__(256) norm_columns_kernel(NormBackwardArgs a) {
     }
 }
 
-// Sums of n parts of 2 cols values (dw, then db), 16 columns a workgroup, 64 threads each.
+// Sums of n parts of 2 cols values (dw, then db), 32 columns a workgroup (whole cache
+// lines), 32 threads each.
 __global__ void __launch_bounds__(1024) norm_parts_kernel(const float* parts, uint32_t n, int cols, float* dw, float* db,
                                                           int accumulate) {
-    __shared__ float lds[16][16];
-    const int c = threadIdx.x % 16, slice = threadIdx.x / 16;
-    const int64_t at = (int64_t)blockIdx.x * 16 + c;
+    __shared__ float lds[16][32];
+    const int c = threadIdx.x % 32, slice = threadIdx.x / 32;
+    const int64_t at = (int64_t)blockIdx.x * 32 + c;
     float sum = 0.0f;
     if (at < 2 * cols)
-#pragma unroll 8
-        for (uint32_t p = slice; p < n; p += 64) sum += parts[p * (int64_t)(2 * cols) + at];
-    // a wave's four slices, then the waves
-    sum += __shfl_xor(sum, 16, 64);
+#pragma unroll 16
+        for (uint32_t p = slice; p < n; p += 32) sum += parts[p * (int64_t)(2 * cols) + at];
+    // a wave's two slices, then the waves
     sum += __shfl_xor(sum, 32, 64);
-    if (threadIdx.x % 64 < 16) lds[slice / 4][c] = sum;
+    if (threadIdx.x % 64 < 32) lds[slice / 2][c] = sum;
     __syncthreads();
-    if (threadIdx.x >= 16 || at >= 2 * cols) return;
+    if (threadIdx.x >= 32 || at >= 2 * cols) return;
     sum = lds[0][c];
 #pragma unroll
     for (int w = 1; w < 16; ++w) sum += lds[w][c];
@@ -432,7 +439,11 @@ uint32_t backward_groups(int64_t rows, int cols, int n_cu) {
     // two workgroups of 512 threads a compute unit, eight of 256 where they share columns
     const int64_t most = lanes ? (int64_t)n_cu * 1024 / backward_threads(lanes) : (int64_t)n_cu * 8 / ((cols + 2047) / 2048) + 1;
     if (need <= 2) return need ? 1 : 0;
-    return (uint32_t)(need < most ? need : most);
+    // A workgroup of a few rows leaves a part as large as they are, and a row takes one
+    // 1.5 us: four of rows of 4096 columns and more (314 x 5543 18 us, 21 with one row a
+    // workgroup), one of others (1021 x 283 9 us, 15 with four).
+    const int64_t some = lanes >= 512 ? (need + 3) / 4 : need;
+    return (uint32_t)(some < most ? some : most);
 }
 
 template <class X, class Z, int L, int C>
@@ -463,7 +474,7 @@ hipError_t backward_by_width(NormBackwardArgs a, float* workspace, int n_cu, hip
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.parts) return e;
-    hipLaunchKernelGGL(norm_parts_kernel, dim3((2 * a.cols + 15) / 16), dim3(1024), 0, s, a.parts, wg, a.cols, a.dw, a.db, a.accumulate);
+    hipLaunchKernelGGL(norm_parts_kernel, dim3((2 * a.cols + 31) / 32), dim3(1024), 0, s, a.parts, wg, a.cols, a.dw, a.db, a.accumulate);
     return hipGetLastError();
 }
 

@@ -40,15 +40,16 @@ __global__ void __launch_bounds__(256) embedding_kernel(EmbeddingArgs a) {
 constexpr int kThreads = 1024;        // of the gradient's workgroups
 constexpr int kWaves = kThreads / 64;
 
-// Zeros into rows [begin, end), but for those whose flag is set (by row - begin).
-__device__ __forceinline__ void fill_rows(const ZeroFill& z, int64_t begin, int64_t end, const uint32_t* flags) {
+// Zeros into rows [begin, end) by workgroup `at` of `all`, in turns, but for rows whose flag
+// is set (by row - begin).
+__device__ __forceinline__ void fill_rows(const ZeroFill& z, int64_t begin, int64_t end, uint32_t at, uint32_t all, const uint32_t* flags) {
     // 4 columns a lane; a row's lanes a power of two, up to a wave
     int bits = 0;
     while (bits < 6 && 4 << bits < z.cols) ++bits;
     const int lane = threadIdx.x & ((1 << bits) - 1), per = kThreads >> bits;
     const int quads = z.cols & ~3;
     const float zero[4] = {0, 0, 0, 0};
-    for (int64_t row = begin + (threadIdx.x >> bits); row < end; row += per) {
+    for (int64_t row = begin + (int64_t)at * per + (threadIdx.x >> bits); row < end; row += (int64_t)all * per) {
         const uint32_t f = (uint32_t)(row - begin);
         if (flags && flags[f / 32] >> f % 32 & 1) continue;
         float* const to = z.table + row * z.ld;
@@ -56,11 +57,8 @@ __device__ __forceinline__ void fill_rows(const ZeroFill& z, int64_t begin, int6
         for (int k = quads + lane; k < z.cols; k += 1 << bits) to[k] = 0.0f;
     }
 }
-// The share of workgroup `at` of `all` in the rows of a fill.
-__device__ __forceinline__ void fill_share(const ZeroFill& z, uint32_t at, uint32_t all) {
-    const int64_t n = z.end - z.begin;
-    fill_rows(z, z.begin + n * at / all, z.begin + n * (at + 1) / all, nullptr);
-}
+// A workgroup's share of the rows of a fill.
+__device__ __forceinline__ void fill_share(const ZeroFill& z, uint32_t at, uint32_t all) { fill_rows(z, z.begin, z.end, at, all, nullptr); }
 
 // ---------------------------------------------------------------- sort
 
@@ -136,13 +134,12 @@ __global__ void __launch_bounds__(kThreads) sort_scan_kernel(SortPass s) {
 struct SortLds {
     uint32_t at[kMostBins];               // where the next key of each bin goes
     uint32_t before[kMostBins];
-    uint16_t waves[kWaves][kMostBins];    // keys of each wave, then of the waves before
+    alignas(16) uint16_t waves[kWaves][kMostBins];    // keys of each wave, then of the waves before
     uint32_t sums[kWaves];
 };
 
 // at[b] becomes the sum of totals before bin b, and before[b].
-template <class Lds>
-__device__ __forceinline__ void bin_starts(Lds& l, uint32_t total, uint32_t before, uint32_t n_bins) {
+__device__ __forceinline__ void bin_starts(SortLds& l, uint32_t total, uint32_t before, uint32_t n_bins) {
     // a thread a bin: kMostBins of them at most
     static_assert(kMostBins <= kThreads);
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
@@ -167,7 +164,7 @@ __device__ __forceinline__ void bin_starts(Lds& l, uint32_t total, uint32_t befo
 __device__ __forceinline__ uint32_t place_keys(SortLds& l, uint32_t bin, bool live, int bits) {
     const uint32_t n_bins = 1u << bits;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    for (uint32_t b = threadIdx.x; b < kWaves << bits; b += kThreads) l.waves[b >> bits][b & (n_bins - 1)] = 0;
+    for (uint32_t i = threadIdx.x; i < sizeof(l.waves) / 16; i += kThreads) ((u32x4*)l.waves)[i] = u32x4{0, 0, 0, 0};
     __syncthreads();
     uint64_t same = __ballot(live);   // the live lanes with this lane's bin
     for (int b = 0; b < bits; ++b) {
@@ -250,89 +247,73 @@ __global__ void __launch_bounds__(kThreads) sort_scatter_kernel(SortPass s, Zero
     }
 }
 
-// All passes of up to ITEMS keys a thread, by one workgroup in LDS; the others write
-// zeros meanwhile.  Waves take consecutive keys and count their own.
+// Up to ITEMS keys a thread in one launch.  Keys are dealt to workgroups by their low
+// bits; each reads all of them, keeps its own in their order, sorts them by the other
+// bits, and knows from the others' number where they go: equal keys end up side by side,
+// which is all that the sums ask for.  The remaining workgroups write zeros meanwhile.
 template <int ITEMS>
-struct SortAllLds {
-    uint32_t at[kMostBins];
-    uint16_t waves[kWaves][kMostBins];   // keys of each wave, then of the waves before
-    uint32_t sums[kWaves];
-    uint32_t keys[ITEMS * kThreads];
+struct BucketLds {
+    SortLds sort;
+    uint32_t mine[kWaves], before[kWaves];   // each wave's keys of this bucket, and of those before
+    uint16_t keys[ITEMS * kThreads];         // the bits above the bucket's
     uint16_t rows[ITEMS * kThreads];
 };
 template <int ITEMS>
-__global__ void __launch_bounds__(kThreads) sort_all_kernel(SortPass s, ZeroFill z, int passes) {
-    static_assert(ITEMS * kThreads <= 65536);
-    __shared__ SortAllLds<ITEMS> l;
-    if (blockIdx.x > 0) return fill_share(z, blockIdx.x - 1, gridDim.x - 1);
-    const uint32_t n_bins = 1u << s.bits;
+__global__ void __launch_bounds__(kThreads) sort_buckets_kernel(SortPass s, ZeroFill z) {
+    static_assert(ITEMS * kThreads <= 65536 && kSortBits <= 16);
+    __shared__ BucketLds<ITEMS> l;
+    if (blockIdx.x >= s.tiles) return fill_share(z, blockIdx.x - s.tiles, gridDim.x - s.tiles);
+    const uint32_t n_bins = 1u << s.bits, bucket = blockIdx.x, buckets = 1u << s.shift;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const uint32_t at0 = wave * ITEMS * 64 + lane;   // the first of this lane's places, 64 apart
-    uint32_t key[ITEMS], row[ITEMS], rank[ITEMS];
+    const uint32_t at0 = wave * ITEMS * 64 + lane;   // a wave takes consecutive keys, 64 at a time
+    uint32_t key[ITEMS];
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j) key[j] = sort_key(s, at0 + 64 * j < s.rows ? at0 + 64 * j : s.rows - 1);
+    uint32_t mine = 0, less = 0;
 #pragma unroll
     for (int j = 0; j < ITEMS; ++j) {
-        row[j] = at0 + 64 * j;
-        key[j] = sort_key(s, row[j] < s.rows ? row[j] : s.rows - 1);
+        const bool live = at0 + 64 * j < s.rows;
+        const uint32_t b = key[j] & (buckets - 1);
+        mine += (uint32_t)__popcll(__ballot(live && b == bucket));
+        less += (uint32_t)__popcll(__ballot(live && b < bucket));
     }
-#pragma unroll 1
-    for (int p = 0; p < passes; ++p) {
-        const int shift = p * s.bits;
-        for (uint32_t b = threadIdx.x; b < kWaves << s.bits; b += kThreads) l.waves[b >> s.bits][b & (n_bins - 1)] = 0;
-        __syncthreads();
-        // (conditions on places are asked anew at every step: held ones fill the registers)
-        auto steps = [&](auto f) {
-            uint32_t at = at0;
-            asm volatile("" : "+v"(at));
+    if (lane == 0) l.mine[wave] = mine, l.before[wave] = less;
+    if (threadIdx.x < n_bins) l.sort.before[threadIdx.x] = 0;
+    __syncthreads();
+    uint32_t to = 0, n = 0, base = 0;   // this wave's place, the bucket's keys, and where they go
 #pragma unroll
-            for (int j = 0; j < ITEMS; ++j) {
-                f(j, at);
-                at += 64;
-                asm volatile("" : "+v"(at));
-            }
-        };
-        steps([&](int j, uint32_t at) {
-            const uint32_t bin = key[j] >> shift & (n_bins - 1);
-            const bool live = at < s.rows;
-            uint64_t same = __ballot(live);   // the live lanes with this lane's bin
-#pragma unroll 1
-            for (int b = 0; b < s.bits; ++b) {
-                const uint64_t ones = __ballot(bin >> b & 1);
-                same &= bin >> b & 1 ? ones : ~ones;
-            }
-            const uint32_t before = (uint32_t)__popcll(same & ((1ull << lane) - 1));
-            const uint32_t seen = l.waves[wave][bin];
-            wave_lds_fence();
-            if (live && before == 0) l.waves[wave][bin] = (uint16_t)(seen + __popcll(same));
-            wave_lds_fence();
-            rank[j] = seen + before;
-        });
-        __syncthreads();
-        uint32_t total = 0;
-        if (threadIdx.x < n_bins)
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                const uint32_t v = l.waves[w][threadIdx.x];
-                l.waves[w][threadIdx.x] = (uint16_t)total;
-                total += v;
-            }
-        bin_starts(l, total, 0, n_bins);
-        steps([&](int j, uint32_t at) {
-            if (at >= s.rows) return;
-            const uint32_t bin = key[j] >> shift & (n_bins - 1), to = l.at[bin] + l.waves[wave][bin] + rank[j];
-            l.keys[to] = key[j];
-            l.rows[to] = (uint16_t)row[j];
-        });
-        __syncthreads();
-        steps([&](int j, uint32_t at) {
-            key[j] = l.keys[at];   // what lies behind the last one is not used
-            row[j] = l.rows[at];
-        });
+    for (int w = 0; w < kWaves; ++w) {
+        if (w < wave) to += l.mine[w];
+        n += l.mine[w];
+        base += l.before[w];
     }
 #pragma unroll
     for (int j = 0; j < ITEMS; ++j) {
-        if (at0 + 64 * j >= s.rows) continue;
-        s.keys_out[at0 + 64 * j] = key[j];
-        s.rows_out[at0 + 64 * j] = row[j];
+        const bool own = at0 + 64 * j < s.rows && (key[j] & (buckets - 1)) == bucket;
+        const uint64_t m = __ballot(own);
+        if (own) {
+            const uint32_t i = to + (uint32_t)__popcll(m & ((1ull << lane) - 1));
+            l.keys[i] = (uint16_t)(key[j] >> s.shift);
+            l.rows[i] = (uint16_t)(at0 + 64 * j);
+        }
+        to += (uint32_t)__popcll(m);
+    }
+    __syncthreads();
+    for (uint32_t i0 = 0; i0 < n; i0 += kThreads) {
+        const uint32_t i = i0 + threadIdx.x;
+        count_bin(l.sort.before, i < n ? l.keys[i] : 0, i < n);
+    }
+    __syncthreads();
+    const uint32_t total = threadIdx.x < n_bins ? l.sort.before[threadIdx.x] : 0;
+    bin_starts(l.sort, total, 0, n_bins);
+    for (uint32_t i0 = 0; i0 < n; i0 += kThreads) {
+        const uint32_t i = i0 + threadIdx.x;
+        const uint32_t k = i < n ? l.keys[i] : 0;
+        const uint32_t out = base + place_keys(l.sort, k, i < n, s.bits);
+        if (i < n) {
+            s.keys_out[out] = k << s.shift | bucket;
+            s.rows_out[out] = l.rows[i];
+        }
     }
 }
 
@@ -556,7 +537,7 @@ __global__ void __launch_bounds__(kThreads) embedding_small_kernel(EmbeddingGrad
             __syncthreads();
             if (live && key >= v0 && key < v1) atomicOr(&l.flags[(uint32_t)(key - v0) / 32], 1u << (uint32_t)(key - v0) % 32);
             __syncthreads();
-            fill_rows(z, v0, v1, l.flags);
+            fill_rows(z, v0, v1, 0, 1, l.flags);
             __syncthreads();
         }
         return;
@@ -613,9 +594,10 @@ __global__ void __launch_bounds__(kThreads) embedding_small_kernel(EmbeddingGrad
 
 // ---------------------------------------------------------------- launches
 
-// Rows that one workgroup sorts by itself, and counts of all tiles that each tile's
-// workgroup adds up by itself.
-constexpr int64_t kMostSortedAtOnce = 4 * kThreads, kMostTileCounts = 65536;
+// Rows and buckets (as a power of two) of a sort in one launch, and counts of all tiles
+// that each tile's workgroup adds up by itself.
+constexpr int64_t kMostSortedAtOnce = 16 * kThreads, kMostTileCounts = 65536;
+constexpr int kMostBucketBits = 8;
 
 template <class T, int L>
 hipError_t lookup_launch(const EmbeddingArgs& a, int n_cu, hipStream_t s) {
@@ -633,8 +615,9 @@ hipError_t lookup_by_width(const EmbeddingArgs& a, int n_cu, hipStream_t s) {
 // How the gradient's rows are sorted and summed, and where its workspace's parts are.
 struct GradPlan {
     int passes, bits;        // of the sort
-    bool at_once;            // by one workgroup
-    uint32_t tile, tiles;    // else: keys of a workgroup
+    bool at_once;            // in one launch
+    int bucket_bits;         // of its workgroups
+    uint32_t tile, tiles;    // keys of a workgroup, workgroups
     int scanned;             // the tiles' counts are added up in a launch of their own
     int lanes;               // of a row in the sums
     uint32_t part, parts;    // sorted rows of a sum
@@ -656,7 +639,15 @@ GradPlan grad_plan(int64_t rows, int64_t n, int cols) {
     };
     p.tile = cut(kThreads, 2048);
     p.tiles = (uint32_t)((rows + p.tile - 1) / p.tile);
-    p.at_once = rows <= kMostSortedAtOnce;
+    p.at_once = rows <= kMostSortedAtOnce && bits <= kMostBucketBits + kSortBits;
+    if (p.at_once) {
+        // so many buckets that one pass sorts each, and that they hold 256 keys or so (16,384 keys of
+        // 32,000 beside 131 MB of zeros 30.4 us, 31.7 with 1024 each)
+        p.bucket_bits = bits > kSortBits ? bits - kSortBits : 0;
+        while (p.bucket_bits < bits - 1 && p.bucket_bits < 7 && (kThreads / 4) << p.bucket_bits < rows) ++p.bucket_bits;
+        p.bits = bits - p.bucket_bits;
+        p.tiles = 1u << p.bucket_bits;
+    }
     p.scanned = (int64_t)p.tiles << p.bits > kMostTileCounts;
     p.lanes = cols <= 64 ? 8 : cols <= 128 ? 16 : cols <= 256 ? 32 : 64;
     // 2048 parts of 8 to 32 rows: fewer leave the chip idle, more take long to join.  Beyond 2
@@ -752,8 +743,10 @@ hipError_t launch_train_embedding_backward(EmbeddingGradArgs a, const IntRows& i
         s.rows_out = (uint32_t*)(ws + p.order[i % 2]);
         const dim3 threads(kThreads);
         if (p.at_once) {
-            const dim3 grid(1 + share());
-            hipLaunchKernelGGL((sort_all_kernel<4>), grid, threads, 0, stream, s, z, p.passes);
+            const dim3 grid(p.tiles + share());
+            s.shift = p.bucket_bits;
+            if (a.rows <= 4 * kThreads) hipLaunchKernelGGL((sort_buckets_kernel<4>), grid, threads, 0, stream, s, z);
+            else hipLaunchKernelGGL((sort_buckets_kernel<16>), grid, threads, 0, stream, s, z);
         } else {
             const dim3 counters(p.tiles + share());
             hipLaunchKernelGGL(sort_count_kernel, counters, threads, 0, stream, s, z);

@@ -289,6 +289,7 @@ struct NormBackwardArgs {
     int32_t cols;
     float inv_cols;
     float* parts;            // set by the launch: each workgroup's dw and db, or null
+    uint32_t row_groups;     // and the workgroups of the rows, where others sum the columns
 };
 size_t norm_backward_workspace(int64_t rows, int cols, int n_cu);
 hipError_t launch_train_norm_backward(const NormBackwardArgs& a, int x_type, bool dz_bf16, void* workspace, int n_cu,

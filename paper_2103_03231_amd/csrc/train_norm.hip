@@ -117,40 +117,93 @@ struct NormInput<uint8_t> : Mx8In {
     __device__ __forceinline__ explicit NormInput(const NormBackwardArgs& a) : Mx8In(a.x, a.cols) {}
 };
 
-// A result of one workgroup alone, or its part of one.
+// A workgroup's part of dw and db.
 struct NormSums {
     float* w;
     float* b;
-    bool add;
-    __device__ __forceinline__ explicit NormSums(const NormBackwardArgs& a)
-        : w(a.parts ? a.parts + (int64_t)blockIdx.x * 2 * a.cols : a.dw), b(a.parts ? w + a.cols : a.db), add(!a.parts && a.accumulate) {}
-    __device__ __forceinline__ void put(float* out, int k, float v) const {
-        if (out) out[k] = add ? out[k] + v : v;
-    }
-    __device__ __forceinline__ void put8(float* out, int k, const float (&v)[8]) const {
-        if (!out) return;
-        float s[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s[i] = v[i];
-        if (add) {
-            float old[8];
-            __builtin_memcpy(old, out + k, 32);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s[i] = old[i] + v[i];
-        }
-        __builtin_memcpy(out + k, s, 32);
-    }
+    __device__ __forceinline__ explicit NormSums(const NormBackwardArgs& a) : w(a.parts + (int64_t)blockIdx.x * 2 * a.cols), b(w + a.cols) {}
 };
-
 // Threads of a workgroup of the backward pass.
 constexpr int backward_threads(int L) { return L > 512 ? L : 512; }
 
-template <class X, class Z, int L, int C>
+// The sum of v over the lanes of a wave with the same number modulo 4, in its first four.
+__device__ __forceinline__ float fourths_all(float v) {
+    v += dpp<0x124>(v);   // rotated by 4 and by 8 among 16
+    v += dpp<0x128>(v);
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(q[0]) + __uint_as_float(q[1]);
+}
+
+// dw and db of 32 columns, all rows, by a workgroup: four lanes a row.  The last slab is
+// that of the single columns.
+__host__ __device__ inline uint32_t column_slabs(int cols) { return (uint32_t)((cols & ~7) + 31) / 32 + (cols % 8 ? 1 : 0); }
+template <class X, class Z, int THREADS>
+__device__ __forceinline__ void sum_columns(const NormBackwardArgs& a, uint32_t slab, float (*lds)[64]) {
+    const NormInput<X> x(a);
+    const RowsIn<Z> dz((const Z*)a.dz, a.lddz, a.cols);
+    const Columns& c = dz.c;
+    const int lane = threadIdx.x % 4, wave = threadIdx.x / 64, k = 32 * (int)slab + 8 * lane;
+    float dw[8] = {0, 0, 0, 0, 0, 0, 0, 0}, db[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    const bool singles = 32 * (int)slab >= c.whole;
+    if (singles) {   // lanes 0 to 3 have two each
+        for (uint32_t row = threadIdx.x / 4; row < a.rows; row += THREADS / 4) {
+            const f32x2 st = *(const f32x2*)(a.stats + 2 * (int64_t)row);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float z = dz.load_single(row, lane + 4 * i);
+                dw[i] = __builtin_fmaf(z, (x.load_single(row, lane + 4 * i) - st[0]) * st[1], dw[i]);
+                db[i] += z;
+            }
+        }
+    } else if (c.has(k)) {
+#pragma unroll 4
+        for (uint32_t row = threadIdx.x / 4; row < a.rows; row += THREADS / 4) {
+            const f32x2 st = *(const f32x2*)(a.stats + 2 * (int64_t)row);
+            float v[8], z[8];
+            x.load(row, k).values(v);
+            dz.load(row, k).values(z);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                dw[i] = __builtin_fmaf(z[i], (v[i] - st[0]) * st[1], dw[i]);
+                db[i] += z[i];
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        dw[i] = fourths_all(dw[i]);
+        db[i] = fourths_all(db[i]);
+        if (threadIdx.x % 64 < 4) lds[wave][8 * lane + i] = dw[i], lds[wave][32 + 8 * lane + i] = db[i];
+    }
+    __syncthreads();
+    if (threadIdx.x >= 64) return;
+    float sum = lds[0][threadIdx.x];
+#pragma unroll
+    for (int w = 1; w < THREADS / 64; ++w) sum += lds[w][threadIdx.x];
+    const int t = threadIdx.x % 32;
+    const int col = singles ? (t % 8 < 2 ? c.whole + t / 8 + 4 * (t % 8) : a.cols) : 32 * (int)slab + t < c.whole ? 32 * (int)slab + t : a.cols;
+    float* const out = threadIdx.x < 32 ? a.dw : a.db;
+    if (out && col < a.cols) out[col] = a.accumulate ? out[col] + sum : sum;
+}
+template <class X, class Z>
+__global__ void __launch_bounds__(512) norm_few_columns_kernel(NormBackwardArgs a) {
+    __shared__ float lds[8][64];
+    sum_columns<X, Z, 512>(a, blockIdx.x, lds);
+}
+
+// SUMS: each workgroup adds up dw and db of its rows on the way.  Without: the workgroups
+// behind those of the rows (a.row_groups of them) do, each for its columns.
+template <class X, class Z, int L, int C, bool SUMS>
 __global__ void __launch_bounds__(backward_threads(L), 4) norm_backward_kernel(NormBackwardArgs a) {
     constexpr int kThreads = backward_threads(L), kGroups = kThreads / L;
     typedef RowReduce<L, 2, kThreads> Reduce;
     __shared__ typename Reduce::Lds lds;
-    __shared__ float parts[kGroups > 1 ? 8 * kThreads : 1];
+    __shared__ float parts[!SUMS ? kThreads : kGroups > 1 ? 8 * kThreads : 1];
+    if constexpr (!SUMS)
+        if (blockIdx.x >= a.row_groups) return sum_columns<X, Z, kThreads>(a, blockIdx.x - a.row_groups, (float (*)[64])parts);
+    const uint32_t workgroups = SUMS ? gridDim.x : a.row_groups;
     Reduce reduce(&lds);
     const int lane = threadIdx.x % L, group = threadIdx.x / L;
     const NormInput<X> x(a);
@@ -166,7 +219,7 @@ __global__ void __launch_bounds__(backward_threads(L), 4) norm_backward_kernel(N
         if (a.w) ws.load(0, 8 * (lane + L * j)).values(w[j]);
     }
     if (a.w) w1 = ws.load_single(0, lane);
-    for (uint32_t r0 = blockIdx.x * kGroups; r0 < a.rows; r0 += gridDim.x * kGroups) {
+    for (uint32_t r0 = blockIdx.x * kGroups; r0 < a.rows; r0 += workgroups * kGroups) {
         const bool live = r0 + group < a.rows;
         const int64_t row = live ? r0 + group : a.rows - 1;
         typename NormInput<X>::Held xr[C];
@@ -188,8 +241,10 @@ __global__ void __launch_bounds__(backward_threads(L), 4) norm_backward_kernel(N
             const float xh = (v1 - mean) * r, g = z1 * w1;
             s[0] = g;
             s[1] = g * xh;
-            dw1 = __builtin_fmaf(z1, xh, dw1);
-            db1 += z1;
+            if (SUMS) {
+                dw1 = __builtin_fmaf(z1, xh, dw1);
+                db1 += z1;
+            }
         }
 #pragma unroll
         for (int j = 0; j < C; ++j) {
@@ -202,8 +257,10 @@ __global__ void __launch_bounds__(backward_threads(L), 4) norm_backward_kernel(N
                     const float xh = (v[i] - mean) * r, g = z[i] * w[j][i];
                     s[0] += g;
                     s[1] = __builtin_fmaf(g, xh, s[1]);
-                    dw[j][i] = __builtin_fmaf(z[i], xh, dw[j][i]);
-                    db[j][i] += z[i];
+                    if (SUMS) {
+                        dw[j][i] = __builtin_fmaf(z[i], xh, dw[j][i]);
+                        db[j][i] += z[i];
+                    }
                 }
             }
             xr[j].hold();
@@ -230,7 +287,7 @@ __global__ void __launch_bounds__(backward_threads(L), 4) norm_backward_kernel(N
         if (c.has_single(lane))
             store1(a.dx, row, c.single(lane), a.relu && x.single_is_zero(v1, row, lane) ? 0.0f : grad(v1, z1, w1));
     }
-    if (!a.parts && !a.dw && !a.db) return;
+    if (!SUMS) return;
     const NormSums out(a);
     if constexpr (kGroups > 1) {
         // the row groups' sums in their order, 8 columns of each lane at a time
@@ -241,7 +298,7 @@ __global__ void __launch_bounds__(backward_threads(L), 4) norm_backward_kernel(N
             for (int t = threadIdx.x; t < 8 * L; t += kThreads) {
                 float sum = parts[t];
                 for (int g = 1; g < kGroups; ++g) sum += parts[g * 8 * L + t];
-                if (c.has(k0 + t)) out.put(to, k0 + t, sum);
+                if (c.has(k0 + t)) to[k0 + t] = sum;
             }
             __syncthreads();
         };
@@ -259,8 +316,8 @@ __global__ void __launch_bounds__(backward_threads(L), 4) norm_backward_kernel(N
                     dw1 += parts[2 * (g * L + lane)];
                     db1 += parts[2 * (g * L + lane) + 1];
                 }
-                out.put(out.w, c.single(lane), dw1);
-                out.put(out.b, c.single(lane), db1);
+                out.w[c.single(lane)] = dw1;
+                out.b[c.single(lane)] = db1;
             }
         }
     } else {
@@ -268,12 +325,12 @@ __global__ void __launch_bounds__(backward_threads(L), 4) norm_backward_kernel(N
         for (int j = 0; j < C; ++j) {
             const int k = 8 * (lane + L * j);
             if (!c.has(k)) continue;
-            out.put8(out.w, k, dw[j]);
-            out.put8(out.b, k, db[j]);
+            __builtin_memcpy(out.w + k, dw[j], 32);
+            __builtin_memcpy(out.b + k, db[j], 32);
         }
         if (c.has_single(lane)) {
-            out.put(out.w, c.single(lane), dw1);
-            out.put(out.b, c.single(lane), db1);
+            out.w[c.single(lane)] = dw1;
+            out.b[c.single(lane)] = db1;
         }
     }
 }
@@ -355,8 +412,8 @@ __global__ void __launch_bounds__(256) norm_columns_kernel(NormBackwardArgs a) {
                 db[i] += z[i];
             }
         }
-        out.put8(out.w, k, dw);
-        out.put8(out.b, k, db);
+        __builtin_memcpy(out.w + k, dw, 32);
+        __builtin_memcpy(out.b + k, db, 32);
     }
     if (c.has_single(t)) {
         float dw = 0.0f, db = 0.0f;
@@ -366,8 +423,8 @@ __global__ void __launch_bounds__(256) norm_columns_kernel(NormBackwardArgs a) {
             dw = __builtin_fmaf(z, (x.load_single(row, t) - st[0]) * st[1], dw);
             db += z;
         }
-        out.put(out.w, c.single(t), dw);
-        out.put(out.b, c.single(t), db);
+        out.w[c.single(t)] = dw;
+        out.b[c.single(t)] = db;
     }
 }
 
@@ -431,30 +488,35 @@ int backward_lanes(int cols) {
     while (lanes < 1024 && 16 * lanes < cols) lanes *= 2;
     return cols <= 16 * 1024 ? lanes : 0;
 }
-// Workgroups of the backward pass: each leaves a part of dw and db.
+// So few values that dw and db are summed by columns, from the caches, in the launch that
+// makes dx.
+bool few_values(int64_t rows, int cols) { return rows <= 2048 && rows * cols <= (int64_t)1 << 23; }
+// Workgroups of the backward pass that each leave a part of dw and db.
 uint32_t backward_groups(int64_t rows, int cols, int n_cu) {
     const int lanes = backward_lanes(cols);
     const int64_t per = lanes ? backward_threads(lanes) / lanes : 16;
     const int64_t need = (rows + per - 1) / per;
     // two workgroups of 512 threads a compute unit, eight of 256 where they share columns
     const int64_t most = lanes ? (int64_t)n_cu * 1024 / backward_threads(lanes) : (int64_t)n_cu * 8 / ((cols + 2047) / 2048) + 1;
-    if (need <= 2) return need ? 1 : 0;
-    // A workgroup of a few rows leaves a part as large as they are, and a row takes one
-    // 1.5 us: four of rows of 4096 columns and more (314 x 5543 18 us, 21 with one row a
-    // workgroup), one of others (1021 x 283 9 us, 15 with four).
-    const int64_t some = lanes >= 512 ? (need + 3) / 4 : need;
-    return (uint32_t)(some < most ? some : most);
+    return (uint32_t)(need < most ? need : most);
 }
 
 template <class X, class Z, int L, int C>
-void backward_kernel(const NormBackwardArgs& a, uint32_t wg, hipStream_t s) {
-    hipLaunchKernelGGL((norm_backward_kernel<X, Z, L, C>), dim3(wg), dim3(backward_threads(L)), 0, s, a);
+void backward_kernel(NormBackwardArgs a, uint32_t wg, hipStream_t s) {
+    const dim3 threads(backward_threads(L));
+    if (a.parts) {
+        hipLaunchKernelGGL((norm_backward_kernel<X, Z, L, C, true>), dim3(wg), threads, 0, s, a);
+    } else {
+        a.row_groups = a.dx.base ? wg : 0;
+        const uint32_t columns = a.dw || a.db ? column_slabs(a.cols) : 0;
+        hipLaunchKernelGGL((norm_backward_kernel<X, Z, L, C, false>), dim3(a.row_groups + columns), threads, 0, s, a);
+    }
 }
 template <class X, class Z>
 hipError_t backward_by_width(NormBackwardArgs a, float* workspace, int n_cu, hipStream_t s) {
-    const uint32_t wg = backward_groups(a.rows, a.cols, n_cu);
-    const bool sums = a.dw || a.db;
-    a.parts = sums && wg > 1 ? workspace : nullptr;
+    const bool few = few_values(a.rows, a.cols), sums = a.dw || a.db;
+    a.parts = sums && !few ? workspace : nullptr;
+    uint32_t wg = backward_groups(a.rows, a.cols, n_cu);
     switch (backward_lanes(a.cols)) {
         case 8: backward_kernel<X, Z, 8, 2>(a, wg, s); break;
         case 16: backward_kernel<X, Z, 16, 2>(a, wg, s); break;
@@ -469,8 +531,8 @@ hipError_t backward_by_width(NormBackwardArgs a, float* workspace, int n_cu, hip
                 const uint32_t full = (uint32_t)n_cu * 2;
                 hipLaunchKernelGGL((norm_backward_wide_kernel<X, Z>), dim3(a.rows < full ? a.rows : full), dim3(1024), 0, s, a);
             }
-            if (sums)
-                hipLaunchKernelGGL((norm_columns_kernel<X, Z>), dim3(wg, (a.cols + 2047) / 2048), dim3(256), 0, s, a);
+            if (sums && few) hipLaunchKernelGGL((norm_few_columns_kernel<X, Z>), dim3(column_slabs(a.cols)), dim3(512), 0, s, a);
+            else if (sums) hipLaunchKernelGGL((norm_columns_kernel<X, Z>), dim3(wg, (a.cols + 2047) / 2048), dim3(256), 0, s, a);
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.parts) return e;
@@ -485,8 +547,7 @@ hipError_t launch_train_norm(const NormArgs& a, bool x_bf16, int n_cu, hipStream
 }
 
 size_t norm_backward_workspace(int64_t rows, int cols, int n_cu) {
-    const uint32_t wg = backward_groups(rows, cols, n_cu);
-    return wg > 1 ? (size_t)wg * 2 * (size_t)cols * sizeof(float) : 0;
+    return few_values(rows, cols) ? 0 : (size_t)backward_groups(rows, cols, n_cu) * 2 * (size_t)cols * sizeof(float);
 }
 
 hipError_t launch_train_norm_backward(const NormBackwardArgs& a, int x_type, bool dz_bf16, void* workspace, int n_cu,

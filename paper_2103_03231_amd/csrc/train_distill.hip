@@ -301,9 +301,9 @@ hipError_t distill_by_width(const DistillArgs& a, int n_cu, hipStream_t s) {
         return c <= 64 ? distill_launch<T, 4, 2>(a, n_cu, s) : distill_launch<T, 4, 4>(a, n_cu, s);
     return c <= 64 ? distill_launch<T, 8, 1>(a, n_cu, s) : c <= 128 ? distill_launch<T, 8, 2>(a, n_cu, s) : c <= 256 ? distill_launch<T, 8, 4>(a, n_cu, s)
          : c <= 512 ? distill_launch<T, 16, 4>(a, n_cu, s) : c <= 1024 ? distill_launch<T, 32, 4>(a, n_cu, s)
-         : c <= 2048 ? distill_launch<T, 64, 4>(a, n_cu, s) : c <= 4096 ? distill_launch<T, 128, 4>(a, n_cu, s)
-         : c <= 8192 ? distill_launch<T, 256, 4>(a, n_cu, s) : c <= 16384 ? distill_launch<T, 512, 4>(a, n_cu, s)
-         : c <= 32768 ? distill_launch<T, 1024, 4>(a, n_cu, s) : distill_wide<T>(a, n_cu, s);
+         : c <= 2048 ? distill_launch<T, 64, 4>(a, n_cu, s) : c <= 4096 ? distill_launch<T, 64, 8>(a, n_cu, s)
+         : c <= 8192 ? distill_launch<T, 128, 8>(a, n_cu, s) : c <= 16384 ? distill_launch<T, 256, 8>(a, n_cu, s)
+         : c <= 32768 ? distill_launch<T, sizeof(T) == 2 ? 1024 : 512, sizeof(T) == 2 ? 4 : 8>(a, n_cu, s) : distill_wide<T>(a, n_cu, s);
 }
 
 }  // namespace

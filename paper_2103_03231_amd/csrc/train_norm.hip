@@ -28,6 +28,7 @@ template <class T, int L, int C, bool KEEP>
 __global__ void __launch_bounds__(row_threads(L)) norm_kernel(NormArgs a) {
     constexpr int kGroups = row_threads(L) / L;
     constexpr bool kHeld = C <= 2;   // w and b in registers, too
+    constexpr bool kAhead = L <= 256;
     __shared__ typename RowReduce<L, 1>::Lds lds;
     RowReduce<L, 1> reduce(&lds);
     const int lane = threadIdx.x % L, group = threadIdx.x / L;
@@ -38,15 +39,26 @@ __global__ void __launch_bounds__(row_threads(L)) norm_kernel(NormArgs a) {
 #pragma unroll
         for (int j = 0; j < C; ++j) affine_at(a, c, 8 * (lane + L * j), w[j], b[j]);
     auto act = [&](float z) { return a.relu ? __builtin_elementwise_maximum(z, 0.0f) : z; };
+    Raw<T> next[C];   // the row to come
+    float one_next = 0.0f;
+    auto load = [&](uint32_t r0) {
+        const int64_t row = r0 + group < a.rows ? r0 + group : a.rows - 1;
+#pragma unroll
+        for (int j = 0; j < C; ++j) next[j] = x.load(row, 8 * (lane + L * j));
+        if (c.any_single()) one_next = x.load_single(row, lane);
+    };
+    if (kAhead) load(blockIdx.x * kGroups);
     // the same number of rows for every wave: sums over a workgroup's waves need them all
-    for (uint32_t r0 = blockIdx.x * kGroups; r0 < a.rows; r0 += gridDim.x * kGroups) {
+    const uint32_t step = gridDim.x * kGroups;
+    for (uint32_t r0 = blockIdx.x * kGroups; r0 < a.rows; r0 += step) {
         const bool live = r0 + group < a.rows;
         const int64_t row = live ? r0 + group : a.rows - 1;
+        if (!kAhead) load(r0);
         Raw<T> raw[C];
 #pragma unroll
-        for (int j = 0; j < C; ++j) raw[j] = x.load(row, 8 * (lane + L * j));
-        float one = 0.0f;
-        if (c.any_single()) one = x.load_single(row, lane);
+        for (int j = 0; j < C; ++j) raw[j] = next[j];
+        const float one = one_next;
+        if (kAhead && r0 + step < a.rows) load(r0 + step);
         auto total = [&](auto f) {   // of f over the row's values
             float sum = c.has_single(lane) ? f(one) : 0.0f;
 #pragma unroll
@@ -473,10 +485,10 @@ hipError_t forward_launch(const NormArgs& a, int n_cu, hipStream_t stream) {
 template <class T>
 hipError_t forward_by_width(const NormArgs& a, int n_cu, hipStream_t s) {
     const int c = a.cols;
-    return c <= 64 ? forward_launch<T, 8, 1>(a, n_cu, s) : c <= 128 ? forward_launch<T, 16, 1>(a, n_cu, s)
-         : c <= 256 ? forward_launch<T, 32, 1>(a, n_cu, s) : c <= 512 ? forward_launch<T, 64, 1>(a, n_cu, s)
-         : c <= 1024 ? forward_launch<T, 64, 2>(a, n_cu, s) : c <= 2048 ? forward_launch<T, 64, 4>(a, n_cu, s)
-         : c <= 4096 ? forward_launch<T, 256, 2>(a, n_cu, s) : c <= 8192 ? forward_launch<T, 256, 4>(a, n_cu, s)
+    return c <= 64 ? forward_launch<T, 8, 1>(a, n_cu, s) : c <= 128 ? forward_launch<T, 8, 2>(a, n_cu, s)
+         : c <= 256 ? forward_launch<T, 16, 2>(a, n_cu, s) : c <= 512 ? forward_launch<T, 32, 2>(a, n_cu, s)
+         : c <= 1024 ? forward_launch<T, 64, 2>(a, n_cu, s) : c <= 2048 ? forward_launch<T, 128, 2>(a, n_cu, s)
+         : c <= 4096 ? forward_launch<T, 256, 2>(a, n_cu, s) : c <= 8192 ? forward_launch<T, 512, 2>(a, n_cu, s)
          : c <= 16384 ? forward_launch<T, 512, 4>(a, n_cu, s) : c <= 32768 ? forward_launch<T, 1024, 4>(a, n_cu, s)
          : forward_launch<T, 1024, 8>(a, n_cu, s);
 }

@@ -311,6 +311,7 @@ struct ZeroFill {
     float* table;
     int64_t ld;
     int32_t cols;
+    int32_t past;            // by stores that pass the caches
     int64_t begin, end;
 };
 // One pass of the sort of rows by their ids.

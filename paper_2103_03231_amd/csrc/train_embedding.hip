@@ -48,12 +48,16 @@ __device__ __forceinline__ void fill_rows(const ZeroFill& z, int64_t begin, int6
     while (bits < 6 && 4 << bits < z.cols) ++bits;
     const int lane = threadIdx.x & ((1 << bits) - 1), per = kThreads >> bits;
     const int quads = z.cols & ~3;
-    const float zero[4] = {0, 0, 0, 0};
+    typedef float Zeros __attribute__((ext_vector_type(4), aligned(4)));
     for (int64_t row = begin + (int64_t)at * per + (threadIdx.x >> bits); row < end; row += (int64_t)all * per) {
         const uint32_t f = (uint32_t)(row - begin);
         if (flags && flags[f / 32] >> f % 32 & 1) continue;
         float* const to = z.table + row * z.ld;
-        for (int k = 4 * lane; k < quads; k += 4 << bits) __builtin_memcpy(to + k, zero, 16);
+        // (one loop with both stores is compiled to the plain one)
+        if (z.past)
+            for (int k = 4 * lane; k < quads; k += 4 << bits) __builtin_nontemporal_store(Zeros{0, 0, 0, 0}, (Zeros*)(to + k));
+        else
+            for (int k = 4 * lane; k < quads; k += 4 << bits) *(Zeros*)(to + k) = Zeros{0, 0, 0, 0};
         for (int k = quads + lane; k < z.cols; k += 1 << bits) to[k] = 0.0f;
     }
 }
@@ -688,6 +692,14 @@ hipError_t sum_by_width(const EmbeddingGradArgs& a, const GradPlan& p, hipStream
          : p.lanes == 32 ? sum_launch<T, 32>(a, p.parts, s) : sum_launch<T, 64>(a, p.parts, s);
 }
 
+// Whether zeros pass the caches (bytes of dy and of the table).  Where both do not fit into
+// the last level beside what else is there (256 MB in all), zeros that stay push dy out of it
+// and are themselves pushed out while the sums read and write: 24,000 rows of 32,000 x 1024
+// (49 and 131 MB) 67 us, 54 past the caches, and with a pass over the result behind the call 105
+// and 98; 65,536 of 128,000 x 512 97 and 79, with the pass 191 and 179; 8192 of 32,000 x 1024
+// (148 MB) level.  With few rows of dy there is little to push out, and what reads the result
+// finds a part of it: 4096 of 32,000 x 1024 32 us and 37, with the pass 65 and 72.
+bool zeros_past_caches(int64_t dy, int64_t table) { return dy >= table / 8 && dy + table >= (int64_t)144 << 20; }
 // Workgroups that write zeros into n rows.
 uint32_t fill_groups(int64_t n, int cols, int n_cu) {
     const int64_t need = (n * cols + 16383) / 16384;   // 64 KB each, or more
@@ -707,7 +719,7 @@ hipError_t launch_train_embedding_backward(EmbeddingGradArgs a, const IntRows& i
                                            hipStream_t stream) {
     if (a.rows == 0 && a.accumulate) return hipSuccess;
     const GradPlan p = grad_plan(a.rows, a.n, a.cols);
-    ZeroFill z{a.dtable, a.lddt, a.cols, 0, a.n};
+    ZeroFill z{a.dtable, a.lddt, a.cols, zeros_past_caches(a.rows * a.cols * (dy_bf16 ? 2 : 4), a.n * a.cols * 4), 0, a.n};
     a.part = p.part;
     if (a.rows <= kThreads) {
         a.slabs = a.rows ? (uint32_t)((a.cols + 8 * kSmallLanes - 1) / (8 * kSmallLanes)) : 0;

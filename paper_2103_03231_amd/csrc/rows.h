@@ -178,7 +178,8 @@ __device__ __forceinline__ float lanes_all(float v) {
     return v;
 }
 
-// Over the L lanes of a row, N values at once.  Rows of several waves meet in LDS,
+// Over the L lanes of a row, N values at once, in registers: steps of a few cycles where LDS
+// would take a hundred each.  Rows of several waves meet in LDS,
 // in two places by turns: a wave that is a call ahead writes to the other one, and
 // cannot be two ahead.
 template <int L, int N, int THREADS = row_threads(L)>

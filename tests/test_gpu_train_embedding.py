@@ -162,6 +162,23 @@ def test_what_lies_between_the_rows_stays(r):
     assert torch.equal(wide[:, :cols], r.train_embedding_backward(dy, ids, n)) and (wide[:, cols:] == 7).all() and (ws[need:] == 5).all()
 
 
+@pytest.mark.parametrize("rows,n,cols,dtype", [(1000, 500, 40001, BF16), (16000, 30000, 1021, BF16), (70000, 60000, 517, BF16), (10000, 10000, 2051, F32)])
+def test_tables_larger_than_the_caches(r, rows, n, cols, dtype):
+    """Their zeros are stored another way.  Whole numbers, whose sums are exact; rows that
+    are not a multiple of 16 bytes, and what lies between them stays."""
+    dy = torch.randint(-8, 9, (rows, cols), generator=torch.Generator().manual_seed(3), dtype=torch.int8).cuda().to(dtype)
+    ids = ids_of(5, rows, n, "tokens")
+    safe = torch.where((ids >= 0) & (ids < n), ids, n)
+    wide = torch.full((n, cols + 2), float("nan"), device="cuda")
+    need = b.donerf_train_embedding_backward_workspace(r.h, rows, n, cols)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    kind = b.TYPE_FP32 if dtype is F32 else b.TYPE_BF16
+    b.donerf_train_embedding_backward(r.h, (dy.data_ptr(), cols, kind), (ids.data_ptr(), 1, b.TYPE_INT64), 1.0, (wide.data_ptr(), cols + 2, b.TYPE_FP32),
+                                      0, rows, n, cols, ws.data_ptr() if need else 0, need)
+    ref = torch.zeros(n + 1, cols, device="cuda").index_add_(0, safe, dy.float())[:-1]
+    assert torch.equal(wide[:, :cols], ref) and torch.isnan(wide[:, cols:]).all()
+
+
 def test_refusals(r):
     table, ids, dy = normal(1, 5, 8, F32), ids_of(1, 6, 5, "even"), normal(2, 6, 8, F32)
     for call in (lambda: r.train_embedding(table.half(), ids), lambda: r.train_embedding(table, ids.float()), lambda: r.train_embedding(table, ids.cpu()),

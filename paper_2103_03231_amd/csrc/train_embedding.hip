@@ -416,7 +416,7 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(EmbeddingGradArgs a)
 
 // Joins the runs that begin in 16 parts, a wave each, and go on: 256 columns a workgroup.
 // Runs of more than kLongRun further parts are summed by all waves together.  5.8 us for 5000
-// parts of 120 ids, 10 us for 2048 of tokens some of which come in hundreds of parts: round
+// parts of 120 ids, 10 us for 2048 of tokens whose commonest has a hundred parts and more: round
 // trips, of the keys, the search for a run's end and its parts.
 constexpr int kLongRun = 8;
 __global__ void __launch_bounds__(kThreads) embedding_join_kernel(EmbeddingGradArgs a) {

@@ -28,7 +28,7 @@ __device__ __forceinline__ void affine_at(const NormArgs& a, const Columns& c, i
     if (a.b) bs.load(0, k).values(b);
 }
 
-// 160,000 x 256 bf16 with y and kept: 40.5 us, 207 MB, 5.1 TB/s, the rate of a copy.  The
+// 160,000 x 256 bf16 with y and kept: 40 us, 207 MB, 5.2 TB/s, the rate of a copy.  The
 // next row is on its way while a row's three sums wait for each other: fp32 38.8 -> 37.5 us
 // at 32,768 x 1024, bf16 level; rows of more than four waves lose by it (16,384 fp32
 // columns 46 -> 53 us).

@@ -128,9 +128,10 @@ def test_vectors_flags_and_what_is_missing():
     refused(distill(weight=A + 2), "row_weight not aligned")
     refused(distill(loss=A + 2), "loss not aligned")
     refused(distill(loss=None, dx=None), "neither loss nor dx")
-    refused(lookup_backward(ws=None), "workspace is NULL")
-    refused(lookup_backward(ws=A + 8), "workspace not aligned")
-    refused(lookup_backward(ws_bytes=8), "workspace of", b.E_SIZE)
+    refused(lookup_backward(rows=1025, ws=None), "workspace is NULL")
+    refused(lookup_backward(rows=1025, ws=A + 8), "workspace not aligned")
+    refused(lookup_backward(rows=1025, ws_bytes=8), "workspace of", b.E_SIZE)
+    refused(lookup_backward(rows=1024, ws=None, ws_bytes=0), "handle is NULL")      # needs none
 
 
 def test_offsets_that_64_bits_would_not_hold():

@@ -125,6 +125,23 @@ def test_many_rows(r, rows, cols, k):
     assert ((dx.double() - grad).abs() <= 2 * w[:, None] * (400 * U * big + LEAST)).all()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,cols,k", [(140001, 64, 3), (140001, 128, 4), (66001, 61, 5), (66001, 125, 20), (66001, 250, 3), (33001, 507, 9), (16500, 1001, 33),
+                                         (8300, 2043, 70), (8300, 4090, 5), (4200, 8191, 65), (2100, 16383, 128), (1100, 20007, 64), (600, 33001, 9)])
+def test_rows_of_a_workgroup_after_its_first(r, rows, cols, k, dtype):
+    """Rows are independent of each other: a call that gives each workgroup several has the bits of calls that give it one."""
+    x, _, _, w = inputs_of(1, rows, cols, 1, dtype, pad=1)
+    g = torch.Generator().manual_seed(2)
+    c, t = torch.randint(-1, cols + 1, (rows, k), generator=g).cuda(), torch.randn(rows, k, generator=g).cuda()
+    c[::3, k - 1] = c[::3, 0]       # classes that come twice in some rows
+    loss, dx = r.train_distill(x, c, t, 2.0, w)
+    per = rows // 5 + 1
+    for at in range(0, rows, per):
+        part = slice(at, at + per)
+        loss2, dx2 = r.train_distill(x[part], c[part], t[part], 2.0, w[part])
+        assert torch.equal(loss[part], loss2) and torch.equal(dx[part], dx2)
+
+
 def test_gradient_against_differences(r):
     x, c, t, w = inputs_of(1, 3, 21, 5)
     _, dx = r.train_distill(x, c, t, 1.5, w, out=F32)

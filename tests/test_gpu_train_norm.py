@@ -178,6 +178,25 @@ def test_many_rows(r, rows, cols):
             assert torch.linalg.norm(got.double() - ref) <= 16 * U * torch.linalg.norm(mag)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,cols", [(66001, 61), (66001, 100), (33001, 250), (16500, 507), (8300, 1001), (4200, 2043), (2100, 4090), (1100, 8191),
+                                       (1100, 12003), (600, 20007), (600, 33001)])
+def test_rows_of_a_workgroup_after_its_first(r, rows, cols, dtype):
+    """Rows are independent of each other: a call that gives each workgroup several has the bits of calls that give it one."""
+    x, w, bias = rows_of(1, rows, cols, dtype, pad=1), 1 + normal(2, cols, scale=0.2), normal(3, cols)
+    y, kept, stats = r.train_norm(x, w, bias, relu=True)
+    dz = normal(4, rows, cols, dtype=BF16)
+    dx, _, _ = r.train_norm_backward(dz, x, stats, w)
+    per = rows // 5 + 1
+    for at in range(0, rows, per):
+        part = slice(at, at + per)
+        y2, kept2, stats2 = r.train_norm(x[part], w, bias, relu=True)
+        assert torch.equal(y[part], y2) and torch.equal(stats[part], stats2)
+        blocks = (cols + 31) // 32
+        assert torch.equal(kept.codes[part, :cols], kept2.codes[:, :cols]) and torch.equal(kept.scales[part, :blocks], kept2.scales[:, :blocks])
+        assert torch.equal(dx[part], r.train_norm_backward(dz[part], x[part], stats2, w)[0])
+
+
 def test_gradient_against_differences(r):
     """The whole way, forwards and backwards, with fp32 rows: central differences of the forward pass in 64 bits."""
     x, w, bias, dz = rows_of(5, 4, 37), 1 + normal(6, 37, scale=0.2), normal(7, 37), normal(8, 4, 37)
@@ -293,6 +312,13 @@ def test_refusals(r):
     with pytest.raises(b.DonerfError, match="dx overlaps"):
         b.donerf_train_norm_backward(r.h, (x.data_ptr(), 32, b.TYPE_FP32), (y.data_ptr(), 32, b.TYPE_BF16), 0, None, stats.data_ptr(),
                                      (x.data_ptr(), 32, b.TYPE_FP32), None, None, 0, 8, 32)
+    v = torch.zeros(3000 * 32, device="cuda")
+    need = b.donerf_train_norm_backward_workspace(r.h, 3000, 32)
+    assert need > 0 == b.donerf_train_norm_backward_workspace(r.h, 2048, 32)
+    for ws, size, what in ((None, need, "workspace is NULL"), (v.data_ptr() + 8, need, "workspace not aligned"), (v.data_ptr(), need - 1, "workspace of")):
+        with pytest.raises(b.DonerfError, match=what):
+            b.donerf_train_norm_backward(r.h, (v.data_ptr(), 32, b.TYPE_FP32), (v.data_ptr(), 32, b.TYPE_FP32), 0, None, v.data_ptr(), None, y.data_ptr(), None,
+                                         0, 3000, 32, ws, size)
     with torch.cuda.stream(torch.cuda.Stream()):
         with pytest.raises(ValueError, match="stream"):
             r.train_norm(x)

@@ -142,3 +142,10 @@ def test_offsets_that_64_bits_would_not_hold():
 
 def test_workspaces_without_a_handle():
     assert b.donerf_train_norm_backward_workspace(None, 4, 4) == 0 == b.donerf_train_embedding_backward_workspace(None, 4, 4, 4)
+
+
+def test_matrix_arguments_are_the_structure():
+    for m in ((A, 100, b.TYPE_BF16), (A, 1 << 40, b.MXFP8, A + 64, 8), (None, 1, b.TYPE_INT64)):
+        data, ld, kind, scales, ld_scales = m if len(m) == 5 else (*m, None, 0)
+        assert b._mat(m) == bytes(b.donerf_mat(data, ld, scales, ld_scales, kind))
+    assert b._mat(None) is None

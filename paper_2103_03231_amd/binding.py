@@ -368,6 +368,8 @@ class Renderer:
     def __init__(self, cfg: Config, weights):
         import torch
         self.torch = torch
+        # the tensors' types as the library names them
+        self._kinds = {torch.float32: TYPE_FP32, torch.bfloat16: TYPE_BF16, torch.int32: TYPE_INT32, torch.int64: TYPE_INT64}
         self.cfg = cfg
         self.h = donerf_create(cfg, weights)
         donerf_set_stream(self.h, torch.cuda.current_stream().cuda_stream)
@@ -417,8 +419,7 @@ class Renderer:
         return device
 
     def _rows(self, name, x, dtypes, shape=None, device=None):
-        t = self.torch
-        if not isinstance(x, t.Tensor) or x.dtype not in dtypes or x.dim() != 2:
+        if not isinstance(x, self.torch.Tensor) or x.dtype not in dtypes or x.dim() != 2:
             raise ValueError(f"{name} must be a 2-D tensor of {' or '.join(str(d) for d in dtypes)}")
         if x.get_device() != device:
             raise ValueError(f"{name} must be on the handle's device")
@@ -432,9 +433,7 @@ class Renderer:
             ld = cols
         if step != 1 and cols > 1 or ld < cols:
             raise ValueError(f"{name}: columns must be adjacent and rows must not overlap")
-        d = x.dtype
-        return x.data_ptr(), ld, (TYPE_FP32 if d is t.float32 else TYPE_BF16 if d is t.bfloat16 else
-                                  TYPE_INT32 if d is t.int32 else TYPE_INT64), None, 0
+        return x.data_ptr(), ld, self._kinds[x.dtype], None, 0
 
     def _ids(self, ids, device):
         """A vector of whole numbers, of any stride, as a matrix argument of one column."""
@@ -443,11 +442,12 @@ class Renderer:
             raise ValueError("ids must be a 1-D tensor of torch.int32 or torch.int64")
         if ids.get_device() != device:
             raise ValueError("ids must be on the handle's device")
-        n = ids.shape[0]
-        ld = ids.stride(0) if n > 1 else 1
-        if ld < 1:
+        (n,), (ld,) = ids.shape, ids.stride()
+        if n <= 1:
+            ld = 1
+        elif ld < 1:
             raise ValueError("ids must not share memory with each other")
-        return ids.data_ptr(), ld, TYPE_INT32 if ids.dtype is t.int32 else TYPE_INT64, None, 0
+        return ids.data_ptr(), ld, self._kinds[ids.dtype], None, 0
 
     def _out(self, out, default):
         """The type of a new result."""
@@ -483,8 +483,8 @@ class Renderer:
         if v is None:
             return None
         t = self.torch
-        if not (isinstance(v, t.Tensor) and v.dtype is t.float32 and v.get_device() == device and v.dim() == 1
-                and v.shape[0] == n and v.is_contiguous()):
+        if not (isinstance(v, t.Tensor) and v.dtype is t.float32 and v.get_device() == device and v.shape == (n,)
+                and v.is_contiguous()):
             raise ValueError(f"{name} must be a contiguous float32 tensor of {n} on the handle's device")
         return v.data_ptr()
 
@@ -492,6 +492,10 @@ class Renderer:
         """A new matrix and itself as an argument."""
         y = self.torch.empty_strided((rows, cols), (cols, 1), dtype=dtype, device=device)   # cheaper than empty
         return y, (y.data_ptr(), cols, TYPE_FP32 if dtype is self.torch.float32 else TYPE_BF16, None, 0)
+
+    def _new_vector(self, n, device):
+        v = self.torch.empty_strided((n,), (1,), dtype=self.torch.float32, device=device)
+        return v, v.data_ptr()
 
     def _mx_new(self, rows, cols, format, device):
         empty, u8 = self.torch.empty_strided, self.torch.uint8
@@ -640,9 +644,10 @@ class Renderer:
         add = dw is not None
         if add != (db is not None):
             raise ValueError("dw and db are given together or not at all")
-        if not add:
-            dw, db = t.empty(cols, dtype=t.float32, device=dev), t.empty(cols, dtype=t.float32, device=dev)
-        pdw, pdb = self._vector("dw", dw, cols, dev), self._vector("db", db, cols, dev)
+        if add:
+            pdw, pdb = self._vector("dw", dw, cols, dev), self._vector("db", db, cols, dev)
+        else:
+            (dw, pdw), (db, pdb) = self._new_vector(cols, dev), self._new_vector(cols, dev)
         dx, mdx = self._new(rows, cols, self._out(out, t.bfloat16), dev) if need_dx else (None, None)
         need = donerf_train_norm_backward_workspace(self.h, rows, cols)
         ws = self._workspace(need, dev)
@@ -699,9 +704,9 @@ class Renderer:
         if classes.shape[0] != rows:
             raise ValueError(f"x has {rows} rows and classes {classes.shape[0]}")
         pw = self._vector("row_weight", row_weight, rows, dev)
-        loss = t.empty(rows, dtype=t.float32, device=dev)
+        loss, pl = self._new_vector(rows, dev)
         dx, mdx = self._new(rows, cols, self._out(out, t.bfloat16), dev) if need_dx else (None, None)
-        donerf_train_distill(self.h, mx, mc, mt, pw, temperature, loss.data_ptr(), mdx, rows, cols, k)
+        donerf_train_distill(self.h, mx, mc, mt, pw, temperature, pl, mdx, rows, cols, k)
         return loss, dx
 
     def mfma_peak(self, workgroups, iters):

@@ -342,6 +342,7 @@ struct EmbeddingGradArgs {
     const uint32_t* order;
     float* ends;             // sums of runs that cross the parts' ends
     uint32_t part;           // sorted rows of a part
+    int32_t block_bits;      // parts that one workgroup sums, as a power of two
     uint32_t slabs;          // workgroups that sum, where one launch does all
 };
 size_t embedding_backward_workspace(int64_t rows, int64_t n, int cols);

@@ -397,25 +397,68 @@ __device__ __forceinline__ void sum_runs(const EmbeddingGradArgs& a, const RowsI
 // Parts of `part` sorted rows, 8 L columns a workgroup: what comes from the part before is
 // left in ends[2 p], what goes on into the next one in ends[2 p + 1].  160,000 rows of 256 bf16
 // columns 17 us, 82 MB, 4.8 TB/s.
+// A workgroup's parts are a block.  One that is all of one id, before and behind it as well,
+// leaves the sum of its parts as that of the first: long runs have fewer to join.
 template <class T, int L>
 __global__ void __launch_bounds__(256) embedding_sum_kernel(EmbeddingGradArgs a) {
-    const int lane = threadIdx.x % L;
-    const int64_t p = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
-    const int k = 8 * (int)(blockIdx.y * L + lane);
+    constexpr int kParts = 256 / L;
+    __shared__ float lds[kParts][8 * L], lds1[kParts][8];
+    const int lane = threadIdx.x % L, group = threadIdx.x / L;
+    const int64_t p0 = (int64_t)blockIdx.x * kParts, p = p0 + group;
+    const int k0 = 8 * (int)(blockIdx.y * L), k = k0 + 8 * lane;
     const RowsIn<T> dy((const T*)a.dy, a.lddy, a.cols);
     const Columns& c = dy.c;
     const bool single = blockIdx.y == 0 && c.has_single(lane);
-    if (p * a.part >= a.rows || !(c.has(k) || single)) return;
-    const uint32_t first = (uint32_t)(p * a.part), end = (uint32_t)a.rows - first < a.part ? (uint32_t)a.rows : first + a.part;
-    sum_runs(a, dy, a.keys, a.order, first, end, k, lane, single, [&](int which, const float* sum, float sum1) {
-        float* const to = a.ends + (2 * p + which) * a.cols;
-        if (c.has(k)) __builtin_memcpy(to + k, sum, 32);
-        if (single) to[c.single(lane)] = sum1;
-    });
+    const int64_t begin = p0 * a.part, behind = (p0 + kParts) * a.part;
+    const bool whole = begin > 0 && behind < a.rows && a.keys[begin - 1] == a.keys[behind];   // the same for all
+    if (p * a.part < a.rows && (c.has(k) || single)) {
+        const uint32_t first = (uint32_t)(p * a.part), end = (uint32_t)a.rows - first < a.part ? (uint32_t)a.rows : first + a.part;
+        sum_runs(a, dy, a.keys, a.order, first, end, k, lane, single, [&](int which, const float* sum, float sum1) {
+            if (whole) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) lds[group][8 * lane + i] = sum[i];
+                if (single) lds1[group][lane] = sum1;
+                return;
+            }
+            float* const to = a.ends + (2 * p + which) * a.cols;
+            if (c.has(k)) __builtin_memcpy(to + k, sum, 32);
+            if (single) to[c.single(lane)] = sum1;
+        });
+    }
+    if (!whole || a.keys[behind] >= a.n) return;
+    __syncthreads();
+    float* const to = a.ends + 2 * p0 * a.cols;
+    for (int t = threadIdx.x; t < 8 * L && c.has(k0 + t); t += 256) {
+        float sum = lds[0][t];
+#pragma unroll
+        for (int g = 1; g < kParts; ++g) sum += lds[g][t];
+        to[k0 + t] = sum;
+    }
+    if (group == 0 && single) {
+        float sum = lds1[0][lane];
+        for (int g = 1; g < kParts; ++g) sum += lds1[g][lane];
+        to[c.single(lane)] = sum;
+    }
 }
 
+// Where a run's sums are: parts p + 1 up to last, but for one of each block (of 2^bits
+// parts) that they hold with the part behind it.
+struct Run {
+    int64_t first, head, blocks, n;   // first part; parts before the blocks, blocks, sums in all
+    int bits;
+    __device__ __forceinline__ Run(int64_t p, int64_t last, int b) : first(p + 1), bits(b) {
+        const int64_t start = ((p >> bits) + 1) << bits;   // of the first block behind p
+        blocks = start < last ? (last - start) >> bits : 0;
+        head = blocks ? start - first : last - p;
+        n = last - p - (blocks << bits) + blocks;
+    }
+    // The part of sum i.
+    __device__ __forceinline__ int64_t part(int64_t i) const {
+        return first + (i < head ? i : i < head + blocks ? head + ((i - head) << bits) : i + (blocks << bits) - blocks);
+    }
+};
 // Joins the runs that begin in 16 parts, a wave each, and go on: 256 columns a workgroup.
-// Runs of more than kLongRun further parts are summed by all waves together.  5.8 us for 5000
+// Runs of more than kLongRun further sums are added up by all waves together.  5.8 us for 5000
 // parts of 120 ids, 10 us for 2048 of tokens whose commonest has a hundred parts and more: round
 // trips, of the keys, the search for a run's end and its parts.
 constexpr int kLongRun = 8;
@@ -459,16 +502,16 @@ __global__ void __launch_bounds__(kThreads) embedding_join_kernel(EmbeddingGradA
             for (int i = 0; i < 4; ++i) v[i] = k + i < a.cols ? from[i] : 0.0f;
         }
     };
-    // adds the beginnings of parts from, from + step, ..., up to `to`, kLongRun at a time
-    auto add = [&](float* sum, int64_t from, int64_t to, int step) {
-        for (; from <= to; from += kLongRun * step) {
+    // adds a run's sums from, from + step, ..., kLongRun at a time
+    auto add = [&](float* sum, const Run& run, int64_t from, int step) {
+        for (; from < run.n; from += kLongRun * step) {
             float v[kLongRun][4];
 #pragma unroll
             for (int j = 0; j < kLongRun; ++j)
-                if (from + j * step <= to) load(v[j], from + j * step, 0);
+                if (from + j * step < run.n) load(v[j], run.part(from + j * step), 0);
 #pragma unroll
             for (int j = 0; j < kLongRun; ++j)
-                if (from + j * step <= to)
+                if (from + j * step < run.n)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) sum[i] += v[j][i];
         }
@@ -490,7 +533,8 @@ __global__ void __launch_bounds__(kThreads) embedding_join_kernel(EmbeddingGradA
         }
     };
     __syncthreads();
-    if (last - p > kLongRun) {
+    const Run own(p, last, a.block_bits);
+    if (own.n > kLongRun) {
         if (lane == 0) {
             first_of[wave] = p, last_of[wave] = last, id_of[wave] = cur;
             atomicOr(&longs, 1u << wave);
@@ -498,7 +542,7 @@ __global__ void __launch_bounds__(kThreads) embedding_join_kernel(EmbeddingGradA
     } else if (last > p) {
         float sum[4];
         load(sum, p, 1);
-        add(sum, p + 1, last, 1);
+        add(sum, own, 0, 1);
         finish(sum, cur);
     }
     __syncthreads();
@@ -506,7 +550,7 @@ __global__ void __launch_bounds__(kThreads) embedding_join_kernel(EmbeddingGradA
         const int w = __ffs(left) - 1;
         float sum[4] = {0, 0, 0, 0};
         if (wave == 0) load(sum, first_of[w], 1);
-        add(sum, first_of[w] + 1 + wave, last_of[w], kWaves);
+        add(sum, Run(first_of[w], last_of[w], a.block_bits), wave, kWaves);
 #pragma unroll
         for (int i = 0; i < 4; ++i) lds[wave][4 * lane + i] = sum[i];
         __syncthreads();
@@ -691,7 +735,8 @@ GradPlan grad_plan(int64_t rows, int64_t n, int cols) {
 }
 
 template <class T, int L>
-hipError_t sum_launch(const EmbeddingGradArgs& a, uint32_t parts, hipStream_t s) {
+hipError_t sum_launch(EmbeddingGradArgs a, uint32_t parts, hipStream_t s) {
+    a.block_bits = __builtin_ctz(256 / L);
     const uint32_t slabs = (uint32_t)((a.cols + 8 * L - 1) / (8 * L));
     hipLaunchKernelGGL((embedding_sum_kernel<T, L>), dim3((parts + 256 / L - 1) / (256 / L), slabs), dim3(256), 0, s, a);
     hipError_t e = hipGetLastError();

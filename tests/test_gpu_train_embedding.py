@@ -92,7 +92,8 @@ def test_gradient(r, rows, n, cols, spread):
 
 @pytest.mark.parametrize("rows,n,cols,spread", [(160001, 120, 40, "even"), (50000, 1, 256, "same"), (70000, 32000, 72, "tokens"), (100000, 3, 31, "runs"),
                                                 (300000, 1 << 20, 8, "even"), (140000, (1 << 20) + 5, 4, "tokens"), (2000003, 1000, 3, "even"),
-                                                (3000001, 900, 4, "tokens"), (2300000, 2, 9, "runs"), (150000, 2, 20, "same")])
+                                                (3000001, 900, 4, "tokens"), (2300000, 2, 9, "runs"), (150000, 2, 20, "same"),
+                                                (40000, 3, 603, "runs"), (20011, 1, 137, "same"), (30000, 5, 97, "runs")])
 def test_many_rows(r, rows, n, cols, spread):
     """Several tiles of the sort and parts of the sums, in 64 bits on the GPU."""
     for dtype in (BF16, F32):

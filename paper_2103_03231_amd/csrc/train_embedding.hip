@@ -263,7 +263,8 @@ __global__ void __launch_bounds__(kThreads) sort_scatter_kernel(SortPass s, Zero
 // bits, and knows from the others' number where they go: equal keys end up side by side,
 // which is all that the sums ask for.  The remaining workgroups write zeros meanwhile: 16,384
 // keys of 32,000 beside 131 MB 24.3 us, 5.4 TB/s.  Against counts and moves in two passes whole
-// calls are shorter: 1500 rows of 32,000 21 us for 25, 16,000 of 60,000 25 for 32.
+// calls are shorter: 1500 rows of 32,000 x 256 20.5 us for 30, 4096 of 32,000 x 1024 31 for 43,
+// 16,000 of 60,000 x 64 24.5 for 31.
 template <int ITEMS>
 struct BucketLds {
     SortLds sort;
@@ -703,8 +704,8 @@ GradPlan grad_plan(int64_t rows, int64_t n, int cols) {
     p.tiles = (uint32_t)((rows + p.tile - 1) / p.tile);
     p.at_once = rows <= kMostSortedAtOnce && bits <= kMostBucketBits + kSortBits;
     if (p.at_once) {
-        // so many buckets that one pass sorts each, and that they hold 256 keys or so (16,384 keys of
-        // 32,000 beside 131 MB of zeros 30.4 us, 31.7 with 1024 each)
+        // so many buckets that one pass sorts each, and that they hold 256 keys or so (level with 1024
+        // each where zeros are written beside them)
         p.bucket_bits = bits > kSortBits ? bits - kSortBits : 0;
         while (p.bucket_bits < bits - 1 && p.bucket_bits < 7 && (kThreads / 4) << p.bucket_bits < rows) ++p.bucket_bits;
         p.bits = bits - p.bucket_bits;
@@ -755,10 +756,11 @@ hipError_t sum_by_width(const EmbeddingGradArgs& a, const GradPlan& p, hipStream
 // Whether zeros pass the caches (bytes of dy and of the table).  Where both do not fit into
 // the last level beside what else is there (256 MB in all), zeros that stay push dy out of it
 // and are themselves pushed out while the sums read and write: 24,000 rows of 32,000 x 1024
-// (49 and 131 MB) 67 us, 54 past the caches, and with a pass over the result behind the call 105
-// and 98; 65,536 of 128,000 x 512 97 and 79, with the pass 191 and 179; 8192 of 32,000 x 1024
-// (148 MB) level.  With few rows of dy there is little to push out, and what reads the result
-// finds a part of it: 4096 of 32,000 x 1024 32 us and 37, with the pass 65 and 72.
+// (49 and 131 MB) 65 us, 52 past the caches, and with a pass over the result behind the call 103
+// and 95; 65,536 of 128,000 x 512 95 and 78, with the pass 190 and 178; 8192 of 32,000 x 1024
+// (148 MB) 38 and 40, with the pass 80 and 82.  With few rows of dy there is little to push out,
+// and what reads the result finds a part of it: 4096 of 32,000 x 1024 31 us and 37, with the pass
+// 65 and 72.
 bool zeros_past_caches(int64_t dy, int64_t table) { return dy >= table / 8 && dy + table >= (int64_t)144 << 20; }
 // Workgroups that write zeros into n rows.
 uint32_t fill_groups(int64_t n, int cols, int n_cu) {

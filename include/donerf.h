@@ -555,7 +555,9 @@ size_t donerf_train_embedding_backward_workspace(const donerf_t* h, int64_t rows
  * A row of weight 0, without a given entry above -inf or without a class above -inf
  * has no loss and no gradient (0), whatever else it holds.  A class of probability 0
  * that an entry asks for makes the loss infinite; NaN and +inf make it NaN.
- * fp32 arithmetic.  rows 0..2^31 - 1 (0: nothing is done), cols 1..DONERF_MAX_COLS,
+ * fp32 arithmetic.  At temperatures above 4, where p and q come close to each other, loss
+ * and gradient are made of their differences, so that they keep fp32's precision.
+ * rows 0..2^31 - 1 (0: nothing is done), cols 1..DONERF_MAX_COLS,
  * k 1..DONERF_MAX_TOP.
  * Errors: as for donerf_train_norm.
  */

@@ -249,3 +249,141 @@ def test_refusals(r):
     with torch.cuda.stream(torch.cuda.Stream()):
         with pytest.raises(ValueError, match="stream"):
             r.train_distill(x, c, t)
+
+
+# ---- high temperatures: p and q are close to each other, and the loss, T^2 times a sum of their
+# differences' squares, is as large as ever
+
+def reference(x, classes, t, temp, weight):
+    """(loss, dx, the bounds of both without a final rounding) of one row, in 80 bits: those of 64, times T^2, are themselves off by
+    parts in a million."""
+    x, t = x.astype(np.longdouble), t.astype(np.longdouble)
+    given = (classes >= 0) & (classes < len(x))
+    c, t = classes[given], t[given]
+    un, tn = (x - x.max()) / temp, (t - t.max()) / temp
+    e, f = np.exp(un), np.exp(tn)
+    keep = f > 2.0 ** -126
+    c, tn, f = c[keep], tn[keep], f[keep]
+    sq, sp = e.sum(), f.sum()
+    p, q = f / sp, e / sq
+    delta = tn - un[c] - (np.log(sp) - np.log(sq))
+    loss, grad = (p * delta).sum(), q.copy()
+    np.add.at(grad, c, -p)
+    # an argument is off by 3u (difference, 1/T and product), an exponential by 2u more, a sum by SUM
+    _, first = np.unique(c, return_index=True)
+    first = np.isin(np.arange(len(c)), first)
+    rest = np.ones(len(x), bool)
+    rest[c] = False
+    au, at = np.where(np.isfinite(un), np.abs(un), 0), np.abs(tn)
+    rel_q, rel_p = (e * (3 * U * au + 2 * U)).sum() / sq + SUM + 2 * U, (f * (3 * U * at + 2 * U)).sum() / sp + SUM + 2 * U
+    # sp - sq: below 1 an expm1 is off by 3u and 2u of its argument at most; classes without an entry, and entries of a class that has
+    # another, come as they are
+    apart = (5 * U + SUM) * (at + au[c])[first].sum() + ((3 * U * at + 2 * U + SUM) * f)[~first].sum() + (e * (3 * U * au + 2 * U + SUM))[rest].sum()
+    z = (sp - sq) / sq
+    by_ratio = 2 * (apart / sq + abs(z) * (rel_q + 3 * U)) + 2 * U * abs(np.log1p(z))
+    by_logs = rel_p + rel_q + 3 * U * (abs(np.log(sp)) + abs(np.log(sq)))
+    of_log = by_ratio if abs(z) < 0.49 else by_logs if abs(z) > 0.51 else max(by_ratio, by_logs)
+    ed = 3 * U * (at + au[c]) + 2 * U * (at + au[c] + abs(np.log(sp / sq))) + of_log
+    ep, eq, ad = p * (rel_p + 3 * U * at + 4 * U), q * (rel_q + 3 * U * au + 4 * U), np.abs(delta)
+    # e^-d - 1 + d is off by 10 roundings, and by its slope, below 1.7 |d|, times the error of d; further off it is the difference itself
+    close, far = ad < 0.51, ad > 0.49
+    of_terms = np.where(close, (ep + 12 * U * p) * ad ** 2 + p * (1.7 * ad * ed + ed ** 2), 0) + np.where(far, (ep + 3 * U * p) * (ad + 1) + p * ed + eq[c] + 2 * U * q[c], 0)
+    of_grad = np.where(close, (ep + 12 * U * p) * 1.4 * ad + 1.7 * p * ed, 0) + np.where(far, ep + eq[c] + 2 * U * (p + q[c]), 0)
+    terms = np.abs(p * delta + q[c] - p)
+    more = (e[c][~first]).sum() / sq
+    bl = of_terms.sum() + SUM * terms.sum() + eq[rest].sum() + SUM * (q[rest].sum() + more) + eq[c][~first].sum() + rel_q * (q[rest].sum() + more) + 4 * U * abs(loss)
+    bd = np.where(rest, eq, 0)
+    np.add.at(bd, c, of_grad + (0 if first.all() else ep + (len(c) + 4) * U * p))
+    if not first.all():
+        bd += eq
+    w = abs(float(weight))
+    return [np.asarray(v, np.float64) for v in (weight * temp ** 2 * loss, weight * temp * grad, w * temp ** 2 * bl, w * temp * (bd + 4 * U * np.abs(grad) + LEAST))]
+
+
+def check_high(r, x, classes, t, temp, weight):
+    vx, vc, vt, vw = f64(x), classes.cpu().numpy(), f64(t), f64(weight)
+    for out in (F32, BF16):
+        loss, dx = r.train_distill(x, classes, t, temp, weight, out=out)
+        for i in range(len(vx)):
+            ref_l, ref_d, bl, bd = reference(vx[i], vc[i], vt[i], temp, vw[i])
+            assert abs(float(loss[i]) - ref_l) <= bl + U * abs(ref_l), (i, float(loss[i]), ref_l, bl)
+            assert (np.abs(f64(dx[i]) - ref_d) <= bd + HALF[out] * (np.abs(ref_d) + bd)).all(), (i, np.abs(f64(dx[i]) - ref_d).max())
+        again = r.train_distill(x, classes, t, temp, weight, out=out)
+        assert torch.equal(loss, again[0]) and torch.equal(dx, again[1])
+
+
+FULL = [(40, 1, 1), (30, 3, 3), (20, 8, 8), (20, 9, 9), (20, 24, 24), (20, 64, 64), (20, 61, 61), (12, 65, 65), (12, 128, 128), (9, 125, 125), (12, 100, 90),
+        (9, 200, 128), (5, 283, 33), (4, 700, 128), (4, 1500, 50), (3, 3000, 128), (3, 7001, 7), (2, 16384, 128), (2, 20007, 64), (1, 32000, 9),
+        (2, 40001, 128), (1, 65536, 3)]
+
+
+@pytest.mark.parametrize("temp", [4.5, 64.0, 4096.0, 65536.0])
+@pytest.mark.parametrize("rows,cols,k", FULL)
+def test_high_temperatures(r, rows, cols, k, temp):
+    for dtype in (F32, BF16):
+        x, c, t, w = inputs_of(rows + cols, rows, cols, k, dtype, pad=1)
+        check_high(r, x, c, t, temp, w)
+        # all probability with the entries' classes: the others masked, by either value
+        rest = torch.ones_like(x, dtype=torch.bool).scatter(1, c, False)
+        for low in (-INF, torch.finfo(dtype).min):
+            check_high(r, torch.where(rest, low, x), c, t, temp, w)
+        x, c, t, w = inputs_of(rows + cols + 1, rows, cols, k, dtype, torch.int32, twice=True)
+        check_high(r, x, c, t, temp, w)
+        t[:, ::3] = torch.where(torch.arange(k, device="cuda")[::3] > 0, torch.finfo(F32).min, t[:, ::3])       # entries without probability
+        check_high(r, x, c, t, temp, w)
+
+
+@pytest.mark.parametrize("temp", [8.0, 4096.0])
+def test_high_temperature_of_equal_and_near_logits(r, temp):
+    """A student that has its teacher's logits has no loss and no gradient; one next to it a positive loss."""
+    for cols in (5, 64, 100, 128):
+        x, _, _, w = inputs_of(cols, 30, cols, 1)
+        c = torch.stack([torch.randperm(cols, generator=torch.Generator().manual_seed(i)) for i in range(30)]).cuda()
+        loss, dx = r.train_distill(x, c, x.gather(1, c), temp, w, out=F32)
+        # sums of the same terms in two orders: delta is a rounding or two of their size
+        size = f64(x.max(1).values - x.min(1).values) / temp
+        assert (np.abs(f64(loss)) <= temp ** 2 * f64(w) * (SUM * size) ** 2).all() and (np.abs(f64(dx)).max(1) <= temp * f64(w) * SUM * size).all()
+        loss, _ = r.train_distill(x, c, x.gather(1, c) * 1.01, temp, w)
+        assert (loss > 0).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,cols,k", [(140001, 64, 3), (140001, 128, 4), (66001, 61, 5), (66001, 125, 20), (66001, 250, 3), (33001, 507, 9), (16500, 1001, 33),
+                                         (8300, 2043, 70), (8300, 4090, 5), (4200, 8191, 65), (2100, 16383, 128), (1100, 20007, 64), (600, 33001, 9)])
+def test_rows_after_a_workgroups_first_at_high_temperatures(r, rows, cols, k, dtype):
+    x, _, _, w = inputs_of(1, rows, cols, 1, dtype, pad=1)
+    g = torch.Generator().manual_seed(2)
+    c, t = torch.randint(-1, cols + 1, (rows, k), generator=g).cuda(), torch.randn(rows, k, generator=g).cuda()
+    c[::3, k - 1] = c[::3, 0]
+    w[::7] = 0
+    loss, dx = r.train_distill(x, c, t, 32.0, w)
+    per = rows // 5 + 1
+    for at in range(0, rows, per):
+        part = slice(at, at + per)
+        loss2, dx2 = r.train_distill(x[part], c[part], t[part], 32.0, w[part])
+        assert torch.equal(loss[part], loss2) and torch.equal(dx[part], dx2)
+    only, none = r.train_distill(x, c, t, 32.0, w, need_dx=False)
+    assert none is None and torch.equal(loss, only)
+
+
+def test_edges_at_high_temperatures(r):
+    nan = float("nan")
+    for cols in (6, 90, 700, 3000, 40000):
+        x, c, t, _ = inputs_of(4, 10, cols, 2)
+        w = torch.ones(10, device="cuda")
+        x[0, c[0, 1]] = -INF      # an entry of a class without probability
+        x[1, 0] = nan
+        x[2, cols - 1] = INF
+        t[3, 1] = nan
+        t[4, 0] = INF
+        c[5], t[5] = torch.tensor([-1, cols]), nan
+        t[6] = -INF
+        x[7] = -INF
+        w[8], x[8], t[8] = 0.0, nan, nan
+        for out in (F32, BF16):
+            loss, dx = r.train_distill(x, c, t, 1000.0, w, out=out)
+            assert loss[0] == INF and torch.isfinite(dx[0]).all() and dx[0, c[0, 1]] < 0
+            assert torch.isnan(loss[1:5]).all() and torch.isnan(dx[1]).all() and torch.isnan(dx[2]).all()
+            assert torch.isnan(dx[3].gather(0, c[3])).all() and torch.isnan(dx[4].gather(0, c[4])).all()
+            assert (loss[5:9] == 0).all() and (dx[5:9] == 0).all()
+            assert loss[9] > 0 and torch.isfinite(dx[9]).all() and (dx[9] != 0).any()

@@ -461,7 +461,8 @@ size_t donerf_train_linear_backward_workspace(const donerf_t* h, int64_t rows, i
  *   y      rows x cols, FP32 or BF16, or NULL
  *   kept   rows x cols, MXFP8, or NULL; one of the two at least
  *   stats  device, rows x 2 fp32, aligned to 8 bytes: m and r, for the backward pass
- * Sums and stats are fp32.  Where a row's squares do not fit fp32, r is 0.
+ * Sums and stats are fp32.  Where the sum of a row's (x - m)^2 does not fit fp32, r is 0,
+ * and m too if it is 2^102 or more: z is the bias, and the backward pass finds no gradient.
  * rows 0..2^31 - 1 (0: nothing is done), cols 1..DONERF_MAX_COLS.
  * Errors: E_INVALID_ARG (NULL handle, x or stats, a size, type, alignment or value
  * that the above rules out, an output that shares memory), E_DEVICE, E_HIP.

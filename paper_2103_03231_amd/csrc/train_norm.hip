@@ -4,6 +4,8 @@
 //             y = act(z): one pass, the row in registers between its sums.  The
 //             first sum's mean is off by its roundings; the differences to it give
 //             what it lacks, so that rows far from zero, or of one value, are exact.
+//             It is of the values times 2^-17: 65,536 of them do not overflow.  Where
+//             their squares do, r = 0, and m is one that x - m is finite with: xh is 0.
 //   backward  with xh = (x - m) r and g = dz w:
 //             dx = r (g - mean(g) - xh mean(g xh)), dw = sum over rows of dz xh,
 //             db = that of dz.  Each workgroup adds up dw and db of its rows in
@@ -16,6 +18,11 @@
 
 namespace donerf {
 namespace {
+
+constexpr float kLargest = 0x1.fffffep127f;   // finite
+// A row's mean as xh takes it: 0 where r is 0 and a finite value less the mean might not be
+// finite (2^102 is a quarter of the largest value's last place).
+__device__ __forceinline__ float centre_of(float mean, float r) { return r == 0.0f && __builtin_fabsf(mean) >= 0x1p102f ? 0.0f : mean; }
 
 // ---------------------------------------------------------------- forward
 
@@ -67,26 +74,31 @@ __global__ void __launch_bounds__(row_threads(L)) norm_kernel(NormArgs a) {
         for (int j = 0; j < C; ++j) raw[j] = next[j];
         const float one = one_next;
         if (kAhead && r0 + step < a.rows) load(r0 + step);
-        auto total = [&](auto f) {   // of f over the row's values
-            float sum = c.has_single(lane) ? f(one) : 0.0f;
+        auto total = [&](auto add) {   // over the row's values; add: a sum and a value
+            float sum = c.has_single(lane) ? add(0.0f, one) : 0.0f;
 #pragma unroll
             for (int j = 0; j < C; ++j) {
                 if (c.has(8 * (lane + L * j))) {
                     float v[8];
                     raw[j].values(v);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) sum += f(v[i]);
+                    for (int i = 0; i < 8; ++i) sum = add(sum, v[i]);
                 }
                 raw[j].hold();
             }
-            return reduce.template one<Add>(sum) * a.inv_cols;
+            return reduce.template one<Add>(sum);
         };
-        const float first = total([](float v) { return v; });
-        const float mean = first + total([&](float v) { return v - first; });
-        const float var = total([&](float v) { return (v - mean) * (v - mean); });
-        const float r = __builtin_amdgcn_rsqf(var + a.eps);
+        // (times a power of two: the bits of the plain sum, where that is finite)
+        const float sum = total([](float s, float v) { return __builtin_fmaf(v, 0x1p-17f, s); });
+        const float first = __builtin_amdgcn_fmed3f(sum * (a.inv_cols * 0x1p17f), -kLargest, kLargest);
+        const float rest = total([&](float s, float v) { return s + (v - first); }) * a.inv_cols;
+        // where only the differences overflow, the first mean is as good as fp32 has it; where a
+        // value is not finite the mean is NaN
+        const float mean = first + (__builtin_fabsf(rest) <= kLargest ? rest : sum - sum);
+        const float var = total([&](float s, float v) { return s + (v - mean) * (v - mean); }) * a.inv_cols;
+        const float r = __builtin_amdgcn_rsqf(var + a.eps), centre = centre_of(mean, r);
         if (!live) continue;   // behind the last sum of this row
-        if (lane == 0) *(f32x2*)(a.stats + 2 * row) = f32x2{mean, r};
+        if (lane == 0) *(f32x2*)(a.stats + 2 * row) = f32x2{centre, r};
         float tail[8];   // kept values: the chunk that is not whole, by the lane whose turn it is
         if constexpr (KEEP) {
 #pragma unroll
@@ -95,7 +107,7 @@ __global__ void __launch_bounds__(row_threads(L)) norm_kernel(NormArgs a) {
 #pragma unroll
                 for (int i = 0; i < 7; ++i) {
                     const int k = c.whole + i < a.cols ? c.whole + i : a.cols - 1;
-                    const float xh = (value_of(x.base[row * x.ld + k]) - mean) * r;
+                    const float xh = (value_of(x.base[row * x.ld + k]) - centre) * r;
                     const float z = act(__builtin_fmaf(xh, a.w ? a.w[k] : 1.0f, a.b ? a.b[k] : 0.0f));
                     tail[i] = c.whole + i < a.cols ? z : 0.0f;
                 }
@@ -109,7 +121,7 @@ __global__ void __launch_bounds__(row_threads(L)) norm_kernel(NormArgs a) {
             if constexpr (!kHeld) affine_at(a, c, k, wj, bj);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                v[i] = act(__builtin_fmaf((v[i] - mean) * r, kHeld ? w[kHeld ? j : 0][i] : wj[i], kHeld ? b[kHeld ? j : 0][i] : bj[i]));
+                v[i] = act(__builtin_fmaf((v[i] - centre) * r, kHeld ? w[kHeld ? j : 0][i] : wj[i], kHeld ? b[kHeld ? j : 0][i] : bj[i]));
             if (a.y.base && c.has(k)) store8(a.y, row, k, v);
             if constexpr (KEEP) {
                 if (!c.has(k))
@@ -120,7 +132,7 @@ __global__ void __launch_bounds__(row_threads(L)) norm_kernel(NormArgs a) {
         }
         if (c.has_single(lane) && a.y.base) {
             const int k = c.single(lane);
-            store1(a.y, row, k, act(__builtin_fmaf((one - mean) * r, a.w ? a.w[k] : 1.0f, a.b ? a.b[k] : 0.0f)));
+            store1(a.y, row, k, act(__builtin_fmaf((one - centre) * r, a.w ? a.w[k] : 1.0f, a.b ? a.b[k] : 0.0f)));
         }
     }
 }

@@ -322,3 +322,83 @@ def test_refusals(r):
     with torch.cuda.stream(torch.cuda.Stream()):
         with pytest.raises(ValueError, match="stream"):
             r.train_norm(x)
+
+
+BIG = torch.finfo(F32).max
+
+
+@pytest.mark.parametrize("cols", [1, 3, 8, 40, 61, 283, 1000, 2051, 4096, 9001, 16385, 32000, 65536])
+def test_rows_whose_sums_and_squares_do_not_fit(r, cols):
+    """Finite rows of any size: of one value they are exact; of values whose squares overflow r is 0, and z the bias."""
+    half = cols - cols // 2
+    x = rows_of(1, 10, cols)
+    plain, kept0, stats0 = r.train_norm(x[7:], None, None, out=F32)
+    x[0], x[1], x[2] = 1e38, -BIG, BIG
+    x[3] = normal(2, cols) * 1e37                                          # squares
+    x[4] = 3e38
+    x[4, half:] = -3e38                                                    # differences, too
+    x[5] = -1e30
+    x[5, 0] = 2e30
+    x[6] = 3e38                                                            # and the sum
+    x[6, 0] = 2.5e38
+    bias = normal(3, cols)
+    mean = x.double().mean(1)
+    overflow = (x.double() - mean[:, None]).square().sum(1) > float(BIG)
+    for dtype in (F32, BF16):
+        v = x.to(dtype)
+        if dtype is BF16:
+            v[1], v[2] = torch.finfo(BF16).min, torch.finfo(BF16).max
+        mean = v.double().mean(1)
+        y, kept, stats = r.train_norm(v, None, bias, out=F32)
+        one = [0, 1, 2] if cols > 1 else list(range(7))
+        assert torch.equal(stats[one, 0], v[one, 0].float()) and torch.allclose(stats[one, 1], torch.full((len(one),), 1e-5 ** -0.5, device="cuda"), rtol=4 * U, atol=0)
+        assert torch.equal(y[:7], bias.expand(7, cols)) or cols == 1
+        assert torch.equal(y[one], bias.expand(len(one), cols))
+        if cols > 1:
+            assert (stats[3:7, 1] == 0).all() and overflow[3:7].all()
+            # the mean, by the bound of a sum and its correction, with |x| summed; 0 where differences to it may overflow
+            near = torch.where(mean[3:7].abs() < 2.0 ** 102, mean[3:7], 0)
+            assert ((stats[3:7, 0].double() - near).abs() <= (2 * SUM + 8 * U) * v[3:7].double().abs().mean(1)).all()
+        assert torch.isfinite(r.mx_dequantize(kept, F32)).all()
+        if dtype is F32:
+            again = r.train_norm(x[7:], None, None, out=F32)
+            assert torch.equal(again[0], plain) and torch.equal(again[2], stats0) and torch.equal(stats[7:], stats0)
+        # backwards: no part in dw, no gradient where r is 0
+        dz = normal(4, 10, cols)
+        for x_in in (v, r.mx_quantize(v.clamp(-1e38, 1e38), b.MXFP8)):
+            dx, dw, db = r.train_norm_backward(dz, x_in, stats, None, out=F32)
+            assert torch.isfinite(dx).all() or x_in is not v      # (8 bits do not hold the rows of one value)
+            if cols > 1:
+                assert (dx[3:7] == 0).all()
+            if x_in is v:
+                ref = r.train_norm_backward(dz[7:], v[7:], stats[7:], None, out=F32)
+                assert torch.equal(dx[7:], ref[0]) and torch.isfinite(dw).all() and torch.isfinite(db).all()
+                rest = (dz[7:].double() * (v[7:].double() - stats[7:, :1].double()) * stats[7:, 1:].double())
+                assert ((dw.double() - rest.sum(0)).abs() <= 14 * U * rest.abs().sum(0)).all()
+
+
+def test_many_rows_whose_squares_do_not_fit(r):
+    """In the kernels that add up dw on the way, and in those for columns."""
+    for rows, cols in ((4000, 70), (3000, 2050), (2050, 20001)):
+        x = rows_of(1, rows, cols, BF16)
+        x[::3, ::2], x[::3, 1::2] = 3e38, -3e38
+        x[::3, 0] = -3e38
+        _, _, stats = r.train_norm(x, keep=False)
+        dz = normal(2, rows, cols, dtype=BF16)
+        dx, dw, db = r.train_norm_backward(dz, x, stats, out=F32)
+        assert (stats[::3, 1] == 0).all() and torch.isfinite(stats).all() and (dx[::3] == 0).all() and torch.isfinite(dx).all()
+        good = torch.ones(rows, dtype=torch.bool, device="cuda")
+        good[::3] = False
+        rest = dz[good].double() * (x[good].double() - stats[good, :1].double()) * stats[good, 1:].double()
+        assert ((dw.double() - rest.sum(0)).abs() <= (rows + 4) * U * rest.abs().sum(0)).all()
+
+
+def test_what_is_not_finite_is_not_taken_for_an_overflow(r):
+    for cols in (3, 64, 283, 5000, 40000):
+        x = rows_of(9, 5, cols)
+        x[0, 1], x[1, cols - 1], x[2, 0] = float("inf"), -float("inf"), float("nan")
+        x[3, 0], x[3, 1] = float("inf"), -float("inf")
+        y, kept, stats = r.train_norm(x, out=F32)
+        assert torch.isnan(y[:4]).all() and torch.isnan(stats[:4, 1]).all() and torch.isfinite(y[4]).all() and torch.isfinite(stats[4]).all()
+        dx, dw, db = r.train_norm_backward(normal(3, 5, cols), x, stats, out=F32)
+        assert torch.isnan(dx[:4]).all() and torch.isfinite(dx[4]).all() and torch.isnan(dw).all()

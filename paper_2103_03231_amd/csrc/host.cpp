@@ -1134,7 +1134,7 @@ int donerf_train_norm(donerf_t* h, const donerf_mat* x, const float* weight, con
         return rc;
     if (rows > 0 && !stats) return fail(DONERF_E_INVALID_ARG, "stats is NULL");
     if (!y && !kept) return fail(DONERF_E_INVALID_ARG, "neither y nor kept is given");
-    if (!(eps >= 1e-30f && eps <= 3e38f)) return fail(DONERF_E_INVALID_ARG, "eps must be finite and at least 1e-30");
+    if (!(eps >= 1e-30f && std::isfinite(eps))) return fail(DONERF_E_INVALID_ARG, "eps must be finite and at least 1e-30");
     if (relu != 0 && relu != 1) return fail(DONERF_E_INVALID_ARG, "relu must be 0 or 1");
     const size_t vec = (size_t)cols * sizeof(float);
     if ((rc = validate_handle(h)) ||

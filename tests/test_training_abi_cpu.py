@@ -149,3 +149,8 @@ def test_matrix_arguments_are_the_structure():
         data, ld, kind, scales, ld_scales = m if len(m) == 5 else (*m, None, 0)
         assert b._mat(m) == bytes(b.donerf_mat(data, ld, scales, ld_scales, kind))
     assert b._mat(None) is None
+
+
+def test_every_finite_eps_is_taken():
+    for eps in (1e-30, 1.0, 3e38, 3.1e38, 3.4028234663852886e38):
+        refused(norm(eps=eps), "handle is NULL")

@@ -531,10 +531,14 @@ int backward_lanes(int cols) {
     return cols <= 16 * 1024 ? lanes : 0;
 }
 // So few values that dw and db are summed by columns, from the caches, in the launch that
-// makes dx.  Calls with it and in two launches: 1021 x 283 13.1 and 17.1 us, 314 x 5543 13
-// and 21.7, 2048 x 2048 15.4 and 16.6, 512 x 16,384 24 and 33; 2048 x 4096 23 and 21,
-// 1024 x 16,384 42 and 47, 4096 x 1024 21 and 16, 8192 x 256 30 and 17.
-bool few_values(int64_t rows, int cols) { return rows <= 2048 && rows * cols <= (int64_t)1 << 23; }
+// makes dx: 4 million of rows up to 4096 columns, 8 million of wider ones, whose workgroups
+// leave more parts.  Calls with it and in two launches, x in fp32 and in bf16: 1021 x 283
+// 11.6 and 15.8 us, 12.0 and 15.5; 2048 x 2048 15.6 and 16.1, 15.5 and 15.2; 1024 x 4096 13.6 and
+// 17.5, 13.0 and 19.0; 1170 x 5934 27.3 and 25.6, 23.0 and 23.3; 1024 x 8192 23.6 and 26.0, 22.5
+// and 24.1; 512 x 16,384 24.3 and 33.1, 23.0 and 31.6.  Left to two: 1500 x 4096 21.4 and 18.6,
+// 21.9 and 17.8; 2048 x 4096 23.4 and 21.2, 22.9 and 19.6; 1024 x 16,384 42.5 and 48.1, 39.1 and
+// 38.8 (from 8 bits 42.3 and 37.6); 4096 x 512 18.6 and 15.2.
+bool few_values(int64_t rows, int cols) { return rows <= 2048 && rows * cols <= (int64_t)1 << (cols <= 4096 ? 22 : 23); }
 // Workgroups of the backward pass that each leave a part of dw and db.
 uint32_t backward_groups(int64_t rows, int cols, int n_cu) {
     const int lanes = backward_lanes(cols);

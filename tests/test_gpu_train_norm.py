@@ -402,3 +402,20 @@ def test_what_is_not_finite_is_not_taken_for_an_overflow(r):
         assert torch.isnan(y[:4]).all() and torch.isnan(stats[:4, 1]).all() and torch.isfinite(y[4]).all() and torch.isfinite(stats[4]).all()
         dx, dw, db = r.train_norm_backward(normal(3, 5, cols), x, stats, out=F32)
         assert torch.isnan(dx[:4]).all() and torch.isfinite(dx[4]).all() and torch.isnan(dw).all()
+
+
+@pytest.mark.parametrize("rows,cols,one", [(2048, 2048, True), (2047, 2049, True), (2048, 2049, False), (2049, 2048, False), (1024, 4096, True),
+                                           (1025, 4096, False), (2048, 4096, False), (2048, 4095, False), (2047, 4097, True), (2048, 4097, False),
+                                           (1024, 8192, True), (1025, 8192, False), (512, 16384, True), (513, 16384, False), (419, 20000, True),
+                                           (420, 20000, False), (128, 65536, True), (129, 65536, False), (2049, 8, False), (2048, 8, True)])
+def test_gradients_on_either_side_of_one_launch(r, rows, cols, one):
+    """dw and db by columns without a workspace, and as parts in one.  Whole numbers, whose sums are exact: both give the same."""
+    assert (b.donerf_train_norm_backward_workspace(r.h, rows, cols) == 0) is one
+    g = torch.Generator().manual_seed(rows)
+    x = torch.randint(-8, 9, (rows, cols), generator=g, dtype=torch.int8).cuda()
+    dz = torch.randint(-8, 9, (rows, cols), generator=g, dtype=torch.int8).cuda()
+    stats = torch.stack([torch.randint(-3, 4, (rows,), generator=g).float(), torch.randint(1, 3, (rows,), generator=g).float()], 1).cuda()
+    xh = (x.double() - stats[:, :1]) * stats[:, 1:]
+    for dtype in (F32, BF16):
+        _, dw, db = r.train_norm_backward(dz.to(BF16), x.to(dtype), stats, need_dx=False)
+        assert torch.equal(dw.double(), (dz.double() * xh).sum(0)) and torch.equal(db.double(), dz.double().sum(0))

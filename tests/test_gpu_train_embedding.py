@@ -198,3 +198,60 @@ def test_refusals(r):
     with torch.cuda.stream(torch.cuda.Stream()):
         with pytest.raises(ValueError, match="stream"):
             r.train_embedding(table, ids)
+
+
+@pytest.mark.parametrize("rows,n,cols,spread", [(160001, 120, 40, "even"), (50000, 1, 256, "same"), (70000, 32000, 72, "tokens"), (100000, 3, 31, "runs"),
+                                                (2000003, 1000, 3, "even"), (3000001, 900, 4, "tokens"), (2300000, 2, 9, "runs"), (150000, 2, 20, "same"),
+                                                (2200000, 3, 65, "runs"), (2100000, 2, 130, "runs"), (2097200, 1, 300, "same"), (40000, 3, 603, "runs"),
+                                                (20011, 1, 137, "same"), (30000, 5, 97, "runs"), (16000, 4, 260, "runs"), (16384, 1, 515, "same")])
+def test_no_row_is_lost_or_counted_twice(r, rows, n, cols, spread):
+    """Whole numbers, whose sums, below 2^24, are exact in any order: in long runs of every length of a part and every width of
+    its sums, too."""
+    dy = torch.randint(-8, 9, (rows, cols), generator=torch.Generator("cuda").manual_seed(rows), dtype=torch.int8, device="cuda")
+    ids = ids_of(5, rows, n, spread)
+    if n <= 5:
+        ref = torch.stack([torch.where(ids[:, None] == v, dy, 0).sum(0) for v in range(n)])
+    else:
+        ref = torch.zeros(n + 1, cols, dtype=torch.int64, device="cuda").index_add_(0, torch.where((ids >= 0) & (ids < n), ids, n), dy.long())[:-1]
+    assert dy.abs().sum(0).max() < 2 ** 24                           # of any of the rows, in any order
+    for dtype in (BF16, F32):
+        assert torch.equal(r.train_embedding_backward(dy.to(dtype), ids, n).long(), ref)
+
+
+@pytest.mark.parametrize("n,cols", [(1, 5), (2, 100), (3, 64), (5, 300), (128, 64), (255, 5), (256, 300), (257, 100), (1000, 64), (1024, 130), (4096, 5), (4096, 300),
+                                    (4097, 64), (4097, 200), (16000, 70), (70000, 5), (40000, 100)])
+def test_rows_of_an_id_are_added_in_their_order(r, n, cols):
+    """Four rows an id, whose fp32 sum depends on their order: 2^24 + 1 is 2^24.  Parts are of a multiple of four rows."""
+    g = torch.Generator().manual_seed(n)
+    ids = torch.arange(n).repeat(4)[torch.randperm(4 * n, generator=g)]
+    kinds = torch.tensor([2.0 ** 24, -2.0 ** 24, 1.0, 1.0])
+    place = torch.sort(ids, stable=True).indices.view(n, 4)         # each id's rows in their order
+    dy = torch.empty(4 * n, cols)
+    perms = (torch.rand(n, 4, generator=g).argsort(1)[:, :, None] + torch.arange(cols)) % 4      # every column in an order of its own
+    dy[place.reshape(-1)] = kinds[perms].reshape(4 * n, cols)
+    v = dy[place.reshape(-1)].view(n, 4, cols)
+    ref = ((v[:, 0] + v[:, 1]) + v[:, 2]) + v[:, 3]
+    if n > 1:
+        assert len(ref.unique()) == 3                                # 0, 1 and 2
+    for kind in (torch.int32, torch.int64):
+        assert torch.equal(r.train_embedding_backward(dy.cuda(), ids.to(kind).cuda(), n).cpu(), ref)
+
+
+@pytest.mark.parametrize("rows", [1024, 1025, 4096, 4097, 16384, 16385])
+@pytest.mark.parametrize("n", [1, 1023, 1024, (1 << 17) + 3, (1 << 18) - 1, 1 << 18])
+def test_either_side_of_every_rule_of_the_sort(r, rows, n):
+    """In one launch with the sums, in one of its own, and by passes: whole numbers, and the workspace that each way has."""
+    cols = 9
+    need = b.donerf_train_embedding_backward_workspace(r.h, rows, n, cols)
+    ends = -(-(-(-rows // 8) * 2 * cols * 4) // 16) * 16
+    once = rows <= 16384 and n < 1 << 18
+    assert need == 0 if rows <= 1024 else (need == 2 * (-(-rows * 4 // 16) * 16) + ends) is once
+    dy = torch.randint(-8, 9, (rows, cols), generator=torch.Generator().manual_seed(1), dtype=torch.int8)
+    for spread in ("even", "tokens", "same", "none"):
+        ids = ids_of(3, rows, n, spread, torch.int32)
+        if spread == "even":
+            ids[:2] = torch.tensor([0, n - 1], device="cuda")        # the first and the last row
+        safe = torch.where((ids >= 0) & (ids < n), ids, n).long().cpu()
+        ref = torch.zeros(n + 1, cols).index_add_(0, safe, dy.float())[:-1].cuda()
+        for dtype in (BF16, F32):
+            assert torch.equal(r.train_embedding_backward(dy.to(dtype).cuda(), ids, n), ref)

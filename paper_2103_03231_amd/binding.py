@@ -398,10 +398,11 @@ class Renderer:
         donerf_targets(self.h, depth.data_ptr(), P, H, W, K, Z, out.data_ptr())
         return out
 
-    # ---- layer operators, and those around the layers.  Matrices are 2-D tensors with unit column stride (any row
-    # stride); they and the current stream must be those of the handle.  Nothing is
-    # recorded for autograd, also where a tensor requires its gradient: gradients come
-    # from train_linear_backward.
+    # ---- layer operators, and those around the layers.  Matrices are 2-D tensors with
+    # unit column stride (any row stride); they and the current stream must be those of
+    # the handle.  Nothing is recorded for autograd, also where a tensor requires its
+    # gradient: gradients come from train_linear_backward, train_norm_backward,
+    # train_embedding_backward and train_distill itself.
 
     # Checks are written for few attribute reads: on small calls they are most
     # of the time.

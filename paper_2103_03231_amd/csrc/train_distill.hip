@@ -330,7 +330,8 @@ __global__ void __launch_bounds__(row_threads(L)) distill_kernel(DistillArgs a) 
 }
 
 // Rows that registers do not hold, by a workgroup each: read three times, from the
-// caches but for the first.  107 x 48,791 classes: 15 us a call.
+// caches but for the first.  107 x 48,791 classes: 15 us a call; 2048 x 65,536 bf16 150 us,
+// 538 MB, 3.6 TB/s.
 template <class T, bool NEAR>
 __global__ void __launch_bounds__(1024) distill_wide_kernel(DistillArgs a) {
     constexpr int L = 1024;

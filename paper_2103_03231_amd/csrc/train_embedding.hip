@@ -5,8 +5,8 @@
 //             id_i = v.  The rows' numbers are sorted by their ids (rows of one id stay in
 //             the order of i), the sorted rows are summed in parts of equal length, and
 //             runs of one id that cross from part to part are joined from the parts'
-//             sums: no part is longer where all ids are alike, and nothing depends on
-//             the order in which workgroups come.
+//             sums: no part is longer where all ids are alike (the sort in one launch
+//             is, below), and nothing depends on the order in which workgroups come.
 //
 // Both are bound by memory where rows are many (dy is read once and the table written,
 // twice where a row has an id), and by their launches where they are few.
@@ -264,7 +264,10 @@ __global__ void __launch_bounds__(kThreads) sort_scatter_kernel(SortPass s, Zero
 // which is all that the sums ask for.  The remaining workgroups write zeros meanwhile: 16,384
 // keys of 32,000 beside 131 MB 24.3 us, 5.4 TB/s.  Against counts and moves in two passes whole
 // calls are shorter: 1500 rows of 32,000 x 256 20.5 us for 30, 4096 of 32,000 x 1024 31 for 43,
-// 16,000 of 60,000 x 64 24.5 for 31.
+// 16,000 of 60,000 x 64 24.5 for 31; of few ids they are not, 12,000 of 100 x 256 22.2 for 20.3.
+// A workgroup's time goes with its bucket's keys, and equal ids are one bucket's, as are all
+// rows without an id: 16,000 x 64 of 100 ids 19.5 us, of 4 ids 27, of one 44; of 32,000 ids 22,
+// and 47 with nine in ten rows without one.
 template <int ITEMS>
 struct BucketLds {
     SortLds sort;
@@ -714,8 +717,9 @@ GradPlan grad_plan(int64_t rows, int64_t n, int cols) {
     p.scanned = (int64_t)p.tiles << p.bits > kMostTileCounts;
     p.lanes = cols <= 64 ? 8 : cols <= 128 ? 16 : cols <= 256 ? 32 : 64;
     // Parts of 8 to 32 rows, for 131,072 lanes: fewer leave the chip idle (60,000 rows of 32
-    // columns in 2048 parts 40 us, in 7500 35), more take long to join (160,000 of 32, 5000 parts
-    // 29 us, 10,000 30).  Beyond 2 million rows, 65,536 longer ones.
+    // columns in 2048 parts 40 us, in 7500 35), more take longer to join than they save (160,000
+    // of 32: the 10,000 parts of this rule 30 us, 5000 29).  Beyond 2 million rows, 65,536
+    // longer ones.
     p.part = cut(kAhead, 2048 * 64 / p.lanes);
     if (p.part > 32) p.part = 32;
     if (rows > 32 * 65536) p.part = cut(kAhead, 65536);

@@ -511,7 +511,10 @@ hipError_t forward_launch(const NormArgs& a, int n_cu, hipStream_t stream) {
 // 16 columns a lane (33.5 million bf16 values: 256 columns 23.6 us, with 8 a lane 25.6;
 // 1024 columns 24.1, with 32 26.9; 2048 24.7, with 32 27.2; 8192 26.8, with 32 28.8), and up
 // to 64 where a row would need more than 512 lanes: 16,384 columns 31 us with 512, 33 with
-// 256 and with 1024.
+// 256 and with 1024.  Beyond 16,384 one row of a compute unit's has nothing to overlap its three
+// sums: 1048 x 32,000 bf16 41.6 us on 26 of memory; and beyond 32,768 a lane's 64 values
+// leave 36 to 248 bytes of it in scratch: 1024 x 65,536 bf16 77 us on 52, and more than twice
+// that where it is read three times instead.
 template <class T>
 hipError_t forward_by_width(const NormArgs& a, int n_cu, hipStream_t s) {
     const int c = a.cols;
